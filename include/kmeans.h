@@ -259,6 +259,104 @@ int kmeans_run_noalloc(const float *X, int64_t n, int32_t M, int32_t K, const fl
                        int32_t max_iter, uint32_t flags, int32_t *labels, float *centers,
                        int32_t *counts, int32_t *iterations, void *stream);
 
+/* ------------------------------------------------------------------------
+ * A key-value cache in K-means codes.
+ *
+ * The keys and values that attention keeps of a head's past tokens are vectors
+ * of `dim` features. Cut into dim / sub sub-vectors of `sub` features, each is
+ * held as one byte: the number of the nearest of K centres (Eq. (2), ties to
+ * the lowest number), which a program has learned with kmeans_run on the
+ * sub-vectors of sample keys and values, one set for each head and sub-vector,
+ * and rounded to the model's 16-bit type. kmeans_kv_write encodes new tokens,
+ * kmeans_kv_read gives back the centres that the codes name, and
+ * kmeans_kv_attend is the attention of one new token of every sequence over
+ * the codes.
+ *
+ * The cache is paged: a page holds `page` tokens of all heads, a slot is page
+ * number * page + place in the page, and a sequence is a row of page numbers.
+ * Keys and values of the caller are 16-bit tensors whose features are
+ * contiguous; their other strides are in elements, multiples of 8, of tensors
+ * aligned to 16 bytes (KMEANS_EINVAL otherwise), as are the centres and codes.
+ * Centres are finite numbers. A code of K or more, which kmeans_kv_write never
+ * leaves, stands for zeros.
+ * Page numbers and slots are device data that no call reads back: one outside
+ * the cache is never followed (see each call).
+ */
+#define KMEANS_KV_BF16 0
+#define KMEANS_KV_FP16 1
+
+typedef struct kmeans_kv {
+    const void *k_centres;  /* [heads][dim / sub][K][sub] of the 16-bit type           */
+    const void *v_centres;  /* likewise                                               */
+    uint8_t *k_codes;       /* [pages][heads][page][dim / sub]                         */
+    uint8_t *v_codes;       /* [pages][heads][dim / sub][page]                         */
+    int64_t pages;          /* 1 <= pages, pages * page <= 2^40                        */
+    int32_t page;           /* tokens of a page: a power of two, 8 to 1024             */
+    int32_t heads;          /* key-value heads, 1 to 1024                              */
+    int32_t dim;            /* 64, 96 or 128                                           */
+    int32_t sub;            /* 2, 4 or 8                                               */
+    int32_t K;              /* centres of each sub-vector, 1 to 256                    */
+    int32_t type;           /* KMEANS_KV_BF16 or KMEANS_KV_FP16                        */
+} kmeans_kv_t;
+
+/*
+ * Encodes `tokens` tokens: k and v are [tokens][heads][dim], slots an int64
+ * [tokens] DEVICE array. Token t goes to slot slots[t]; one whose slot is
+ * negative or past the cache is left out (padding). Two tokens with one slot
+ * leave codes of either. A code is the least j with the least distance
+ *   d_j = sum_i (x_i - c_ji)^2,
+ * formed in fp32 with every operation rounded and neighbours added first,
+ * ((d0 + d1) + (d2 + d3)) + ((d4 + d5) + (d6 + d7)); an x that holds a NaN or
+ * an infinity, or whose distances all overflow, has code 0. tokens = 0 is
+ * KMEANS_OK. Asynchronous on `stream`.
+ */
+int kmeans_kv_write(const kmeans_kv_t *kv, const void *k, int64_t k_token, int64_t k_head,
+                    const void *v, int64_t v_token, int64_t v_head, const int64_t *slots,
+                    int64_t tokens, void *stream);
+
+/*
+ * Reads tokens back: k and v ([tokens][heads][dim], DEVICE) receive the centres
+ * that the codes in slots[t] name, zeros where the slot is negative or past
+ * the cache. tokens = 0 is KMEANS_OK. Asynchronous on `stream`.
+ */
+int kmeans_kv_read(const kmeans_kv_t *kv, const int64_t *slots, int64_t tokens, void *k,
+                   int64_t k_token, int64_t k_head, void *v, int64_t v_token, int64_t v_head,
+                   void *stream);
+
+/* Bytes of device workspace that kmeans_kv_attend needs for this cache and
+ * these numbers of sequences, query heads and pages to a sequence. 0 for
+ * arguments it refuses. Pure host computation; the cache's pointers are not
+ * looked at. */
+size_t kmeans_kv_attend_workspace_bytes(const kmeans_kv_t *kv, int32_t seqs, int32_t q_heads,
+                                        int64_t table_pages);
+
+/*
+ * Attention of one new token of each sequence. q and out are [seqs][q_heads][dim]
+ * of the cache's type; q_heads is a multiple of heads, up to 128 to each, and
+ * query head h reads key-value head h / (q_heads / heads). table is an int32
+ * [seqs][table_pages] DEVICE array of page numbers (rows table_stride apart),
+ * lengths int32 [seqs] the number of cached positions, starts int32 [seqs] the
+ * first position that is attended (NULL: 0), as a sliding window or padding
+ * leaves it. Over the positions i of [starts[b], lengths[b]):
+ *   z_i = scale * (q . k_i),   out = sum_i exp(z_i - lse) v_i,
+ *   lse = log sum_i exp(z_i)   (fp32 [seqs][q_heads], NULL: not wanted),
+ * which join with attention over positions elsewhere. No position, or none
+ * whose z is above -infinity: out = 0, lse = -infinity. Entries of table whose
+ * pages hold no such position are not read. A length is taken as at most
+ * table_pages * page, a negative start as 0; an entry outside [0, pages) is
+ * taken as the nearest page. 1 <= seqs <= 4096 (0 is KMEANS_OK),
+ * seqs * q_heads < 2^24, table_pages * page <= 2^30, and seqs * table_pages *
+ * page / 32 < 2^31. scale is finite. Scores, their maximum and sum and the
+ * output are held in fp32; a weight exp(z_i - max) enters the product with the
+ * values as the sum of two 16-bit numbers. The same inputs give the same bits.
+ * Asynchronous on `stream`.
+ */
+int kmeans_kv_attend(const kmeans_kv_t *kv, const void *q, int64_t q_seq, int64_t q_head,
+                     int32_t seqs, int32_t q_heads, const int32_t *table, int64_t table_stride,
+                     int64_t table_pages, const int32_t *lengths, const int32_t *starts,
+                     float scale, void *out, int64_t out_seq, int64_t out_head, float *lse,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,8 @@ Entry points (same names as the C ABI):
     kmeans_run_noalloc(X, K, init_centers, max_iter, out, ...) -> iterations
     kmeans_workspace_bytes(n, M, K, flags=0), kmeans_init_workspace_bytes(n, M, K),
     kmeans_strerror(code)
+and, from kv.py, a key-value cache in K-means codes: KVCodes, kmeans_kv_write,
+kmeans_kv_read, kmeans_kv_attend.
 """
 from __future__ import annotations
 
@@ -44,7 +46,9 @@ EXPORTED = ("kmeans_workspace_bytes", "kmeans_strerror", "kmeans_assign", "kmean
             "kmeans_run", "kmeans_init_workspace_bytes", "kmeans_init_farthest",
             "kmeans_init_farthest_from",
             "kmeans_centroid_workspace_bytes", "kmeans_centroid",
-            "kmeans_diameter_workspace_bytes", "kmeans_diameter", "kmeans_run_noalloc")
+            "kmeans_diameter_workspace_bytes", "kmeans_diameter", "kmeans_run_noalloc",
+            "kmeans_kv_write", "kmeans_kv_read", "kmeans_kv_attend_workspace_bytes",
+            "kmeans_kv_attend")
 
 
 class KmeansTiming(ctypes.Structure):
@@ -347,3 +351,6 @@ def ctl_reruns(ws: torch.Tensor) -> int:
     again, and batches of up to 64 that it decided without, during the last
     kmeans_run that used `ws` (read from the control block)."""
     return int(ws[16:20].view(torch.int32).item())
+
+
+from .kv import KVCodes, kmeans_kv_attend, kmeans_kv_read, kmeans_kv_write  # noqa: E402,F401

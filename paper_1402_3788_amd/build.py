@@ -34,6 +34,8 @@ SOURCES = ([("kmeans_api.hip", [], "kmeans_api.o"), ("lloyd_ctl.hip", [], "lloyd
             ("lloyd_centres.hip", [], "lloyd_centres.o"), ("farthest.hip", [], "farthest.o"),
             ("lloyd_accum.hip", [], "lloyd_accum.o"),
             ("diameter.hip", [], "diameter.o"), ("lloyd_l1.hip", UNIT_FLAGS["lloyd_l1.hip"], "lloyd_l1.o")]
+           + [(f"kv_{f}.hip", [], f"kv_{f}.o") for f in ("api", "write", "read")]
+           + [("kv_attend.hip", [f"-DKV_SUB={sub}"], f"kv_attend_sub{sub}.o") for sub in (2, 4, 8)]
            + [(f, [f"-DLLOYD_PART={p}", *UNIT_FLAGS.get(f, [])], f.replace(".hip", f"_part{p}.o"))
               for f in ("lloyd_tile.hip", "lloyd_lane.hip", "lloyd_lane_mfma.hip")
               for p in range(PARTS)])

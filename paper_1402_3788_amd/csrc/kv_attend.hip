@@ -1,0 +1,556 @@
+// Attention of one new token of every sequence over the cache of codes.
+#include "kv_device.h"
+
+#ifndef KV_SUB
+#define KV_SUB 4
+#endif
+
+namespace lloyd {
+
+hipError_t launch_kv_attend_2(const KvCache &, const KvAttend &, const KvAttendPlan &, hipStream_t);
+hipError_t launch_kv_attend_4(const KvCache &, const KvAttend &, const KvAttendPlan &, hipStream_t);
+hipError_t launch_kv_attend_8(const KvCache &, const KvAttend &, const KvAttendPlan &, hipStream_t);
+
+namespace {
+
+constexpr int kThreads = kKvWaves * kWave;
+
+typedef float f4v __attribute__((ext_vector_type(4)));
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef __bf16 b2v __attribute__((ext_vector_type(2)));
+typedef __bf16 b8v __attribute__((ext_vector_type(8)));
+typedef float f2v __attribute__((ext_vector_type(2)));
+
+template <bool FP16>
+__device__ inline f4v mfma(u4v a, u4v b, f4v c)
+{
+    if constexpr (FP16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8v, a),
+                                                      __builtin_bit_cast(h8v, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8v, a),
+                                                       __builtin_bit_cast(b8v, b), c, 0, 0, 0);
+}
+
+template <bool FP16>
+__device__ inline uint32_t pack2(float a, float b)
+{
+    const f2v v = {a, b};
+    if constexpr (FP16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2v));
+    else
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
+}
+
+// Sizes of one form of the kernel.
+template <int D, int SUB>
+struct Form {
+    static constexpr int S = D / SUB;                  // codes of a head's vector
+    static constexpr int SL = S / 4;                   // of them, those of a lane's keys
+    static constexpr int VS = SUB < 4 ? SUB : 4;       // features of a value row (granule)
+    static constexpr int NG = D / VS;                  // granules
+    static constexpr int NH = (NG + 15) / 16;          // rows of 16 granules
+    static constexpr int NV = NH * VS;                 // accumulator tiles
+    static constexpr int kBook = S * 256 * SUB * 2;    // bytes of a head's centres in LDS
+    static constexpr int kEntry = NV * 256;            // floats of one wave's accumulators
+};
+
+// Positions [start, len) of sequence b, and the 32-position tiles they touch.
+struct Span {
+    int start, len;
+    __device__ int tile0() const { return start >> 5; }
+    __device__ int tiles() const { return len > start ? ((len + 31) >> 5) - (start >> 5) : 0; }
+};
+
+__device__ inline Span span_of(const KvCache &c, const KvAttend &a, int b)
+{
+    const int cap = a.table_pages << c.page_log2;
+    Span s;
+    s.len = min(max(a.lengths[b], 0), cap);
+    s.start = a.starts ? max(a.starts[b], 0) : 0;
+    return s;
+}
+
+// The workgroups that share a head's tiles: no more than leave each a tile
+// for every wave.
+__device__ inline int splits_used(int tiles, int splits)
+{
+    return min(splits, max(1, (tiles + kKvWaves - 1) / kKvWaves));
+}
+
+__device__ inline int split_begin(int tiles, int j, int used)
+{
+    return (int)((int64_t)tiles * j / used);
+}
+
+// Codes of one tile of 32 positions in a lane. Keys: position 8 (r / 4) + 4 t +
+// r % 4 (r = lane % 16) for the two products t, codes [SL (lane / 16), + SL).
+// Values: granule 16 hh + r, positions [8 (lane / 16), + 8).
+template <int D, int SUB>
+struct Codes {
+    using F = Form<D, SUB>;
+    uint32_t k[2][(F::SL + 3) / 4];
+    uint32_t v[F::NH][2];
+};
+
+template <int N>
+__device__ inline void load_bytes(uint32_t *dst, const uint8_t *src)
+{
+    constexpr int align = N % 16 == 0 ? 16 : N % 8 == 0 ? 8 : N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
+    dst[(N - 1) / 4] = 0;
+    __builtin_memcpy(dst, __builtin_assume_aligned(src, align), N);
+}
+
+__device__ inline int byte_of(const uint32_t *w, int j) { return (w[j >> 2] >> (8 * (j & 3))) & 255; }
+
+template <int D, int SUB, bool FP16>
+__global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend a, int splits,
+                                                             int qblocks)
+{
+    using F = Form<D, SUB>;
+    extern __shared__ uint4 lds[];
+    char *const kbook = reinterpret_cast<char *>(lds);
+    char *const vbook = kbook + F::kBook;
+    int *const first = reinterpret_cast<int *>(vbook + F::kBook);     // [seqs + 1]
+    __shared__ int wave_sum[kKvWaves];
+    __shared__ int tag[2 * kKvWaves];
+    __shared__ float ml[2 * kKvWaves][32];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x % c.heads;
+    const int qb = blockIdx.x / c.heads % qblocks;
+    const int j = blockIdx.x / c.heads / qblocks;
+    const int nq = min(kKvQueries, a.group - qb * kKvQueries);
+    const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j;
+    float *const part_o = a.part_o + wg * (kKvWaves + 2) * F::kEntry;
+    float *const part_ml = a.part_ml + wg * 64;
+
+    // Where each sequence's tiles begin in the row of all tiles.
+    {
+        const int per = (a.seqs + kThreads - 1) / kThreads;
+        int sum = 0;
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            if (b < a.seqs) sum += span_of(c, a, b).tiles();
+        }
+        int incl = sum;
+        for (int d = 1; d < kWave; d *= 2) {
+            const int up = __shfl_up(incl, d);
+            if (lane >= d) incl += up;
+        }
+        if (lane == 63) wave_sum[wave] = incl;
+        __syncthreads();
+        int at = incl - sum;
+        for (int w = 0; w < wave; ++w) at += wave_sum[w];
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            if (b < a.seqs) {
+                first[b] = at;
+                at += span_of(c, a, b).tiles();
+                if (b == a.seqs - 1) first[a.seqs] = at;
+            }
+        }
+    }
+    // The centres of this head; entries from K up are zeros.
+    {
+        constexpr int n = F::S * 256;
+        using E = KvEntry<SUB>;
+        const uint16_t *ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
+        const uint16_t *vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
+        for (int i = tid; i < n; i += kThreads) {
+            const int s = i >> 8, code = i & 255;
+            E ke{}, ve{};
+            if (code < c.K) {
+                ke = kv_load<SUB>(ks + ((int64_t)s * c.K + code) * SUB);
+                ve = kv_load<SUB>(vs + ((int64_t)s * c.K + code) * SUB);
+            }
+            reinterpret_cast<E *>(kbook)[i] = ke;
+            reinterpret_cast<E *>(vbook)[i] = ve;
+        }
+    }
+    __syncthreads();
+
+    const int tiles = first[a.seqs];
+    const int used = splits_used(tiles, splits);
+    if (blockIdx.x == 0)
+        for (int b = tid; b <= a.seqs; b += kThreads) a.first_tile[b] = first[b];
+    // Sequences without positions.
+    for (int b = j; b < a.seqs; b += splits) {
+        if (first[b] != first[b + 1]) continue;
+        for (int i = tid; i < nq * D; i += kThreads)
+            a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + i / D) * a.out_head + i % D] = 0;
+        if (a.lse && tid < nq)
+            a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + tid] = -INFINITY;
+    }
+    if (j >= used) return;
+    const int w0 = split_begin(tiles, j, used), w1 = split_begin(tiles, j + 1, used);
+    const int a0 = w0 + (int)((int64_t)(w1 - w0) * wave / kKvWaves);
+    const int a1 = w0 + (int)((int64_t)(w1 - w0) * (wave + 1) / kKvWaves);
+
+    // Final output of query q, feature d of sequence b.
+    const auto put = [&](int b, int q, int d, float x) {
+        a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + q) * a.out_head + d] =
+            (uint16_t)pack2<FP16>(x, 0.f);
+    };
+    const auto put_lse = [&](int b, int q, float m, float l) {
+        if (a.lse)
+            a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + q] =
+                l > 0.f || l != l ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+    };
+
+    f4v acc[F::NV];
+    float m = -INFINITY, l = 0.f;
+    u4v q[D / 32];
+    if (lane == 0) { tag[2 * wave] = -1; tag[2 * wave + 1] = -1; }
+
+    // Sum of l over the four lanes of a query.
+    const auto whole_l = [&]() {
+        float s = l + __shfl_xor(l, 16);
+        return s + __shfl_xor(s, 32);
+    };
+
+    if (a0 < a1) {
+        int b = 0;
+        for (int lo = 0, hi = a.seqs; lo < hi;) {      // the last b with first[b] <= a0
+            const int mid = (lo + hi) >> 1;
+            if (first[mid + 1] <= a0) lo = mid + 1; else hi = mid;
+            b = lo;
+        }
+        b = __builtin_amdgcn_readfirstlane(b);
+        int piece = a0, base = 0, next = 0;
+        Span sp{};
+        bool fresh = true;
+        for (int t = a0; t <= a1; ++t) {
+            if (!fresh && (t == next || t == a1)) {
+                // the piece [piece, t) of sequence b is done
+                const float lw = whole_l();
+                if (piece == base && t == next) {
+                    const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
+                    if (r < nq) {
+#pragma unroll
+                        for (int n = 0; n < F::NV; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int d = (16 * (n / F::VS) + 4 * g + i) * F::VS + n % F::VS;
+                                if (d < D) put(b, r, d, acc[n][i] * inv);
+                            }
+                        if (g == 0) put_lse(b, r, m, lw);
+                    }
+                } else {
+                    const int e = 2 * wave + (t == a1);
+                    if (lane == 0) tag[e] = b;
+                    if (g == 0) { ml[e][r] = m; ml[e][16 + r] = lw; }
+                    if (t != a1) {
+#pragma unroll
+                        for (int n = 0; n < F::NV; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                part_o[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
+                    }
+                }
+                fresh = true;
+                if (t != a1) {
+                    ++b;
+                    while (first[b + 1] <= t) ++b;
+                }
+            }
+            if (t == a1) break;
+            if (fresh) {
+                fresh = false;
+                piece = t;
+                base = first[b];
+                next = first[b + 1];
+                sp = span_of(c, a, b);
+                m = -INFINITY;
+                l = 0.f;
+#pragma unroll
+                for (int n = 0; n < F::NV; ++n) acc[n] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < D / 32; ++st) q[st] = u4v{0, 0, 0, 0};
+                if (r < nq) {
+                    const uint16_t *src = a.q + b * a.q_seq +
+                                          (h * a.group + qb * kKvQueries + r) * a.q_head + g * (D / 4);
+#pragma unroll
+                    for (int st = 0; st < D / 32; ++st)
+                        q[st] = *reinterpret_cast<const u4v *>(src + st * 8);
+                }
+            }
+            const int pos = (t - base + sp.tile0()) * 32;
+            // codes
+            Codes<D, SUB> cd;
+            const auto page_of = [&](int p) {
+                const int at = min(max(p, sp.start & ~7), (sp.len - 1) & ~7);
+                const int64_t page = a.table[b * a.table_stride + (at >> c.page_log2)];
+                const int64_t safe = min(max(page, (int64_t)0), c.pages - 1);
+                return ((safe * c.heads + h) << c.page_log2) * F::S;
+            };
+            const int pm = (1 << c.page_log2) - 1;
+            {
+                const int p = min(max(pos + 8 * (r >> 2), sp.start & ~7), (sp.len - 1) & ~7);
+                const uint8_t *src = c.k_codes + page_of(pos + 8 * (r >> 2)) +
+                                     ((p & pm) + (r & 3)) * F::S + g * F::SL;
+                load_bytes<F::SL>(cd.k[0], src);
+                load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
+            }
+            {
+                const int p = min(max(pos + 8 * g, sp.start & ~7), (sp.len - 1) & ~7);
+                const uint8_t *src = c.v_codes + page_of(pos + 8 * g) + (p & pm);
+#pragma unroll
+                for (int hh = 0; hh < F::NH; ++hh) {
+                    const int gr = min(16 * hh + r, F::NG - 1);
+                    load_bytes<8>(cd.v[hh], src + ((gr * F::VS / SUB) << c.page_log2));
+                }
+            }
+            // scores: rows are positions, columns queries
+            float z[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f4v s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < D / 32; ++st) {
+                    u4v op;
+                    constexpr int per = 8 / SUB;
+#pragma unroll
+                    for (int x = 0; x < per; ++x) {
+                        const int code = byte_of(cd.k[u], st * per + x);
+                        const KvEntry<SUB> e = reinterpret_cast<const KvEntry<SUB> *>(
+                            kbook)[((g * F::SL + st * per + x) << 8) + code];
+#pragma unroll
+                        for (int w = 0; w < SUB / 2; ++w) op[x * (SUB / 2) + w] = e.w[w];
+                    }
+                    s = mfma<FP16>(op, q[st], s);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * u + i] = s[i] * a.scale_log2;
+            }
+            const bool partial = pos < sp.start || pos + 32 > sp.len;
+            if (partial) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int p = pos + 8 * g + i;
+                    if (p < sp.start || p >= sp.len) z[i] = -INFINITY;
+                }
+            }
+            float top = z[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float mn = fmaxf(m, top);
+            const float safe = mn == -INFINITY ? 0.f : mn;
+            const float alpha = exp2f(m - safe);
+            m = mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[i] = exp2f(z[i] - safe);
+                sum += z[i];
+            }
+            l = l * alpha + sum;
+#pragma unroll
+            for (int n = 0; n < F::NV; ++n) acc[n] *= alpha;
+            // each weight as the sum of two 16-bit numbers: one alone (8 bits of
+            // bf16) would cost as much of the result as its own final rounding
+            u4v p, p_lo;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[i] = pack2<FP16>(z[2 * i], z[2 * i + 1]);
+                p_lo[i] = pack2<FP16>(z[2 * i] - kv_float<FP16>(p[i] & 0xFFFFu),
+                                      z[2 * i + 1] - kv_float<FP16>(p[i] >> 16));
+            }
+            // values: rows are features, columns queries
+            u4v keep = {~0u, ~0u, ~0u, ~0u};
+            if (partial) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p0 = pos + 8 * g + 2 * i;
+                    keep[i] = (p0 >= sp.start && p0 < sp.len ? 0xFFFFu : 0u) |
+                              (p0 + 1 >= sp.start && p0 + 1 < sp.len ? 0xFFFF0000u : 0u);
+                }
+            }
+#pragma unroll
+            for (int hh = 0; hh < F::NH; ++hh) {
+                const int gr = min(16 * hh + r, F::NG - 1);
+                const int s = gr * F::VS / SUB, half = gr * F::VS % SUB / F::VS;
+                KvEntry<F::VS> e[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    e[x] = *reinterpret_cast<const KvEntry<F::VS> *>(
+                        vbook + ((s << 8) + byte_of(cd.v[hh], x)) * (SUB * 2) + half * (F::VS * 2));
+#pragma unroll
+                for (int i = 0; i < F::VS; ++i) {
+                    u4v op;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        op[x] = __builtin_amdgcn_perm(e[2 * x + 1].w[i / 2], e[2 * x].w[i / 2],
+                                                      i % 2 ? 0x07060302u : 0x05040100u) & keep[x];
+                    acc[hh * F::VS + i] = mfma<FP16>(op, p_lo, acc[hh * F::VS + i]);
+                    acc[hh * F::VS + i] = mfma<FP16>(op, p, acc[hh * F::VS + i]);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    // The centres are done with: their place takes each wave's last piece.
+    float *const last = reinterpret_cast<float *>(lds);
+    if (tag[2 * wave + 1] >= 0) {
+#pragma unroll
+        for (int n = 0; n < F::NV; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                last[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
+    }
+    __syncthreads();
+    for (int e0 = 0; e0 < 2 * kKvWaves;) {
+        const int b = tag[e0];
+        if (b < 0) { ++e0; continue; }
+        int e1 = e0 + 1;
+        while (e1 < 2 * kKvWaves && (tag[e1] == b || tag[e1] < 0)) ++e1;
+        const bool whole = first[b] >= w0 && first[b + 1] <= w1;
+        const int slot = first[b] < w0 ? 0 : 1;
+        const int qq = tid & 15;
+        float top = -INFINITY;
+        for (int e = e0; e < e1; ++e)
+            if (tag[e] == b) top = fmaxf(top, ml[e][qq]);
+        const float safe = top == -INFINITY ? 0.f : top;
+        float lw = 0.f;
+        for (int e = e0; e < e1; ++e)
+            if (tag[e] == b) lw += ml[e][16 + qq] * exp2f(ml[e][qq] - safe);
+        const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
+        if (qq < nq) {
+            for (int x = tid; x < F::kEntry; x += kThreads) {
+                float o = 0.f;
+                for (int e = e0; e < e1; ++e)
+                    if (tag[e] == b)
+                        o += (e & 1 ? last[(e >> 1) * F::kEntry + x] : part_o[(e >> 1) * F::kEntry + x]) *
+                             exp2f(ml[e][qq] - safe);
+                if (whole) {
+                    const int n = x >> 8, i = (x >> 6) & 3, gg = (x >> 4) & 3;
+                    const int d = (16 * (n / F::VS) + 4 * gg + i) * F::VS + n % F::VS;
+                    if (d < D) put(b, qq, d, o * inv);
+                } else {
+                    part_o[(kKvWaves + slot) * F::kEntry + x] = o;
+                }
+            }
+            if (tid < 16) {
+                if (whole) {
+                    put_lse(b, qq, top, lw);
+                } else {
+                    part_ml[slot * 32 + qq] = top;
+                    part_ml[slot * 32 + 16 + qq] = lw;
+                }
+            }
+        }
+        e0 = e1;
+    }
+}
+
+// Joins what the workgroups left of the sequences that several shared.
+template <int D, int SUB, bool FP16>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int splits)
+{
+    using F = Form<D, SUB>;
+    const int b = blockIdx.x % a.seqs, hq = blockIdx.x / a.seqs;
+    const int h = hq % c.heads, qb = hq / c.heads;
+    const int nq = min(kKvQueries, a.group - qb * kKvQueries);
+    const int tiles = a.first_tile[a.seqs], p0 = a.first_tile[b], p1 = a.first_tile[b + 1];
+    if (p0 == p1) return;
+    const int used = splits_used(tiles, splits);
+    const int j0 = (int)(((int64_t)(p0 + 1) * used + tiles - 1) / tiles) - 1;
+    const int j1 = (int)(((int64_t)p1 * used + tiles - 1) / tiles) - 1;
+    if (j0 == j1) return;
+    const int tid = threadIdx.x, q = tid & 15;
+    if (q >= nq) return;
+    const int64_t wg = ((int64_t)qb * c.heads + h) * splits;
+    const auto slot_of = [&](int j) { return p0 < split_begin(tiles, j, used) ? 0 : 1; };
+    float top = -INFINITY;
+    for (int j = j0; j <= j1; ++j) top = fmaxf(top, a.part_ml[(wg + j) * 64 + slot_of(j) * 32 + q]);
+    const float safe = top == -INFINITY ? 0.f : top;
+    float lw = 0.f;
+    for (int j = j0; j <= j1; ++j) {
+        const float *ml = a.part_ml + (wg + j) * 64 + slot_of(j) * 32;
+        lw += ml[16 + q] * exp2f(ml[q] - safe);
+    }
+    const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
+    const int head = h * a.group + qb * kKvQueries + q;
+    for (int x = tid; x < F::kEntry; x += 256) {
+        const int n = x >> 8, i = (x >> 6) & 3, gg = (x >> 4) & 3;
+        const int d = (16 * (n / F::VS) + 4 * gg + i) * F::VS + n % F::VS;
+        if (d >= D) continue;
+        float o = 0.f;
+        for (int j = j0; j <= j1; ++j)
+            o += a.part_o[((wg + j) * (kKvWaves + 2) + kKvWaves + slot_of(j)) * F::kEntry + x] *
+                 exp2f(a.part_ml[(wg + j) * 64 + slot_of(j) * 32 + q] - safe);
+        a.out[b * a.out_seq + head * a.out_head + d] = (uint16_t)pack2<FP16>(o * inv, 0.f);
+    }
+    if (a.lse && tid < 16)
+        a.lse[(int64_t)b * c.heads * a.group + head] =
+            lw > 0.f || lw != lw ? (top + __log2f(lw)) * 0.69314718055994531f : -INFINITY;
+}
+
+template <int D, int SUB, bool FP16>
+hipError_t launch(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hipStream_t s)
+{
+    using F = Form<D, SUB>;
+    const size_t lds = 2 * F::kBook + (a.seqs + 1) * sizeof(int);
+    const unsigned grid = (unsigned)c.heads * p.qblocks * p.splits;
+    hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16>), dim3(grid), dim3(kThreads), lds, s, c, a,
+                       p.splits, p.qblocks);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>), dim3((unsigned)a.seqs * c.heads * p.qblocks),
+                       dim3(256), 0, s, c, a, p.splits);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_type(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hipStream_t s)
+{
+    return c.fp16 ? launch<D, KV_SUB, true>(c, a, p, s) : launch<D, KV_SUB, false>(c, a, p, s);
+}
+
+}  // namespace
+
+#define KV_CAT2(a, b) a##b
+#define KV_CAT(a, b) KV_CAT2(a, b)
+hipError_t KV_CAT(launch_kv_attend_, KV_SUB)(const KvCache &c, const KvAttend &a,
+                                             const KvAttendPlan &p, hipStream_t s)
+{
+    return c.dim == 64 ? launch_type<64>(c, a, p, s)
+         : c.dim == 96 ? launch_type<96>(c, a, p, s) : launch_type<128>(c, a, p, s);
+}
+
+#if KV_SUB == 2
+KvAttendPlan plan_kv_attend(const KvCache &c, int seqs, int group, int64_t table_pages)
+{
+    KvAttendPlan p{};
+    p.qblocks = (group + kKvQueries - 1) / kKvQueries;
+    const int64_t span = table_pages << c.page_log2;
+    const int64_t tiles = seqs * ((span + kKvTile - 1) / kKvTile);
+    const int per_cu = c.dim == 64 ? 2 : 1;      // workgroups whose centres fit a CU's LDS
+    int64_t splits = (int64_t)kCUs * per_cu / (c.heads * p.qblocks);
+    if (splits > (tiles + kKvWaves - 1) / kKvWaves) splits = (tiles + kKvWaves - 1) / kKvWaves;
+    p.splits = splits < 1 ? 1 : (int)splits;
+    const int gran = c.sub < 4 ? c.sub : 4;
+    const size_t entry = (size_t)((c.dim / gran + 15) / 16 * gran) * 256 * sizeof(float);
+    const size_t wgs = (size_t)c.heads * p.qblocks * p.splits;
+    const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    p.first_tile_off = 0;
+    p.part_o_off = up((size_t)(seqs + 1) * sizeof(int32_t));
+    p.part_ml_off = p.part_o_off + wgs * (kKvWaves + 2) * entry;
+    p.total = p.part_ml_off + up(wgs * 64 * sizeof(float));
+    return p;
+}
+
+hipError_t launch_kv_attend(const KvCache &c, const KvAttend &a, const KvAttendPlan &p,
+                            hipStream_t s)
+{
+    return c.sub == 2 ? launch_kv_attend_2(c, a, p, s)
+         : c.sub == 4 ? launch_kv_attend_4(c, a, p, s) : launch_kv_attend_8(c, a, p, s);
+}
+#endif
+
+}  // namespace lloyd

@@ -1,0 +1,231 @@
+"""The key-value cache in K-means codes (include/kmeans.h): Python binding.
+
+    cache = KVCodes.empty(k_centres, v_centres, pages, page)
+    kmeans_kv_write(cache, k, v, slots)
+    kmeans_kv_read(cache, slots, out=None) -> (k, v)
+    kmeans_kv_attend(cache, q, table, lengths, scale=None, starts=None, out=None,
+                     lse=None, ws=None) -> (out, lse)
+
+Everything runs on the current stream of the cache's device; no call waits for
+it or reads device data back.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import KmeansError, KMEANS_EUNSUPPORTED, _lib, _stream_ptr
+
+_TYPES = {torch.bfloat16: 0, torch.float16: 1}      # KMEANS_KV_BF16, KMEANS_KV_FP16
+
+
+class _Desc(ctypes.Structure):
+    """kmeans_kv_t"""
+    _fields_ = [("k_centres", ctypes.c_void_p), ("v_centres", ctypes.c_void_p),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("sub", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
+
+
+def _bind():
+    p, i64, i32, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+    d = ctypes.POINTER(_Desc)
+    _lib.kmeans_kv_write.argtypes = [d, p, i64, i64, p, i64, i64, p, i64, p]
+    _lib.kmeans_kv_write.restype = ctypes.c_int
+    _lib.kmeans_kv_read.argtypes = [d, p, i64, p, i64, i64, p, i64, i64, p]
+    _lib.kmeans_kv_read.restype = ctypes.c_int
+    _lib.kmeans_kv_attend_workspace_bytes.argtypes = [d, i32, i32, i64]
+    _lib.kmeans_kv_attend_workspace_bytes.restype = sz
+    _lib.kmeans_kv_attend.argtypes = [d, p, i64, i64, i32, i32, p, i64, i64, p, p, ctypes.c_float,
+                                      p, i64, i64, p, p, sz, p]
+    _lib.kmeans_kv_attend.restype = ctypes.c_int
+
+
+_bind()
+
+
+class KVCodes:
+    """A paged cache of codes and the centres they name.
+
+    k_centres, v_centres  [heads, dim / sub, K, sub], bfloat16 or float16
+    k_codes               [pages, heads, page, dim / sub], uint8
+    v_codes               [pages, heads, dim / sub, page], uint8
+
+    all contiguous on one GPU. The tensors are kept, not copied: what is written
+    to them is what the calls see."""
+
+    def __init__(self, k_centres, v_centres, k_codes, v_codes):
+        tensors = (k_centres, v_centres, k_codes, v_codes)
+        if not all(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4
+                   and t.is_contiguous() and t.device == k_centres.device for t in tensors):
+            raise ValueError("centres and codes must be contiguous 4-D tensors on one GPU")
+        if k_centres.dtype not in _TYPES or v_centres.dtype != k_centres.dtype:
+            raise ValueError("centres must be bfloat16 or float16, both alike")
+        if k_codes.dtype != torch.uint8 or v_codes.dtype != torch.uint8:
+            raise ValueError("codes must be uint8")
+        heads, S, K, sub = k_centres.shape
+        pages, _, page, _ = k_codes.shape
+        if (v_centres.shape != k_centres.shape or k_codes.shape != (pages, heads, page, S)
+                or v_codes.shape != (pages, heads, S, page)):
+            raise ValueError("shapes of centres and codes do not belong together")
+        self.k_centres, self.v_centres, self.k_codes, self.v_codes = tensors
+        self.pages, self.page, self.heads, self.dim, self.sub, self.K = (
+            pages, page, heads, S * sub, sub, K)
+        self.dtype, self.device = k_centres.dtype, k_centres.device
+        self._desc = _Desc(*(t.data_ptr() for t in tensors), pages, page, heads, S * sub, sub, K,
+                           _TYPES[self.dtype])
+        self._ref = ctypes.byref(self._desc)
+        # the library says what it takes; it looks at no pointer here
+        if not self.attend_workspace_bytes(1, heads, 1):
+            raise KmeansError("KVCodes", KMEANS_EUNSUPPORTED)
+
+    @classmethod
+    def empty(cls, k_centres, v_centres, pages: int, page: int):
+        """A cache of `pages` pages of `page` tokens, all codes 0."""
+        if not (isinstance(k_centres, torch.Tensor) and k_centres.dim() == 4):
+            raise ValueError("centres must be [heads, dim / sub, K, sub]")
+        heads, S = k_centres.shape[:2]
+        codes = [torch.zeros(shape, dtype=torch.uint8, device=k_centres.device)
+                 for shape in ((pages, heads, page, S), (pages, heads, S, page))]
+        return cls(k_centres, v_centres, *codes)
+
+    def attend_workspace_bytes(self, seqs: int, q_heads: int, table_pages: int) -> int:
+        return int(_lib.kmeans_kv_attend_workspace_bytes(self._ref, seqs, q_heads, table_pages))
+
+
+def _rows(cache, t, what, n=None):
+    """t as the library takes it, [n, heads, dim] with its features contiguous
+    and its rows on 16 bytes, and its two strides; a copy where it is not."""
+    if not (isinstance(t, torch.Tensor) and t.dim() == 3 and t.device == cache.device
+            and t.dtype == cache.dtype and t.shape[2] == cache.dim):
+        raise ValueError(f"{what} must be a [n, heads, {cache.dim}] tensor of the cache's type "
+                         "on its GPU")
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"{what} must have {n} rows")
+    a, b, c = t.stride()
+    if c != 1 or (a | b) & 7 or t.data_ptr() & 15:
+        t = t.contiguous()
+        if t.data_ptr() & 15:
+            t = t.clone()
+        a, b, c = t.stride()
+    return t, a, b
+
+
+def _target(cache, t, shape, what):
+    """An output that the caller gave, or a new one."""
+    if t is None:
+        t = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+        return t, shape[1] * shape[2], shape[2]
+    if not (isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape)
+            and t.dtype == cache.dtype and t.device == cache.device):
+        raise ValueError(f"{what} must be {tuple(shape)} of the cache's type on its GPU")
+    a, b, c = t.stride()
+    if c != 1 or (a | b) & 7 or t.data_ptr() & 15 or (a == 0 and shape[0] > 1) \
+            or (b == 0 and shape[1] > 1):
+        raise ValueError(f"{what} needs contiguous features, rows on 16 bytes, and no two "
+                         "elements in one place")
+    return t, a, b
+
+
+def _ints(cache, t, dtype, n, what):
+    if not (isinstance(t, torch.Tensor) and t.dim() == 1 and t.dtype == dtype
+            and t.device == cache.device and (n is None or t.shape[0] == n)):
+        raise ValueError(f"{what} must be a 1-D {dtype} tensor"
+                         + ("" if n is None else f" of {n}") + " on the cache's GPU")
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _call(cache, fn, name, *args):
+    """fn on the cache's device and current stream."""
+    dev = cache.device
+    if dev.index == torch.cuda.current_device():
+        rc = fn(cache._ref, *args, _stream_ptr(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(cache._ref, *args, _stream_ptr(dev))
+    if rc:
+        raise KmeansError(name, rc)
+
+
+def kmeans_kv_write(cache: KVCodes, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
+    """Encodes the tokens k, v ([n, heads, dim]) into the slots of `slots` (int64
+    [n]; page number * page + place). A token whose slot is negative or past
+    the cache is left out."""
+    slots = _ints(cache, slots, torch.int64, None, "slots")
+    n = slots.shape[0]
+    k, ka, kb = _rows(cache, k, "k", n)
+    v, va, vb = _rows(cache, v, "v", n)
+    if k.shape[1] != cache.heads or v.shape[1] != cache.heads:
+        raise ValueError(f"k and v must have {cache.heads} heads")
+    _call(cache, _lib.kmeans_kv_write, "kmeans_kv_write", k.data_ptr(), ka, kb, v.data_ptr(), va,
+          vb, slots.data_ptr(), n)
+
+
+def kmeans_kv_read(cache: KVCodes, slots: torch.Tensor, out=None):
+    """The keys and values in the slots of `slots` (int64 [n]), as the centres
+    that their codes name: (k, v), each [n, heads, dim]; zeros for a slot that
+    is not in the cache. `out` may supply both tensors."""
+    slots = _ints(cache, slots, torch.int64, None, "slots")
+    n = slots.shape[0]
+    shape = (n, cache.heads, cache.dim)
+    k, v = (None, None) if out is None else out
+    k, ka, kb = _target(cache, k, shape, "k")
+    v, va, vb = _target(cache, v, shape, "v")
+    _call(cache, _lib.kmeans_kv_read, "kmeans_kv_read", slots.data_ptr(), n, k.data_ptr(), ka, kb,
+          v.data_ptr(), va, vb)
+    return k, v
+
+
+def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                     scale: float | None = None, starts: torch.Tensor | None = None, out=None,
+                     lse=None, ws: torch.Tensor | None = None):
+    """Attention of one new token of every sequence over its cached positions.
+
+    q        [seqs, q_heads, dim], q_heads a multiple of the cache's heads
+    table    int32 [seqs, pages of a sequence]: page numbers
+    lengths  int32 [seqs]: cached positions
+    scale    of the scores, 1 / sqrt(dim) if None
+    starts   int32 [seqs]: the first attended position, 0 if None
+
+    Returns (out, lse): out like q, lse float32 [seqs, q_heads], the logarithm
+    of the sum of the scores' exponentials (-inf, with out 0, where nothing is
+    attended). `out` and `lse` may supply the tensors, `ws` the workspace
+    (cache.attend_workspace_bytes)."""
+    q, qa, qb = _rows(cache, q, "q")
+    seqs, q_heads, dim = q.shape
+    if q_heads < 1 or q_heads % cache.heads:
+        raise ValueError(f"q must have a multiple of {cache.heads} heads")
+    if not (isinstance(table, torch.Tensor) and table.dim() == 2 and table.dtype == torch.int32
+            and table.device == cache.device and table.shape[0] == seqs):
+        raise ValueError(f"table must be an int32 [{seqs}, pages] tensor on the cache's GPU")
+    if table.stride(1) != 1:
+        table = table.contiguous()
+    lengths = _ints(cache, lengths, torch.int32, seqs, "lengths")
+    if starts is not None:
+        starts = _ints(cache, starts, torch.int32, seqs, "starts")
+    out, oa, ob = _target(cache, out, (seqs, q_heads, dim), "out")
+    if lse is None:
+        lse = torch.empty((seqs, q_heads), dtype=torch.float32, device=cache.device)
+    elif not (lse.dtype == torch.float32 and tuple(lse.shape) == (seqs, q_heads)
+              and lse.is_contiguous() and lse.device == cache.device):
+        raise ValueError(f"lse must be a contiguous float32 [{seqs}, {q_heads}] tensor on the "
+                         "cache's GPU")
+    width = table.shape[1]
+    if width == 0 or seqs == 0:         # no position anywhere
+        return out.zero_(), lse.fill_(-math.inf)
+    if ws is None:
+        nbytes = cache.attend_workspace_bytes(seqs, q_heads, width)
+        if nbytes == 0:
+            raise KmeansError("kmeans_kv_attend", KMEANS_EUNSUPPORTED)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+    elif ws.device != cache.device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the cache's GPU")
+    _call(cache, _lib.kmeans_kv_attend, "kmeans_kv_attend", q.data_ptr(), qa, qb, seqs, q_heads,
+          table.data_ptr(), table.stride(0), width, lengths.data_ptr(),
+          None if starts is None else starts.data_ptr(),
+          1.0 / math.sqrt(dim) if scale is None else scale, out.data_ptr(), oa, ob, lse.data_ptr(),
+          ws.data_ptr(), ws.numel() * ws.element_size())
+    return out, lse
