@@ -105,6 +105,18 @@ __device__ inline void load_bytes(uint32_t *dst, const uint8_t *src)
 
 __device__ inline int byte_of(const uint32_t *w, int j) { return (w[j >> 2] >> (8 * (j & 3))) & 255; }
 
+// 16 bytes of each lane of a wave from memory to LDS, to the 1024 from `dst` on
+// (the same for all lanes), without registers between. A wave's own are there
+// after lds_landed(), all waves' after a barrier behind it.
+__device__ inline void to_lds16(const void *src, void *dst)
+{
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void *)src,
+        (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+}
+
+__device__ inline void lds_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 template <int D, int SUB, bool FP16>
 __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend a, int splits,
                                                              int qblocks)
@@ -128,6 +140,35 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
     float *const part_o = a.part_o + wg * (kKvWaves + 2) * F::kEntry;
     float *const part_ml = a.part_ml + wg * 64;
 
+    // The centres of this head, entries from K up zeros. With all 256 they are
+    // one run of bytes for each book and go straight to LDS, 16 to a lane,
+    // while the lengths below are read.
+    {
+        const uint16_t *ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
+        const uint16_t *vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
+        if (c.K == 256) {
+            static_assert(F::kBook % (kThreads * 16) == 0, "whole rounds of the workgroup");
+#pragma unroll
+            for (int i = 0; i < F::kBook / (kThreads * 16); ++i) {
+                const int at = (i * kThreads + (wave << 6)) * 16;      // of the wave's first lane
+                to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
+                to_lds16(reinterpret_cast<const char *>(vs) + at + lane * 16, vbook + at);
+            }
+        } else {
+            using E = KvEntry<SUB>;
+#pragma unroll 4
+            for (int i = tid; i < F::S * 256; i += kThreads) {
+                const int s = i >> 8, code = i & 255;
+                E ke{}, ve{};
+                if (code < c.K) {
+                    ke = kv_load<SUB>(ks + (s * c.K + code) * SUB);
+                    ve = kv_load<SUB>(vs + (s * c.K + code) * SUB);
+                }
+                reinterpret_cast<E *>(kbook)[i] = ke;
+                reinterpret_cast<E *>(vbook)[i] = ve;
+            }
+        }
+    }
     // Where each sequence's tiles begin in the row of all tiles.
     {
         const int per = (a.seqs + kThreads - 1) / kThreads;
@@ -154,23 +195,7 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
             }
         }
     }
-    // The centres of this head; entries from K up are zeros.
-    {
-        constexpr int n = F::S * 256;
-        using E = KvEntry<SUB>;
-        const uint16_t *ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
-        const uint16_t *vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
-        for (int i = tid; i < n; i += kThreads) {
-            const int s = i >> 8, code = i & 255;
-            E ke{}, ve{};
-            if (code < c.K) {
-                ke = kv_load<SUB>(ks + ((int64_t)s * c.K + code) * SUB);
-                ve = kv_load<SUB>(vs + ((int64_t)s * c.K + code) * SUB);
-            }
-            reinterpret_cast<E *>(kbook)[i] = ke;
-            reinterpret_cast<E *>(vbook)[i] = ve;
-        }
-    }
+    lds_landed();
     __syncthreads();
 
     const int tiles = first[a.seqs];
@@ -213,57 +238,90 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
     };
 
     if (a0 < a1) {
-        int b = 0;
-        for (int lo = 0, hi = a.seqs; lo < hi;) {      // the last b with first[b] <= a0
+        int lo = 0;
+        for (int hi = a.seqs; lo < hi;) {               // the last b with first[b] <= a0
             const int mid = (lo + hi) >> 1;
             if (first[mid + 1] <= a0) lo = mid + 1; else hi = mid;
-            b = lo;
         }
-        b = __builtin_amdgcn_readfirstlane(b);
-        int piece = a0, base = 0, next = 0;
-        Span sp{};
-        bool fresh = true;
-        for (int t = a0; t <= a1; ++t) {
-            if (!fresh && (t == next || t == a1)) {
-                // the piece [piece, t) of sequence b is done
-                const float lw = whole_l();
-                if (piece == base && t == next) {
-                    const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
-                    if (r < nq) {
+        // A place in the row of tiles: sequence b, which has tiles [base, next).
+        struct Cursor {
+            int b, base, next;
+            Span sp;
+        };
+        const auto enter = [&](int b) {
+            Cursor x;
+            x.b = __builtin_amdgcn_readfirstlane(b);
+            x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
+            x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
+            x.sp = span_of(c, a, x.b);
+            return x;
+        };
+        // to tile t (the next one, below a1)
+        const auto advance = [&](Cursor &x, int t) {
+            if (t < x.next) return;
+            int b = x.b + 1;
+            while (first[b + 1] <= t) ++b;
+            x = enter(b);
+        };
+        // Tile t's codes are loaded while t - 1 is worked on, and the numbers of
+        // the pages they lie on while t - 2 is.
+        struct Where {
+            int k_at, v_at;          // first position of the lane's keys and values
+            int k_page, v_page;
+        };
+        const int pm = (1 << c.page_log2) - 1;
+        const auto find = [&](const Cursor &x, int t) {
+            Where w;
+            const int pos = (t - x.base + x.sp.tile0()) * 32;
+            const int low = x.sp.start & ~7, high = (x.sp.len - 1) & ~7;
+            const int32_t *row = a.table + x.b * a.table_stride;
+            // positions outside the span are taken as the nearest inside
+            w.k_at = min(max(pos + 8 * (r >> 2), low), high);
+            w.v_at = min(max(pos + 8 * g, low), high);
+            w.k_page = row[w.k_at >> c.page_log2];
+            w.v_page = row[w.v_at >> c.page_log2];
+            return w;
+        };
+        const auto head_of = [&](int page) {            // codes before this head's on the page
+            const int64_t safe = min(max((int64_t)page, (int64_t)0), c.pages - 1);
+            return ((safe * c.heads + h) << c.page_log2) * F::S;
+        };
+        const auto load = [&](const Where &w) {
+            Codes<D, SUB> cd;
+            const uint8_t *src = c.k_codes + head_of(w.k_page) +
+                                 ((w.k_at & pm) + (r & 3)) * F::S + g * F::SL;
+            load_bytes<F::SL>(cd.k[0], src);
+            load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
+            src = c.v_codes + head_of(w.v_page) + (w.v_at & pm);
 #pragma unroll
-                        for (int n = 0; n < F::NV; ++n)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int d = (16 * (n / F::VS) + 4 * g + i) * F::VS + n % F::VS;
-                                if (d < D) put(b, r, d, acc[n][i] * inv);
-                            }
-                        if (g == 0) put_lse(b, r, m, lw);
-                    }
-                } else {
-                    const int e = 2 * wave + (t == a1);
-                    if (lane == 0) tag[e] = b;
-                    if (g == 0) { ml[e][r] = m; ml[e][16 + r] = lw; }
-                    if (t != a1) {
-#pragma unroll
-                        for (int n = 0; n < F::NV; ++n)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                part_o[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
-                    }
-                }
-                fresh = true;
-                if (t != a1) {
-                    ++b;
-                    while (first[b + 1] <= t) ++b;
-                }
+            for (int hh = 0; hh < F::NH; ++hh) {
+                const int gr = min(16 * hh + r, F::NG - 1);
+                load_bytes<8>(cd.v[hh], src + ((gr * F::VS / SUB) << c.page_log2));
             }
-            if (t == a1) break;
+            return cd;
+        };
+
+        Cursor cur = enter(lo), ahead = cur;
+        Where where = find(ahead, a0);
+        Codes<D, SUB> coming = load(where);
+        if (a0 + 1 < a1) {
+            advance(ahead, a0 + 1);
+            where = find(ahead, a0 + 1);
+        }
+        int piece = a0;
+        bool fresh = true;
+        for (int t = a0; t < a1; ++t) {
+            const int b = cur.b;
+            const Span sp = cur.sp;
+            const Codes<D, SUB> cd = coming;
+            if (t + 1 < a1) coming = load(where);
+            if (t + 2 < a1) {
+                advance(ahead, t + 2);
+                where = find(ahead, t + 2);
+            }
             if (fresh) {
                 fresh = false;
                 piece = t;
-                base = first[b];
-                next = first[b + 1];
-                sp = span_of(c, a, b);
                 m = -INFINITY;
                 l = 0.f;
 #pragma unroll
@@ -278,32 +336,7 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
                         q[st] = *reinterpret_cast<const u4v *>(src + st * 8);
                 }
             }
-            const int pos = (t - base + sp.tile0()) * 32;
-            // codes
-            Codes<D, SUB> cd;
-            const auto page_of = [&](int p) {
-                const int at = min(max(p, sp.start & ~7), (sp.len - 1) & ~7);
-                const int64_t page = a.table[b * a.table_stride + (at >> c.page_log2)];
-                const int64_t safe = min(max(page, (int64_t)0), c.pages - 1);
-                return ((safe * c.heads + h) << c.page_log2) * F::S;
-            };
-            const int pm = (1 << c.page_log2) - 1;
-            {
-                const int p = min(max(pos + 8 * (r >> 2), sp.start & ~7), (sp.len - 1) & ~7);
-                const uint8_t *src = c.k_codes + page_of(pos + 8 * (r >> 2)) +
-                                     ((p & pm) + (r & 3)) * F::S + g * F::SL;
-                load_bytes<F::SL>(cd.k[0], src);
-                load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
-            }
-            {
-                const int p = min(max(pos + 8 * g, sp.start & ~7), (sp.len - 1) & ~7);
-                const uint8_t *src = c.v_codes + page_of(pos + 8 * g) + (p & pm);
-#pragma unroll
-                for (int hh = 0; hh < F::NH; ++hh) {
-                    const int gr = min(16 * hh + r, F::NG - 1);
-                    load_bytes<8>(cd.v[hh], src + ((gr * F::VS / SUB) << c.page_log2));
-                }
-            }
+            const int pos = (t - cur.base + sp.tile0()) * 32;
             // scores: rows are positions, columns queries
             float z[8];
 #pragma unroll
@@ -391,6 +424,35 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
                     acc[hh * F::VS + i] = mfma<FP16>(op, p, acc[hh * F::VS + i]);
                 }
             }
+            if (t + 1 != cur.next && t + 1 != a1) continue;
+            // the piece [piece, t] of sequence b is done
+            const float lw = whole_l();
+            if (piece == cur.base && t + 1 == cur.next) {
+                const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
+                if (r < nq) {
+#pragma unroll
+                    for (int n = 0; n < F::NV; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int d = (16 * (n / F::VS) + 4 * g + i) * F::VS + n % F::VS;
+                            if (d < D) put(b, r, d, acc[n][i] * inv);
+                        }
+                    if (g == 0) put_lse(b, r, m, lw);
+                }
+            } else {
+                const int e = 2 * wave + (t + 1 == a1);
+                if (lane == 0) tag[e] = b;
+                if (g == 0) { ml[e][r] = m; ml[e][16 + r] = lw; }
+                if (t + 1 != a1) {
+#pragma unroll
+                    for (int n = 0; n < F::NV; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            part_o[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
+                }
+            }
+            fresh = true;
+            if (t + 1 < a1) advance(cur, t + 1);
         }
     }
     __syncthreads();
@@ -448,12 +510,17 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
     }
 }
 
-// Joins what the workgroups left of the sequences that several shared.
+// Joins what the workgroups left of the sequences that several shared. A
+// workgroup takes one sequence, one block of a head's queries and 256 of its
+// outputs, one to a thread, so that the sums over up to 512 parts run in
+// parallel.
 template <int D, int SUB, bool FP16>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int splits)
 {
     using F = Form<D, SUB>;
-    const int b = blockIdx.x % a.seqs, hq = blockIdx.x / a.seqs;
+    constexpr int chunks = F::kEntry / 256;
+    const int b = blockIdx.x / chunks % a.seqs, hq = blockIdx.x / chunks / a.seqs;
+    const int x = blockIdx.x % chunks * 256 + threadIdx.x;
     const int h = hq % c.heads, qb = hq / c.heads;
     const int nq = min(kKvQueries, a.group - qb * kKvQueries);
     const int tiles = a.first_tile[a.seqs], p0 = a.first_tile[b], p1 = a.first_tile[b + 1];
@@ -462,33 +529,48 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const int j0 = (int)(((int64_t)(p0 + 1) * used + tiles - 1) / tiles) - 1;
     const int j1 = (int)(((int64_t)p1 * used + tiles - 1) / tiles) - 1;
     if (j0 == j1) return;
-    const int tid = threadIdx.x, q = tid & 15;
-    if (q >= nq) return;
-    const int64_t wg = ((int64_t)qb * c.heads + h) * splits;
-    const auto slot_of = [&](int j) { return p0 < split_begin(tiles, j, used) ? 0 : 1; };
+    // weight of each part, for each query: [part][query]
+    __shared__ float weight[512 * 16];
+    __shared__ float s_top[16 * 16], s_sum[16 * 16];
+    const int tid = threadIdx.x, q = tid & 15, n = j1 - j0 + 1;
+    const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j0;
+    const float *const ml = a.part_ml + wg * 64 + q;
+    const int slot0 = p0 < split_begin(tiles, j0, used) ? 0 : 1;      // later parts: slot 0
     float top = -INFINITY;
-    for (int j = j0; j <= j1; ++j) top = fmaxf(top, a.part_ml[(wg + j) * 64 + slot_of(j) * 32 + q]);
+    for (int i = tid >> 4; i < n; i += 16) {
+        const float v = ml[i * 64 + (i == 0 ? slot0 * 32 : 0)];
+        weight[i * 16 + q] = v;
+        top = fmaxf(top, v);
+    }
+    s_top[tid] = top;
+    __syncthreads();
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s_top[i * 16 + q]);
     const float safe = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    for (int i = tid >> 4; i < n; i += 16) {
+        const float w = exp2f(weight[i * 16 + q] - safe);
+        sum += w * ml[i * 64 + 16 + (i == 0 ? slot0 * 32 : 0)];
+        weight[i * 16 + q] = w;
+    }
+    s_sum[tid] = sum;
+    __syncthreads();
     float lw = 0.f;
-    for (int j = j0; j <= j1; ++j) {
-        const float *ml = a.part_ml + (wg + j) * 64 + slot_of(j) * 32;
-        lw += ml[16 + q] * exp2f(ml[q] - safe);
-    }
-    const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
+    for (int i = 0; i < 16; ++i) lw += s_sum[i * 16 + q];
+    if (q >= nq) return;
     const int head = h * a.group + qb * kKvQueries + q;
-    for (int x = tid; x < F::kEntry; x += 256) {
-        const int n = x >> 8, i = (x >> 6) & 3, gg = (x >> 4) & 3;
-        const int d = (16 * (n / F::VS) + 4 * gg + i) * F::VS + n % F::VS;
-        if (d >= D) continue;
-        float o = 0.f;
-        for (int j = j0; j <= j1; ++j)
-            o += a.part_o[((wg + j) * (kKvWaves + 2) + kKvWaves + slot_of(j)) * F::kEntry + x] *
-                 exp2f(a.part_ml[(wg + j) * 64 + slot_of(j) * 32 + q] - safe);
-        a.out[b * a.out_seq + head * a.out_head + d] = (uint16_t)pack2<FP16>(o * inv, 0.f);
-    }
-    if (a.lse && tid < 16)
+    if (x < 16 && a.lse)
         a.lse[(int64_t)b * c.heads * a.group + head] =
             lw > 0.f || lw != lw ? (top + __log2f(lw)) * 0.69314718055994531f : -INFINITY;
+    const int d = (16 * ((x >> 8) / F::VS) + ((x >> 4) & 3) * 4 + ((x >> 6) & 3)) * F::VS +
+                  (x >> 8) % F::VS;
+    if (d >= D) return;
+    const float *const o0 = a.part_o + (wg * (kKvWaves + 2) + kKvWaves) * F::kEntry + x;
+    float o = weight[q] * o0[slot0 * F::kEntry];
+#pragma unroll 8
+    for (int i = 1; i < n; ++i)
+        o += weight[i * 16 + q] * o0[(int64_t)i * (kKvWaves + 2) * F::kEntry];
+    a.out[b * a.out_seq + head * a.out_head + d] =
+        (uint16_t)pack2<FP16>(lw > 0.f || lw != lw ? o / lw : 0.f, 0.f);
 }
 
 template <int D, int SUB, bool FP16>
@@ -501,7 +583,7 @@ hipError_t launch(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hi
                        p.splits, p.qblocks);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>), dim3((unsigned)a.seqs * c.heads * p.qblocks),
+    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>), dim3((unsigned)a.seqs * c.heads * p.qblocks * (F::kEntry / 256)),
                        dim3(256), 0, s, c, a, p.splits);
     return hipGetLastError();
 }
