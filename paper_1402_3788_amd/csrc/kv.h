@@ -10,7 +10,9 @@ constexpr int kKvMaxSeqs = 4096;
 constexpr int kKvMaxGroup = 128;     // query heads of one key-value head
 constexpr int kKvTile = 32;          // positions of one step of a wave's attention
 constexpr int kKvQueries = 16;       // query heads of one workgroup (columns of an MFMA)
-constexpr int kKvWaves = 8;          // wavefronts of an attention workgroup
+
+// Wavefronts of an attention workgroup.
+constexpr int kv_waves(int dim) { return dim == 64 ? 16 : 8; }
 
 // The cache as the caller describes it (kmeans_kv_t, checked).
 struct KvCache {

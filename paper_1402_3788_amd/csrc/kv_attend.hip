@@ -1,6 +1,8 @@
 // Attention of one new token of every sequence over the cache of codes.
 #include "kv_device.h"
 
+#include <type_traits>
+
 #ifndef KV_SUB
 #define KV_SUB 4
 #endif
@@ -13,7 +15,9 @@ hipError_t launch_kv_attend_8(const KvCache &, const KvAttend &, const KvAttendP
 
 namespace {
 
-constexpr int kThreads = kKvWaves * kWave;
+// How far the reference of the exponents may lie below the largest score before
+// what is summed is scaled: weights stay below 2^8, which fp16 holds.
+constexpr float kLag = 8.f;
 
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
@@ -53,8 +57,17 @@ struct Form {
     static constexpr int NG = D / VS;                  // granules
     static constexpr int NH = (NG + 15) / 16;          // rows of 16 granules
     static constexpr int NV = NH * VS;                 // accumulator tiles
-    static constexpr int kBook = S * 256 * SUB * 2;    // bytes of a head's centres in LDS
+    static constexpr int kWaves = kv_waves(D);
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int kKeys = D * 512;              // LDS bytes of the key centres: [S][256][SUB]
+    static constexpr int kRow = 256;                   // of one code's value centres
+    static constexpr int kValues = 256 * kRow;         // of the value centres: [256][D], rows on 256 bytes
     static constexpr int kEntry = NV * 256;            // floats of one wave's accumulators
+    static constexpr size_t lds_bytes(int seqs)
+    {
+        return kKeys + kValues + (2 * kWaves * 32 + 3 * kWaves + seqs + 1) * 4;
+    }
+    static_assert(kWaves * kEntry * 4 <= kKeys + kValues, "the last pieces fit the centres' place");
 };
 
 // Positions [start, len) of sequence b, and the 32-position tiles they touch.
@@ -75,9 +88,9 @@ __device__ inline Span span_of(const KvCache &c, const KvAttend &a, int b)
 
 // The workgroups that share a head's tiles: no more than leave each a tile
 // for every wave.
-__device__ inline int splits_used(int tiles, int splits)
+__device__ inline int splits_used(int tiles, int splits, int waves)
 {
-    return min(splits, max(1, (tiles + kKvWaves - 1) / kKvWaves));
+    return min(splits, max(1, (tiles + waves - 1) / waves));
 }
 
 __device__ inline int split_begin(int tiles, int j, int used)
@@ -103,7 +116,27 @@ __device__ inline void load_bytes(uint32_t *dst, const uint8_t *src)
     __builtin_memcpy(dst, __builtin_assume_aligned(src, align), N);
 }
 
-__device__ inline int byte_of(const uint32_t *w, int j) { return (w[j >> 2] >> (8 * (j & 3))) & 255; }
+// base + code n * the size of an entry, in two instructions: base has no bits
+// below 256 entries.
+template <int SUB>
+__device__ inline uint32_t code_offset(const uint32_t *w, int n, uint32_t base)
+{
+    constexpr int shift = SUB == 2 ? 2 : SUB == 4 ? 3 : 4;
+    const int low = 8 * (n & 3);
+    const uint32_t at = low < shift ? w[n >> 2] << (shift - low) : w[n >> 2] >> (low - shift);
+    return (at & (255u << shift)) | base;
+}
+
+// The entry at a byte of LDS (the kernel has no LDS but its dynamic one, which
+// so begins at 0).
+template <int N>
+__device__ inline KvEntry<N> lds_entry(uint32_t at)
+{
+    typedef uint32_t V __attribute__((ext_vector_type(N / 2 > 1 ? N / 2 : 2)));
+    typedef std::conditional_t<N == 2, uint32_t, V> T;
+    return __builtin_bit_cast(KvEntry<N>,
+                              *(const __attribute__((address_space(3))) T *)(uintptr_t)at);
+}
 
 // 16 bytes of each lane of a wave from memory to LDS, to the 1024 from `dst` on
 // (the same for all lanes), without registers between. A wave's own are there
@@ -117,18 +150,29 @@ __device__ inline void to_lds16(const void *src, void *dst)
 
 __device__ inline void lds_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-template <int D, int SUB, bool FP16>
-__global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend a, int splits,
-                                                             int qblocks)
+// The value of the lane 8 away in its row of 16.
+__device__ inline float from_8_away(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, true));
+}
+
+// WIDE: more than 8 queries, so that the high and the low parts of the weights
+// are operands of their own. Else the queries stand twice in the 16 columns,
+// the first eight of which take the high parts and the others the low ones.
+template <int D, int SUB, bool FP16, bool WIDE>
+__global__ __launch_bounds__((Form<D, SUB>::kThreads)) void
+kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 {
     using F = Form<D, SUB>;
+    constexpr int W = F::kWaves;
     extern __shared__ uint4 lds[];
-    char *const kbook = reinterpret_cast<char *>(lds);
-    char *const vbook = kbook + F::kBook;
-    int *const first = reinterpret_cast<int *>(vbook + F::kBook);     // [seqs + 1]
-    __shared__ int wave_sum[kKvWaves];
-    __shared__ int tag[2 * kKvWaves];
-    __shared__ float ml[2 * kKvWaves][32];
+    // the values first: their addresses below 2^16 fit the offset of a load
+    char *const vbook = reinterpret_cast<char *>(lds);
+    char *const kbook = vbook + F::kValues;
+    float(*const ml)[32] = reinterpret_cast<float(*)[32]>(kbook + F::kKeys);
+    int *const tag = reinterpret_cast<int *>(ml + 2 * W);
+    int *const wave_sum = tag + 2 * W;
+    int *const first = wave_sum + W;                     // [seqs + 1]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -136,42 +180,54 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
     const int qb = blockIdx.x / c.heads % qblocks;
     const int j = blockIdx.x / c.heads / qblocks;
     const int nq = min(kKvQueries, a.group - qb * kKvQueries);
+    const int rq = WIDE ? r : r & 7;                     // the lane's query
     const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j;
-    float *const part_o = a.part_o + wg * (kKvWaves + 2) * F::kEntry;
+    float *const part_o = a.part_o + wg * (W + 2) * F::kEntry;
     float *const part_ml = a.part_ml + wg * 64;
 
-    // The centres of this head, entries from K up zeros. With all 256 they are
-    // one run of bytes for each book and go straight to LDS, 16 to a lane,
-    // while the lengths below are read.
-    {
-        const uint16_t *ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
-        const uint16_t *vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
-        if (c.K == 256) {
-            static_assert(F::kBook % (kThreads * 16) == 0, "whole rounds of the workgroup");
+    // The centres of this head, entries from K up zeros. With all 256 the keys'
+    // are one run of bytes and go straight to LDS, 16 to a lane, and the
+    // values' wait in registers while the lengths below are read: they are
+    // turned to one row of all features for each code.
+    constexpr int per16 = 8 / SUB;                       // centres in 16 bytes
+    constexpr int rounds = D * 32 / F::kThreads;
+    static_assert(D * 32 % F::kThreads == 0, "whole rounds of the workgroup");
+    const uint16_t *const ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
+    const uint16_t *const vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
+    // lanes: 4 runs of 16 bytes in each of 16 sub-vectors, for whole sectors
+    // from memory and few conflicts in LDS
+    const auto value_s = [&](int i) { return ((i * F::kThreads + tid) >> 2) % F::S; };
+    const auto value_code = [&](int i) {
+        const int n = i * F::kThreads + tid;
+        return ((n >> 2) / F::S * 4 + (n & 3)) * per16;
+    };
+    uint4 vreg[rounds];
+    if (c.K == 256) {
 #pragma unroll
-            for (int i = 0; i < F::kBook / (kThreads * 16); ++i) {
-                const int at = (i * kThreads + (wave << 6)) * 16;      // of the wave's first lane
-                to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
-                to_lds16(reinterpret_cast<const char *>(vs) + at + lane * 16, vbook + at);
-            }
-        } else {
-            using E = KvEntry<SUB>;
+        for (int i = 0; i < rounds; ++i) {
+            const int at = (i * F::kThreads + (wave << 6)) * 16;         // of the wave's first lane
+            to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
+        }
+#pragma unroll
+        for (int i = 0; i < rounds; ++i)
+            vreg[i] = *reinterpret_cast<const uint4 *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
+    } else {
+        using E = KvEntry<SUB>;
 #pragma unroll 4
-            for (int i = tid; i < F::S * 256; i += kThreads) {
-                const int s = i >> 8, code = i & 255;
-                E ke{}, ve{};
-                if (code < c.K) {
-                    ke = kv_load<SUB>(ks + (s * c.K + code) * SUB);
-                    ve = kv_load<SUB>(vs + (s * c.K + code) * SUB);
-                }
-                reinterpret_cast<E *>(kbook)[i] = ke;
-                reinterpret_cast<E *>(vbook)[i] = ve;
+        for (int i = tid; i < F::S * 256; i += F::kThreads) {
+            const int s = i >> 8, code = i & 255;
+            E ke{}, ve{};
+            if (code < c.K) {
+                ke = kv_load<SUB>(ks + (s * c.K + code) * SUB);
+                ve = kv_load<SUB>(vs + (s * c.K + code) * SUB);
             }
+            reinterpret_cast<E *>(kbook)[i] = ke;
+            *reinterpret_cast<E *>(vbook + code * F::kRow + s * (SUB * 2)) = ve;
         }
     }
     // Where each sequence's tiles begin in the row of all tiles.
     {
-        const int per = (a.seqs + kThreads - 1) / kThreads;
+        const int per = (a.seqs + F::kThreads - 1) / F::kThreads;
         int sum = 0;
         for (int i = 0; i < per; ++i) {
             const int b = tid * per + i;
@@ -195,25 +251,36 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
             }
         }
     }
+    if (c.K == 256) {
+#pragma unroll
+        for (int i = 0; i < rounds; ++i) {
+            KvEntry<SUB> e[per16];
+            __builtin_memcpy(e, &vreg[i], 16);
+#pragma unroll
+            for (int x = 0; x < per16; ++x)
+                *reinterpret_cast<KvEntry<SUB> *>(vbook + (value_code(i) + x) * F::kRow +
+                                                  value_s(i) * (SUB * 2)) = e[x];
+        }
+    }
     lds_landed();
     __syncthreads();
 
     const int tiles = first[a.seqs];
-    const int used = splits_used(tiles, splits);
+    const int used = splits_used(tiles, splits, W);
     if (blockIdx.x == 0)
-        for (int b = tid; b <= a.seqs; b += kThreads) a.first_tile[b] = first[b];
+        for (int b = tid; b <= a.seqs; b += F::kThreads) a.first_tile[b] = first[b];
     // Sequences without positions.
     for (int b = j; b < a.seqs; b += splits) {
         if (first[b] != first[b + 1]) continue;
-        for (int i = tid; i < nq * D; i += kThreads)
+        for (int i = tid; i < nq * D; i += F::kThreads)
             a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + i / D) * a.out_head + i % D] = 0;
         if (a.lse && tid < nq)
             a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + tid] = -INFINITY;
     }
     if (j >= used) return;
     const int w0 = split_begin(tiles, j, used), w1 = split_begin(tiles, j + 1, used);
-    const int a0 = w0 + (int)((int64_t)(w1 - w0) * wave / kKvWaves);
-    const int a1 = w0 + (int)((int64_t)(w1 - w0) * (wave + 1) / kKvWaves);
+    const int a0 = w0 + (int)((int64_t)(w1 - w0) * wave / W);
+    const int a1 = w0 + (int)((int64_t)(w1 - w0) * (wave + 1) / W);
 
     // Final output of query q, feature d of sequence b.
     const auto put = [&](int b, int q, int d, float x) {
@@ -227,15 +294,12 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
     };
 
     f4v acc[F::NV];
-    float m = -INFINITY, l = 0.f;
+    // m: what the exponents are taken relative to (base 2), within kLag below
+    // the largest score so far; -inf before the first; m0 is m, or 0 for -inf.
+    // l: the lane's part of the sum of the weights.
+    float m = -INFINITY, m0 = 0.f, l = 0.f;
     u4v q[D / 32];
     if (lane == 0) { tag[2 * wave] = -1; tag[2 * wave + 1] = -1; }
-
-    // Sum of l over the four lanes of a query.
-    const auto whole_l = [&]() {
-        float s = l + __shfl_xor(l, 16);
-        return s + __shfl_xor(s, 32);
-    };
 
     if (a0 < a1) {
         int lo = 0;
@@ -253,7 +317,9 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
             x.b = __builtin_amdgcn_readfirstlane(b);
             x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
             x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
-            x.sp = span_of(c, a, x.b);
+            const Span s = span_of(c, a, x.b);
+            x.sp.start = __builtin_amdgcn_readfirstlane(s.start);
+            x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
             return x;
         };
         // to tile t (the next one, below a1)
@@ -269,7 +335,6 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
             int k_at, v_at;          // first position of the lane's keys and values
             int k_page, v_page;
         };
-        const int pm = (1 << c.page_log2) - 1;
         const auto find = [&](const Cursor &x, int t) {
             Where w;
             const int pos = (t - x.base + x.sp.tile0()) * 32;
@@ -282,23 +347,136 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
             w.v_page = row[w.v_at >> c.page_log2];
             return w;
         };
-        const auto head_of = [&](int page) {            // codes before this head's on the page
-            const int64_t safe = min(max((int64_t)page, (int64_t)0), c.pages - 1);
-            return ((safe * c.heads + h) << c.page_log2) * F::S;
-        };
+        const unsigned pm = (1u << c.page_log2) - 1;
+        const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
+        const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
+        const int64_t head_bytes = ((int64_t)h * F::S) << c.page_log2;
+        const uint8_t *const k_lane = c.k_codes + head_bytes + (r & 3) * F::S + g * F::SL;
+        const uint8_t *const v_lane = c.v_codes + head_bytes;
         const auto load = [&](const Where &w) {
             Codes<D, SUB> cd;
-            const uint8_t *src = c.k_codes + head_of(w.k_page) +
-                                 ((w.k_at & pm) + (r & 3)) * F::S + g * F::SL;
+            // a number that is no page's is some page's here, never followed out
+            const uint8_t *src = k_lane + (uint64_t)min((unsigned)w.k_page, last_page) * page_bytes +
+                                 (w.k_at & pm) * F::S;
             load_bytes<F::SL>(cd.k[0], src);
             load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
-            src = c.v_codes + head_of(w.v_page) + (w.v_at & pm);
+            src = v_lane + (uint64_t)min((unsigned)w.v_page, last_page) * page_bytes + (w.v_at & pm);
 #pragma unroll
             for (int hh = 0; hh < F::NH; ++hh) {
                 const int gr = min(16 * hh + r, F::NG - 1);
-                load_bytes<8>(cd.v[hh], src + ((gr * F::VS / SUB) << c.page_log2));
+                load_bytes<8>(cd.v[hh], src + ((unsigned)(gr * F::VS / SUB) << c.page_log2));
             }
             return cd;
+        };
+        const float scale = fabsf(a.scale_log2);          // its sign is in the queries
+        const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+
+        const uint32_t k_base = F::kValues + g * (F::SL * 512 * SUB);
+        // One tile of 32 positions from `pos` on. What the span leaves out of it
+        // is masked in branches of its own, which most tiles skip.
+        const auto step = [&](const Codes<D, SUB> &cd, int pos, const Span &sp) {
+            const bool partial = pos < sp.start || pos + 32 > sp.len;
+            const auto seen = [&](int i) {
+                const int p = pos + 8 * g + i;
+                return p >= sp.start && p < sp.len;
+            };
+            // All centres of the tile are asked for before any is waited for: a
+            // lookup takes far longer than its turn, and a SIMD has two waves.
+            KvEntry<SUB> ke[2][F::SL];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int n = 0; n < F::SL; ++n)
+                    ke[u][n] = lds_entry<SUB>(code_offset<SUB>(cd.k[u], n, k_base) + n * (512 * SUB));
+            __builtin_amdgcn_sched_barrier(0);
+            KvEntry<F::VS> ve[F::NH][8];
+#pragma unroll
+            for (int hh = 0; hh < F::NH; ++hh)
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    // code * 256 + the granule's place in the row, in one byte selection
+                    ve[hh][x] = lds_entry<F::VS>(
+                        __builtin_amdgcn_perm(cd.v[hh][x >> 2],
+                                              (uint32_t)(min(16 * hh + r, F::NG - 1) * F::VS * 2),
+                                              0x0C0C0000u | (4 + (x & 3)) << 8));
+            __builtin_amdgcn_sched_barrier(0);
+            // scores: rows are positions, columns queries
+            float z[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f4v s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < D / 32; ++st) {
+                    u4v op;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) op[i] = ke[u][(st * 8 + 2 * i) / SUB].w[i % (SUB / 2)];
+                    s = mfma<FP16>(op, q[st], s);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * u + i] = s[i];
+            }
+            if (partial) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = seen(i) ? z[i] : -INFINITY;
+            }
+            float top = fmaxf(z[0], z[1]);
+#pragma unroll
+            for (int i = 2; i < 8; ++i) top = fmaxf(top, z[i]);
+            top *= scale;
+            if (__any(!(top <= m + kLag))) {              // NaN included
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                top = fmaxf(top, m);
+                m0 = top == -INFINITY ? 0.f : top;
+                const float alpha = __builtin_amdgcn_exp2f(m - m0);
+                m = top;
+                l *= alpha;
+#pragma unroll
+                for (int n = 0; n < F::NV; ++n) acc[n] *= alpha;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = __builtin_fmaf(z[i], scale, -m0);
+            if (partial) {                                // again: a scale of 0 gave NaN
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = seen(i) ? z[i] : -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[i] = __builtin_amdgcn_exp2f(z[i]);
+                l += z[i];
+            }
+            // each weight as the sum of two 16-bit numbers: one alone (8 bits of
+            // bf16) would cost as much of the result as its own final rounding
+            u4v p, p_lo;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[i] = pack2<FP16>(z[2 * i], z[2 * i + 1]);
+                p_lo[i] = pack2<FP16>(z[2 * i] - kv_float<FP16>(p[i] & 0xFFFFu),
+                                      z[2 * i + 1] - kv_float<FP16>(p[i] >> 16));
+                if (!WIDE) p[i] = r < 8 ? p[i] : p_lo[i];
+            }
+            // values: rows are features, columns queries
+#pragma unroll
+            for (int hh = 0; hh < F::NH; ++hh) {
+                KvEntry<F::VS> (&e)[8] = ve[hh];
+                if (partial) {                            // 0 weighs nothing, not 0 * NaN
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+#pragma unroll
+                        for (int w = 0; w < F::VS / 2; ++w) e[x].w[w] = seen(x) ? e[x].w[w] : 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < F::VS; ++i) {
+                    u4v op;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        op[x] = __builtin_amdgcn_perm(e[2 * x + 1].w[i / 2], e[2 * x].w[i / 2],
+                                                      i % 2 ? 0x07060302u : 0x05040100u);
+                    f4v &o = acc[hh * F::VS + i];
+                    if (WIDE) o = mfma<FP16>(op, p_lo, o);
+                    o = mfma<FP16>(op, p, o);
+                }
+            }
         };
 
         Cursor cur = enter(lo), ahead = cur;
@@ -312,7 +490,6 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
         bool fresh = true;
         for (int t = a0; t < a1; ++t) {
             const int b = cur.b;
-            const Span sp = cur.sp;
             const Codes<D, SUB> cd = coming;
             if (t + 1 < a1) coming = load(where);
             if (t + 2 < a1) {
@@ -323,110 +500,35 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
                 fresh = false;
                 piece = t;
                 m = -INFINITY;
+                m0 = 0.f;
                 l = 0.f;
 #pragma unroll
                 for (int n = 0; n < F::NV; ++n) acc[n] = f4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int st = 0; st < D / 32; ++st) q[st] = u4v{0, 0, 0, 0};
-                if (r < nq) {
+                if (rq < nq) {
                     const uint16_t *src = a.q + b * a.q_seq +
-                                          (h * a.group + qb * kKvQueries + r) * a.q_head + g * (D / 4);
+                                          (h * a.group + qb * kKvQueries + rq) * a.q_head + g * (D / 4);
 #pragma unroll
-                    for (int st = 0; st < D / 32; ++st)
+                    for (int st = 0; st < D / 32; ++st) {
                         q[st] = *reinterpret_cast<const u4v *>(src + st * 8);
-                }
-            }
-            const int pos = (t - cur.base + sp.tile0()) * 32;
-            // scores: rows are positions, columns queries
-            float z[8];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                f4v s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int st = 0; st < D / 32; ++st) {
-                    u4v op;
-                    constexpr int per = 8 / SUB;
-#pragma unroll
-                    for (int x = 0; x < per; ++x) {
-                        const int code = byte_of(cd.k[u], st * per + x);
-                        const KvEntry<SUB> e = reinterpret_cast<const KvEntry<SUB> *>(
-                            kbook)[((g * F::SL + st * per + x) << 8) + code];
-#pragma unroll
-                        for (int w = 0; w < SUB / 2; ++w) op[x * (SUB / 2) + w] = e.w[w];
+                        for (int i = 0; i < 4; ++i) q[st][i] ^= flip;
                     }
-                    s = mfma<FP16>(op, q[st], s);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z[4 * u + i] = s[i] * a.scale_log2;
-            }
-            const bool partial = pos < sp.start || pos + 32 > sp.len;
-            if (partial) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int p = pos + 8 * g + i;
-                    if (p < sp.start || p >= sp.len) z[i] = -INFINITY;
                 }
             }
-            float top = z[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float mn = fmaxf(m, top);
-            const float safe = mn == -INFINITY ? 0.f : mn;
-            const float alpha = exp2f(m - safe);
-            m = mn;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[i] = exp2f(z[i] - safe);
-                sum += z[i];
-            }
-            l = l * alpha + sum;
-#pragma unroll
-            for (int n = 0; n < F::NV; ++n) acc[n] *= alpha;
-            // each weight as the sum of two 16-bit numbers: one alone (8 bits of
-            // bf16) would cost as much of the result as its own final rounding
-            u4v p, p_lo;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[i] = pack2<FP16>(z[2 * i], z[2 * i + 1]);
-                p_lo[i] = pack2<FP16>(z[2 * i] - kv_float<FP16>(p[i] & 0xFFFFu),
-                                      z[2 * i + 1] - kv_float<FP16>(p[i] >> 16));
-            }
-            // values: rows are features, columns queries
-            u4v keep = {~0u, ~0u, ~0u, ~0u};
-            if (partial) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int p0 = pos + 8 * g + 2 * i;
-                    keep[i] = (p0 >= sp.start && p0 < sp.len ? 0xFFFFu : 0u) |
-                              (p0 + 1 >= sp.start && p0 + 1 < sp.len ? 0xFFFF0000u : 0u);
-                }
-            }
-#pragma unroll
-            for (int hh = 0; hh < F::NH; ++hh) {
-                const int gr = min(16 * hh + r, F::NG - 1);
-                const int s = gr * F::VS / SUB, half = gr * F::VS % SUB / F::VS;
-                KvEntry<F::VS> e[8];
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    e[x] = *reinterpret_cast<const KvEntry<F::VS> *>(
-                        vbook + ((s << 8) + byte_of(cd.v[hh], x)) * (SUB * 2) + half * (F::VS * 2));
-#pragma unroll
-                for (int i = 0; i < F::VS; ++i) {
-                    u4v op;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        op[x] = __builtin_amdgcn_perm(e[2 * x + 1].w[i / 2], e[2 * x].w[i / 2],
-                                                      i % 2 ? 0x07060302u : 0x05040100u) & keep[x];
-                    acc[hh * F::VS + i] = mfma<FP16>(op, p_lo, acc[hh * F::VS + i]);
-                    acc[hh * F::VS + i] = mfma<FP16>(op, p, acc[hh * F::VS + i]);
-                }
-            }
+            const int pos = (t - cur.base + cur.sp.tile0()) * 32;
+            step(cd, pos, cur.sp);
             if (t + 1 != cur.next && t + 1 != a1) continue;
             // the piece [piece, t] of sequence b is done
-            const float lw = whole_l();
+            float lw = l + __shfl_xor(l, 16);
+            lw += __shfl_xor(lw, 32);
+            if (!WIDE) {
+#pragma unroll
+                for (int n = 0; n < F::NV; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][i] += from_8_away(acc[n][i]);
+            }
             if (piece == cur.base && t + 1 == cur.next) {
                 const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
                 if (r < nq) {
@@ -466,11 +568,11 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
                 last[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
     }
     __syncthreads();
-    for (int e0 = 0; e0 < 2 * kKvWaves;) {
+    for (int e0 = 0; e0 < 2 * W;) {
         const int b = tag[e0];
         if (b < 0) { ++e0; continue; }
         int e1 = e0 + 1;
-        while (e1 < 2 * kKvWaves && (tag[e1] == b || tag[e1] < 0)) ++e1;
+        while (e1 < 2 * W && (tag[e1] == b || tag[e1] < 0)) ++e1;
         const bool whole = first[b] >= w0 && first[b + 1] <= w1;
         const int slot = first[b] < w0 ? 0 : 1;
         const int qq = tid & 15;
@@ -480,21 +582,21 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
         const float safe = top == -INFINITY ? 0.f : top;
         float lw = 0.f;
         for (int e = e0; e < e1; ++e)
-            if (tag[e] == b) lw += ml[e][16 + qq] * exp2f(ml[e][qq] - safe);
+            if (tag[e] == b) lw += ml[e][16 + qq] * __builtin_amdgcn_exp2f(ml[e][qq] - safe);
         const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
         if (qq < nq) {
-            for (int x = tid; x < F::kEntry; x += kThreads) {
+            for (int x = tid; x < F::kEntry; x += F::kThreads) {
                 float o = 0.f;
                 for (int e = e0; e < e1; ++e)
                     if (tag[e] == b)
                         o += (e & 1 ? last[(e >> 1) * F::kEntry + x] : part_o[(e >> 1) * F::kEntry + x]) *
-                             exp2f(ml[e][qq] - safe);
+                             __builtin_amdgcn_exp2f(ml[e][qq] - safe);
                 if (whole) {
                     const int n = x >> 8, i = (x >> 6) & 3, gg = (x >> 4) & 3;
                     const int d = (16 * (n / F::VS) + 4 * gg + i) * F::VS + n % F::VS;
                     if (d < D) put(b, qq, d, o * inv);
                 } else {
-                    part_o[(kKvWaves + slot) * F::kEntry + x] = o;
+                    part_o[(W + slot) * F::kEntry + x] = o;
                 }
             }
             if (tid < 16) {
@@ -512,7 +614,7 @@ __global__ __launch_bounds__(kThreads) void kv_attend_kernel(KvCache c, KvAttend
 
 // Joins what the workgroups left of the sequences that several shared. A
 // workgroup takes one sequence, one block of a head's queries and 256 of its
-// outputs, one to a thread, so that the sums over up to 512 parts run in
+// outputs, one to a thread, so that the sums over up to 256 parts run in
 // parallel.
 template <int D, int SUB, bool FP16>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int splits)
@@ -525,12 +627,12 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const int nq = min(kKvQueries, a.group - qb * kKvQueries);
     const int tiles = a.first_tile[a.seqs], p0 = a.first_tile[b], p1 = a.first_tile[b + 1];
     if (p0 == p1) return;
-    const int used = splits_used(tiles, splits);
+    const int used = splits_used(tiles, splits, F::kWaves);
     const int j0 = (int)(((int64_t)(p0 + 1) * used + tiles - 1) / tiles) - 1;
     const int j1 = (int)(((int64_t)p1 * used + tiles - 1) / tiles) - 1;
     if (j0 == j1) return;
     // weight of each part, for each query: [part][query]
-    __shared__ float weight[512 * 16];
+    __shared__ float weight[kCUs * 16];
     __shared__ float s_top[16 * 16], s_sum[16 * 16];
     const int tid = threadIdx.x, q = tid & 15, n = j1 - j0 + 1;
     const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j0;
@@ -548,7 +650,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const float safe = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
     for (int i = tid >> 4; i < n; i += 16) {
-        const float w = exp2f(weight[i * 16 + q] - safe);
+        const float w = __builtin_amdgcn_exp2f(weight[i * 16 + q] - safe);
         sum += w * ml[i * 64 + 16 + (i == 0 ? slot0 * 32 : 0)];
         weight[i * 16 + q] = w;
     }
@@ -564,11 +666,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const int d = (16 * ((x >> 8) / F::VS) + ((x >> 4) & 3) * 4 + ((x >> 6) & 3)) * F::VS +
                   (x >> 8) % F::VS;
     if (d >= D) return;
-    const float *const o0 = a.part_o + (wg * (kKvWaves + 2) + kKvWaves) * F::kEntry + x;
+    const float *const o0 = a.part_o + (wg * (F::kWaves + 2) + F::kWaves) * F::kEntry + x;
     float o = weight[q] * o0[slot0 * F::kEntry];
 #pragma unroll 8
     for (int i = 1; i < n; ++i)
-        o += weight[i * 16 + q] * o0[(int64_t)i * (kKvWaves + 2) * F::kEntry];
+        o += weight[i * 16 + q] * o0[(int64_t)i * (F::kWaves + 2) * F::kEntry];
     a.out[b * a.out_seq + head * a.out_head + d] =
         (uint16_t)pack2<FP16>(lw > 0.f || lw != lw ? o / lw : 0.f, 0.f);
 }
@@ -577,14 +679,19 @@ template <int D, int SUB, bool FP16>
 hipError_t launch(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hipStream_t s)
 {
     using F = Form<D, SUB>;
-    const size_t lds = 2 * F::kBook + (a.seqs + 1) * sizeof(int);
+    const size_t lds = F::lds_bytes(a.seqs);
     const unsigned grid = (unsigned)c.heads * p.qblocks * p.splits;
-    hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16>), dim3(grid), dim3(kThreads), lds, s, c, a,
-                       p.splits, p.qblocks);
+    if (a.group > kKvQueries / 2)
+        hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16, true>), dim3(grid), dim3(F::kThreads), lds,
+                           s, c, a, p.splits, p.qblocks);
+    else
+        hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16, false>), dim3(grid), dim3(F::kThreads), lds,
+                           s, c, a, p.splits, p.qblocks);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>), dim3((unsigned)a.seqs * c.heads * p.qblocks * (F::kEntry / 256)),
-                       dim3(256), 0, s, c, a, p.splits);
+    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>),
+                       dim3((unsigned)a.seqs * c.heads * p.qblocks * (F::kEntry / 256)), dim3(256), 0,
+                       s, c, a, p.splits);
     return hipGetLastError();
 }
 
@@ -612,9 +719,10 @@ KvAttendPlan plan_kv_attend(const KvCache &c, int seqs, int group, int64_t table
     p.qblocks = (group + kKvQueries - 1) / kKvQueries;
     const int64_t span = table_pages << c.page_log2;
     const int64_t tiles = seqs * ((span + kKvTile - 1) / kKvTile);
-    const int per_cu = c.dim == 64 ? 2 : 1;      // workgroups whose centres fit a CU's LDS
-    int64_t splits = (int64_t)kCUs * per_cu / (c.heads * p.qblocks);
-    if (splits > (tiles + kKvWaves - 1) / kKvWaves) splits = (tiles + kKvWaves - 1) / kKvWaves;
+    // one workgroup to a CU: the centres fill its LDS
+    int64_t splits = (int64_t)kCUs / (c.heads * p.qblocks);
+    const int waves = kv_waves(c.dim);
+    if (splits > (tiles + waves - 1) / waves) splits = (tiles + waves - 1) / waves;
     p.splits = splits < 1 ? 1 : (int)splits;
     const int gran = c.sub < 4 ? c.sub : 4;
     const size_t entry = (size_t)((c.dim / gran + 15) / 16 * gran) * 256 * sizeof(float);
@@ -622,7 +730,7 @@ KvAttendPlan plan_kv_attend(const KvCache &c, int seqs, int group, int64_t table
     const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     p.first_tile_off = 0;
     p.part_o_off = up((size_t)(seqs + 1) * sizeof(int32_t));
-    p.part_ml_off = p.part_o_off + wgs * (kKvWaves + 2) * entry;
+    p.part_ml_off = p.part_o_off + wgs * (waves + 2) * entry;
     p.total = p.part_ml_off + up(wgs * 64 * sizeof(float));
     return p;
 }

@@ -17,7 +17,7 @@ __device__ inline float kv_float(uint32_t bits)
 
 // SUB packed 16-bit features, two to a dword.
 template <int SUB>
-struct KvEntry {
+struct alignas(SUB * 2) KvEntry {
     uint32_t w[SUB / 2];
 };
 
