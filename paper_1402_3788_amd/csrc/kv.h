@@ -12,7 +12,7 @@ constexpr int kKvTile = 32;          // positions of one step of a wave's attent
 constexpr int kKvQueries = 16;       // query heads of one workgroup (columns of an MFMA)
 
 // Wavefronts of an attention workgroup.
-constexpr int kv_waves(int dim) { return dim == 64 ? 16 : 8; }
+constexpr int kv_waves(int dim) { return dim == 64 ? 16 : 12; }
 
 // The cache as the caller describes it (kmeans_kv_t, checked).
 struct KvCache {

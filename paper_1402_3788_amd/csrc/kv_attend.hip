@@ -63,11 +63,20 @@ struct Form {
     static constexpr int kRow = 256;                   // of one code's value centres
     static constexpr int kValues = 256 * kRow;         // of the value centres: [256][D], rows on 256 bytes
     static constexpr int kEntry = NV * 256;            // floats of one wave's accumulators
+    // the centres, whose place the waves' last pieces take at the end
+    static constexpr int kRoom = kKeys + kValues > kWaves * kEntry * 4 ? kKeys + kValues
+                                                                       : kWaves * kEntry * 4;
+    // the feature of place x among a wave's accumulators (from D up: none)
+    static __device__ int feature(int x)
+    {
+        const int n = x >> 8, i = (x >> 6) & 3, g = (x >> 4) & 3;
+        return (16 * (n / VS) + 4 * g + i) * VS + n % VS;
+    }
     static constexpr size_t lds_bytes(int seqs)
     {
-        return kKeys + kValues + (2 * kWaves * 32 + 3 * kWaves + seqs + 1) * 4;
+        return kRoom + (4 * kWaves * 32 + 3 * kWaves + seqs + 1) * 4;
     }
-    static_assert(kWaves * kEntry * 4 <= kKeys + kValues, "the last pieces fit the centres' place");
+    static_assert(kRoom + (4 * kWaves * 32 + 3 * kWaves + kKvMaxSeqs + 1) * 4 <= kMaxLds, "LDS");
 };
 
 // Positions [start, len) of sequence b, and the 32-position tiles they touch.
@@ -93,9 +102,18 @@ __device__ inline int splits_used(int tiles, int splits, int waves)
     return min(splits, max(1, (tiles + waves - 1) / waves));
 }
 
-__device__ inline int split_begin(int tiles, int j, int used)
+// Even shares of n things: where share i of k begins (the first n % k shares
+// have one more), and the share that thing t is in.
+__device__ inline int share_begin(int n, int i, int k)
 {
-    return (int)((int64_t)tiles * j / used);
+    return (int)((unsigned)n / (unsigned)k) * i + min(i, (int)((unsigned)n % (unsigned)k));
+}
+
+__device__ inline int share_of(int n, int t, int k)
+{
+    const unsigned each = (unsigned)n / (unsigned)k, more = (unsigned)n % (unsigned)k;
+    const unsigned long_end = more * (each + 1);
+    return (int)((unsigned)t < long_end ? (unsigned)t / (each + 1) : more + ((unsigned)t - long_end) / each);
 }
 
 // Codes of one tile of 32 positions in a lane. Keys: position 8 (r / 4) + 4 t +
@@ -169,8 +187,9 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     // the values first: their addresses below 2^16 fit the offset of a load
     char *const vbook = reinterpret_cast<char *>(lds);
     char *const kbook = vbook + F::kValues;
-    float(*const ml)[32] = reinterpret_cast<float(*)[32]>(kbook + F::kKeys);
-    int *const tag = reinterpret_cast<int *>(ml + 2 * W);
+    float(*const ml)[32] = reinterpret_cast<float(*)[32]>(vbook + F::kRoom);
+    float(*const weight)[32] = ml + 2 * W;
+    int *const tag = reinterpret_cast<int *>(ml + 4 * W);
     int *const wave_sum = tag + 2 * W;
     int *const first = wave_sum + W;                     // [seqs + 1]
 
@@ -190,8 +209,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     // values' wait in registers while the lengths below are read: they are
     // turned to one row of all features for each code.
     constexpr int per16 = 8 / SUB;                       // centres in 16 bytes
-    constexpr int rounds = D * 32 / F::kThreads;
-    static_assert(D * 32 % F::kThreads == 0, "whole rounds of the workgroup");
+    constexpr int rounds = (D * 32 + F::kThreads - 1) / F::kThreads;
+    static_assert(D * 32 % kWave == 0, "whole waves");
     const uint16_t *const ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
     const uint16_t *const vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
     // lanes: 4 runs of 16 bytes in each of 16 sub-vectors, for whole sectors
@@ -206,11 +225,12 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
         for (int i = 0; i < rounds; ++i) {
             const int at = (i * F::kThreads + (wave << 6)) * 16;         // of the wave's first lane
-            to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
+            if (at < F::kKeys) to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
         }
 #pragma unroll
         for (int i = 0; i < rounds; ++i)
-            vreg[i] = *reinterpret_cast<const uint4 *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
+            if (i * F::kThreads + tid < D * 32)
+                vreg[i] = *reinterpret_cast<const uint4 *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
     } else {
         using E = KvEntry<SUB>;
 #pragma unroll 4
@@ -246,25 +266,12 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             const int b = tid * per + i;
             if (b < a.seqs) {
                 first[b] = at;
-                at += span_of(c, a, b).tiles();
+                at += per == 1 ? sum : span_of(c, a, b).tiles();
                 if (b == a.seqs - 1) first[a.seqs] = at;
             }
         }
     }
-    if (c.K == 256) {
-#pragma unroll
-        for (int i = 0; i < rounds; ++i) {
-            KvEntry<SUB> e[per16];
-            __builtin_memcpy(e, &vreg[i], 16);
-#pragma unroll
-            for (int x = 0; x < per16; ++x)
-                *reinterpret_cast<KvEntry<SUB> *>(vbook + (value_code(i) + x) * F::kRow +
-                                                  value_s(i) * (SUB * 2)) = e[x];
-        }
-    }
-    lds_landed();
     __syncthreads();
-
     const int tiles = first[a.seqs];
     const int used = splits_used(tiles, splits, W);
     if (blockIdx.x == 0)
@@ -278,9 +285,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + tid] = -INFINITY;
     }
     if (j >= used) return;
-    const int w0 = split_begin(tiles, j, used), w1 = split_begin(tiles, j + 1, used);
-    const int a0 = w0 + (int)((int64_t)(w1 - w0) * wave / W);
-    const int a1 = w0 + (int)((int64_t)(w1 - w0) * (wave + 1) / W);
+    const int w0 = share_begin(tiles, j, used), w1 = share_begin(tiles, j + 1, used);
+    const int a0 = w0 + share_begin(w1 - w0, wave, W), a1 = w0 + share_begin(w1 - w0, wave + 1, W);
 
     // Final output of query q, feature d of sequence b.
     const auto put = [&](int b, int q, int d, float x) {
@@ -301,76 +307,121 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     u4v q[D / 32];
     if (lane == 0) { tag[2 * wave] = -1; tag[2 * wave + 1] = -1; }
 
+    // A place in the row of tiles: sequence b, which has tiles [base, next).
+    struct Cursor {
+        int b, base, next;
+        Span sp;
+    };
+    const auto enter = [&](int b) {
+        Cursor x;
+        x.b = __builtin_amdgcn_readfirstlane(b);
+        x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
+        x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
+        const Span s = span_of(c, a, x.b);
+        x.sp.start = __builtin_amdgcn_readfirstlane(s.start);
+        x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
+        return x;
+    };
+    // to tile t (the next one, below a1)
+    const auto advance = [&](Cursor &x, int t) {
+        if (t < x.next) return;
+        int b = x.b + 1;
+        while (first[b + 1] <= t) ++b;
+        x = enter(b);
+    };
+    // Tile t's codes are loaded while t - 1 is worked on, and the numbers of
+    // the pages they lie on while t - 2 is.
+    struct Where {
+        int k_at, v_at;          // first position of the lane's keys and values
+        int k_page, v_page;
+    };
+    const auto find = [&](const Cursor &x, int t) {
+        Where w;
+        const int pos = (t - x.base + x.sp.tile0()) * 32;
+        const int low = x.sp.start & ~7, high = (x.sp.len - 1) & ~7;
+        const int32_t *row = a.table + x.b * a.table_stride;
+        // positions outside the span are taken as the nearest inside
+        w.k_at = min(max(pos + 8 * (r >> 2), low), high);
+        w.v_at = min(max(pos + 8 * g, low), high);
+        w.k_page = row[w.k_at >> c.page_log2];
+        w.v_page = row[w.v_at >> c.page_log2];
+        return w;
+    };
+    const unsigned pm = (1u << c.page_log2) - 1;
+    const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
+    const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
+    const int64_t head_bytes = ((int64_t)h * F::S) << c.page_log2;
+    const uint8_t *const k_lane = c.k_codes + head_bytes + (r & 3) * F::S + g * F::SL;
+    const uint8_t *const v_lane = c.v_codes + head_bytes;
+    const auto load = [&](const Where &w) {
+        Codes<D, SUB> cd;
+        // a number that is no page's is some page's here, never followed out
+        const uint8_t *src = k_lane + (uint64_t)min((unsigned)w.k_page, last_page) * page_bytes +
+                             (w.k_at & pm) * F::S;
+        load_bytes<F::SL>(cd.k[0], src);
+        load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
+        src = v_lane + (uint64_t)min((unsigned)w.v_page, last_page) * page_bytes + (w.v_at & pm);
+#pragma unroll
+        for (int hh = 0; hh < F::NH; ++hh) {
+            const int gr = min(16 * hh + r, F::NG - 1);
+            load_bytes<8>(cd.v[hh], src + ((unsigned)(gr * F::VS / SUB) << c.page_log2));
+        }
+        return cd;
+    };
+    const float scale = fabsf(a.scale_log2);
+    const bool negative = a.scale_log2 < 0.f;
+
+    const auto load_q = [&](int b) {
+#pragma unroll
+        for (int st = 0; st < D / 32; ++st) q[st] = u4v{0, 0, 0, 0};
+        if (rq < nq) {
+            const uint16_t *src = a.q + b * a.q_seq +
+                                  (h * a.group + qb * kKvQueries + rq) * a.q_head + g * (D / 4);
+#pragma unroll
+            for (int st = 0; st < D / 32; ++st)
+                q[st] = *reinterpret_cast<const u4v *>(src + st * 8);
+        }
+        m = -INFINITY;
+        m0 = 0.f;
+        l = 0.f;
+#pragma unroll
+        for (int n = 0; n < F::NV; ++n) acc[n] = f4v{0.f, 0.f, 0.f, 0.f};
+    };
+    // The first tiles' loads are on their way before the centres are waited for.
+    Cursor cur{}, ahead{};
+    Where where{};
+    Codes<D, SUB> coming;
     if (a0 < a1) {
         int lo = 0;
         for (int hi = a.seqs; lo < hi;) {               // the last b with first[b] <= a0
             const int mid = (lo + hi) >> 1;
             if (first[mid + 1] <= a0) lo = mid + 1; else hi = mid;
         }
-        // A place in the row of tiles: sequence b, which has tiles [base, next).
-        struct Cursor {
-            int b, base, next;
-            Span sp;
-        };
-        const auto enter = [&](int b) {
-            Cursor x;
-            x.b = __builtin_amdgcn_readfirstlane(b);
-            x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
-            x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
-            const Span s = span_of(c, a, x.b);
-            x.sp.start = __builtin_amdgcn_readfirstlane(s.start);
-            x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
-            return x;
-        };
-        // to tile t (the next one, below a1)
-        const auto advance = [&](Cursor &x, int t) {
-            if (t < x.next) return;
-            int b = x.b + 1;
-            while (first[b + 1] <= t) ++b;
-            x = enter(b);
-        };
-        // Tile t's codes are loaded while t - 1 is worked on, and the numbers of
-        // the pages they lie on while t - 2 is.
-        struct Where {
-            int k_at, v_at;          // first position of the lane's keys and values
-            int k_page, v_page;
-        };
-        const auto find = [&](const Cursor &x, int t) {
-            Where w;
-            const int pos = (t - x.base + x.sp.tile0()) * 32;
-            const int low = x.sp.start & ~7, high = (x.sp.len - 1) & ~7;
-            const int32_t *row = a.table + x.b * a.table_stride;
-            // positions outside the span are taken as the nearest inside
-            w.k_at = min(max(pos + 8 * (r >> 2), low), high);
-            w.v_at = min(max(pos + 8 * g, low), high);
-            w.k_page = row[w.k_at >> c.page_log2];
-            w.v_page = row[w.v_at >> c.page_log2];
-            return w;
-        };
-        const unsigned pm = (1u << c.page_log2) - 1;
-        const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
-        const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
-        const int64_t head_bytes = ((int64_t)h * F::S) << c.page_log2;
-        const uint8_t *const k_lane = c.k_codes + head_bytes + (r & 3) * F::S + g * F::SL;
-        const uint8_t *const v_lane = c.v_codes + head_bytes;
-        const auto load = [&](const Where &w) {
-            Codes<D, SUB> cd;
-            // a number that is no page's is some page's here, never followed out
-            const uint8_t *src = k_lane + (uint64_t)min((unsigned)w.k_page, last_page) * page_bytes +
-                                 (w.k_at & pm) * F::S;
-            load_bytes<F::SL>(cd.k[0], src);
-            load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
-            src = v_lane + (uint64_t)min((unsigned)w.v_page, last_page) * page_bytes + (w.v_at & pm);
+        cur = ahead = enter(lo);
+        where = find(ahead, a0);
+        load_q(cur.b);
+        coming = load(where);
+        if (a0 + 1 < a1) {
+            advance(ahead, a0 + 1);
+            where = find(ahead, a0 + 1);
+        }
+    }
+    if (c.K == 256) {
 #pragma unroll
-            for (int hh = 0; hh < F::NH; ++hh) {
-                const int gr = min(16 * hh + r, F::NG - 1);
-                load_bytes<8>(cd.v[hh], src + ((unsigned)(gr * F::VS / SUB) << c.page_log2));
-            }
-            return cd;
-        };
-        const float scale = fabsf(a.scale_log2);          // its sign is in the queries
-        const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+        for (int i = 0; i < rounds; ++i) {
+            if (i * F::kThreads + tid >= D * 32) break;
+            KvEntry<SUB> e[per16];
+            __builtin_memcpy(e, &vreg[i], 16);
+#pragma unroll
+            for (int x = 0; x < per16; ++x)
+                *reinterpret_cast<KvEntry<SUB> *>(vbook + (value_code(i) + x) * F::kRow +
+                                                  value_s(i) * (SUB * 2)) = e[x];
+        }
+    }
+    lds_landed();
+    __syncthreads();
 
+    if (a0 < a1) {
         const uint32_t k_base = F::kValues + g * (F::SL * 512 * SUB);
         // One tile of 32 positions from `pos` on. What the span leaves out of it
         // is masked in branches of its own, which most tiles skip.
@@ -389,17 +440,6 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 for (int n = 0; n < F::SL; ++n)
                     ke[u][n] = lds_entry<SUB>(code_offset<SUB>(cd.k[u], n, k_base) + n * (512 * SUB));
             __builtin_amdgcn_sched_barrier(0);
-            KvEntry<F::VS> ve[F::NH][8];
-#pragma unroll
-            for (int hh = 0; hh < F::NH; ++hh)
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    // code * 256 + the granule's place in the row, in one byte selection
-                    ve[hh][x] = lds_entry<F::VS>(
-                        __builtin_amdgcn_perm(cd.v[hh][x >> 2],
-                                              (uint32_t)(min(16 * hh + r, F::NG - 1) * F::VS * 2),
-                                              0x0C0C0000u | (4 + (x & 3)) << 8));
-            __builtin_amdgcn_sched_barrier(0);
             // scores: rows are positions, columns queries
             float z[8];
 #pragma unroll
@@ -414,6 +454,22 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) z[4 * u + i] = s[i];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            KvEntry<F::VS> ve[F::NH][8];
+#pragma unroll
+            for (int hh = 0; hh < F::NH; ++hh)
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    // code * 256 + the granule's place in the row, in one byte selection
+                    ve[hh][x] = lds_entry<F::VS>(
+                        __builtin_amdgcn_perm(cd.v[hh][x >> 2],
+                                              (uint32_t)(min(16 * hh + r, F::NG - 1) * F::VS * 2),
+                                              0x0C0C0000u | (4 + (x & 3)) << 8));
+            __builtin_amdgcn_sched_barrier(0);
+            if (negative) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = -z[i];
             }
             if (partial) {
 #pragma unroll
@@ -479,15 +535,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             }
         };
 
-        Cursor cur = enter(lo), ahead = cur;
-        Where where = find(ahead, a0);
-        Codes<D, SUB> coming = load(where);
-        if (a0 + 1 < a1) {
-            advance(ahead, a0 + 1);
-            where = find(ahead, a0 + 1);
-        }
         int piece = a0;
-        bool fresh = true;
         for (int t = a0; t < a1; ++t) {
             const int b = cur.b;
             const Codes<D, SUB> cd = coming;
@@ -495,27 +543,6 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             if (t + 2 < a1) {
                 advance(ahead, t + 2);
                 where = find(ahead, t + 2);
-            }
-            if (fresh) {
-                fresh = false;
-                piece = t;
-                m = -INFINITY;
-                m0 = 0.f;
-                l = 0.f;
-#pragma unroll
-                for (int n = 0; n < F::NV; ++n) acc[n] = f4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int st = 0; st < D / 32; ++st) q[st] = u4v{0, 0, 0, 0};
-                if (rq < nq) {
-                    const uint16_t *src = a.q + b * a.q_seq +
-                                          (h * a.group + qb * kKvQueries + rq) * a.q_head + g * (D / 4);
-#pragma unroll
-                    for (int st = 0; st < D / 32; ++st) {
-                        q[st] = *reinterpret_cast<const u4v *>(src + st * 8);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) q[st][i] ^= flip;
-                    }
-                }
             }
             const int pos = (t - cur.base + cur.sp.tile0()) * 32;
             step(cd, pos, cur.sp);
@@ -553,8 +580,11 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                             part_o[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
                 }
             }
-            fresh = true;
-            if (t + 1 < a1) advance(cur, t + 1);
+            if (t + 1 < a1) {
+                piece = t + 1;
+                advance(cur, t + 1);
+                load_q(cur.b);
+            }
         }
     }
     __syncthreads();
@@ -568,47 +598,64 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 last[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
     }
     __syncthreads();
-    for (int e0 = 0; e0 < 2 * W;) {
-        const int b = tag[e0];
-        if (b < 0) { ++e0; continue; }
-        int e1 = e0 + 1;
-        while (e1 < 2 * W && (tag[e1] == b || tag[e1] < 0)) ++e1;
-        const bool whole = first[b] >= w0 && first[b + 1] <= w1;
-        const int slot = first[b] < w0 ? 0 : 1;
-        const int qq = tid & 15;
-        float top = -INFINITY;
-        for (int e = e0; e < e1; ++e)
-            if (tag[e] == b) top = fmaxf(top, ml[e][qq]);
+    // The pieces in order, wave by wave; those of one sequence follow each other.
+    // Their weights against the sequence's largest reference, and its sum:
+    const int tag_of = lane < 2 * W ? tag[lane] : -1;
+    if (tid < 2 * W * 16) {
+        const int e = tid >> 4, qq = tid & 15, b = tag[e];
+        float top = -INFINITY, lw = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i)
+            top = fmaxf(top, tag[i] == b ? ml[i][qq] : -INFINITY);
         const float safe = top == -INFINITY ? 0.f : top;
-        float lw = 0.f;
-        for (int e = e0; e < e1; ++e)
-            if (tag[e] == b) lw += ml[e][16 + qq] * __builtin_amdgcn_exp2f(ml[e][qq] - safe);
-        const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
-        if (qq < nq) {
-            for (int x = tid; x < F::kEntry; x += F::kThreads) {
-                float o = 0.f;
-                for (int e = e0; e < e1; ++e)
-                    if (tag[e] == b)
-                        o += (e & 1 ? last[(e >> 1) * F::kEntry + x] : part_o[(e >> 1) * F::kEntry + x]) *
-                             __builtin_amdgcn_exp2f(ml[e][qq] - safe);
-                if (whole) {
-                    const int n = x >> 8, i = (x >> 6) & 3, gg = (x >> 4) & 3;
-                    const int d = (16 * (n / F::VS) + 4 * gg + i) * F::VS + n % F::VS;
-                    if (d < D) put(b, qq, d, o * inv);
-                } else {
-                    part_o[(W + slot) * F::kEntry + x] = o;
-                }
-            }
-            if (tid < 16) {
-                if (whole) {
-                    put_lse(b, qq, top, lw);
-                } else {
-                    part_ml[slot * 32 + qq] = top;
-                    part_ml[slot * 32 + 16 + qq] = lw;
-                }
+#pragma unroll
+        for (int i = 0; i < 2 * W; ++i)
+            if (tag[i] == b) lw += ml[i][16 + qq] * __builtin_amdgcn_exp2f(ml[i][qq] - safe);
+        weight[e][qq] = __builtin_amdgcn_exp2f(ml[e][qq] - safe);
+        weight[e][16 + qq] = lw;
+        if (b >= 0 && qq < nq) {
+            if (first[b] >= w0 && first[b + 1] <= w1) {
+                put_lse(b, qq, top, lw);                 // each piece says the same
+            } else {
+                const int slot = first[b] < w0 ? 0 : 1;
+                part_ml[slot * 32 + qq] = top;
+                part_ml[slot * 32 + 16 + qq] = lw;
             }
         }
-        e0 = e1;
+    }
+    __syncthreads();
+    constexpr int mine = (F::kEntry + F::kThreads - 1) / F::kThreads;
+    const int qq = tid & 15;
+    float o[mine] = {};
+    for (int e = 0; e < 2 * W; ++e) {
+        const int b = __builtin_amdgcn_readlane(tag_of, e);
+        if (b < 0) continue;
+        const float w = weight[e][qq];
+        const float *src = e & 1 ? last + (e >> 1) * F::kEntry : part_o + (e >> 1) * F::kEntry;
+#pragma unroll
+        for (int i = 0; i < mine; ++i) {
+            const int x = i * F::kThreads + tid;
+            if (x < F::kEntry) o[i] += w * src[x];
+        }
+        int after = -1;                                  // the next piece's sequence
+        for (int n = e + 1; n < 2 * W && after < 0; ++n) after = __builtin_amdgcn_readlane(tag_of, n);
+        if (after == b) continue;
+        const bool whole = first[b] >= w0 && first[b + 1] <= w1;
+        const int slot = first[b] < w0 ? 0 : 1;
+        const float lw = weight[e][16 + qq];
+        const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
+#pragma unroll
+        for (int i = 0; i < mine; ++i) {
+            const int x = i * F::kThreads + tid;
+            const int d = F::feature(x);
+            if (qq < nq && x < F::kEntry) {
+                if (!whole)
+                    part_o[(W + slot) * F::kEntry + x] = o[i];
+                else if (d < D)
+                    put(b, qq, d, o[i] * inv);
+            }
+            o[i] = 0.f;
+        }
     }
 }
 
@@ -628,8 +675,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const int tiles = a.first_tile[a.seqs], p0 = a.first_tile[b], p1 = a.first_tile[b + 1];
     if (p0 == p1) return;
     const int used = splits_used(tiles, splits, F::kWaves);
-    const int j0 = (int)(((int64_t)(p0 + 1) * used + tiles - 1) / tiles) - 1;
-    const int j1 = (int)(((int64_t)p1 * used + tiles - 1) / tiles) - 1;
+    const int j0 = share_of(tiles, p0, used), j1 = share_of(tiles, p1 - 1, used);
     if (j0 == j1) return;
     // weight of each part, for each query: [part][query]
     __shared__ float weight[kCUs * 16];
@@ -637,7 +683,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const int tid = threadIdx.x, q = tid & 15, n = j1 - j0 + 1;
     const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j0;
     const float *const ml = a.part_ml + wg * 64 + q;
-    const int slot0 = p0 < split_begin(tiles, j0, used) ? 0 : 1;      // later parts: slot 0
+    const int slot0 = p0 < share_begin(tiles, j0, used) ? 0 : 1;      // later parts: slot 0
     float top = -INFINITY;
     for (int i = tid >> 4; i < n; i += 16) {
         const float v = ml[i * 64 + (i == 0 ? slot0 * 32 : 0)];
@@ -663,8 +709,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     if (x < 16 && a.lse)
         a.lse[(int64_t)b * c.heads * a.group + head] =
             lw > 0.f || lw != lw ? (top + __log2f(lw)) * 0.69314718055994531f : -INFINITY;
-    const int d = (16 * ((x >> 8) / F::VS) + ((x >> 4) & 3) * 4 + ((x >> 6) & 3)) * F::VS +
-                  (x >> 8) % F::VS;
+    const int d = F::feature(x);
     if (d >= D) return;
     const float *const o0 = a.part_o + (wg * (F::kWaves + 2) + F::kWaves) * F::kEntry + x;
     float o = weight[q] * o0[slot0 * F::kEntry];
