@@ -599,18 +599,22 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     }
     __syncthreads();
     // The pieces in order, wave by wave; those of one sequence follow each other.
-    // Their weights against the sequence's largest reference, and its sum:
+    // This runs once a launch, so its instructions come from memory: short loops
+    // take less time than long straight code.
     const int tag_of = lane < 2 * W ? tag[lane] : -1;
     if (tid < 2 * W * 16) {
+        // the piece's weight against the sequence's largest reference, and the
+        // sequence's sum
         const int e = tid >> 4, qq = tid & 15, b = tag[e];
         float top = -INFINITY, lw = 0.f;
-#pragma unroll
-        for (int i = 0; i < 2 * W; ++i)
-            top = fmaxf(top, tag[i] == b ? ml[i][qq] : -INFINITY);
+#pragma unroll 4
+        for (int i = 0; i < 2 * W; ++i) top = fmaxf(top, tag[i] == b ? ml[i][qq] : -INFINITY);
         const float safe = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int i = 0; i < 2 * W; ++i)
-            if (tag[i] == b) lw += ml[i][16 + qq] * __builtin_amdgcn_exp2f(ml[i][qq] - safe);
+#pragma unroll 4
+        for (int i = 0; i < 2 * W; ++i) {
+            const float part = ml[i][16 + qq] * __builtin_amdgcn_exp2f(ml[i][qq] - safe);
+            lw += tag[i] == b ? part : 0.f;
+        }
         weight[e][qq] = __builtin_amdgcn_exp2f(ml[e][qq] - safe);
         weight[e][16 + qq] = lw;
         if (b >= 0 && qq < nq) {
@@ -626,31 +630,39 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     __syncthreads();
     constexpr int mine = (F::kEntry + F::kThreads - 1) / F::kThreads;
     const int qq = tid & 15;
-    float o[mine] = {};
-    for (int e = 0; e < 2 * W; ++e) {
-        const int b = __builtin_amdgcn_readlane(tag_of, e);
-        if (b < 0) continue;
-        const float w = weight[e][qq];
+    float o[mine] = {}, in[mine], w_in = 0.f;
+    uint64_t left = __ballot(tag_of >= 0);               // pieces not yet asked for
+    int e = -1;                                          // the piece in `in`
+    const auto ask = [&]() {
+        e = left ? __builtin_ctzll(left) : -1;
+        if (e < 0) return;
+        left &= left - 1;
+        w_in = weight[e][qq];
         const float *src = e & 1 ? last + (e >> 1) * F::kEntry : part_o + (e >> 1) * F::kEntry;
 #pragma unroll
-        for (int i = 0; i < mine; ++i) {
-            const int x = i * F::kThreads + tid;
-            if (x < F::kEntry) o[i] += w * src[x];
-        }
-        int after = -1;                                  // the next piece's sequence
-        for (int n = e + 1; n < 2 * W && after < 0; ++n) after = __builtin_amdgcn_readlane(tag_of, n);
-        if (after == b) continue;
+        for (int i = 0; i < mine; ++i) in[i] = src[min(i * F::kThreads + tid, F::kEntry - 1)];
+    };
+    ask();
+#pragma unroll 1
+    while (e >= 0) {
+        const int b = __builtin_amdgcn_readlane(tag_of, e);
+        const float lw = weight[e][16 + qq], w = w_in;
+        float x[mine];
+#pragma unroll
+        for (int i = 0; i < mine; ++i) x[i] = in[i];
+        ask();
+#pragma unroll
+        for (int i = 0; i < mine; ++i) o[i] += w * x[i];
+        if (e >= 0 && __builtin_amdgcn_readlane(tag_of, e) == b) continue;
         const bool whole = first[b] >= w0 && first[b + 1] <= w1;
         const int slot = first[b] < w0 ? 0 : 1;
-        const float lw = weight[e][16 + qq];
         const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
 #pragma unroll
         for (int i = 0; i < mine; ++i) {
-            const int x = i * F::kThreads + tid;
-            const int d = F::feature(x);
-            if (qq < nq && x < F::kEntry) {
+            const int at = i * F::kThreads + tid, d = F::feature(at);
+            if (qq < nq && at < F::kEntry) {
                 if (!whole)
-                    part_o[(W + slot) * F::kEntry + x] = o[i];
+                    part_o[(W + slot) * F::kEntry + at] = o[i];
                 else if (d < D)
                     put(b, qq, d, o[i] * inv);
             }
