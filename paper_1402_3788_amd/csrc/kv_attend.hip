@@ -168,10 +168,24 @@ __device__ inline void to_lds16(const void *src, void *dst)
 
 __device__ inline void lds_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// The value of the lane 8 away in its row of 16.
-__device__ inline float from_8_away(float x)
+// The value of the lane N away in its row of 16, around its ends.
+template <int N>
+__device__ inline float turned(float x)
 {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, true));
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xF, 0xF, true));
+}
+
+// Sum of x over the lanes up to this one.
+__device__ inline int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);      // 1, 2, 4, 8 lanes down the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // rows 0 and 2 to 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);     // the lower half to the upper
+    return x;
 }
 
 // WIDE: more than 8 queries, so that the high and the low parts of the weights
@@ -245,44 +259,69 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             *reinterpret_cast<E *>(vbook + code * F::kRow + s * (SUB * 2)) = ve;
         }
     }
-    // Where each sequence's tiles begin in the row of all tiles.
-    {
+    // Where each sequence's tiles begin in the row of all tiles. Up to 64
+    // sequences every wave has them in its lanes, and looks nothing up later.
+    const bool in_lanes = a.seqs <= kWave;
+    int tiles;
+    Span my_span{0, 0};
+    int my_first = 0, my_next = 0;
+    if (in_lanes) {
+        if (lane < a.seqs) my_span = span_of(c, a, lane);
+        const int n = my_span.tiles();
+        my_next = wave_scan(n);
+        my_first = my_next - n;
+        tiles = __builtin_amdgcn_readlane(my_next, 63);
+        if (wave == 0) {
+            if (lane < a.seqs) first[lane] = my_first;
+            if (lane == 0) first[a.seqs] = tiles;
+        }
+    } else {
         const int per = (a.seqs + F::kThreads - 1) / F::kThreads;
         int sum = 0;
         for (int i = 0; i < per; ++i) {
             const int b = tid * per + i;
             if (b < a.seqs) sum += span_of(c, a, b).tiles();
         }
-        int incl = sum;
-        for (int d = 1; d < kWave; d *= 2) {
-            const int up = __shfl_up(incl, d);
-            if (lane >= d) incl += up;
-        }
+        const int incl = wave_scan(sum);
         if (lane == 63) wave_sum[wave] = incl;
         __syncthreads();
-        int at = incl - sum;
-        for (int w = 0; w < wave; ++w) at += wave_sum[w];
+        const int each = lane < W ? wave_sum[lane] : 0;
+        const int upto = wave_scan(each);
+        int at = incl - sum + (wave ? __builtin_amdgcn_readlane(upto, wave - 1) : 0);
+        tiles = __builtin_amdgcn_readlane(upto, 63);
         for (int i = 0; i < per; ++i) {
             const int b = tid * per + i;
             if (b < a.seqs) {
                 first[b] = at;
                 at += per == 1 ? sum : span_of(c, a, b).tiles();
-                if (b == a.seqs - 1) first[a.seqs] = at;
             }
         }
+        if (tid == 0) first[a.seqs] = tiles;
+        __syncthreads();
     }
-    __syncthreads();
-    const int tiles = first[a.seqs];
     const int used = splits_used(tiles, splits, W);
-    if (blockIdx.x == 0)
-        for (int b = tid; b <= a.seqs; b += F::kThreads) a.first_tile[b] = first[b];
-    // Sequences without positions.
-    for (int b = j; b < a.seqs; b += splits) {
-        if (first[b] != first[b + 1]) continue;
+    const auto empty = [&](int b) {
         for (int i = tid; i < nq * D; i += F::kThreads)
             a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + i / D) * a.out_head + i % D] = 0;
         if (a.lse && tid < nq)
             a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + tid] = -INFINITY;
+    };
+    // Sequences without positions.
+    if (in_lanes) {
+        if (blockIdx.x == 0 && wave == 0) {
+            if (lane < a.seqs) a.first_tile[lane] = my_first;
+            if (lane == 0) a.first_tile[a.seqs] = tiles;
+        }
+        uint64_t none = __ballot(lane < a.seqs && my_first == my_next);
+        for (; none; none &= none - 1) {
+            const int b = __builtin_ctzll(none);
+            if (b % splits == j) empty(b);
+        }
+    } else {
+        if (blockIdx.x == 0)
+            for (int b = tid; b <= a.seqs; b += F::kThreads) a.first_tile[b] = first[b];
+        for (int b = j; b < a.seqs; b += splits)
+            if (first[b] == first[b + 1]) empty(b);
     }
     if (j >= used) return;
     const int w0 = share_begin(tiles, j, used), w1 = share_begin(tiles, j + 1, used);
@@ -315,6 +354,13 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     const auto enter = [&](int b) {
         Cursor x;
         x.b = __builtin_amdgcn_readfirstlane(b);
+        if (in_lanes) {
+            x.base = __builtin_amdgcn_readlane(my_first, x.b);
+            x.next = __builtin_amdgcn_readlane(my_next, x.b);
+            x.sp.start = __builtin_amdgcn_readlane(my_span.start, x.b);
+            x.sp.len = __builtin_amdgcn_readlane(my_span.len, x.b);
+            return x;
+        }
         x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
         x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
         const Span s = span_of(c, a, x.b);
@@ -322,11 +368,21 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
         return x;
     };
+    // the sequence of tile t, from sequence b on
+    const auto sequence_of = [&](int t, int b) {
+        if (in_lanes) return (int)__popcll(__ballot(lane < a.seqs && my_next <= t));
+        for (int hi = a.seqs; b < hi;) {                // the last with first[] <= t
+            const int mid = (b + hi) >> 1;
+            if (first[mid + 1] <= t) b = mid + 1; else hi = mid;
+        }
+        return b;
+    };
     // to tile t (the next one, below a1)
     const auto advance = [&](Cursor &x, int t) {
         if (t < x.next) return;
         int b = x.b + 1;
-        while (first[b + 1] <= t) ++b;
+        if (in_lanes) b = sequence_of(t, b);
+        else while (first[b + 1] <= t) ++b;
         x = enter(b);
     };
     // Tile t's codes are loaded while t - 1 is worked on, and the numbers of
@@ -392,12 +448,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     Where where{};
     Codes<D, SUB> coming;
     if (a0 < a1) {
-        int lo = 0;
-        for (int hi = a.seqs; lo < hi;) {               // the last b with first[b] <= a0
-            const int mid = (lo + hi) >> 1;
-            if (first[mid + 1] <= a0) lo = mid + 1; else hi = mid;
-        }
-        cur = ahead = enter(lo);
+        cur = ahead = enter(sequence_of(a0, 0));
         where = find(ahead, a0);
         load_q(cur.b);
         coming = load(where);
@@ -554,7 +605,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
                 for (int n = 0; n < F::NV; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][i] += from_8_away(acc[n][i]);
+                    for (int i = 0; i < 4; ++i) acc[n][i] += turned<8>(acc[n][i]);
             }
             if (piece == cur.base && t + 1 == cur.next) {
                 const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
@@ -598,28 +649,40 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 last[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
     }
     __syncthreads();
-    // The pieces in order, wave by wave; those of one sequence follow each other.
-    // This runs once a launch, so its instructions come from memory: short loops
-    // take less time than long straight code.
-    const int tag_of = lane < 2 * W ? tag[lane] : -1;
-    if (tid < 2 * W * 16) {
-        // the piece's weight against the sequence's largest reference, and the
-        // sequence's sum
-        const int e = tid >> 4, qq = tid & 15, b = tag[e];
-        float top = -INFINITY, lw = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < 2 * W; ++i) top = fmaxf(top, tag[i] == b ? ml[i][qq] : -INFINITY);
-        const float safe = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
-        for (int i = 0; i < 2 * W; ++i) {
-            const float part = ml[i][16 + qq] * __builtin_amdgcn_exp2f(ml[i][qq] - safe);
-            lw += tag[i] == b ? part : 0.f;
-        }
-        weight[e][qq] = __builtin_amdgcn_exp2f(ml[e][qq] - safe);
-        weight[e][16 + qq] = lw;
-        if (b >= 0 && qq < nq) {
+    // Piece e = 2 * wave is the one before a wave's last, e + 1 its last. Those of
+    // one sequence are last pieces of waves that follow each other, and at most
+    // one that the next wave ended. All of this runs once a launch, when its
+    // instructions come from memory: it is kept short.
+    static_assert(W >= 8 && W <= 16, "two queries to each of 8 waves, pieces to half a wave");
+    if (wave < 8) {
+        // lanes: pieces; halves: queries. The pieces' weights against the
+        // sequence's largest reference, and the sequence's sum.
+        const int e = lane & 31, qq = 2 * wave + (lane >> 5);
+        const int b = e < 2 * W ? tag[e] : -1;
+        const float em = e < 2 * W ? ml[e][qq] : 0.f, el = e < 2 * W ? ml[e][16 + qq] : 0.f;
+        for (uint64_t todo = __ballot(b >= 0); todo;) {
+            const int lead = __builtin_ctzll(todo);
+            const bool in = b == __builtin_amdgcn_readlane(b, lead);
+            todo &= ~__ballot(in);
+            float top = in ? em : -INFINITY;
+            top = fmaxf(top, turned<1>(top));
+            top = fmaxf(top, turned<2>(top));
+            top = fmaxf(top, turned<4>(top));
+            top = fmaxf(top, turned<8>(top));
+            top = fmaxf(top, __shfl_xor(top, 16));
+            const float w = __builtin_amdgcn_exp2f(em - (top == -INFINITY ? 0.f : top));
+            float lw = in ? el * w : 0.f;
+            lw += turned<1>(lw);
+            lw += turned<2>(lw);
+            lw += turned<4>(lw);
+            lw += turned<8>(lw);
+            lw += __shfl_xor(lw, 16);
+            if (!in) continue;
+            weight[e][qq] = w;
+            weight[e][16 + qq] = lw;
+            if (e != lead || qq >= nq) continue;
             if (first[b] >= w0 && first[b + 1] <= w1) {
-                put_lse(b, qq, top, lw);                 // each piece says the same
+                put_lse(b, qq, top, lw);
             } else {
                 const int slot = first[b] < w0 ? 0 : 1;
                 part_ml[slot * 32 + qq] = top;
@@ -630,30 +693,37 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     __syncthreads();
     constexpr int mine = (F::kEntry + F::kThreads - 1) / F::kThreads;
     const int qq = tid & 15;
-    float o[mine] = {}, in[mine], w_in = 0.f;
-    uint64_t left = __ballot(tag_of >= 0);               // pieces not yet asked for
-    int e = -1;                                          // the piece in `in`
-    const auto ask = [&]() {
-        e = left ? __builtin_ctzll(left) : -1;
-        if (e < 0) return;
-        left &= left - 1;
-        w_in = weight[e][qq];
-        const float *src = e & 1 ? last + (e >> 1) * F::kEntry : part_o + (e >> 1) * F::kEntry;
-#pragma unroll
-        for (int i = 0; i < mine; ++i) in[i] = src[min(i * F::kThreads + tid, F::kEntry - 1)];
-    };
-    ask();
+    const int tag_of = lane < 2 * W ? tag[lane] : -1;
+    uint64_t todo = __ballot(tag_of >= 0);
 #pragma unroll 1
-    while (e >= 0) {
-        const int b = __builtin_amdgcn_readlane(tag_of, e);
-        const float lw = weight[e][16 + qq], w = w_in;
-        float x[mine];
+    while (todo) {
+        const int b = __builtin_amdgcn_readlane(tag_of, __builtin_ctzll(todo));
+        const uint64_t in = __ballot(tag_of == b);
+        todo &= ~in;
+        float o[mine] = {}, lw = 0.f;
+        if (const uint64_t heads = in & 0x5555555555555555ull) {
+            const int e = __builtin_ctzll(heads);
+            const float w = weight[e][qq];
+            lw = weight[e][16 + qq];
 #pragma unroll
-        for (int i = 0; i < mine; ++i) x[i] = in[i];
-        ask();
+            for (int i = 0; i < mine; ++i)
+                o[i] = w * part_o[(e >> 1) * F::kEntry + min(i * F::kThreads + tid, F::kEntry - 1)];
+        }
+        if (const uint64_t lasts = in & 0xAAAAAAAAAAAAAAAAull) {
+            const int from = __builtin_ctzll(lasts) >> 1, to = (63 - __builtin_clzll(lasts)) >> 1;
+            lw = weight[2 * from + 1][16 + qq];
+#pragma unroll 1
+            for (int n = from; n <= to; n += 4) {
 #pragma unroll
-        for (int i = 0; i < mine; ++i) o[i] += w * x[i];
-        if (e >= 0 && __builtin_amdgcn_readlane(tag_of, e) == b) continue;
+                for (int k = 0; k < 4; ++k) {
+                    const int at = min(n + k, to);       // the last again, with no weight
+                    const float w = n + k <= to ? weight[2 * at + 1][qq] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < mine; ++i)
+                        o[i] += w * last[at * F::kEntry + min(i * F::kThreads + tid, F::kEntry - 1)];
+                }
+            }
+        }
         const bool whole = first[b] >= w0 && first[b + 1] <= w1;
         const int slot = first[b] < w0 ? 0 : 1;
         const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
@@ -666,7 +736,6 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 else if (d < D)
                     put(b, qq, d, o[i] * inv);
             }
-            o[i] = 0.f;
         }
     }
 }
