@@ -587,6 +587,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         };
 
         int piece = a0;
+        int turn = (wave >> 2) % 3;
         for (int t = a0; t < a1; ++t) {
             const int b = cur.b;
             const Codes<D, SUB> cd = coming;
@@ -596,6 +597,10 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 where = find(ahead, t + 2);
             }
             const int pos = (t - cur.base + cur.sp.tile0()) * 32;
+            if (turn == 0) __builtin_amdgcn_s_setprio(2);
+            else if (turn == 1) __builtin_amdgcn_s_setprio(1);
+            else __builtin_amdgcn_s_setprio(0);
+            turn = turn == 2 ? 0 : turn + 1;
             step(cd, pos, cur.sp);
             if (t + 1 != cur.next && t + 1 != a1) continue;
             // the piece [piece, t] of sequence b is done
