@@ -48,6 +48,25 @@ __device__ inline uint32_t pack2(float a, float b)
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
 }
 
+// x cut off to the 16-bit type, where mask is all ones; 0 where it is 0. (The
+// weights are at most 2^kLag, and below the least normal number of fp16 the
+// cut leaves more bits than fp16 has there: cut2 of the rest takes them off.)
+template <bool FP16>
+__device__ inline float cut(float x, uint32_t mask)
+{
+    return __uint_as_float(__float_as_uint(x) & (FP16 ? 0xFFFFE000u : 0xFFFF0000u) & mask);
+}
+
+// Two numbers cut off to the 16-bit type.
+template <bool FP16>
+__device__ inline uint32_t cut2(float a, float b)
+{
+    if constexpr (FP16)
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+    else
+        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+
 // Sizes of one form of the kernel.
 template <int D, int SUB>
 struct Form {
@@ -388,44 +407,51 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     // Tile t's codes are loaded while t - 1 is worked on, and the numbers of
     // the pages they lie on while t - 2 is.
     struct Where {
-        int k_at, v_at;          // first position of the lane's keys and values
-        int k_page, v_page;
+        int pos;                 // the tile's first position
+        int k_page, v_page;      // numbers of the pages of the lane's keys and values
+    };
+    const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
+    const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
+    const uint8_t *const k_head = c.k_codes + (((int64_t)h * F::S) << c.page_log2);
+    const uint8_t *const v_head = c.v_codes + (((int64_t)h * F::S) << c.page_log2);
+    // A lane's codes lie at the same place of each of its pages, for tiles begin on
+    // multiples of 32 positions; where pages are larger, the tile's place is added.
+    const unsigned pm = (1u << c.page_log2) - 1;
+    const unsigned k_off = ((8 * (r >> 2) & pm) + (r & 3)) * F::S + g * F::SL;
+    const unsigned v_off = 8 * g & pm;
+    const auto v_sub = [&](int hh) {             // of a lane's granule in its sub-vectors
+        return (unsigned)(min(16 * hh + r, F::NG - 1) * F::VS / SUB) << c.page_log2;
     };
     const auto find = [&](const Cursor &x, int t) {
         Where w;
-        const int pos = (t - x.base + x.sp.tile0()) * 32;
-        const int low = x.sp.start & ~7, high = (x.sp.len - 1) & ~7;
-        const int32_t *row = a.table + x.b * a.table_stride;
-        // positions outside the span are taken as the nearest inside
-        w.k_at = min(max(pos + 8 * (r >> 2), low), high);
-        w.v_at = min(max(pos + 8 * g, low), high);
-        w.k_page = row[w.k_at >> c.page_log2];
-        w.v_page = row[w.v_at >> c.page_log2];
+        w.pos = (t - x.base + x.sp.tile0()) * 32;
+        const char *row = reinterpret_cast<const char *>(a.table + x.b * a.table_stride);
+        const auto entry = [&](int page) {
+            return *reinterpret_cast<const int32_t *>(row + (uint32_t)page * 4u);
+        };
+        // groups of 8 positions outside the span: the nearest page inside
+        const int low = x.sp.start >> c.page_log2, high = (x.sp.len - 1) >> c.page_log2;
+        w.k_page = entry(min(max((w.pos + 8 * (r >> 2)) >> c.page_log2, low), high));
+        w.v_page = entry(min(max((w.pos + 8 * g) >> c.page_log2, low), high));
         return w;
     };
-    const unsigned pm = (1u << c.page_log2) - 1;
-    const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
-    const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
-    const int64_t head_bytes = ((int64_t)h * F::S) << c.page_log2;
-    const uint8_t *const k_lane = c.k_codes + head_bytes + (r & 3) * F::S + g * F::SL;
-    const uint8_t *const v_lane = c.v_codes + head_bytes;
     const auto load = [&](const Where &w) {
         Codes<D, SUB> cd;
         // a number that is no page's is some page's here, never followed out
-        const uint8_t *src = k_lane + (uint64_t)min((unsigned)w.k_page, last_page) * page_bytes +
-                             (w.k_at & pm) * F::S;
-        load_bytes<F::SL>(cd.k[0], src);
-        load_bytes<F::SL>(cd.k[1], src + 4 * F::S);
-        src = v_lane + (uint64_t)min((unsigned)w.v_page, last_page) * page_bytes + (w.v_at & pm);
+        const unsigned in = (unsigned)w.pos & pm;        // 0 for pages of up to 32
+        const uint8_t *const k = k_head + in * F::S + k_off +
+                                 (uint64_t)min((unsigned)w.k_page, last_page) * page_bytes;
+        const uint8_t *const v = v_head + in + v_off +
+                                 (uint64_t)min((unsigned)w.v_page, last_page) * page_bytes;
+        load_bytes<F::SL>(cd.k[0], k);
+        load_bytes<F::SL>(cd.k[1], k + 4 * F::S);
 #pragma unroll
-        for (int hh = 0; hh < F::NH; ++hh) {
-            const int gr = min(16 * hh + r, F::NG - 1);
-            load_bytes<8>(cd.v[hh], src + ((unsigned)(gr * F::VS / SUB) << c.page_log2));
-        }
+        for (int hh = 0; hh < F::NH; ++hh) load_bytes<8>(cd.v[hh], v + v_sub(hh));
         return cd;
     };
     const float scale = fabsf(a.scale_log2);
     const bool negative = a.scale_log2 < 0.f;
+    const uint32_t low_parts = r >= 8 ? ~0u : 0u;        // lanes whose columns take them
 
     const auto load_q = [&](int b) {
 #pragma unroll
@@ -552,15 +578,19 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 z[i] = __builtin_amdgcn_exp2f(z[i]);
                 l += z[i];
             }
-            // each weight as the sum of two 16-bit numbers: one alone (8 bits of
-            // bf16) would cost as much of the result as its own final rounding
+            // each weight as the sum of two 16-bit numbers, both cut off and not
+            // rounded: one alone (8 bits of bf16) would cost as much of the result
+            // as its own final rounding
             u4v p, p_lo;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                p[i] = pack2<FP16>(z[2 * i], z[2 * i + 1]);
-                p_lo[i] = pack2<FP16>(z[2 * i] - kv_float<FP16>(p[i] & 0xFFFFu),
-                                      z[2 * i + 1] - kv_float<FP16>(p[i] >> 16));
-                if (!WIDE) p[i] = r < 8 ? p[i] : p_lo[i];
+                const float z0 = z[2 * i], z1 = z[2 * i + 1];
+                if constexpr (WIDE) {
+                    p[i] = cut2<FP16>(z0, z1);
+                    p_lo[i] = cut2<FP16>(z0 - cut<FP16>(z0, ~0u), z1 - cut<FP16>(z1, ~0u));
+                } else {
+                    p[i] = cut2<FP16>(z0 - cut<FP16>(z0, low_parts), z1 - cut<FP16>(z1, low_parts));
+                }
             }
             // values: rows are features, columns queries
 #pragma unroll
@@ -586,24 +616,27 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             }
         };
 
-        int piece = a0;
+        // A sequence's tiles of the wave at a time, the work on a tile in a loop of
+        // its own, which so keeps its registers.
         int turn = (wave >> 2) % 3;
-        for (int t = a0; t < a1; ++t) {
-            const int b = cur.b;
-            const Codes<D, SUB> cd = coming;
-            if (t + 1 < a1) coming = load(where);
-            if (t + 2 < a1) {
-                advance(ahead, t + 2);
-                where = find(ahead, t + 2);
+        for (int t = a0; t < a1;) {
+            const int b = cur.b, piece = t, end = min(cur.next, a1);
+            for (; t < end; ++t) {
+                const Codes<D, SUB> cd = coming;
+                if (t + 1 < a1) coming = load(where);
+                if (t + 2 < a1) {
+                    advance(ahead, t + 2);
+                    where = find(ahead, t + 2);
+                }
+                // The SIMD's waves take turns at the highest priority: the oldest
+                // would have it always, end first and leave the last ones to
+                // run alone.
+                if (turn == 0) __builtin_amdgcn_s_setprio(2);
+                else if (turn == 1) __builtin_amdgcn_s_setprio(1);
+                else __builtin_amdgcn_s_setprio(0);
+                turn = turn == 2 ? 0 : turn + 1;
+                step(cd, (t - cur.base + cur.sp.tile0()) * 32, cur.sp);
             }
-            const int pos = (t - cur.base + cur.sp.tile0()) * 32;
-            if (turn == 0) __builtin_amdgcn_s_setprio(2);
-            else if (turn == 1) __builtin_amdgcn_s_setprio(1);
-            else __builtin_amdgcn_s_setprio(0);
-            turn = turn == 2 ? 0 : turn + 1;
-            step(cd, pos, cur.sp);
-            if (t + 1 != cur.next && t + 1 != a1) continue;
-            // the piece [piece, t] of sequence b is done
             float lw = l + __shfl_xor(l, 16);
             lw += __shfl_xor(lw, 32);
             if (!WIDE) {
@@ -612,7 +645,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[n][i] += turned<8>(acc[n][i]);
             }
-            if (piece == cur.base && t + 1 == cur.next) {
+            if (piece == cur.base && end == cur.next) {  // the whole sequence
                 const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
                 if (r < nq) {
 #pragma unroll
@@ -625,10 +658,10 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                     if (g == 0) put_lse(b, r, m, lw);
                 }
             } else {
-                const int e = 2 * wave + (t + 1 == a1);
+                const int e = 2 * wave + (end == a1);
                 if (lane == 0) tag[e] = b;
                 if (g == 0) { ml[e][r] = m; ml[e][16 + r] = lw; }
-                if (t + 1 != a1) {
+                if (end != a1) {
 #pragma unroll
                     for (int n = 0; n < F::NV; ++n)
 #pragma unroll
@@ -636,9 +669,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                             part_o[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
                 }
             }
-            if (t + 1 < a1) {
-                piece = t + 1;
-                advance(cur, t + 1);
+            if (end < a1) {
+                advance(cur, end);
                 load_q(cur.b);
             }
         }
