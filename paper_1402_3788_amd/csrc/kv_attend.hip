@@ -165,14 +165,15 @@ __device__ inline uint32_t code_offset(const uint32_t *w, int n, uint32_t base)
 }
 
 // The entry at a byte of LDS (the kernel has no LDS but its dynamic one, which
-// so begins at 0).
+// so begins at 0), `more` bytes on.
 template <int N>
-__device__ inline KvEntry<N> lds_entry(uint32_t at)
+__device__ inline KvEntry<N> lds_entry(uint32_t at, int more = 0)
 {
     typedef uint32_t V __attribute__((ext_vector_type(N / 2 > 1 ? N / 2 : 2)));
     typedef std::conditional_t<N == 2, uint32_t, V> T;
+    const auto p = (const __attribute__((address_space(3))) char *)(uintptr_t)at;
     return __builtin_bit_cast(KvEntry<N>,
-                              *(const __attribute__((address_space(3))) T *)(uintptr_t)at);
+                              *(const __attribute__((address_space(3))) T *)(p + more));
 }
 
 // 16 bytes of each lane of a wave from memory to LDS, to the 1024 from `dst` on
@@ -404,8 +405,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         else while (first[b + 1] <= t) ++b;
         x = enter(b);
     };
-    // Tile t's codes are loaded while t - 1 is worked on, and the numbers of
-    // the pages they lie on while t - 2 is.
+    // Tile t's codes are loaded when those of t - 1 have been looked up, to the
+    // same registers, and the numbers of the pages they lie on a tile before.
     struct Where {
         int pos;                 // the tile's first position
         int k_page, v_page;      // numbers of the pages of the lane's keys and values
@@ -435,19 +436,20 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         w.v_page = entry(min(max((w.pos + 8 * g) >> c.page_log2, low), high));
         return w;
     };
-    const auto load = [&](const Where &w) {
-        Codes<D, SUB> cd;
-        // a number that is no page's is some page's here, never followed out
-        const unsigned in = (unsigned)w.pos & pm;        // 0 for pages of up to 32
-        const uint8_t *const k = k_head + in * F::S + k_off +
-                                 (uint64_t)min((unsigned)w.k_page, last_page) * page_bytes;
-        const uint8_t *const v = v_head + in + v_off +
-                                 (uint64_t)min((unsigned)w.v_page, last_page) * page_bytes;
+    Codes<D, SUB> cd;            // of the tile at hand, then of the next
+    // A number that is no page's is some page's here, never followed out.
+    const auto place = [&](const Where &w, int page, int S) {
+        return (uint64_t)min((unsigned)page, last_page) * page_bytes + ((unsigned)w.pos & pm) * S;
+    };
+    const auto load_k = [&](const Where &w) {
+        const uint8_t *const k = k_head + k_off + place(w, w.k_page, F::S);
         load_bytes<F::SL>(cd.k[0], k);
         load_bytes<F::SL>(cd.k[1], k + 4 * F::S);
+    };
+    const auto load_v = [&](const Where &w) {
+        const uint8_t *const v = v_head + v_off + place(w, w.v_page, 1);
 #pragma unroll
         for (int hh = 0; hh < F::NH; ++hh) load_bytes<8>(cd.v[hh], v + v_sub(hh));
-        return cd;
     };
     const float scale = fabsf(a.scale_log2);
     const bool negative = a.scale_log2 < 0.f;
@@ -472,12 +474,12 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     // The first tiles' loads are on their way before the centres are waited for.
     Cursor cur{}, ahead{};
     Where where{};
-    Codes<D, SUB> coming;
     if (a0 < a1) {
         cur = ahead = enter(sequence_of(a0, 0));
         where = find(ahead, a0);
         load_q(cur.b);
-        coming = load(where);
+        load_k(where);
+        load_v(where);
         if (a0 + 1 < a1) {
             advance(ahead, a0 + 1);
             where = find(ahead, a0 + 1);
@@ -502,7 +504,9 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         const uint32_t k_base = F::kValues + g * (F::SL * 512 * SUB);
         // One tile of 32 positions from `pos` on. What the span leaves out of it
         // is masked in branches of its own, which most tiles skip.
-        const auto step = [&](const Codes<D, SUB> &cd, int pos, const Span &sp) {
+        const auto step = [&](int t) {
+            const int pos = (t - cur.base + cur.sp.tile0()) * 32;
+            const Span &sp = cur.sp;
             const bool partial = pos < sp.start || pos + 32 > sp.len;
             const auto seen = [&](int i) {
                 const int p = pos + 8 * g + i;
@@ -515,8 +519,14 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int n = 0; n < F::SL; ++n)
-                    ke[u][n] = lds_entry<SUB>(code_offset<SUB>(cd.k[u], n, k_base) + n * (512 * SUB));
+                    ke[u][n] = lds_entry<SUB>(code_offset<SUB>(cd.k[u], n, k_base), n * (512 * SUB));
             __builtin_amdgcn_sched_barrier(0);
+            const Where coming = where;
+            if (t + 1 < a1) load_k(coming);
+            if (t + 2 < a1) {
+                advance(ahead, t + 2);
+                where = find(ahead, t + 2);
+            }
             // scores: rows are positions, columns queries
             float z[8];
 #pragma unroll
@@ -544,6 +554,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                                               (uint32_t)(min(16 * hh + r, F::NG - 1) * F::VS * 2),
                                               0x0C0C0000u | (4 + (x & 3)) << 8));
             __builtin_amdgcn_sched_barrier(0);
+            if (t + 1 < a1) load_v(coming);
             if (negative) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = -z[i];
@@ -622,12 +633,6 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         for (int t = a0; t < a1;) {
             const int b = cur.b, piece = t, end = min(cur.next, a1);
             for (; t < end; ++t) {
-                const Codes<D, SUB> cd = coming;
-                if (t + 1 < a1) coming = load(where);
-                if (t + 2 < a1) {
-                    advance(ahead, t + 2);
-                    where = find(ahead, t + 2);
-                }
                 // The SIMD's waves take turns at the highest priority: the oldest
                 // would have it always, end first and leave the last ones to
                 // run alone.
@@ -635,7 +640,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 else if (turn == 1) __builtin_amdgcn_s_setprio(1);
                 else __builtin_amdgcn_s_setprio(0);
                 turn = turn == 2 ? 0 : turn + 1;
-                step(cd, (t - cur.base + cur.sp.tile0()) * 32, cur.sp);
+                step(t);
             }
             float lw = l + __shfl_xor(l, 16);
             lw += __shfl_xor(lw, 32);
