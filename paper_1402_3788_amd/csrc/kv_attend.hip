@@ -176,6 +176,15 @@ __device__ inline KvEntry<N> lds_entry(uint32_t at, int more = 0)
                               *(const __attribute__((address_space(3))) T *)(p + more));
 }
 
+// p, worked out here: addresses of what is written once would else be kept in
+// registers through the loop before.
+template <typename T>
+__device__ inline T *here(T *p)
+{
+    asm volatile("" : "+v"(p));
+    return p;
+}
+
 // 16 bytes of each lane of a wave from memory to LDS, to the 1024 from `dst` on
 // (the same for all lanes), without registers between. A wave's own are there
 // after lds_landed(), all waves' after a barrier behind it.
@@ -653,12 +662,16 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             if (piece == cur.base && end == cur.next) {  // the whole sequence
                 const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
                 if (r < nq) {
+                    uint16_t *const dst =
+                        here(a.out + b * a.out_seq +
+                             (h * a.group + qb * kKvQueries + r) * a.out_head + 4 * g * F::VS);
 #pragma unroll
                     for (int n = 0; n < F::NV; ++n)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int d = (16 * (n / F::VS) + 4 * g + i) * F::VS + n % F::VS;
-                            if (d < D) put(b, r, d, acc[n][i] * inv);
+                            const int d = (16 * (n / F::VS) + i) * F::VS + n % F::VS;
+                            if (d + 4 * g * F::VS < D)
+                                dst[d] = (uint16_t)pack2<FP16>(acc[n][i] * inv, 0.f);
                         }
                     if (g == 0) put_lse(b, r, m, lw);
                 }
@@ -667,11 +680,11 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 if (lane == 0) tag[e] = b;
                 if (g == 0) { ml[e][r] = m; ml[e][16 + r] = lw; }
                 if (end != a1) {
+                    float *const dst = here(part_o + wave * F::kEntry + lane);
 #pragma unroll
                     for (int n = 0; n < F::NV; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            part_o[wave * F::kEntry + (n * 4 + i) * 64 + lane] = acc[n][i];
+                        for (int i = 0; i < 4; ++i) dst[(n * 4 + i) * 64] = acc[n][i];
                 }
             }
             if (end < a1) {
