@@ -31,6 +31,12 @@ struct KvTokens {
     int64_t k_token, k_head, v_token, v_head;
 };
 
+// The sequence that begins in a workgroup's share of the tiles and ends in
+// another's (b < 0: there is none), and the workgroups that have a part of it.
+struct KvShared {
+    int32_t b, parts;
+};
+
 struct KvAttend {
     const uint16_t *q;
     int64_t q_seq, q_head;
@@ -44,7 +50,7 @@ struct KvAttend {
     int64_t out_seq, out_head;
     float *lse;
     // workspace
-    int32_t *first_tile;             // [seqs + 1]
+    KvShared *shared;                // [workgroups]
     float *part_o, *part_ml;
 };
 
@@ -52,7 +58,7 @@ struct KvAttend {
 struct KvAttendPlan {
     int splits;                      // workgroups of one head and block of queries
     int qblocks;                     // blocks of kKvQueries query heads
-    size_t first_tile_off, part_o_off, part_ml_off, total;   // workspace
+    size_t shared_off, part_o_off, part_ml_off, total;   // workspace
 };
 
 KvAttendPlan plan_kv_attend(const KvCache &c, int seqs, int group, int64_t table_pages);

@@ -158,7 +158,7 @@ int kmeans_kv_attend(const kmeans_kv_t *kv, const void *q, int64_t q_seq, int64_
     a.out_seq = out_seq;
     a.out_head = out_head;
     a.lse = lse;
-    a.first_tile = reinterpret_cast<int32_t *>(ws + p.first_tile_off);
+    a.shared = reinterpret_cast<KvShared *>(ws + p.shared_off);
     a.part_o = reinterpret_cast<float *>(ws + p.part_o_off);
     a.part_ml = reinterpret_cast<float *>(ws + p.part_ml_off);
     return hip_status(launch_kv_attend(c, a, p, static_cast<hipStream_t>(stream)));

@@ -337,21 +337,16 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     };
     // Sequences without positions.
     if (in_lanes) {
-        if (blockIdx.x == 0 && wave == 0) {
-            if (lane < a.seqs) a.first_tile[lane] = my_first;
-            if (lane == 0) a.first_tile[a.seqs] = tiles;
-        }
         uint64_t none = __ballot(lane < a.seqs && my_first == my_next);
         for (; none; none &= none - 1) {
             const int b = __builtin_ctzll(none);
             if (b % splits == j) empty(b);
         }
     } else {
-        if (blockIdx.x == 0)
-            for (int b = tid; b <= a.seqs; b += F::kThreads) a.first_tile[b] = first[b];
         for (int b = j; b < a.seqs; b += splits)
             if (first[b] == first[b + 1]) empty(b);
     }
+    if (tid == 0) a.shared[wg] = KvShared{-1, 0};        // unless found below
     if (j >= used) return;
     const int w0 = share_begin(tiles, j, used), w1 = share_begin(tiles, j + 1, used);
     const int a0 = w0 + share_begin(w1 - w0, wave, W), a1 = w0 + share_begin(w1 - w0, wave + 1, W);
@@ -792,53 +787,62 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                     put(b, qq, d, o[i] * inv);
             }
         }
+        if (!whole && slot && tid == 0)
+            a.shared[wg] = KvShared{b, share_of(tiles, first[b + 1] - 1, used) - j + 1};
     }
 }
 
-// Joins what the workgroups left of the sequences that several shared. A
-// workgroup takes one sequence, one block of a head's queries and 256 of its
-// outputs, one to a thread, so that the sums over up to 256 parts run in
-// parallel.
+// Joins what the workgroups left of the sequences that several shared. Joining
+// workgroup j of a head takes the sequence that begins in share j and does not
+// end there, if there is one: its parts are that share's second and the first
+// of the shares after it. It takes 256 of the outputs, one to a thread, and asks
+// for the parts and for what weighs them at once: this launch is a chain of two
+// trips to memory.
 template <int D, int SUB, bool FP16>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int splits)
 {
     using F = Form<D, SUB>;
-    constexpr int chunks = F::kEntry / 256;
-    const int b = blockIdx.x / chunks % a.seqs, hq = blockIdx.x / chunks / a.seqs;
+    constexpr int chunks = F::kEntry / 256, batch = 8;
     const int x = blockIdx.x % chunks * 256 + threadIdx.x;
+    const int j = blockIdx.x / chunks % (splits - 1), hq = blockIdx.x / chunks / (splits - 1);
     const int h = hq % c.heads, qb = hq / c.heads;
     const int nq = min(kKvQueries, a.group - qb * kKvQueries);
-    const int tiles = a.first_tile[a.seqs], p0 = a.first_tile[b], p1 = a.first_tile[b + 1];
-    if (p0 == p1) return;
-    const int used = splits_used(tiles, splits, F::kWaves);
-    const int j0 = share_of(tiles, p0, used), j1 = share_of(tiles, p1 - 1, used);
-    if (j0 == j1) return;
+    const int64_t wg = (int64_t)hq * splits + j;
+    const KvShared found = a.shared[wg];
+    if (found.b < 0) return;
+    const int b = found.b, n = found.parts;              // 2 <= n <= splits <= kCUs
+    const int tid = threadIdx.x, q = tid & 15;
+    const auto part = [&](int i) {                       // of this thread's output
+        return a.part_o[((wg + i) * (F::kWaves + 2) + F::kWaves + (i == 0)) * F::kEntry + x];
+    };
+    const auto ml = [&](int i) { return a.part_ml + (wg + i) * 64 + (i == 0) * 32 + q; };
+    float in[batch];
+#pragma unroll
+    for (int k = 0; k < batch; ++k) in[k] = part(min(k, n - 1));
     // weight of each part, for each query: [part][query]
     __shared__ float weight[kCUs * 16];
     __shared__ float s_top[16 * 16], s_sum[16 * 16];
-    const int tid = threadIdx.x, q = tid & 15, n = j1 - j0 + 1;
-    const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j0;
-    const float *const ml = a.part_ml + wg * 64 + q;
-    const int slot0 = p0 < share_begin(tiles, j0, used) ? 0 : 1;      // later parts: slot 0
     float top = -INFINITY;
     for (int i = tid >> 4; i < n; i += 16) {
-        const float v = ml[i * 64 + (i == 0 ? slot0 * 32 : 0)];
+        const float v = *ml(i);
         weight[i * 16 + q] = v;
         top = fmaxf(top, v);
     }
     s_top[tid] = top;
     __syncthreads();
+#pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s_top[i * 16 + q]);
     const float safe = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
     for (int i = tid >> 4; i < n; i += 16) {
         const float w = __builtin_amdgcn_exp2f(weight[i * 16 + q] - safe);
-        sum += w * ml[i * 64 + 16 + (i == 0 ? slot0 * 32 : 0)];
+        sum += w * ml(i)[16];
         weight[i * 16 + q] = w;
     }
     s_sum[tid] = sum;
     __syncthreads();
     float lw = 0.f;
+#pragma unroll
     for (int i = 0; i < 16; ++i) lw += s_sum[i * 16 + q];
     if (q >= nq) return;
     const int head = h * a.group + qb * kKvQueries + q;
@@ -847,11 +851,19 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
             lw > 0.f || lw != lw ? (top + __log2f(lw)) * 0.69314718055994531f : -INFINITY;
     const int d = F::feature(x);
     if (d >= D) return;
-    const float *const o0 = a.part_o + (wg * (F::kWaves + 2) + F::kWaves) * F::kEntry + x;
-    float o = weight[q] * o0[slot0 * F::kEntry];
-#pragma unroll 8
-    for (int i = 1; i < n; ++i)
-        o += weight[i * 16 + q] * o0[(int64_t)i * (F::kWaves + 2) * F::kEntry];
+    float o = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < n; i += batch) {
+        float now[batch];
+#pragma unroll
+        for (int k = 0; k < batch; ++k) now[k] = in[k];
+        if (i + batch < n)
+#pragma unroll
+            for (int k = 0; k < batch; ++k) in[k] = part(min(i + batch + k, n - 1));
+#pragma unroll
+        for (int k = 0; k < batch; ++k)
+            if (i + k < n) o += weight[(i + k) * 16 + q] * now[k];
+    }
     a.out[b * a.out_seq + head * a.out_head + d] =
         (uint16_t)pack2<FP16>(lw > 0.f || lw != lw ? o / lw : 0.f, 0.f);
 }
@@ -871,7 +883,7 @@ hipError_t launch(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hi
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>),
-                       dim3((unsigned)a.seqs * c.heads * p.qblocks * (F::kEntry / 256)), dim3(256), 0,
+                       dim3((unsigned)c.heads * p.qblocks * (p.splits - 1) * (F::kEntry / 256)), dim3(256), 0,
                        s, c, a, p.splits);
     return hipGetLastError();
 }
@@ -909,8 +921,8 @@ KvAttendPlan plan_kv_attend(const KvCache &c, int seqs, int group, int64_t table
     const size_t entry = (size_t)((c.dim / gran + 15) / 16 * gran) * 256 * sizeof(float);
     const size_t wgs = (size_t)c.heads * p.qblocks * p.splits;
     const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    p.first_tile_off = 0;
-    p.part_o_off = up((size_t)(seqs + 1) * sizeof(int32_t));
+    p.shared_off = 0;
+    p.part_o_off = up(wgs * sizeof(KvShared));
     p.part_ml_off = p.part_o_off + wgs * (waves + 2) * entry;
     p.total = p.part_ml_off + up(wgs * 64 * sizeof(float));
     return p;
