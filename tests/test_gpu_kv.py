@@ -164,6 +164,38 @@ def test_write_unusual_values(dtype, sub):
     assert kc[3, 0, s] == 0 and kc[4, 0, 9 // sub] == 0 and kc[5, 0, 10 // sub] == 0
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("sub", [2, 4, 8])
+def test_write_below_the_normal_range(dtype, sub):
+    """Centres and tokens among the least numbers of the type, and tokens of
+    ordinary size that such centres tell apart."""
+    cache = make_cache(2, 64, sub, 256, dtype, 20, 32, seed=12)
+    tiny = 2.0 ** -17 if dtype is FP else 2.0 ** -130
+    cache.k_centres.copy_((tiny * torch.randn(cache.k_centres.shape, device=DEV)).to(dtype))
+    k, v = tokens(cache, 600, 6)
+    k[:200] = (tiny * k[:200].float()).to(dtype)
+    cache.v_centres[..., 0] = (4 * tiny * torch.randn(2, 64 // sub, 256, device=DEV)).to(dtype)
+    cache.v_centres[..., 1:] = 0
+    v[..., ::sub] = 1.0
+    slots = torch.arange(600)
+    km.kmeans_kv_write(cache, k, v, slots.to(DEV))
+    kc, vc = codes_at(cache, slots)
+    assert np.array_equal(kc, nearest(k, cache.k_centres))
+    assert np.array_equal(vc, nearest(v, cache.v_centres))
+
+
+@pytest.mark.parametrize("n", [129, 2000, 5000])
+def test_write_many_tokens(n):
+    """More tokens than one round of the launch takes."""
+    cache = make_cache(1 if n > 4000 else 6, 64, 4, 64, BF, -(-n // 64), 64, seed=n)
+    k, v = tokens(cache, n, 7)
+    slots = torch.randperm(n, generator=torch.Generator().manual_seed(n))
+    km.kmeans_kv_write(cache, k, v, slots.to(DEV))
+    kc, vc = codes_at(cache, slots)
+    assert np.array_equal(kc, nearest(k, cache.k_centres))
+    assert np.array_equal(vc, nearest(v, cache.v_centres))
+
+
 def test_write_strides_and_padding():
     cache = make_cache(3, 64, 4, 50, BF, 10, 16, random_codes=False)
     n = 45
