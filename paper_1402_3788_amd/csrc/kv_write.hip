@@ -10,14 +10,14 @@
 //   the stated distance is off by 6.5 * 2^-24 of itself, itself <= 2 (|x|^2 + |c|^2).
 // So the centre that the definition chooses scores at least the best score less
 // 2 E + 6.5 * 2^-23 (|x|^2 + C^2) < 2^-17 (|x|^2 + C^2), C the largest |c|. The
-// groups of 16 centres whose best score is not below that are evaluated as the
-// definition says, nearly always one group of the 16. Where a bound is not a
+// groups of 8 centres whose best score is not below that are evaluated as the
+// definition says, nearly always one group of the 32. Where a bound is not a
 // number (overflow, NaN) every group is.
 //
-// A sub-vector costs 128 scores to a lane at half an instruction each (the
-// maximum of three), and 8 distances at 18: the vector ALU bounds it. 4096 tokens
-// of 8 heads of 128 features in sub-vectors of 4 (2.1 million of 256 centres):
-// FIGURE.
+// A wave keeps the 256 centres of one sub-vector as matrix operands in its
+// registers and takes 32 tokens a step. A lane then has 128 scores, at half an
+// instruction each (the maximum of three), and 4 distances at some 17: the vector
+// ALU bounds it. FIGURE.
 #include "kv_device.h"
 
 namespace lloyd {
@@ -25,7 +25,6 @@ namespace lloyd {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kSubs = 4;             // sub-vectors of a workgroup: a dword of key codes
 constexpr int kTokens = 32;          // tokens of a wave's step, columns of the product
 
 typedef float f16v __attribute__((ext_vector_type(16)));
@@ -59,176 +58,193 @@ __device__ inline f16v product(bool fp16, const Operand<SUB> &a, const Operand<S
 
 __device__ inline uint32_t bf16_bits(float x) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// A workgroup takes kSubs sub-vectors of one head of the keys or the values
-// (their centres in LDS), and of the tokens the steps y, y + gridDim.y, ...
+// The nearest of 8 centres' worth of distances: see below.
+template <bool FP16, int SUB>
+__device__ inline void evaluate(const Operand<SUB> *centre, int row, const float (&x)[SUB],
+                                float &near, int &code)
+{
+    float d[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const Operand<SUB> o = centre[row + k];
+        KvEntry<SUB> e;
+#pragma unroll
+        for (int i = 0; i < SUB / 2; ++i) e.w[i] = o.w[i];
+        float y[SUB];
+        kv_unpack<FP16>(e, y);
+        d[k] = kv_distance(x, y);
+    }
+    const float least = fminf(fminf(d[0], d[1]), fminf(d[2], d[3]));
+    const int j = row + (d[0] == least ? 0 : d[1] == least ? 1 : d[2] == least ? 2 : 3);
+    if (least < near || (least == near && j < code)) {   // not for a NaN
+        near = least;
+        code = j;
+    }
+}
+
+// A workgroup takes kWaves sub-vectors of one head of the keys or the values, one
+// to a wave, and of the tokens the steps y, y + gridDim.y, ... The waves share
+// nothing but the lines of memory their tokens lie on.
 template <int SUB, bool FP16>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens t)
 {
-    __shared__ Operand<SUB> centre[kSubs][256];
-    __shared__ Operand<SUB> half_norm[kSubs][256];
-    __shared__ float largest[kSubs][kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int S = c.dim / SUB, groups = S / kSubs;
-    const int s0 = (int)(blockIdx.x % groups) * kSubs;
+    __shared__ Operand<SUB> centres_of[kWaves][256];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, up = lane >> 5;
+    const int S = c.dim / SUB, groups = S / kWaves;
+    const int s = (int)(blockIdx.x % groups) * kWaves + wave;
     const int h = (int)(blockIdx.x / groups) % c.heads;
     const bool values = (int)(blockIdx.x / groups) >= c.heads;
     const uint16_t *const centres = (values ? c.v_centres : c.k_centres) +
-                                    ((int64_t)h * S + s0) * c.K * SUB;
-#pragma unroll 1
-    for (int s = 0; s < kSubs; ++s) {
-        // one centre to a thread
-        static_assert(kThreads == 256, "");
-        Operand<SUB> op{}, rec{};
-        float norm = 0.f;
-        if (tid < c.K) {
-            const KvEntry<SUB> e = kv_load<SUB>(centres + (s * c.K + tid) * SUB);
-            float y[SUB];
+                                    ((int64_t)h * S + s) * c.K * SUB;
+    Operand<SUB> *const centre = centres_of[wave];
+    const int64_t stride = (int64_t)gridDim.y * kTokens;
+    const int64_t begin = (int64_t)blockIdx.y * kTokens;
+    const uint16_t *const rows = values ? t.v + h * t.v_head + s * SUB : t.k + h * t.k_head + s * SUB;
+    const int64_t row_stride = values ? t.v_token : t.k_token;
+
+    // Tokens of a step: the lane's sub-vector and slot. Past the end: the last's.
+    KvEntry<SUB> next;
+    int64_t next_slot;
+    const auto ask = [&](int64_t first) {
+        const int64_t tok = min(first + col, t.tokens - 1);
+        next_slot = t.slots[tok];
+        next = kv_load<SUB>(rows + tok * row_stride);
+    };
+    ask(begin);
+
+    // Operands, tile n: centres 32 n + col. bf16: one product, the lower lanes'
+    // values are the centre, the upper ones' the three parts of -|c|^2 / 2; fp16:
+    // a product for each. Places from K on: zeros and a norm that never wins, and
+    // in LDS no number, whose distance never does.
+    Operand<SUB> a[8];
+    Operand<4> norm_of[FP16 ? 8 : 1];
+    float big = 0.f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        const int j = n * 32 + col;
+        Operand<SUB> op{};
+        Operand<4> rec{};
+        rec.w[0] = 0xFF7Fu;
+        KvEntry<SUB> e;
+#pragma unroll
+        for (int i = 0; i < SUB / 2; ++i) e.w[i] = 0x7FFF7FFFu;
+        if (j < c.K) {
+            e = kv_load<SUB>(centres + j * SUB);
+            float y[SUB], norm = 0.f;
             kv_unpack<FP16>(e, y);
 #pragma unroll
-            for (int i = 0; i < SUB / 2; ++i) op.w[i] = e.w[i];
-#pragma unroll
             for (int i = 0; i < SUB; ++i) norm = __builtin_fmaf(y[i], y[i], norm);
-            const float n = -0.5f * norm;
-            const uint32_t hi = bf16_bits(n);
-            const float n1 = n - __uint_as_float(hi << 16);
+            big = fmaxf(big, norm);
+            const float n0 = -0.5f * norm;
+            const uint32_t hi = bf16_bits(n0);
+            const float n1 = n0 - __uint_as_float(hi << 16);
             const uint32_t mid = bf16_bits(n1);
-            const float n2 = n1 - __uint_as_float(mid << 16);
             rec.w[0] = hi | mid << 16;
-            rec.w[1] = bf16_bits(n2);
+            rec.w[1] = bf16_bits(n1 - __uint_as_float(mid << 16));
             if (!(norm < INFINITY)) rec.w[0] = rec.w[1] = 0;     // every group is evaluated
-        } else {
-            rec.w[0] = 0xFF7Fu;                                  // no centre: never the best
+#pragma unroll
+            for (int i = 0; i < SUB / 2; ++i) op.w[i] = e.w[i];
         }
-        centre[s][tid] = op;
-        half_norm[s][tid] = rec;
-        for (int d = 32; d; d /= 2) norm = fmaxf(norm, __shfl_xor(norm, d));
-        if (lane == 0) largest[s][wave] = norm;
+        if (!up) {
+            Operand<SUB> o{};
+#pragma unroll
+            for (int i = 0; i < SUB / 2; ++i) o.w[i] = e.w[i];
+            centre[j] = o;
+        }
+        if constexpr (FP16) {
+            norm_of[n] = rec;
+        } else if (up) {
+            op = Operand<SUB>{};
+            op.w[0] = rec.w[0];
+            op.w[1] = rec.w[1];
+        }
+        a[n] = op;
     }
-    __syncthreads();
-
-    const int col = lane & 31, up = lane >> 5;
+#pragma unroll
+    for (int d = 16; d; d /= 2) big = fmaxf(big, __shfl_xor(big, d));
     const int tiles = (c.K + 31) >> 5;
-    const int64_t stride = (int64_t)gridDim.y * (kWaves * kTokens);
-    for (int64_t first = (int64_t)blockIdx.y * (kWaves * kTokens) + wave * kTokens; first < t.tokens;
-         first += stride) {
-        const int64_t tok = first + col;
-        int64_t page = 0;
-        int off = 0;
-        const bool live = tok < t.tokens && kv_slot(c, t.slots[tok], &page, &off);
-        const int64_t from = live ? tok : first;
-        const uint16_t *const src = (values ? t.v + from * t.v_token + h * t.v_head
-                                            : t.k + from * t.k_token + h * t.k_head) + s0 * SUB;
-        KvEntry<SUB> in[kSubs];
-        __builtin_memcpy(in, __builtin_assume_aligned(src, 16), sizeof(in));
-        uint32_t codes = 0;
-#pragma unroll 1
-        for (int s = 0; s < kSubs; ++s) {
-            float x[SUB];
-            KvEntry<SUB> e = in[0];
+    // columns of the norms' product: ones for the three parts
+    Operand<4> ones{};
+    if (FP16 ? !up : up) {
+        ones.w[0] = 0x3F803F80u;
+        ones.w[1] = 0x3F80u;
+    }
+    __builtin_amdgcn_wave_barrier();                     // a wave's LDS is its own, in order
+
+    for (int64_t first = begin; first < t.tokens; first += stride) {
+        const KvEntry<SUB> e = next;
+        const int64_t slot = next_slot;
+        if (first + stride < t.tokens) ask(first + stride);
+        float x[SUB], norm = 0.f;
+        kv_unpack<FP16>(e, x);
 #pragma unroll
-            for (int i = 1; i < kSubs; ++i)
-                if (s == i) e = in[i];
-            kv_unpack<FP16>(e, x);
-            float norm = 0.f;
+        for (int i = 0; i < SUB; ++i) norm = __builtin_fmaf(x[i], x[i], norm);
+        Operand<SUB> bx{};
 #pragma unroll
-            for (int i = 0; i < SUB; ++i) norm = __builtin_fmaf(x[i], x[i], norm);
-            // columns of the product: tokens. bf16: the lower lanes' values are x,
-            // the upper ones' take the three parts of the norm; fp16: a product for each.
-            Operand<SUB> bx{}, ones{};
-            if (FP16 || up == 0)
-#pragma unroll
-                for (int i = 0; i < SUB / 2; ++i) bx.w[i] = FP16 && up ? 0u : e.w[i];
-            if (FP16 ? up == 0 : up == 1) {
-                ones.w[0] = 0x3F803F80u;
-                ones.w[1] = 0x3F80u;
-            }
-            if (!FP16 && up) bx = ones;
-            const Operand<SUB> *const a = !FP16 && up ? half_norm[s] : centre[s];
-            float top[8];
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                top[n] = -INFINITY;
-                if (n >= tiles) continue;
-                f16v d = {};
-                if (FP16) {
-                    Operand<4> rec, one;
-                    rec.w[0] = half_norm[s][n * 32 + col].w[0];
-                    rec.w[1] = half_norm[s][n * 32 + col].w[1];
-                    one.w[0] = ones.w[0];
-                    one.w[1] = ones.w[1];
-                    d = product<4>(false, rec, one, d);
-                }
-                d = product<SUB>(FP16, a[n * 32 + col], bx, d);
-                float m = fmaxf(d[0], d[1]);
-#pragma unroll
-                for (int i = 2; i < 16; ++i) m = fmaxf(m, d[i]);
-                top[n] = m;
-            }
-            float best = top[0];
-#pragma unroll
-            for (int n = 1; n < 8; ++n) best = fmaxf(best, top[n]);
-            best = fmaxf(best, __shfl_xor(best, 32));
-            const float big = fmaxf(fmaxf(largest[s][0], largest[s][1]),
-                                    fmaxf(largest[s][2], largest[s][3]));
-            const float least = best - (0x1p-17f * (norm + big) + 1e-30f);
-            // bit n: rows 32 n + 8 i + 0..3 for i = 0..3; bit 8 + n: those + 4
-            uint32_t open = 0;
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-                if (n < tiles && !(top[n] < least)) open |= 1u << n;
-            const uint32_t other = __shfl_xor(open, 32);
-            open = up ? open << 8 | other : open | other << 8;
-            // both lanes of a token evaluate half of a group's 16 centres each
-            float near = INFINITY;
-            int code = 0;
-            while (__any(open)) {
-                if (open) {
-                    const int bit = __builtin_ctz(open);
-                    open &= open - 1;
-                    const int row = (bit & 7) * 32 + (bit >> 3) * 4 + up * 16;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int j = row + (k >> 2) * 8 + (k & 3);
-                        KvEntry<SUB> ce;
-                        const Operand<SUB> o = centre[s][j];
-#pragma unroll
-                        for (int i = 0; i < SUB / 2; ++i) ce.w[i] = o.w[i];
-                        float y[SUB];
-                        kv_unpack<FP16>(ce, y);
-                        const float d = kv_distance(x, y);
-                        if (j < c.K && (d < near || (d == near && j < code))) {
-                            near = d;
-                            code = j;
-                        }
-                    }
-                }
-            }
-            const float near2 = __shfl_xor(near, 32);
-            const int code2 = __shfl_xor(code, 32);
-            if (near2 < near || (near2 == near && code2 < code)) code = code2;
-            codes |= (uint32_t)code << (8 * s);
+        for (int i = 0; i < SUB / 2; ++i) bx.w[i] = up ? 0u : e.w[i];
+        if (!FP16 && up) {
+            bx.w[0] = ones.w[0];
+            bx.w[1] = ones.w[1];
         }
-        if (!live) continue;
+        // top[2 n + u]: of the lane's rows 32 n + 16 u + 8 i + 4 up + 0..3, i = 0, 1
+        float top[16];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            top[2 * n] = top[2 * n + 1] = -INFINITY;
+            if (n >= tiles) continue;
+            f16v d = {};
+            if constexpr (FP16) d = product<4>(false, norm_of[n], ones, d);
+            d = product<SUB>(FP16, a[n], bx, d);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float m = fmaxf(d[8 * u], d[8 * u + 1]);
+#pragma unroll
+                for (int i = 2; i < 8; ++i) m = fmaxf(m, d[8 * u + i]);
+                top[2 * n + u] = m;
+            }
+        }
+        float best = top[0];
+#pragma unroll
+        for (int n = 1; n < 16; ++n) best = fmaxf(best, top[n]);
+        best = fmaxf(best, __shfl_xor(best, 32));
+        const float least = best - (0x1p-17f * (norm + big) + 1e-30f);
+        uint32_t open = 0;
+#pragma unroll
+        for (int n = 0; n < 16; ++n) open |= top[n] < least ? 0u : 1u << n;
+        open &= (1u << (2 * tiles)) - 1;
+        const uint32_t other = __shfl_xor(open, 32);
+        open = up ? open << 16 | other : open | other << 16;
+        // both lanes of a token evaluate half of a group's 8 centres each
+        float near = INFINITY;
+        int code = 0;
+        while (__any(open)) {
+            if (open) {
+                const int bit = __builtin_ctz(open);
+                open &= open - 1;
+                evaluate<FP16>(centre, (bit & 15) * 16 + (bit >> 4) * 4 + up * 8, x, near, code);
+            }
+        }
+        const float near2 = __shfl_xor(near, 32);
+        const int code2 = __shfl_xor(code, 32);
+        if (near2 < near || (near2 == near && code2 < code)) code = code2;
+        int64_t page;
+        int off;
+        if (up || first + col >= t.tokens || !kv_slot(c, slot, &page, &off)) continue;
         const int64_t head = (page * c.heads + h) << c.page_log2;
-        if (!values) {
-            if (!up)
-                *reinterpret_cast<uint32_t *>(c.k_codes + (head + off) * S + s0) = codes;
-        } else {
-            uint8_t *const dst = c.v_codes + head * S + off;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                dst[(int64_t)(s0 + 2 * up + s) << c.page_log2] = (uint8_t)(codes >> (8 * (2 * up + s)));
-        }
+        uint8_t *const dst = values ? c.v_codes + head * S + ((int64_t)s << c.page_log2) + off
+                                    : c.k_codes + (head + off) * S + s;
+        *dst = (uint8_t)code;
     }
 }
 
 template <int SUB>
 hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
 {
-    const unsigned kinds = 2 * c.heads * (c.dim / SUB / kSubs);
-    const int64_t steps = (t.tokens + kWaves * kTokens - 1) / (kWaves * kTokens);
-    // enough workgroups for every CU to hold several, no more: each loads centres
-    const int64_t most = (8 * kCUs + kinds - 1) / kinds;
+    const unsigned kinds = 2 * c.heads * (c.dim / SUB / kWaves);
+    const int64_t steps = (t.tokens + kTokens - 1) / kTokens;
+    // enough workgroups for every CU to hold several, no more: each reads centres
+    const int64_t most = (6 * kCUs + kinds - 1) / kinds;
     const unsigned y = (unsigned)(steps < most ? steps : most);
     if (c.fp16)
         hipLaunchKernelGGL((kv_write_kernel<SUB, true>), dim3(kinds, y), dim3(kThreads), 0, s, c, t);
