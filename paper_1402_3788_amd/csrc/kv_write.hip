@@ -1,18 +1,20 @@
 // Encoding of keys and values into the cache: every sub-vector x gets the number
 // of its nearest centre (Eq. (2), in the fp32 operations kmeans.h states).
 //
-// The matrix cores screen: score_j = x . c_j - |c_j|^2 / 2, the largest of which
-// belongs to the nearest centre but for rounding. What rounding can do is bounded:
-//   products of 16-bit numbers are exact in fp32; up to 11 of them and of the
-//   parts of |c|^2 / 2 are added, each addition off by at most 2^-23 of the
-//   magnitudes summed (no more than faithful rounding assumed), and |c|^2 / 2 by
-//   10 such units of itself, so a score is off by E <= 21 * 2^-23 (|x|^2 + |c|^2);
-//   the stated distance is off by 6.5 * 2^-24 of itself, itself <= 2 (|x|^2 + |c|^2).
+// The matrix cores screen: score_j = T + x . c_j - |c_j|^2 / 2, the largest of
+// which belongs to the nearest centre but for rounding. T, the same for all
+// centres, is a little over M = |x|^2 + C^2, C the largest |c|, so that no score is
+// negative and their bits compare as whole numbers do (a maximum of three needs
+// no instruction to quiet its inputs then). What rounding can do is bounded:
+//   products of 16-bit numbers are exact in fp32; up to 8 of them, the three parts
+//   of |c|^2 / 2 and T are added, each addition off by at most 2^-23 of what it
+//   adds up to, here below 2.1 M (no more than faithful rounding assumed), and
+//   |c|^2 / 2 by 10 such units of itself: a score is off by E <= 31 * 2^-23 M;
+//   the stated distance is off by 6.5 * 2^-24 of itself, itself <= 2 M.
 // So the centre that the definition chooses scores at least the best score less
-// 2 E + 6.5 * 2^-23 (|x|^2 + C^2) < 2^-17 (|x|^2 + C^2), C the largest |c|. The
-// groups of 8 centres whose best score is not below that are evaluated as the
-// definition says, nearly always one group of the 32. Where a bound is not a
-// number (overflow, NaN) every group is.
+// 2 E + 6.5 * 2^-23 M < 2^-16 M. The groups of 8 centres whose best score is not
+// below that are evaluated as the definition says, nearly always one group of the
+// 32. Where a bound is not a finite number (overflow, NaN) every group is.
 //
 // A wave keeps the 256 centres of one sub-vector as matrix operands in its
 // registers and takes 32 tokens a step. A lane then has 128 scores, at half an
@@ -86,7 +88,7 @@ __device__ inline void evaluate(const Operand<SUB> *centre, int row, const float
 // to a wave, and of the tokens the steps y, y + gridDim.y, ... The waves share
 // nothing but the lines of memory their tokens lie on.
 template <int SUB, bool FP16>
-__global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens t)
+__global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvTokens t)
 {
     __shared__ Operand<SUB> centres_of[kWaves][256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens 
         const int j = n * 32 + col;
         Operand<SUB> op{};
         Operand<4> rec{};
-        rec.w[0] = 0xFF7Fu;
+        rec.w[0] = 0xFF7Fu;                              // bf16, as all of the record
         KvEntry<SUB> e;
 #pragma unroll
         for (int i = 0; i < SUB / 2; ++i) e.w[i] = 0x7FFF7FFFu;
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens 
             const float n1 = n0 - __uint_as_float(hi << 16);
             const uint32_t mid = bf16_bits(n1);
             rec.w[0] = hi | mid << 16;
-            rec.w[1] = bf16_bits(n1 - __uint_as_float(mid << 16));
+            rec.w[1] = bf16_bits(n1 - __uint_as_float(mid << 16)) | 0x3F800000u;
             if (!(norm < INFINITY)) rec.w[0] = rec.w[1] = 0;     // every group is evaluated
 #pragma unroll
             for (int i = 0; i < SUB / 2; ++i) op.w[i] = e.w[i];
@@ -164,12 +166,8 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens 
 #pragma unroll
     for (int d = 16; d; d /= 2) big = fmaxf(big, __shfl_xor(big, d));
     const int tiles = (c.K + 31) >> 5;
-    // columns of the norms' product: ones for the three parts
-    Operand<4> ones{};
-    if (FP16 ? !up : up) {
-        ones.w[0] = 0x3F803F80u;
-        ones.w[1] = 0x3F80u;
-    }
+    // columns of the norms' product: ones for the three parts, T for its 1
+    const bool takes_norm = FP16 ? !up : up;
     __builtin_amdgcn_wave_barrier();                     // a wave's LDS is its own, in order
 
     for (int64_t first = begin; first < t.tokens; first += stride) {
@@ -180,6 +178,12 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens 
         kv_unpack<FP16>(e, x);
 #pragma unroll
         for (int i = 0; i < SUB; ++i) norm = __builtin_fmaf(x[i], x[i], norm);
+        const float total = norm + big;
+        Operand<4> ones{};
+        if (takes_norm) {
+            ones.w[0] = 0x3F803F80u;
+            ones.w[1] = 0x3F80u | bf16_bits(1.01f * total) << 16;
+        }
         Operand<SUB> bx{};
 #pragma unroll
         for (int i = 0; i < SUB / 2; ++i) bx.w[i] = up ? 0u : e.w[i];
@@ -187,32 +191,43 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens 
             bx.w[0] = ones.w[0];
             bx.w[1] = ones.w[1];
         }
-        // top[2 n + u]: of the lane's rows 32 n + 16 u + 8 i + 4 up + 0..3, i = 0, 1
-        float top[16];
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            top[2 * n] = top[2 * n + 1] = -INFINITY;
-            if (n >= tiles) continue;
+        // top[2 n + u]: the bits of the best score of the lane's rows
+        // 32 n + 16 u + 8 i + 4 up + 0..3, i = 0, 1
+        int top[16];
+        const auto score = [&](int n) {
             f16v d = {};
             if constexpr (FP16) d = product<4>(false, norm_of[n], ones, d);
             d = product<SUB>(FP16, a[n], bx, d);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                float m = fmaxf(d[8 * u], d[8 * u + 1]);
+                int m = max(__float_as_int(d[8 * u]), __float_as_int(d[8 * u + 1]));
 #pragma unroll
-                for (int i = 2; i < 8; ++i) m = fmaxf(m, d[8 * u + i]);
+                for (int i = 2; i < 8; ++i) m = max(m, __float_as_int(d[8 * u + i]));
                 top[2 * n + u] = m;
             }
+        };
+        if (tiles == 8) {                                // without branches between the products
+#pragma unroll
+            for (int n = 0; n < 8; ++n) score(n);
+        } else {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                top[2 * n] = top[2 * n + 1] = (int)0x80000000;
+                if (n < tiles) score(n);
+            }
         }
-        float best = top[0];
+        int best = top[0];
 #pragma unroll
-        for (int n = 1; n < 16; ++n) best = fmaxf(best, top[n]);
-        best = fmaxf(best, __shfl_xor(best, 32));
-        const float least = best - (0x1p-17f * (norm + big) + 1e-30f);
-        uint32_t open = 0;
+        for (int n = 1; n < 16; ++n) best = max(best, top[n]);
+        best = max(best, __shfl_xor(best, 32));
+        const float least = __int_as_float(best) - (0x1p-16f * total + 1e-30f);
+        // bit 15 - n: group n is below the least that could be the nearest's
+        uint32_t below = 0;
 #pragma unroll
-        for (int n = 0; n < 16; ++n) open |= top[n] < least ? 0u : 1u << n;
-        open &= (1u << (2 * tiles)) - 1;
+        for (int n = 0; n < 16; ++n)
+            below = __builtin_amdgcn_alignbit(below, __float_as_uint(__int_as_float(top[n]) - least), 31);
+        uint32_t open = least < INFINITY ? ~below & 0xFFFFu : 0xFFFFu;   // all for a NaN
+        open &= 0xFFFFu << (16 - 2 * tiles);
         const uint32_t other = __shfl_xor(open, 32);
         open = up ? open << 16 | other : open | other << 16;
         // both lanes of a token evaluate half of a group's 8 centres each
@@ -222,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvTokens 
             if (open) {
                 const int bit = __builtin_ctz(open);
                 open &= open - 1;
-                evaluate<FP16>(centre, (bit & 15) * 16 + (bit >> 4) * 4 + up * 8, x, near, code);
+                evaluate<FP16>(centre, (~bit & 15) * 16 + (bit >> 4) * 4 + up * 8, x, near, code);
             }
         }
         const float near2 = __shfl_xor(near, 32);
