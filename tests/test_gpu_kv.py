@@ -233,6 +233,15 @@ READ = [
     (2, 96, 4, 256, FP, 1025, 64),
     (5, 64, 8, 16, FP, 2000, 1024),
     (1, 128, 2, 256, BF, 4099, 16),
+    (64, 64, 2, 256, BF, 1030, 16),
+    (64, 96, 8, 31, FP, 1500, 8),
+    (32, 128, 4, 256, FP, 5003, 64),
+    (40, 64, 8, 256, BF, 2047, 32),
+    (32, 96, 4, 200, BF, 1999, 16),
+    (33, 96, 2, 256, FP, 1024, 128),
+    (64, 128, 2, 255, BF, 1111, 8),
+    (48, 64, 4, 256, FP, 1201, 1024),
+    (64, 128, 8, 256, BF, 513, 16),
 ]
 
 
