@@ -5,7 +5,8 @@
 // memory, one sub-vector to a thread. Many take them from LDS, where a workgroup
 // keeps the centres of one head of the keys or the values (16 to 64 KB): looked up
 // in the L2, each of 8 bytes moves a line of 128, and 65536 tokens of 8 heads of
-// 128 features took 193 us (1.6 TB/s) instead of FIGURE.
+// 128 features took 193 us (1.6 TB/s) instead of 78 (3.9 TB/s,
+// where a copy of 2 GiB moves 4.8).
 #include "kv_device.h"
 
 namespace lloyd {
@@ -38,12 +39,15 @@ __global__ __launch_bounds__(kThreads) void kv_read_few_kernel(KvCache c, KvToke
     }
 }
 
-constexpr int kWaves = 8;
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 16;
 constexpr int kTokens = 16;          // of a wave's step
 
 // A workgroup takes one head of the keys or the values, and a run of the tokens.
-// A step of a wave is 16 tokens: lane 16 g + r has token r and of its row of
-// dim / 8 runs of 16 bytes those numbered g, g + 4, ...
+// A step of a wave is 16 tokens, their rows' runs of 16 bytes in order over its
+// lanes: each store covers whole rows, and past the caches, for the rows are as
+// large as those and not read here again.
 template <int D, int SUB>
 __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTokens t, int parts)
 {
@@ -51,7 +55,6 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
     constexpr int runs = D / 32;                         // of a lane
     __shared__ KvEntry<SUB> book[S][256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int r = lane & 15, g = lane >> 4;
     const int h = (int)(blockIdx.x % c.heads);
     const bool values = blockIdx.x / c.heads % 2;
     const int64_t steps = (t.tokens + kTokens - 1) / kTokens;
@@ -74,48 +77,56 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
     __syncthreads();
     uint16_t *const out = values ? t.v + h * t.v_head : t.k + h * t.k_head;
     const int64_t out_stride = values ? t.v_token : t.k_token;
-    // the slot of the next step's token is asked for a step ahead
-    const auto slot_of = [&](int64_t step) {
-        const int64_t tok = step * kTokens + r;
-        return step < to && tok < t.tokens ? t.slots[tok] : (int64_t)-1;
+    // run i of the lane: of token (64 i + lane) / (D / 8) of the step
+    const auto token_of = [&](int i) { return (i * kWave + lane) / (D / 8); };
+    const auto run_of = [&](int i) { return (i * kWave + lane) % (D / 8); };
+    // the slots of the next step's tokens are asked for a step ahead
+    int64_t next[runs];
+    const auto ask = [&](int64_t step) {
+#pragma unroll
+        for (int i = 0; i < runs; ++i) {
+            const int64_t tok = step * kTokens + token_of(i);
+            next[i] = step < to && tok < t.tokens ? t.slots[tok] : (int64_t)-1;
+        }
     };
-    int64_t next = slot_of(from + wave);
+    ask(from + wave);
     for (int64_t step = from + wave; step < to; step += kWaves) {
-        const int64_t tok = step * kTokens + r;
-        int64_t page;
-        int off;
-        const bool live = kv_slot(c, next, &page, &off);
-        next = slot_of(step + kWaves);
         uint32_t codes[runs];
-        if (live) {
+        bool live[runs];
+#pragma unroll
+        for (int i = 0; i < runs; ++i) {
+            int64_t page;
+            int off;
+            live[i] = kv_slot(c, next[i], &page, &off);
+            codes[i] = 0;
+            if (!live[i]) continue;
             const int64_t head = (page * c.heads + h) << c.page_log2;
-            const uint8_t *const k = c.k_codes + (head + off) * S + g * per;
-            const uint8_t *const v = c.v_codes + head * S + off + ((int64_t)(g * per) << c.page_log2);
+            const int s = run_of(i) * per;
+            if (values) {
+                const uint8_t *const v = c.v_codes + head * S + off + ((int64_t)s << c.page_log2);
 #pragma unroll
-            for (int i = 0; i < runs; ++i) {
-                codes[i] = 0;
-                if (values) {
-#pragma unroll
-                    for (int x = 0; x < per; ++x)
-                        codes[i] |= (uint32_t)v[(int64_t)(i * 4 * per + x) << c.page_log2] << (8 * x);
-                } else {
-                    __builtin_memcpy(&codes[i], __builtin_assume_aligned(k + i * 4 * per, per), per);
-                }
+                for (int x = 0; x < per; ++x) codes[i] |= (uint32_t)v[x << c.page_log2] << (8 * x);
+            } else {
+                __builtin_memcpy(&codes[i],
+                                 __builtin_assume_aligned(c.k_codes + (head + off) * S + s, per), per);
             }
         }
-        if (tok >= t.tokens) continue;
-        uint16_t *const dst = out + tok * out_stride + g * 8;
+        ask(step + kWaves);
 #pragma unroll
         for (int i = 0; i < runs; ++i) {
             KvEntry<8> row{};
-            if (live)
+            if (live[i])
 #pragma unroll
                 for (int x = 0; x < per; ++x) {
-                    const KvEntry<SUB> e = book[(i * 4 + g) * per + x][(codes[i] >> (8 * x)) & 255];
+                    const KvEntry<SUB> e = book[run_of(i) * per + x][(codes[i] >> (8 * x)) & 255];
 #pragma unroll
                     for (int w = 0; w < SUB / 2; ++w) row.w[x * (SUB / 2) + w] = e.w[w];
                 }
-            *reinterpret_cast<KvEntry<8> *>(dst + i * 32) = row;
+            const int64_t tok = step * kTokens + token_of(i);
+            if (tok < t.tokens)
+                __builtin_nontemporal_store(
+                    __builtin_bit_cast(u4v, row),
+                    reinterpret_cast<u4v *>(out + tok * out_stride + run_of(i) * 8));
         }
     }
 }
