@@ -16,7 +16,12 @@ import math
 
 import torch
 
-from . import KmeansError, KMEANS_EUNSUPPORTED, _lib, _stream_ptr
+from . import KmeansError, KMEANS_EUNSUPPORTED, _lib
+
+# a tenth of the time of torch.cuda.current_stream and current_device, which
+# small calls would mostly consist of
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}      # KMEANS_KV_BF16, KMEANS_KV_FP16
 
@@ -78,6 +83,8 @@ class KVCodes:
         self._desc = _Desc(*(t.data_ptr() for t in tensors), pages, page, heads, S * sub, sub, K,
                            _TYPES[self.dtype])
         self._ref = ctypes.byref(self._desc)
+        self.index = k_centres.get_device()
+        self._ws_bytes = {}
         # the library says what it takes; it looks at no pointer here
         if not self.attend_workspace_bytes(1, heads, 1):
             raise KmeansError("KVCodes", KMEANS_EUNSUPPORTED)
@@ -93,46 +100,54 @@ class KVCodes:
         return cls(k_centres, v_centres, *codes)
 
     def attend_workspace_bytes(self, seqs: int, q_heads: int, table_pages: int) -> int:
-        return int(_lib.kmeans_kv_attend_workspace_bytes(self._ref, seqs, q_heads, table_pages))
+        """Bytes that kmeans_kv_attend takes for its workspace; 0 if it refuses."""
+        key = (seqs, q_heads, table_pages)
+        nbytes = self._ws_bytes.get(key)
+        if nbytes is None:
+            nbytes = int(_lib.kmeans_kv_attend_workspace_bytes(self._ref, *key))
+            if len(self._ws_bytes) < 4096:
+                self._ws_bytes[key] = nbytes
+        return nbytes
 
 
-def _rows(cache, t, what, n=None):
+def _rows(cache, t, what):
     """t as the library takes it, [n, heads, dim] with its features contiguous
-    and its rows on 16 bytes, and its two strides; a copy where it is not."""
-    if not (isinstance(t, torch.Tensor) and t.dim() == 3 and t.device == cache.device
-            and t.dtype == cache.dtype and t.shape[2] == cache.dim):
+    and its rows on 16 bytes (a copy where it is not), its address, its shape
+    and its two strides."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is cache.dtype
+            and t.get_device() == cache.index and t.dim() == 3 and t.shape[2] == cache.dim):
         raise ValueError(f"{what} must be a [n, heads, {cache.dim}] tensor of the cache's type "
                          "on its GPU")
-    if n is not None and t.shape[0] != n:
-        raise ValueError(f"{what} must have {n} rows")
     a, b, c = t.stride()
-    if c != 1 or (a | b) & 7 or t.data_ptr() & 15:
+    at = t.data_ptr()
+    if c != 1 or (a | b) & 7 or at & 15:
         t = t.contiguous()
         if t.data_ptr() & 15:
             t = t.clone()
         a, b, c = t.stride()
-    return t, a, b
+        at = t.data_ptr()
+    return t, at, t.shape, a, b
 
 
 def _target(cache, t, shape, what):
-    """An output that the caller gave, or a new one."""
+    """An output that the caller gave, or a new one; its address and strides."""
     if t is None:
         t = torch.empty(shape, dtype=cache.dtype, device=cache.device)
-        return t, shape[1] * shape[2], shape[2]
+        return t, t.data_ptr(), shape[1] * shape[2], shape[2]
     if not (isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape)
-            and t.dtype == cache.dtype and t.device == cache.device):
+            and t.dtype is cache.dtype and t.get_device() == cache.index):
         raise ValueError(f"{what} must be {tuple(shape)} of the cache's type on its GPU")
     a, b, c = t.stride()
     if c != 1 or (a | b) & 7 or t.data_ptr() & 15 or (a == 0 and shape[0] > 1) \
             or (b == 0 and shape[1] > 1):
         raise ValueError(f"{what} needs contiguous features, rows on 16 bytes, and no two "
                          "elements in one place")
-    return t, a, b
+    return t, t.data_ptr(), a, b
 
 
 def _ints(cache, t, dtype, n, what):
-    if not (isinstance(t, torch.Tensor) and t.dim() == 1 and t.dtype == dtype
-            and t.device == cache.device and (n is None or t.shape[0] == n)):
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == cache.index
+            and t.dim() == 1 and (n is None or t.shape[0] == n)):
         raise ValueError(f"{what} must be a 1-D {dtype} tensor"
                          + ("" if n is None else f" of {n}") + " on the cache's GPU")
     return t if t.is_contiguous() else t.contiguous()
@@ -140,12 +155,11 @@ def _ints(cache, t, dtype, n, what):
 
 def _call(cache, fn, name, *args):
     """fn on the cache's device and current stream."""
-    dev = cache.device
-    if dev.index == torch.cuda.current_device():
-        rc = fn(cache._ref, *args, _stream_ptr(dev))
+    if _current_device() == cache.index:
+        rc = fn(cache._ref, *args, _raw_stream(cache.index))
     else:
-        with torch.cuda.device(dev):
-            rc = fn(cache._ref, *args, _stream_ptr(dev))
+        with torch.cuda.device(cache.device):
+            rc = fn(cache._ref, *args, _raw_stream(cache.index))
     if rc:
         raise KmeansError(name, rc)
 
@@ -156,12 +170,13 @@ def kmeans_kv_write(cache: KVCodes, k: torch.Tensor, v: torch.Tensor, slots: tor
     the cache is left out."""
     slots = _ints(cache, slots, torch.int64, None, "slots")
     n = slots.shape[0]
-    k, ka, kb = _rows(cache, k, "k", n)
-    v, va, vb = _rows(cache, v, "v", n)
-    if k.shape[1] != cache.heads or v.shape[1] != cache.heads:
-        raise ValueError(f"k and v must have {cache.heads} heads")
-    _call(cache, _lib.kmeans_kv_write, "kmeans_kv_write", k.data_ptr(), ka, kb, v.data_ptr(), va,
-          vb, slots.data_ptr(), n)
+    k, kp, shape, ka, kb = _rows(cache, k, "k")
+    v, vp, v_shape, va, vb = _rows(cache, v, "v")
+    if shape[0] != n or shape[1] != cache.heads or v_shape != shape:
+        raise ValueError(f"k and v must be [{n}, {cache.heads}, {cache.dim}], as slots and the "
+                         "cache are")
+    _call(cache, _lib.kmeans_kv_write, "kmeans_kv_write", kp, ka, kb, vp, va, vb,
+          slots.data_ptr(), n)
 
 
 def kmeans_kv_read(cache: KVCodes, slots: torch.Tensor, out=None):
@@ -172,10 +187,10 @@ def kmeans_kv_read(cache: KVCodes, slots: torch.Tensor, out=None):
     n = slots.shape[0]
     shape = (n, cache.heads, cache.dim)
     k, v = (None, None) if out is None else out
-    k, ka, kb = _target(cache, k, shape, "k")
-    v, va, vb = _target(cache, v, shape, "v")
-    _call(cache, _lib.kmeans_kv_read, "kmeans_kv_read", slots.data_ptr(), n, k.data_ptr(), ka, kb,
-          v.data_ptr(), va, vb)
+    k, kp, ka, kb = _target(cache, k, shape, "k")
+    v, vp, va, vb = _target(cache, v, shape, "v")
+    _call(cache, _lib.kmeans_kv_read, "kmeans_kv_read", slots.data_ptr(), n, kp, ka, kb, vp, va,
+          vb)
     return k, v
 
 
@@ -194,23 +209,25 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
     of the sum of the scores' exponentials (-inf, with out 0, where nothing is
     attended). `out` and `lse` may supply the tensors, `ws` the workspace
     (cache.attend_workspace_bytes)."""
-    q, qa, qb = _rows(cache, q, "q")
-    seqs, q_heads, dim = q.shape
+    q, qp, shape, qa, qb = _rows(cache, q, "q")
+    seqs, q_heads, dim = shape
     if q_heads < 1 or q_heads % cache.heads:
         raise ValueError(f"q must have a multiple of {cache.heads} heads")
-    if not (isinstance(table, torch.Tensor) and table.dim() == 2 and table.dtype == torch.int32
-            and table.device == cache.device and table.shape[0] == seqs):
+    if not (isinstance(table, torch.Tensor) and table.dtype is torch.int32 and table.dim() == 2
+            and table.get_device() == cache.index and table.shape[0] == seqs):
         raise ValueError(f"table must be an int32 [{seqs}, pages] tensor on the cache's GPU")
-    if table.stride(1) != 1:
+    row, one = table.stride()
+    if one != 1:
         table = table.contiguous()
+        row = table.stride(0)
     lengths = _ints(cache, lengths, torch.int32, seqs, "lengths")
     if starts is not None:
         starts = _ints(cache, starts, torch.int32, seqs, "starts")
-    out, oa, ob = _target(cache, out, (seqs, q_heads, dim), "out")
+    out, op, oa, ob = _target(cache, out, shape, "out")
     if lse is None:
         lse = torch.empty((seqs, q_heads), dtype=torch.float32, device=cache.device)
-    elif not (lse.dtype == torch.float32 and tuple(lse.shape) == (seqs, q_heads)
-              and lse.is_contiguous() and lse.device == cache.device):
+    elif not (lse.dtype is torch.float32 and tuple(lse.shape) == (seqs, q_heads)
+              and lse.is_contiguous() and lse.get_device() == cache.index):
         raise ValueError(f"lse must be a contiguous float32 [{seqs}, {q_heads}] tensor on the "
                          "cache's GPU")
     width = table.shape[1]
@@ -221,11 +238,13 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
         if nbytes == 0:
             raise KmeansError("kmeans_kv_attend", KMEANS_EUNSUPPORTED)
         ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
-    elif ws.device != cache.device or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous tensor on the cache's GPU")
-    _call(cache, _lib.kmeans_kv_attend, "kmeans_kv_attend", q.data_ptr(), qa, qb, seqs, q_heads,
-          table.data_ptr(), table.stride(0), width, lengths.data_ptr(),
+    else:
+        if ws.get_device() != cache.index or not ws.is_contiguous():
+            raise ValueError("ws must be a contiguous tensor on the cache's GPU")
+        nbytes = ws.numel() * ws.element_size()
+    _call(cache, _lib.kmeans_kv_attend, "kmeans_kv_attend", qp, qa, qb, seqs, q_heads,
+          table.data_ptr(), row, width, lengths.data_ptr(),
           None if starts is None else starts.data_ptr(),
-          1.0 / math.sqrt(dim) if scale is None else scale, out.data_ptr(), oa, ob, lse.data_ptr(),
-          ws.data_ptr(), ws.numel() * ws.element_size())
+          1.0 / math.sqrt(dim) if scale is None else scale, op, oa, ob, lse.data_ptr(),
+          ws.data_ptr(), nbytes)
     return out, lse
