@@ -93,9 +93,9 @@ struct Form {
     }
     static constexpr size_t lds_bytes(int seqs)
     {
-        return kRoom + (4 * kWaves * 32 + 3 * kWaves + seqs + 1) * 4;
+        return kRoom + (4 * kWaves * 32 + 3 * kWaves + 2 * kWave + seqs + 1) * 4;
     }
-    static_assert(kRoom + (4 * kWaves * 32 + 3 * kWaves + kKvMaxSeqs + 1) * 4 <= kMaxLds, "LDS");
+    static_assert(kRoom + (4 * kWaves * 32 + 3 * kWaves + 2 * kWave + kKvMaxSeqs + 1) * 4 <= kMaxLds, "LDS");
 };
 
 // Positions [start, len) of sequence b, and the 32-position tiles they touch.
@@ -234,7 +234,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     float(*const weight)[32] = ml + 2 * W;
     int *const tag = reinterpret_cast<int *>(ml + 4 * W);
     int *const wave_sum = tag + 2 * W;
-    int *const first = wave_sum + W;                     // [seqs + 1]
+    Span *const spans = reinterpret_cast<Span *>(wave_sum + W);          // of up to 64 sequences
+    int *const first = reinterpret_cast<int *>(spans + kWave);           // [seqs + 1]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -300,10 +301,12 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         my_next = wave_scan(n);
         my_first = my_next - n;
         tiles = __builtin_amdgcn_readlane(my_next, 63);
-        if (wave == 0) {
-            if (lane < a.seqs) first[lane] = my_first;
-            if (lane == 0) first[a.seqs] = tiles;
+        // all waves write the same, and read it before the others have
+        if (lane < a.seqs) {
+            first[lane] = my_first;
+            spans[lane] = my_span;
         }
+        if (lane == 0) first[a.seqs] = tiles;
     } else {
         const int per = (a.seqs + F::kThreads - 1) / F::kThreads;
         int sum = 0;
@@ -378,36 +381,20 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     const auto enter = [&](int b) {
         Cursor x;
         x.b = __builtin_amdgcn_readfirstlane(b);
-        if (in_lanes) {
-            x.base = __builtin_amdgcn_readlane(my_first, x.b);
-            x.next = __builtin_amdgcn_readlane(my_next, x.b);
-            x.sp.start = __builtin_amdgcn_readlane(my_span.start, x.b);
-            x.sp.len = __builtin_amdgcn_readlane(my_span.len, x.b);
-            return x;
-        }
         x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
         x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
-        const Span s = span_of(c, a, x.b);
+        const Span s = in_lanes ? spans[x.b] : span_of(c, a, x.b);
         x.sp.start = __builtin_amdgcn_readfirstlane(s.start);
         x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
         return x;
     };
-    // the sequence of tile t, from sequence b on
-    const auto sequence_of = [&](int t, int b) {
-        if (in_lanes) return (int)__popcll(__ballot(lane < a.seqs && my_next <= t));
-        for (int hi = a.seqs; b < hi;) {                // the last with first[] <= t
-            const int mid = (b + hi) >> 1;
-            if (first[mid + 1] <= t) b = mid + 1; else hi = mid;
-        }
-        return b;
-    };
     // to tile t (the next one, below a1)
     const auto advance = [&](Cursor &x, int t) {
-        if (t < x.next) return;
+        if (t < x.next) return false;
         int b = x.b + 1;
-        if (in_lanes) b = sequence_of(t, b);
-        else while (first[b + 1] <= t) ++b;
+        while (first[b + 1] <= t) ++b;
         x = enter(b);
+        return true;
     };
     // Tile t's codes are loaded when those of t - 1 have been looked up, to the
     // same registers, and the numbers of the pages they lie on a tile before.
@@ -415,29 +402,47 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         int pos;                 // the tile's first position
         int k_page, v_page;      // numbers of the pages of the lane's keys and values
     };
+    // The place of the next numbers to ask for, and of their sequence its row of
+    // the table and the first and last entry that may be read (in bytes).
+    struct Ahead {
+        int pos, low, high;
+        const char *row;
+    };
+    const auto look = [&](const Cursor &x, int t) {
+        Ahead y;
+        y.pos = (t - x.base + x.sp.tile0()) * 32;
+        y.low = x.sp.start >> c.page_log2 << 2;
+        y.high = (x.sp.len - 1) >> c.page_log2 << 2;
+        y.row = reinterpret_cast<const char *>(a.table + x.b * a.table_stride);
+        return y;
+    };
     const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
     const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
-    const uint8_t *const k_head = c.k_codes + (((int64_t)h * F::S) << c.page_log2);
-    const uint8_t *const v_head = c.v_codes + (((int64_t)h * F::S) << c.page_log2);
     // A lane's codes lie at the same place of each of its pages, for tiles begin on
     // multiples of 32 positions; where pages are larger, the tile's place is added.
     const unsigned pm = (1u << c.page_log2) - 1;
-    const unsigned k_off = ((8 * (r >> 2) & pm) + (r & 3)) * F::S + g * F::SL;
-    const unsigned v_off = 8 * g & pm;
-    const auto v_sub = [&](int hh) {             // of a lane's granule in its sub-vectors
+    const int64_t head_codes = ((int64_t)h * F::S) << c.page_log2;
+    const uint8_t *const k_lane =
+        c.k_codes + head_codes + ((8 * (r >> 2) & pm) + (r & 3)) * F::S + g * F::SL;
+    const auto v_sub = [&](int hh) {             // of a lane's granule, in its sub-vectors
         return (unsigned)(min(16 * hh + r, F::NG - 1) * F::VS / SUB) << c.page_log2;
     };
-    const auto find = [&](const Cursor &x, int t) {
+    const uint8_t *const v_lane = c.v_codes + head_codes + (8 * g & pm) + v_sub(0);
+    const auto v_step = [&](int hh) {            // from granule row 0 to hh: one for all lanes
+        return F::NG % 16 == 0 ? (unsigned)(16 * hh * F::VS / SUB) << c.page_log2
+                               : v_sub(hh) - v_sub(0);
+    };
+    const int k_entry = 8 * (r >> 2) >> c.page_log2 << 2, v_entry = 8 * g >> c.page_log2 << 2;
+    const auto find = [&](Ahead &y) {
         Where w;
-        w.pos = (t - x.base + x.sp.tile0()) * 32;
-        const char *row = reinterpret_cast<const char *>(a.table + x.b * a.table_stride);
-        const auto entry = [&](int page) {
-            return *reinterpret_cast<const int32_t *>(row + (uint32_t)page * 4u);
-        };
+        w.pos = y.pos;
         // groups of 8 positions outside the span: the nearest page inside
-        const int low = x.sp.start >> c.page_log2, high = (x.sp.len - 1) >> c.page_log2;
-        w.k_page = entry(min(max((w.pos + 8 * (r >> 2)) >> c.page_log2, low), high));
-        w.v_page = entry(min(max((w.pos + 8 * g) >> c.page_log2, low), high));
+        const int at = y.pos >> c.page_log2 << 2;
+        w.k_page = *reinterpret_cast<const int32_t *>(
+            y.row + (uint32_t)min(max(at + k_entry, y.low), y.high));
+        w.v_page = *reinterpret_cast<const int32_t *>(
+            y.row + (uint32_t)min(max(at + v_entry, y.low), y.high));
+        y.pos += 32;
         return w;
     };
     Codes<D, SUB> cd;            // of the tile at hand, then of the next
@@ -446,14 +451,14 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         return (uint64_t)min((unsigned)page, last_page) * page_bytes + ((unsigned)w.pos & pm) * S;
     };
     const auto load_k = [&](const Where &w) {
-        const uint8_t *const k = k_head + k_off + place(w, w.k_page, F::S);
+        const uint8_t *const k = k_lane + place(w, w.k_page, F::S);
         load_bytes<F::SL>(cd.k[0], k);
         load_bytes<F::SL>(cd.k[1], k + 4 * F::S);
     };
     const auto load_v = [&](const Where &w) {
-        const uint8_t *const v = v_head + v_off + place(w, w.v_page, 1);
+        const uint8_t *const v = v_lane + place(w, w.v_page, 1);
 #pragma unroll
-        for (int hh = 0; hh < F::NH; ++hh) load_bytes<8>(cd.v[hh], v + v_sub(hh));
+        for (int hh = 0; hh < F::NH; ++hh) load_bytes<8>(cd.v[hh], v + v_step(hh));
     };
     const float scale = fabsf(a.scale_log2);
     const bool negative = a.scale_log2 < 0.f;
@@ -476,17 +481,33 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         for (int n = 0; n < F::NV; ++n) acc[n] = f4v{0.f, 0.f, 0.f, 0.f};
     };
     // The first tiles' loads are on their way before the centres are waited for.
-    Cursor cur{}, ahead{};
+    Cursor cur{}, then{};        // of the tile at hand, and of `ahead`
+    Ahead ahead{};
     Where where{};
     if (a0 < a1) {
-        cur = ahead = enter(sequence_of(a0, 0));
-        where = find(ahead, a0);
+        if (in_lanes) {
+            cur.b = (int)__popcll(__ballot(lane < a.seqs && my_next <= a0));
+            cur.base = __builtin_amdgcn_readlane(my_first, cur.b);
+            cur.next = __builtin_amdgcn_readlane(my_next, cur.b);
+            cur.sp.start = __builtin_amdgcn_readlane(my_span.start, cur.b);
+            cur.sp.len = __builtin_amdgcn_readlane(my_span.len, cur.b);
+        } else {
+            int lo = 0;
+            for (int hi = a.seqs; lo < hi;) {            // the last with first[] <= a0
+                const int mid = (lo + hi) >> 1;
+                if (first[mid + 1] <= a0) lo = mid + 1; else hi = mid;
+            }
+            cur = enter(lo);
+        }
+        then = cur;
+        ahead = look(then, a0);
+        where = find(ahead);
         load_q(cur.b);
         load_k(where);
         load_v(where);
         if (a0 + 1 < a1) {
-            advance(ahead, a0 + 1);
-            where = find(ahead, a0 + 1);
+            if (advance(then, a0 + 1)) ahead = look(then, a0 + 1);
+            where = find(ahead);
         }
     }
     if (c.K == 256) {
@@ -508,8 +529,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         const uint32_t k_base = F::kValues + g * (F::SL * 512 * SUB);
         // One tile of 32 positions from `pos` on. What the span leaves out of it
         // is masked in branches of its own, which most tiles skip.
-        const auto step = [&](int t) {
-            const int pos = (t - cur.base + cur.sp.tile0()) * 32;
+        const auto step = [&](int t, int pos) {
             const Span &sp = cur.sp;
             const bool partial = pos < sp.start || pos + 32 > sp.len;
             const auto seen = [&](int i) {
@@ -528,8 +548,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             const Where coming = where;
             if (t + 1 < a1) load_k(coming);
             if (t + 2 < a1) {
-                advance(ahead, t + 2);
-                where = find(ahead, t + 2);
+                if (advance(then, t + 2)) ahead = look(then, t + 2);
+                where = find(ahead);
             }
             // scores: rows are positions, columns queries
             float z[8];
@@ -636,6 +656,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         int turn = (wave >> 2) % 3;
         for (int t = a0; t < a1;) {
             const int b = cur.b, piece = t, end = min(cur.next, a1);
+            int pos = (t - cur.base + cur.sp.tile0()) * 32;
             for (; t < end; ++t) {
                 // The SIMD's waves take turns at the highest priority: the oldest
                 // would have it always, end first and leave the last ones to
@@ -644,7 +665,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 else if (turn == 1) __builtin_amdgcn_s_setprio(1);
                 else __builtin_amdgcn_s_setprio(0);
                 turn = turn == 2 ? 0 : turn + 1;
-                step(t);
+                step(t, pos);
+                pos += 32;
             }
             float lw = l + __shfl_xor(l, 16);
             lw += __shfl_xor(lw, 32);

@@ -223,7 +223,11 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
     lengths = _ints(cache, lengths, torch.int32, seqs, "lengths")
     if starts is not None:
         starts = _ints(cache, starts, torch.int32, seqs, "starts")
-    out, op, oa, ob = _target(cache, out, shape, "out")
+    if out is None and q.is_contiguous():
+        out, oa, ob = torch.empty_like(q), qa, qb
+        op = out.data_ptr()
+    else:
+        out, op, oa, ob = _target(cache, out, shape, "out")
     if lse is None:
         lse = torch.empty((seqs, q_heads), dtype=torch.float32, device=cache.device)
     elif not (lse.dtype is torch.float32 and tuple(lse.shape) == (seqs, q_heads)
