@@ -15,9 +15,14 @@ hipError_t launch_kv_attend_8(const KvCache &, const KvAttend &, const KvAttendP
 
 namespace {
 
-// How far the reference of the exponents may lie below the largest score before
-// what is summed is scaled: weights stay below 2^8, which fp16 holds.
+// The weights are exp2(score - reference). A new reference lies kLift below the
+// largest score, and holds until a score is kLag above that one, when what is
+// summed is scaled: weights stay below 2^15, which fp16 holds. For it they are
+// lifted, for what is left of small ones is a multiple of 2^-24: a long tail of
+// them would lose some of its sum to that.
 constexpr float kLag = 8.f;
+template <bool FP16>
+constexpr float kLift = FP16 ? 7.f : 0.f;
 
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
@@ -48,9 +53,9 @@ __device__ inline uint32_t pack2(float a, float b)
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
 }
 
-// x cut off to the 16-bit type, where mask is all ones; 0 where it is 0. (The
-// weights are at most 2^kLag, and below the least normal number of fp16 the
-// cut leaves more bits than fp16 has there: cut2 of the rest takes them off.)
+// x cut off to the 16-bit type, where mask is all ones; 0 where it is 0. (Below
+// the least normal number of fp16 the cut leaves more bits than fp16 has there,
+// less than 2^-24 that neither part takes up.)
 template <bool FP16>
 __device__ inline float cut(float x, uint32_t mask)
 {
@@ -366,8 +371,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     };
 
     f4v acc[F::NV];
-    // m: what the exponents are taken relative to (base 2), within kLag below
-    // the largest score so far; -inf before the first; m0 is m, or 0 for -inf.
+    // m: the reference of the exponents (base 2), -inf before the first score
+    // above that; m0 is m, or 0 for -inf.
     // l: the lane's part of the sum of the weights.
     float m = -INFINITY, m0 = 0.f, l = 0.f;
     u4v q[D / 32];
@@ -591,10 +596,10 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
             for (int i = 2; i < 8; ++i) top = fmaxf(top, z[i]);
             top *= scale;
-            if (__any(!(top <= m + kLag))) {              // NaN included
+            if (__any(!(top <= m + (kLag + kLift<FP16>)))) {      // NaN included
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                top = fmaxf(top, m);
+                top = fmaxf(top - kLift<FP16>, m);
                 m0 = top == -INFINITY ? 0.f : top;
                 const float alpha = __builtin_amdgcn_exp2f(m - m0);
                 m = top;

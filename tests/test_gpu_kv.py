@@ -468,6 +468,33 @@ def test_attend_rising_and_falling_scores():
                 check_against(cache, q, torch.tensor(table), [511], None, scale, got)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attend_long_tail_of_small_weights(dtype):
+    """120000 positions that weigh 2^-16.3 of the first one each, 1.5 together."""
+    n = 120001
+    cache = make_cache(1, 64, 4, 4, dtype, 1876, 64, seed=15)
+    cache.k_centres.zero_()
+    cache.v_centres.zero_()
+    cache.k_centres[0, 0, 1, 0] = 1.0
+    cache.v_centres[0, :, 2] = 1.0
+    cache.k_codes.zero_()
+    cache.v_codes.fill_(2)
+    table = torch.arange(1876, dtype=torch.int32, device=DEV)[None]
+    cache.k_codes[0, 0, 0, 0] = 1
+    cache.v_codes[0, 0, :, 0] = 0
+    q = torch.zeros(1, 1, 64, device=DEV, dtype=dtype)
+    q[0, 0, 0] = 1.0
+    out, lse = km.kmeans_kv_attend(cache, q, table, torch.tensor([n], dtype=torch.int32, device=DEV),
+                                   scale=16.3 * math.log(2.0))
+    tail = (n - 1) * 2.0 ** -16.3
+    want = tail / (1 + tail)
+    # the output's own rounding (it lies in [1/2, 1)), the weights' 16 (bf16) or 20 bits, what fp16 cuts
+    # off below 2^-24 of weights lifted by 2^7, and the score's rounding
+    u, w = (2.0 ** -9, 2.0 ** -15) if dtype is BF else (2.0 ** -12, 2.0 ** -20 + 2.0 ** (16.3 - 31))
+    assert (out.double() - want).abs().max() <= u + want * (w + 16.3 * 2.0 ** -21)
+    assert abs(lse.item() - (16.3 * math.log(2.0) + math.log1p(tail))) < 1e-5
+
+
 def test_attend_infinite_scores_and_masked_nan():
     """Scores of +inf give NaN and of -inf weight nothing, as the formula says;
     a centre that only positions outside the span name does not enter, NaN
