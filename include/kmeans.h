@@ -290,7 +290,7 @@ typedef struct kmeans_kv {
     const void *v_centres;  /* likewise                                               */
     uint8_t *k_codes;       /* [pages][heads][page][dim / sub]                         */
     uint8_t *v_codes;       /* [pages][heads][dim / sub][page]                         */
-    int64_t pages;          /* 1 <= pages, pages * page <= 2^40                        */
+    int64_t pages;          /* 1 to 2^31 - 1                                           */
     int32_t page;           /* tokens of a page: a power of two, 8 to 1024             */
     int32_t heads;          /* key-value heads, 1 to 1024                              */
     int32_t dim;            /* 64, 96 or 128                                           */

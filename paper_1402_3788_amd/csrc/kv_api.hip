@@ -24,7 +24,7 @@ int check_shape(const kmeans_kv_t *kv)
         return KMEANS_EINVAL;
     if (kv->type != KMEANS_KV_BF16 && kv->type != KMEANS_KV_FP16) return KMEANS_EINVAL;
     if (kv->page < 8 || kv->page > 1024 || (kv->page & (kv->page - 1))) return KMEANS_EUNSUPPORTED;
-    if (kv->pages > ((int64_t)1 << 40) / kv->page || kv->heads > 1024 || kv->K > 256)
+    if (kv->pages >= (int64_t)1 << 31 || kv->heads > 1024 || kv->K > 256)
         return KMEANS_EUNSUPPORTED;
     if (kv->dim != 64 && kv->dim != 96 && kv->dim != 128) return KMEANS_EUNSUPPORTED;
     if (kv->sub != 2 && kv->sub != 4 && kv->sub != 8) return KMEANS_EUNSUPPORTED;

@@ -54,13 +54,20 @@ __device__ inline float kv_distance(const float (&x)[SUB], const float (&c)[SUB]
     return d[0];
 }
 
-// Where slot's codes begin: the page's, and the token's place in it; false for
-// a slot that is not in the cache.
-__device__ inline bool kv_slot(const KvCache &c, int64_t slot, int64_t *page, int *off)
+// A slot's page and the token's place in it; false for a slot that is not in the
+// cache.
+__device__ inline bool kv_slot(const KvCache &c, int64_t slot, uint32_t *page, uint32_t *off)
 {
-    *page = slot >> c.page_log2;
-    *off = (int)(slot & ((1 << c.page_log2) - 1));
-    return slot >= 0 && *page < c.pages;
+    *page = (uint32_t)(slot >> c.page_log2);
+    *off = (uint32_t)slot & ((1u << c.page_log2) - 1);
+    return (uint64_t)slot < (uint64_t)c.pages << c.page_log2;
+}
+
+// Codes before those of head h on a page; S of them to a token.
+__device__ inline int64_t kv_head(const KvCache &c, uint32_t page, int h, int S)
+{
+    return (uint64_t)page * ((uint32_t)(c.heads * S) << c.page_log2) +
+           ((uint32_t)(h * S) << c.page_log2);
 }
 
 }  // namespace lloyd

@@ -24,13 +24,12 @@ __global__ __launch_bounds__(kThreads) void kv_read_few_kernel(KvCache c, KvToke
          u += (int64_t)gridDim.x * kThreads) {
         const int64_t tok = u / kinds;
         const int kind = (int)(u - tok * kinds), h = kind / S, s = kind - h * S;
-        int64_t page;
-        int off;
+        uint32_t page, off;
         KvEntry<SUB> k{}, v{};
         if (kv_slot(c, t.slots[tok], &page, &off)) {
-            const int64_t head = (page * c.heads + h) << c.page_log2;
-            const int kc = c.k_codes[(head + off) * S + s];
-            const int vc = c.v_codes[head * S + ((int64_t)s << c.page_log2) + off];
+            const int64_t head = kv_head(c, page, h, S);
+            const int kc = c.k_codes[head + off * S + s];
+            const int vc = c.v_codes[head + ((unsigned)s << c.page_log2) + off];
             if (kc < c.K) k = kv_load<SUB>(c.k_centres + ((int64_t)kind * c.K + kc) * SUB);
             if (vc < c.K) v = kv_load<SUB>(c.v_centres + ((int64_t)kind * c.K + vc) * SUB);
         }
@@ -95,20 +94,19 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
         bool live[runs];
 #pragma unroll
         for (int i = 0; i < runs; ++i) {
-            int64_t page;
-            int off;
+            uint32_t page, off;
             live[i] = kv_slot(c, next[i], &page, &off);
             codes[i] = 0;
             if (!live[i]) continue;
-            const int64_t head = (page * c.heads + h) << c.page_log2;
+            const int64_t head = kv_head(c, page, h, S);
             const int s = run_of(i) * per;
             if (values) {
-                const uint8_t *const v = c.v_codes + head * S + off + ((int64_t)s << c.page_log2);
+                const uint8_t *const v = c.v_codes + head + off + ((unsigned)s << c.page_log2);
 #pragma unroll
                 for (int x = 0; x < per; ++x) codes[i] |= (uint32_t)v[x << c.page_log2] << (8 * x);
             } else {
                 __builtin_memcpy(&codes[i],
-                                 __builtin_assume_aligned(c.k_codes + (head + off) * S + s, per), per);
+                                 __builtin_assume_aligned(c.k_codes + head + off * S + s, per), per);
             }
         }
         ask(step + kWaves);

@@ -100,18 +100,24 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
     const uint16_t *const centres = (values ? c.v_centres : c.k_centres) +
                                     ((int64_t)h * S + s) * c.K * SUB;
     Operand<SUB> *const centre = centres_of[wave];
-    const int64_t stride = (int64_t)gridDim.y * kTokens;
-    const int64_t begin = (int64_t)blockIdx.y * kTokens;
-    const uint16_t *const rows = values ? t.v + h * t.v_head + s * SUB : t.k + h * t.k_head + s * SUB;
+    const uint32_t tokens = (uint32_t)t.tokens, stride = gridDim.y * kTokens;      // both below 2^31
+    const uint32_t begin = blockIdx.y * kTokens;
+    // Tokens of a step: the lane's sub-vector and slot. Past the end they stay
+    // those before, and go nowhere.
     const int64_t row_stride = values ? t.v_token : t.k_token;
-
-    // Tokens of a step: the lane's sub-vector and slot. Past the end: the last's.
-    KvEntry<SUB> next;
-    int64_t next_slot;
-    const auto ask = [&](int64_t first) {
-        const int64_t tok = min(first + col, t.tokens - 1);
-        next_slot = t.slots[tok];
-        next = kv_load<SUB>(rows + tok * row_stride);
+    const uint16_t *row = (values ? t.v + h * t.v_head : t.k + h * t.k_head) + s * SUB +
+                          (int64_t)(begin + col) * row_stride;
+    const int64_t *slots = t.slots + begin + col;
+    const int64_t row_step = row_stride * stride;
+    KvEntry<SUB> next{};
+    int64_t next_slot = -1;
+    const auto ask = [&](uint32_t first) {
+        if (first + col < tokens) {
+            next_slot = *slots;
+            next = kv_load<SUB>(row);
+        }
+        slots += stride;
+        row += row_step;
     };
     ask(begin);
 
@@ -170,10 +176,12 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
     const bool takes_norm = FP16 ? !up : up;
     __builtin_amdgcn_wave_barrier();                     // a wave's LDS is its own, in order
 
-    for (int64_t first = begin; first < t.tokens; first += stride) {
+    uint8_t *const codes = values ? c.v_codes + ((uint32_t)s << c.page_log2) : c.k_codes + s;
+    const uint32_t code_step = values ? 1 : S;           // from token to token of a page
+    for (uint32_t first = begin; first < tokens; first += stride) {
         const KvEntry<SUB> e = next;
         const int64_t slot = next_slot;
-        if (first + stride < t.tokens) ask(first + stride);
+        ask(first + stride);
         float x[SUB], norm = 0.f;
         kv_unpack<FP16>(e, x);
 #pragma unroll
@@ -243,13 +251,9 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
         const float near2 = __shfl_xor(near, 32);
         const int code2 = __shfl_xor(code, 32);
         if (near2 < near || (near2 == near && code2 < code)) code = code2;
-        int64_t page;
-        int off;
-        if (up || first + col >= t.tokens || !kv_slot(c, slot, &page, &off)) continue;
-        const int64_t head = (page * c.heads + h) << c.page_log2;
-        uint8_t *const dst = values ? c.v_codes + head * S + ((int64_t)s << c.page_log2) + off
-                                    : c.k_codes + (head + off) * S + s;
-        *dst = (uint8_t)code;
+        uint32_t page, off;
+        if (up || first + col >= tokens || !kv_slot(c, slot, &page, &off)) continue;
+        codes[kv_head(c, page, h, S) + off * code_step] = (uint8_t)code;
     }
 }
 
