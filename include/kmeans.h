@@ -344,9 +344,9 @@ size_t kmeans_kv_attend_workspace_bytes(const kmeans_kv_t *kv, int32_t seqs, int
  * whose z is above -infinity: out = 0, lse = -infinity. Entries of table whose
  * pages hold no such position are not read. A length is taken as at most
  * table_pages * page, a negative start as 0; an entry outside [0, pages) is
- * taken as the nearest page. 1 <= seqs <= 4096 (0 is KMEANS_OK),
- * seqs * q_heads < 2^24, table_pages * page <= 2^30, and seqs * table_pages *
- * page / 32 < 2^31. scale is finite. Scores, their maximum and sum and the
+ * taken as some page of the cache. out and lse overlap nothing that is read.
+ * 1 <= seqs <= 4096 (0 is KMEANS_OK), seqs * q_heads < 2^24, table_pages * page
+ * <= 2^30, and seqs * table_pages * page / 32 < 2^31. scale is finite. Scores, their maximum and sum and the
  * output are held in fp32; a weight exp(z_i - max) enters the product with the
  * values as the sum of two 16-bit numbers. The same inputs give the same bits.
  * Asynchronous on `stream`.

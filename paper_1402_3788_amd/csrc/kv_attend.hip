@@ -1,4 +1,36 @@
 // Attention of one new token of every sequence over the cache of codes.
+//
+// With the scores z_i = scale (q . k_i) in base 2 and a reference m, one pass over
+// the positions keeps sum_i 2^(z_i - m) and sum_i 2^(z_i - m) v_i, both scaled when
+// the reference is moved up; parts with references of their own are joined by
+// 2^(m - largest m).
+//
+// A workgroup keeps the centres of one head in LDS, 64 KB of keys' (dim = 128) and
+// 64 KB of values', fills a CU with them and looks codes up there: from the L2 each
+// centre of 8 bytes would move a line of 128. So the row of all sequences' tiles
+// (32 positions) is shared evenly by the workgroups of a head, whatever the
+// sequences' lengths are, and a workgroup's share by its waves; what is cut that
+// way is joined, in the workgroup at its end and between workgroups by a second
+// launch. Workgroup b has head b % heads: with 8 heads each XCD's L2 serves one.
+//
+// A tile: the centres of its keys are the rows of one matrix operand as they come
+// from LDS (v_mfma_f32_16x16x32: a lane holds 8 features of one position), the
+// queries the columns of the other; the scores come out with the queries in the
+// columns, so that their exponentials are an operand of the product with the
+// values without leaving their lanes, the positions being numbered to that end
+// (Codes below). The values' rows are features: four features of eight positions,
+// looked up, are turned in registers.
+//
+// On gfx950 a SIMD's vector instructions and matrix products add up, and their sum
+// bounds the kernel: per tile and wave 185 of the former (32 to find the keys'
+// centres in LDS, 48 to find and turn the values', some 60 for the weights, the
+// rest loads ahead) and 16 of the latter, about 1250 cycles, against 183 of LDS
+// (a random key lookup of a wave takes 7 cycles instead of 4; the values' rows are
+// laid out to be free of conflicts). 64 sequences of 8192 to 16384 positions, 8
+// heads of 128 features in sub-vectors of 4, 64 query heads: 111 us, 3.4 TB/s of
+// codes (a copy moves 4.8), of which 6 are the centres and the joining in the
+// workgroup; the joining launch takes 6 more. Sub-vectors of 2, with twice the bytes:
+// 4.4 TB/s.
 #include "kv_device.h"
 
 #include <type_traits>
@@ -81,6 +113,9 @@ struct Form {
     static constexpr int NG = D / VS;                  // granules
     static constexpr int NH = (NG + 15) / 16;          // rows of 16 granules
     static constexpr int NV = NH * VS;                 // accumulator tiles
+    // Waves of the workgroup: as many as the registers allow, 168 each with 12 and
+    // 128 with 16 (8 waves: 128 us instead of 111 for the case above; 16 with
+    // registers spilled: 138).
     static constexpr int kWaves = kv_waves(D);
     static constexpr int kThreads = kWaves * kWave;
     static constexpr int kKeys = D * 512;              // LDS bytes of the key centres: [S][256][SUB]
@@ -90,6 +125,7 @@ struct Form {
     // the centres, whose place the waves' last pieces take at the end
     static constexpr int kRoom = kKeys + kValues > kWaves * kEntry * 4 ? kKeys + kValues
                                                                        : kWaves * kEntry * 4;
+    static constexpr int kSpans = 1024;                // sequences whose spans are kept in LDS
     // the feature of place x among a wave's accumulators (from D up: none)
     static __device__ int feature(int x)
     {
@@ -98,9 +134,9 @@ struct Form {
     }
     static constexpr size_t lds_bytes(int seqs)
     {
-        return kRoom + (4 * kWaves * 32 + 3 * kWaves + 2 * kWave + seqs + 1) * 4;
+        return kRoom + (4 * kWaves * 32 + 3 * kWaves + 2 * kSpans + seqs + 1) * 4;
     }
-    static_assert(kRoom + (4 * kWaves * 32 + 3 * kWaves + 2 * kWave + kKvMaxSeqs + 1) * 4 <= kMaxLds, "LDS");
+    static_assert(kRoom + (4 * kWaves * 32 + 3 * kWaves + 2 * kSpans + kKvMaxSeqs + 1) * 4 <= kMaxLds, "LDS");
 };
 
 // Positions [start, len) of sequence b, and the 32-position tiles they touch.
@@ -239,8 +275,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     float(*const weight)[32] = ml + 2 * W;
     int *const tag = reinterpret_cast<int *>(ml + 4 * W);
     int *const wave_sum = tag + 2 * W;
-    Span *const spans = reinterpret_cast<Span *>(wave_sum + W);          // of up to 64 sequences
-    int *const first = reinterpret_cast<int *>(spans + kWave);           // [seqs + 1]
+    Span *const spans = reinterpret_cast<Span *>(wave_sum + W);          // [kSpans]
+    int *const first = reinterpret_cast<int *>(spans + F::kSpans);       // [seqs + 1]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -317,7 +353,10 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         int sum = 0;
         for (int i = 0; i < per; ++i) {
             const int b = tid * per + i;
-            if (b < a.seqs) sum += span_of(c, a, b).tiles();
+            if (b >= a.seqs) break;
+            const Span x = span_of(c, a, b);
+            sum += x.tiles();
+            if (b < F::kSpans) spans[b] = x;
         }
         const int incl = wave_scan(sum);
         if (lane == 63) wave_sum[wave] = incl;
@@ -388,7 +427,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         x.b = __builtin_amdgcn_readfirstlane(b);
         x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
         x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
-        const Span s = in_lanes ? spans[x.b] : span_of(c, a, x.b);
+        const Span s = x.b < F::kSpans ? spans[x.b] : span_of(c, a, x.b);
         x.sp.start = __builtin_amdgcn_readfirstlane(s.start);
         x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
         return x;
@@ -497,12 +536,10 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             cur.sp.start = __builtin_amdgcn_readlane(my_span.start, cur.b);
             cur.sp.len = __builtin_amdgcn_readlane(my_span.len, cur.b);
         } else {
-            int lo = 0;
-            for (int hi = a.seqs; lo < hi;) {            // the last with first[] <= a0
-                const int mid = (lo + hi) >> 1;
-                if (first[mid + 1] <= a0) lo = mid + 1; else hi = mid;
-            }
-            cur = enter(lo);
+            // the last b with first[b] <= a0: of every 64th, then of the 64
+            const int block = __popcll(__ballot(first[min((lane + 1) * kWave, a.seqs)] <= a0));
+            const int b = min(block * kWave + lane + 1, a.seqs);
+            cur = enter(block * kWave + __popcll(__ballot(first[b] <= a0)));
         }
         then = cur;
         ahead = look(then, a0);

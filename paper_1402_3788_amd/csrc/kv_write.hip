@@ -18,8 +18,11 @@
 //
 // A wave keeps the 256 centres of one sub-vector as matrix operands in its
 // registers and takes 32 tokens a step. A lane then has 128 scores, at half an
-// instruction each (the maximum of three), and 4 distances at some 17: the vector
-// ALU bounds it. FIGURE.
+// instruction each (the maximum of three), 16 groups at 2, and 4 distances at some
+// 17: about 290 vector instructions and 8 matrix products a step, which add up on
+// gfx950 and bound it. 4096 tokens of 8 heads of 128 features in sub-vectors of 4,
+// keys and values (2.1 million sub-vectors, 537 million distances): 40 us, 13.4
+// distances a picosecond, where all of them on the vector ALU took 153; one token: 6 us.
 #include "kv_device.h"
 
 namespace lloyd {
@@ -60,7 +63,8 @@ __device__ inline f16v product(bool fp16, const Operand<SUB> &a, const Operand<S
 
 __device__ inline uint32_t bf16_bits(float x) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// The nearest of 8 centres' worth of distances: see below.
+// The nearest of 4 centres from `row` on to x, if it is nearer than `near` or as
+// near and lower in number.
 template <bool FP16, int SUB>
 __device__ inline void evaluate(const Operand<SUB> *centre, int row, const float (&x)[SUB],
                                 float &near, int &code)
