@@ -246,6 +246,15 @@ __device__ inline float turned(float x)
         __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xF, 0xF, true));
 }
 
+// x of rows 0 and 2 of the wave's rows of 16 in both rows of their half, and that
+// of rows 1 and 3.
+__device__ inline void row_pair(float x, float *even, float *odd)
+{
+    const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    *even = __uint_as_float(both[0]);
+    *odd = __uint_as_float(both[1]);
+}
+
 // Sum of x over the lanes up to this one.
 __device__ inline int wave_scan(int x)
 {
@@ -288,48 +297,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j;
     float *const part_o = a.part_o + wg * (W + 2) * F::kEntry;
     float *const part_ml = a.part_ml + wg * 64;
-
-    // The centres of this head, entries from K up zeros. With all 256 the keys'
-    // are one run of bytes and go straight to LDS, 16 to a lane, and the
-    // values' wait in registers while the lengths below are read: they are
-    // turned to one row of all features for each code.
     constexpr int per16 = 8 / SUB;                       // centres in 16 bytes
-    constexpr int rounds = (D * 32 + F::kThreads - 1) / F::kThreads;
-    static_assert(D * 32 % kWave == 0, "whole waves");
-    const uint16_t *const ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
-    const uint16_t *const vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
-    // lanes: 4 runs of 16 bytes in each of 16 sub-vectors, for whole sectors
-    // from memory and few conflicts in LDS
-    const auto value_s = [&](int i) { return ((i * F::kThreads + tid) >> 2) % F::S; };
-    const auto value_code = [&](int i) {
-        const int n = i * F::kThreads + tid;
-        return ((n >> 2) / F::S * 4 + (n & 3)) * per16;
-    };
-    uint4 vreg[rounds];
-    if (c.K == 256) {
-#pragma unroll
-        for (int i = 0; i < rounds; ++i) {
-            const int at = (i * F::kThreads + (wave << 6)) * 16;         // of the wave's first lane
-            if (at < F::kKeys) to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
-        }
-#pragma unroll
-        for (int i = 0; i < rounds; ++i)
-            if (i * F::kThreads + tid < D * 32)
-                vreg[i] = *reinterpret_cast<const uint4 *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
-    } else {
-        using E = KvEntry<SUB>;
-#pragma unroll 4
-        for (int i = tid; i < F::S * 256; i += F::kThreads) {
-            const int s = i >> 8, code = i & 255;
-            E ke{}, ve{};
-            if (code < c.K) {
-                ke = kv_load<SUB>(ks + (s * c.K + code) * SUB);
-                ve = kv_load<SUB>(vs + (s * c.K + code) * SUB);
-            }
-            reinterpret_cast<E *>(kbook)[i] = ke;
-            *reinterpret_cast<E *>(vbook + code * F::kRow + s * (SUB * 2)) = ve;
-        }
-    }
+
     // Where each sequence's tiles begin in the row of all tiles. Up to 64
     // sequences every wave has them in its lanes, and looks nothing up later.
     const bool in_lanes = a.seqs <= kWave;
@@ -524,7 +493,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
         for (int n = 0; n < F::NV; ++n) acc[n] = f4v{0.f, 0.f, 0.f, 0.f};
     };
-    // The first tiles' loads are on their way before the centres are waited for.
+    // Loads come back in order, so the small ones that others hang on go first:
+    // page numbers and queries before the centres, the first codes behind them.
     Cursor cur{}, then{};        // of the tile at hand, and of `ahead`
     Ahead ahead{};
     Where where{};
@@ -545,6 +515,48 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         ahead = look(then, a0);
         where = find(ahead);
         load_q(cur.b);
+    }
+    // The centres of this head, entries from K up zeros. With all 256 the keys'
+    // are one run of bytes and go straight to LDS, 16 to a lane; the values'
+    // go through registers, to be turned to one row of all features for each
+    // code.
+    constexpr int rounds = (D * 32 + F::kThreads - 1) / F::kThreads;
+    static_assert(D * 32 % kWave == 0, "whole waves");
+    const uint16_t *const ks = c.k_centres + (int64_t)h * F::S * c.K * SUB;
+    const uint16_t *const vs = c.v_centres + (int64_t)h * F::S * c.K * SUB;
+    // lanes: 4 runs of 16 bytes in each of 16 sub-vectors, for whole sectors
+    // from memory and few conflicts in LDS
+    const auto value_s = [&](int i) { return ((i * F::kThreads + tid) >> 2) % F::S; };
+    const auto value_code = [&](int i) {
+        const int n = i * F::kThreads + tid;
+        return ((n >> 2) / F::S * 4 + (n & 3)) * per16;
+    };
+    uint4 vreg[rounds];
+    if (c.K == 256) {
+#pragma unroll
+        for (int i = 0; i < rounds; ++i) {
+            const int at = (i * F::kThreads + (wave << 6)) * 16;         // of the wave's first lane
+            if (at < F::kKeys) to_lds16(reinterpret_cast<const char *>(ks) + at + lane * 16, kbook + at);
+        }
+#pragma unroll
+        for (int i = 0; i < rounds; ++i)
+            if (i * F::kThreads + tid < D * 32)
+                vreg[i] = *reinterpret_cast<const uint4 *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
+    } else {
+        using E = KvEntry<SUB>;
+#pragma unroll 4
+        for (int i = tid; i < F::S * 256; i += F::kThreads) {
+            const int s = i >> 8, code = i & 255;
+            E ke{}, ve{};
+            if (code < c.K) {
+                ke = kv_load<SUB>(ks + (s * c.K + code) * SUB);
+                ve = kv_load<SUB>(vs + (s * c.K + code) * SUB);
+            }
+            reinterpret_cast<E *>(kbook)[i] = ke;
+            *reinterpret_cast<E *>(vbook + code * F::kRow + s * (SUB * 2)) = ve;
+        }
+    }
+    if (a0 < a1) {
         load_k(where);
         load_v(where);
         if (a0 + 1 < a1) {
@@ -774,6 +786,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         const int e = lane & 31, qq = 2 * wave + (lane >> 5);
         const int b = e < 2 * W ? tag[e] : -1;
         const float em = e < 2 * W ? ml[e][qq] : 0.f, el = e < 2 * W ? ml[e][16 + qq] : 0.f;
+        const int at = b >= 0 ? first[b] : 0, end = b >= 0 ? first[b + 1] : 0;
         for (uint64_t todo = __ballot(b >= 0); todo;) {
             const int lead = __builtin_ctzll(todo);
             const bool in = b == __builtin_amdgcn_readlane(b, lead);
@@ -783,22 +796,25 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             top = fmaxf(top, turned<2>(top));
             top = fmaxf(top, turned<4>(top));
             top = fmaxf(top, turned<8>(top));
-            top = fmaxf(top, __shfl_xor(top, 16));
+            float even, odd;
+            row_pair(top, &even, &odd);
+            top = fmaxf(even, odd);
             const float w = __builtin_amdgcn_exp2f(em - (top == -INFINITY ? 0.f : top));
             float lw = in ? el * w : 0.f;
             lw += turned<1>(lw);
             lw += turned<2>(lw);
             lw += turned<4>(lw);
             lw += turned<8>(lw);
-            lw += __shfl_xor(lw, 16);
+            row_pair(lw, &even, &odd);
+            lw = even + odd;
             if (!in) continue;
             weight[e][qq] = w;
             weight[e][16 + qq] = lw;
             if (e != lead || qq >= nq) continue;
-            if (first[b] >= w0 && first[b + 1] <= w1) {
+            if (at >= w0 && end <= w1) {
                 put_lse(b, qq, top, lw);
             } else {
-                const int slot = first[b] < w0 ? 0 : 1;
+                const int slot = at < w0 ? 0 : 1;
                 part_ml[slot * 32 + qq] = top;
                 part_ml[slot * 32 + 16 + qq] = lw;
             }
@@ -808,10 +824,13 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     constexpr int mine = (F::kEntry + F::kThreads - 1) / F::kThreads;
     const int qq = tid & 15;
     const int tag_of = lane < 2 * W ? tag[lane] : -1;
+    const int at_of = tag_of >= 0 ? first[tag_of] : 0, end_of = tag_of >= 0 ? first[tag_of + 1] : 0;
     uint64_t todo = __ballot(tag_of >= 0);
 #pragma unroll 1
     while (todo) {
-        const int b = __builtin_amdgcn_readlane(tag_of, __builtin_ctzll(todo));
+        const int lead = __builtin_ctzll(todo), b = __builtin_amdgcn_readlane(tag_of, lead);
+        const int at_b = __builtin_amdgcn_readlane(at_of, lead);
+        const int end_b = __builtin_amdgcn_readlane(end_of, lead);
         const uint64_t in = __ballot(tag_of == b);
         todo &= ~in;
         float o[mine] = {}, lw = 0.f;
@@ -838,8 +857,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 }
             }
         }
-        const bool whole = first[b] >= w0 && first[b + 1] <= w1;
-        const int slot = first[b] < w0 ? 0 : 1;
+        const bool whole = at_b >= w0 && end_b <= w1;
+        const int slot = at_b < w0 ? 0 : 1;
         const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
 #pragma unroll
         for (int i = 0; i < mine; ++i) {
@@ -852,7 +871,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             }
         }
         if (!whole && slot && tid == 0)
-            a.shared[wg] = KvShared{b, share_of(tiles, first[b + 1] - 1, used) - j + 1};
+            a.shared[wg] = KvShared{b, share_of(tiles, end_b - 1, used) - j + 1};
     }
 }
 
