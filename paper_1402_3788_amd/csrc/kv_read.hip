@@ -132,12 +132,17 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
 template <int SUB>
 hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
 {
-    // centres from LDS where a workgroup on each half of a CU has 512 tokens and
-    // more to pay for fetching them with
-    const int64_t kinds = 2 * c.heads;
-    const int64_t most = (2 * kCUs + kinds - 1) / kinds, enough = t.tokens / 512;
-    const int parts = (int)(most < enough ? most : enough);
-    if (parts > 0 && parts * kinds >= kCUs / 2) {
+    // Centres from LDS from 2^18 sub-vectors on, whose lookups in the L2 take longer
+    // than fetching the centres does: 8 heads of 128 features, sub-vectors of 4,
+    // 1024 tokens (2^18) 5.3 us from the L2 and 5.7 from LDS, 2048 8.5 and 6.3; one
+    // head, 8192 tokens (2^18) 4.5 and 5.8, 16384 7.0 and 6.4; 8 heads of 64,
+    // sub-vectors of 2, 1024 tokens (2^18) 4.9 and 4.3; 8 of 128 in 8, 1024 (2^17) 3.8
+    // and 4.7, 2048 (2^18) 5.6 and 5.0. A workgroup has 128 tokens or more, two to a
+    // CU at most.
+    const int64_t kinds = 2 * c.heads, units = t.tokens * c.heads * (c.dim / SUB);
+    if (units >= (int64_t)1 << 18) {
+        const int64_t most = (2 * kCUs + kinds - 1) / kinds, enough = (t.tokens + 127) / 128;
+        const int parts = (int)(most < enough ? most : enough);
         const dim3 grid((unsigned)(parts * kinds)), block(kWaves * kWave);
         if (c.dim == 64)
             hipLaunchKernelGGL((kv_read_kernel<64, SUB>), grid, block, 0, s, c, t, parts);
@@ -147,7 +152,6 @@ hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
             hipLaunchKernelGGL((kv_read_kernel<128, SUB>), grid, block, 0, s, c, t, parts);
         return hipGetLastError();
     }
-    const int64_t units = t.tokens * c.heads * (c.dim / SUB);
     const int64_t groups = (units + kThreads - 1) / kThreads;
     hipLaunchKernelGGL((kv_read_few_kernel<SUB>), dim3((unsigned)(groups < 65536 ? groups : 65536)),
                        dim3(kThreads), 0, s, c, t, units);

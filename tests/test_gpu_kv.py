@@ -407,6 +407,18 @@ def test_attend_lengths(heads, dim, sub, K, dtype, page, group):
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("sub", [2, 4, 8])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_attend_every_form(dim, sub, dtype):
+    """Up to 8 query heads to a key head and more, few and more than 64 sequences."""
+    cache = make_cache(1, dim, sub, 256, dtype, 30, 16, seed=dim * sub)
+    check_attend(cache, [70, 5, 411], group=9)
+    check_attend(cache, [70, 5, 411], group=8, seed=1)
+    check_attend(cache, list(range(65)) + [300], group=2, seed=2)
+    check_attend(cache, [33] * 64, group=12, seed=3)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("dim,sub", [(64, 2), (96, 8), (128, 4)])
 def test_attend_starts(dtype, dim, sub):
     cache = make_cache(2, dim, sub, 256, dtype, 50, 16, seed=3)
@@ -432,6 +444,12 @@ def test_attend_many_sequences():
     cache = make_cache(1, 128, 8, 64, FP, 40, 8, seed=6)
     lengths = torch.randint(0, 9, (4096,), generator=g).tolist()
     check_attend(cache, lengths, group=1)
+    # mostly empty, the rest long, some beyond what is looked up in LDS
+    lengths = [0] * 3000
+    for b, n in ((0, 700), (63, 40), (64, 33), (1023, 1500), (1024, 64), (2999, 2000)):
+        lengths[b] = n
+    cache = make_cache(1, 64, 8, 64, BF, 300, 16, seed=7)
+    check_attend(cache, lengths, group=2)
 
 
 def test_attend_head_layouts():
