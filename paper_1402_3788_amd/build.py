@@ -1,4 +1,5 @@
-"""Build libkmeans_mi355x.so (the HIP library behind include/kmeans.h) in-tree.
+"""Build libkmeans_mi355x.so (the HIP library behind include/kmeans.h) and the
+Python module _kv_call in-tree.
 
 Usage: python paper_1402_3788_amd/build.py
 (run as a script: importing the package needs the library this builds)
@@ -14,6 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkmeans_mi355x.so")
+CALLS = os.path.join(HERE, "_kv_call.so")
 # Flags of one translation unit: the small-K kernel is scheduled with the
 # compiler's iterative scheduler aiming at occupancy (measured per launch at
 # n = 2e6, M = 25, K = 16: 38.2 us against 39.1 with the default scheduler and
@@ -57,6 +59,21 @@ def hipcc() -> str:
     return os.path.join(rocm, "bin", "hipcc")
 
 
+def calls_command(out: str) -> list[str]:
+    """Compiles the Python module of the key-value cache's usual calls against
+    the installed torch, whose libraries are loaded before it."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+            + [x for d in (*include_paths(), sysconfig.get_paths()["include"])
+               for x in ("-isystem", d)]
+            + [os.path.join(CSRC, "kv_call.cpp"), "-o", out]
+            + [f"-L{d}" for d in library_paths()] + ["-lc10", "-ltorch_cpu", "-ltorch_python"])
+
+
 def _newest_header() -> float:
     heads = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
     heads.append(os.path.join(ROOT, "include", "kmeans.h"))
@@ -83,6 +100,9 @@ def build(verbose: bool = True, jobs: int = 8, incremental: bool = False) -> str
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
         while sum(p.poll() is None for _, p in procs) >= jobs:
             time.sleep(0.05)
+    calls_new = CALLS + ".tmp"
+    procs.append(("kv_call.cpp", subprocess.Popen(calls_command(calls_new), stdout=subprocess.PIPE,
+                                                  stderr=subprocess.STDOUT)))
     failed = False
     for src, p in procs:
         out, _ = p.communicate()
@@ -100,6 +120,7 @@ def build(verbose: bool = True, jobs: int = 8, incremental: bool = False) -> str
     tmp = LIB + ".tmp"
     subprocess.check_call([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, LIB)
+    os.replace(calls_new, CALLS)
     if verbose:
         print(f"built {LIB} in {time.time() - t0:.1f}s")
     return LIB

@@ -18,6 +18,11 @@ import torch
 
 from . import KmeansError, KMEANS_EUNSUPPORTED, _lib
 
+try:
+    from . import _kv_call as _fast
+except ImportError as e:
+    raise ImportError("_kv_call.so is not built; run `python paper_1402_3788_amd/build.py`") from e
+
 # a tenth of the time of torch.cuda.current_stream and current_device, which
 # small calls would mostly consist of
 _raw_stream = torch._C._cuda_getCurrentRawStream
@@ -47,6 +52,9 @@ def _bind():
     _lib.kmeans_kv_attend.argtypes = [d, p, i64, i64, i32, i32, p, i64, i64, p, p, ctypes.c_float,
                                       p, i64, i64, p, p, sz, p]
     _lib.kmeans_kv_attend.restype = ctypes.c_int
+    _fast.bind(*(ctypes.cast(f, ctypes.c_void_p).value
+                 for f in (_lib.kmeans_kv_write, _lib.kmeans_kv_read,
+                           _lib.kmeans_kv_attend_workspace_bytes, _lib.kmeans_kv_attend)))
 
 
 _bind()
@@ -83,6 +91,7 @@ class KVCodes:
         self._desc = _Desc(*(t.data_ptr() for t in tensors), pages, page, heads, S * sub, sub, K,
                            _TYPES[self.dtype])
         self._ref = ctypes.byref(self._desc)
+        self._at = ctypes.addressof(self._desc)
         self.index = k_centres.get_device()
         self._ws_bytes = {}
         # the library says what it takes; it looks at no pointer here
@@ -168,6 +177,12 @@ def kmeans_kv_write(cache: KVCodes, k: torch.Tensor, v: torch.Tensor, slots: tor
     """Encodes the tokens k, v ([n, heads, dim]) into the slots of `slots` (int64
     [n]; page number * page + place). A token whose slot is negative or past
     the cache is left out."""
+    if _current_device() == cache.index:
+        rc = _fast.write(cache._at, cache.k_centres, _raw_stream(cache.index), k, v, slots)
+        if rc == 0:
+            return
+        if rc is not None:
+            raise KmeansError("kmeans_kv_write", rc)
     slots = _ints(cache, slots, torch.int64, None, "slots")
     n = slots.shape[0]
     k, kp, shape, ka, kb = _rows(cache, k, "k")
@@ -183,6 +198,12 @@ def kmeans_kv_read(cache: KVCodes, slots: torch.Tensor, out=None):
     """The keys and values in the slots of `slots` (int64 [n]), as the centres
     that their codes name: (k, v), each [n, heads, dim]; zeros for a slot that
     is not in the cache. `out` may supply both tensors."""
+    if out is None and _current_device() == cache.index:
+        got = _fast.read(cache._at, cache.k_centres, _raw_stream(cache.index), slots)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            raise KmeansError("kmeans_kv_read", got)
     slots = _ints(cache, slots, torch.int64, None, "slots")
     n = slots.shape[0]
     shape = (n, cache.heads, cache.dim)
@@ -209,6 +230,15 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
     of the sum of the scores' exponentials (-inf, with out 0, where nothing is
     attended). `out` and `lse` may supply the tensors, `ws` the workspace
     (cache.attend_workspace_bytes)."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.dim)
+    if out is None and lse is None and ws is None and _current_device() == cache.index:
+        got = _fast.attend(cache._at, cache.k_centres, _raw_stream(cache.index), q, table, lengths,
+                           scale, starts)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            raise KmeansError("kmeans_kv_attend", got)
     q, qp, shape, qa, qb = _rows(cache, q, "q")
     seqs, q_heads, dim = shape
     if q_heads < 1 or q_heads % cache.heads:
@@ -249,6 +279,5 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
     _call(cache, _lib.kmeans_kv_attend, "kmeans_kv_attend", qp, qa, qb, seqs, q_heads,
           table.data_ptr(), row, width, lengths.data_ptr(),
           None if starts is None else starts.data_ptr(),
-          1.0 / math.sqrt(dim) if scale is None else scale, op, oa, ob, lse.data_ptr(),
-          ws.data_ptr(), nbytes)
+          scale, op, oa, ob, lse.data_ptr(), ws.data_ptr(), nbytes)
     return out, lse
