@@ -22,8 +22,11 @@
 // 17: about 290 vector instructions and 8 matrix products a step, which add up on
 // gfx950 and bound it. 4096 tokens of 8 heads of 128 features in sub-vectors of 4,
 // keys and values (2.1 million sub-vectors, 537 million distances): 40 us, 13.4
-// distances a picosecond, where all of them on the vector ALU took 153; one token: 6 us.
+// distances a picosecond, where all of them on the vector ALU took 153. A few tokens
+// are better off with the latter (kFew below).
 #include "kv_device.h"
+
+#include <type_traits>
 
 namespace lloyd {
 
@@ -31,6 +34,13 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kTokens = 32;          // tokens of a wave's step, columns of the product
+
+// Sub-vectors up to which all distances are taken on the vector ALU: 8 heads of 128
+// features in sub-vectors of 4, 1 token (512 of them) 2.8 us and 5.1 with the
+// screen, 16 tokens 4.9 and 5.4, 24 tokens (12288) 5.2 and 5.4, 32 tokens 6.0 and 5.5;
+// 8 of 128 in 8, 32 tokens (8192) 5.3 and 5.8, 64 6.9 and 5.9; 8 of 64 in 2, 24 tokens
+// (12288) 5.1 and 5.5, 32 5.7 and 5.5; 1 of 128 in 4, 64 tokens (4096) 3.6 and 5.3.
+constexpr int kFew = 12288;
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4v __attribute__((ext_vector_type(4)));
@@ -261,10 +271,82 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
     }
 }
 
+// The least of x over the wave (numbers that are none left out).
+__device__ inline float wave_least(float x)
+{
+    const auto from = [](float v, auto ctrl, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(INFINITY), __float_as_int(v),
+                                                          ctrl.value, rows.value, 0xF, false));
+    };
+    using std::integral_constant;
+    x = fminf(x, from(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{}));
+    x = fminf(x, from(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{}));
+    x = fminf(x, from(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{}));
+    x = fminf(x, from(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{}));
+    x = fminf(x, from(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{}));
+    x = fminf(x, from(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{}));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// A few tokens: all distances as the definition says, four centres to a lane of
+// the wave that has the sub-vector. What counts is how little there is to load and
+// run before the answer.
+template <int SUB, bool FP16>
+__global__ __launch_bounds__(kThreads) void kv_write_few_kernel(KvCache c, KvTokens t)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int S = c.dim / SUB, groups = S / kWaves;
+    const int s = (int)(blockIdx.x % groups) * kWaves + wave;
+    const int h = (int)(blockIdx.x / groups) % c.heads;
+    const bool values = (int)(blockIdx.x / groups) >= c.heads;
+    const uint16_t *const centres = (values ? c.v_centres : c.k_centres) +
+                                    ((int64_t)h * S + s) * c.K * SUB;
+    const uint16_t *const row = (values ? t.v + h * t.v_head : t.k + h * t.k_head) + s * SUB;
+    const int64_t row_stride = values ? t.v_token : t.k_token;
+    KvEntry<SUB> e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = kv_load<SUB>(centres + min(i * kWave + lane, c.K - 1) * SUB);
+#pragma unroll 1
+    for (int64_t tok = blockIdx.y; tok < t.tokens; tok += gridDim.y) {
+        float x[SUB], d[4];
+        kv_unpack<FP16>(kv_load<SUB>(row + tok * row_stride), x);
+        const int64_t slot = t.slots[tok];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float y[SUB];
+            kv_unpack<FP16>(e[i], y);
+            d[i] = kv_distance(x, y);
+            if (i * kWave + lane >= c.K) d[i] = NAN;
+        }
+        const float least = wave_least(fminf(fminf(d[0], d[1]), fminf(d[2], d[3])));
+        int code = 0;                                    // for distances that are no numbers
+#pragma unroll
+        for (int i = 3; i >= 0; --i)
+            if (const uint64_t at = __ballot(d[i] == least)) code = i * kWave + __builtin_ctzll(at);
+        uint32_t page, off;
+        if (lane || !kv_slot(c, slot, &page, &off)) continue;
+        const int64_t head = kv_head(c, page, h, S);
+        if (values)
+            c.v_codes[head + ((uint32_t)s << c.page_log2) + off] = (uint8_t)code;
+        else
+            c.k_codes[head + off * S + s] = (uint8_t)code;
+    }
+}
+
 template <int SUB>
 hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
 {
     const unsigned kinds = 2 * c.heads * (c.dim / SUB / kWaves);
+    if (t.tokens * (kinds * kWaves) <= kFew) {
+        // a token to a workgroup while all fit the chip at once
+        const int64_t most = (8 * kCUs + kinds - 1) / kinds;
+        const dim3 grid(kinds, (unsigned)(t.tokens < most ? t.tokens : most));
+        if (c.fp16)
+            hipLaunchKernelGGL((kv_write_few_kernel<SUB, true>), grid, dim3(kThreads), 0, s, c, t);
+        else
+            hipLaunchKernelGGL((kv_write_few_kernel<SUB, false>), grid, dim3(kThreads), 0, s, c, t);
+        return hipGetLastError();
+    }
     const int64_t steps = (t.tokens + kTokens - 1) / kTokens;
     // enough workgroups for every CU to hold several, no more: each reads centres
     const int64_t most = (6 * kCUs + kinds - 1) / kinds;

@@ -184,6 +184,60 @@ def test_write_below_the_normal_range(dtype, sub):
     assert np.array_equal(vc, nearest(v, cache.v_centres))
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("sub", [2, 4, 8])
+@pytest.mark.parametrize("n", [5, 900])
+def test_write_few_and_many(n, sub, dtype):
+    """The forms for few tokens and for many: ties, values that are no numbers and
+    an odd number of centres, in tokens that both take."""
+    for n_all in (n, 900):
+        cache = make_cache(1, 64, sub, 77, dtype, 60, 16, seed=21, random_codes=False)
+        cache.k_centres[:, :, 40:44] = cache.k_centres[:, :, 9:13]
+        k, v = tokens(cache, 900, 8)
+        k[0, 0, :sub] = cache.k_centres[0, 0, 41]
+        k[1, 0, 3], k[2, 0, 7], k[3] = math.nan, -math.inf, 0.0
+        v[4] = 3e38 if dtype is BF else 65504.0
+        slots = torch.arange(900, device=DEV)
+        for i in range(0, n_all, n):
+            km.kmeans_kv_write(cache, k[i:i + n], v[i:i + n], slots[i:i + n])
+        kc, vc = codes_at(cache, np.arange(n_all))
+        assert np.array_equal(kc, nearest(k[:n_all], cache.k_centres))
+        assert np.array_equal(vc, nearest(v[:n_all], cache.v_centres))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("sub", [2, 4, 8])
+def test_write_many_unusual(sub, dtype):
+    """The screen for many tokens where its bound is no finite number or every
+    centre is within it, from strided tokens, among them padding."""
+    n = 1100
+    cache = make_cache(1, 64, sub, 250, dtype, 70, 16, seed=22, random_codes=False)
+    big = 3e38 if dtype is BF else 65504.0
+    both = torch.randn(1, n, 2, 64, device=DEV).to(dtype)
+    k, v = both[:, :, 0].transpose(0, 1), both[:, :, 1].transpose(0, 1)
+    for t in (k, v):
+        t[3, 0, 5], t[4, 0, 9], t[5, 0, 10] = math.nan, math.inf, -math.inf
+        t[6] = big
+        t[7, 0, ::2] = -big
+        t[8] = 0.0
+        t[9] = 1e-40 if dtype is BF else 6e-8
+        t[10, 0, 1] = 1e4
+        t[700:900] *= 0.001
+    cache.v_centres[0, 1:3, 17] = big          # its square overflows in the first type
+    cache.v_centres[0, 3] *= 2e19 if dtype is BF else 1000.0
+    cache.v_centres[0, 5] *= 1e-22 if dtype is BF else 1e-6
+    cache.k_centres[0, 2:4] = cache.k_centres[0, 2:4, :1]        # all the same
+    slots = torch.arange(n)
+    slots[100], slots[200], slots[300] = -1, 70 * 16, 2 ** 45
+    km.kmeans_kv_write(cache, k, v, slots.to(DEV))
+    live = np.array([i for i in range(n) if i not in (100, 200, 300)])
+    kc, vc = codes_at(cache, live)
+    assert np.array_equal(kc, nearest(k, cache.k_centres)[live])
+    assert np.array_equal(vc, nearest(v, cache.v_centres)[live])
+    kc, vc = codes_at(cache, np.setdiff1d(np.arange(70 * 16), live))
+    assert not kc.any() and not vc.any()
+
+
 @pytest.mark.parametrize("n", [129, 2000, 5000])
 def test_write_many_tokens(n):
     """More tokens than one round of the launch takes."""
