@@ -891,22 +891,37 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     const int h = hq % c.heads, qb = hq / c.heads;
     const int nq = min(kKvQueries, a.group - qb * kKvQueries);
     const int64_t wg = (int64_t)hq * splits + j;
-    const KvShared found = a.shared[wg];
-    if (found.b < 0) return;
-    const int b = found.b, n = found.parts;              // 2 <= n <= splits <= kCUs
     const int tid = threadIdx.x, q = tid & 15;
     const auto part = [&](int i) {                       // of this thread's output
         return a.part_o[((wg + i) * (F::kWaves + 2) + F::kWaves + (i == 0)) * F::kEntry + x];
     };
     const auto ml = [&](int i) { return a.part_ml + (wg + i) * 64 + (i == 0) * 32 + q; };
+    // Most such sequences have two parts: those are asked for along with what says
+    // so (there is a share after this one).
+    const int i0 = tid >> 4;
     float in[batch];
+    in[0] = part(0);
+    in[1] = part(1);
+    float m0 = *ml(min(i0, 1)), l0 = ml(min(i0, 1))[16];
+    const KvShared found = a.shared[wg];
+    if (found.b < 0) return;
+    const int b = found.b, n = found.parts;              // 2 <= n <= splits <= kCUs
+    if (n > 2) {
 #pragma unroll
-    for (int k = 0; k < batch; ++k) in[k] = part(min(k, n - 1));
+        for (int k = 2; k < batch; ++k) in[k] = part(min(k, n - 1));
+        if (i0 >= 2 && i0 < n) {
+            m0 = *ml(i0);
+            l0 = ml(i0)[16];
+        }
+    } else {
+#pragma unroll
+        for (int k = 2; k < batch; ++k) in[k] = 0.f;
+    }
     // weight of each part, for each query: [part][query]
     __shared__ float weight[kCUs * 16];
     __shared__ float s_top[16 * 16], s_sum[16 * 16];
-    float top = -INFINITY;
-    for (int i = tid >> 4; i < n; i += 16) {
+    float top = i0 < n ? m0 : -INFINITY;
+    for (int i = i0 + 16; i < n; i += 16) {
         const float v = *ml(i);
         weight[i * 16 + q] = v;
         top = fmaxf(top, v);
@@ -917,7 +932,12 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s_top[i * 16 + q]);
     const float safe = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int i = tid >> 4; i < n; i += 16) {
+    if (i0 < n) {
+        const float w = __builtin_amdgcn_exp2f(m0 - safe);
+        sum = w * l0;
+        weight[i0 * 16 + q] = w;
+    }
+    for (int i = i0 + 16; i < n; i += 16) {
         const float w = __builtin_amdgcn_exp2f(weight[i * 16 + q] - safe);
         sum += w * ml(i)[16];
         weight[i * 16 + q] = w;
