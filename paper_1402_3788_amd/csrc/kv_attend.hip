@@ -22,15 +22,15 @@
 // looked up, are turned in registers.
 //
 // On gfx950 a SIMD's vector instructions and matrix products add up, and their sum
-// bounds the kernel: per tile and wave 185 of the former (32 to find the keys'
-// centres in LDS, 48 to find and turn the values', some 60 for the weights, the
-// rest loads ahead) and 16 of the latter, about 1250 cycles, against 183 of LDS
+// bounds the kernel: per tile and wave 178 of the former (32 to find the keys'
+// centres in LDS, 48 to find and turn the values', some 55 for the weights, the
+// rest loads ahead) and 16 of the latter, 85 % of all cycles, against 60 % of LDS
 // (a random key lookup of a wave takes 7 cycles instead of 4; the values' rows are
 // laid out to be free of conflicts). 64 sequences of 8192 to 16384 positions, 8
 // heads of 128 features in sub-vectors of 4, 64 query heads: 111 us, 3.4 TB/s of
-// codes (a copy moves 4.8), of which 6 are the centres and the joining in the
-// workgroup; the joining launch takes 6 more. Sub-vectors of 2, with twice the bytes:
-// 4.4 TB/s.
+// codes (a copy moves 4.8; with the loads of codes left out it takes 101), of which
+// 6 are the centres and the joining in the workgroup; the joining launch takes 5
+// more. Sub-vectors of 2, with twice the bytes: 4.4 TB/s.
 #include "kv_device.h"
 
 #include <type_traits>
@@ -474,7 +474,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         for (int hh = 0; hh < F::NH; ++hh) load_bytes<8>(cd.v[hh], v + v_step(hh));
     };
     const float scale = fabsf(a.scale_log2);
-    const bool negative = a.scale_log2 < 0.f;
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;     // the scale's sign, for the queries
     const uint32_t low_parts = r >= 8 ? ~0u : 0u;        // lanes whose columns take them
 
     const auto load_q = [&](int b) {
@@ -633,10 +633,6 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                                               0x0C0C0000u | (4 + (x & 3)) << 8));
             __builtin_amdgcn_sched_barrier(0);
             if (t + 1 < a1) load_v(coming);
-            if (negative) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] = -z[i];
-            }
             if (partial) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = seen(i) ? z[i] : -INFINITY;
@@ -710,6 +706,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         int turn = (wave >> 2) % 3;
         for (int t = a0; t < a1;) {
             const int b = cur.b, piece = t, end = min(cur.next, a1);
+#pragma unroll
+            for (int st = 0; st < D / 32; ++st) q[st] ^= flip;
             int pos = (t - cur.base + cur.sp.tile0()) * 32;
             for (; t < end; ++t) {
                 // The SIMD's waves take turns at the highest priority: the oldest
