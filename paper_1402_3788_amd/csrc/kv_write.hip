@@ -142,6 +142,10 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
     Operand<SUB> a[8];
     Operand<4> norm_of[FP16 ? 8 : 1];
     float big = 0.f;
+    KvEntry<SUB> given[8];                               // all asked for before one is waited for
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+        given[n] = kv_load<SUB>(centres + min(n * 32 + col, c.K - 1) * SUB);
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
         const int j = n * 32 + col;
@@ -152,7 +156,7 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
 #pragma unroll
         for (int i = 0; i < SUB / 2; ++i) e.w[i] = 0x7FFF7FFFu;
         if (j < c.K) {
-            e = kv_load<SUB>(centres + j * SUB);
+            e = given[n];
             float y[SUB], norm = 0.f;
             kv_unpack<FP16>(e, y);
 #pragma unroll
@@ -348,8 +352,13 @@ hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
         return hipGetLastError();
     }
     const int64_t steps = (t.tokens + kTokens - 1) / kTokens;
-    // enough workgroups for every CU to hold several, no more: each reads centres
-    const int64_t most = (6 * kCUs + kinds - 1) / kinds;
+    // Workgroups to a CU: a wave's start (256 centres read, eight operands made)
+    // takes about as long as a step, so where each CU has few steps, three. 1021
+    // tokens, 3 and 6: 8 heads of 128 in 8 (8 steps a CU) 10.4 and 12.6 us, 4 of 64
+    // in 2 (8) 9.7 and 11.1, 8 of 128 in 4 (16) 15.1 and 15.3, in 2 (32) 23.2 and
+    // 22.6; 4096, 8 of 128 in 4 (64) 43.1 and 39.6.
+    const int64_t each = steps * kinds <= 24 * kCUs ? 3 : 6;
+    const int64_t most = (each * kCUs + kinds - 1) / kinds;
     const unsigned y = (unsigned)(steps < most ? steps : most);
     if (c.fp16)
         hipLaunchKernelGGL((kv_write_kernel<SUB, true>), dim3(kinds, y), dim3(kThreads), 0, s, c, t);
