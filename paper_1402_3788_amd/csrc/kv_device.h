@@ -54,6 +54,14 @@ __device__ inline float kv_distance(const float (&x)[SUB], const float (&c)[SUB]
     return d[0];
 }
 
+// What lanes of a wave wrote to LDS before it, other lanes read after it. A wave's
+// LDS instructions are carried out in order: it keeps the compiler's order only.
+__device__ inline void kv_wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A slot's page and the token's place in it; false for a slot that is not in the
 // cache.
 __device__ inline bool kv_slot(const KvCache &c, int64_t slot, uint32_t *page, uint32_t *off)

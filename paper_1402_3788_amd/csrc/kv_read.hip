@@ -5,8 +5,9 @@
 // memory, one sub-vector to a thread. Many take them from LDS, where a workgroup
 // keeps the centres of one head of the keys or the values (16 to 64 KB): looked up
 // in the L2, each of 8 bytes moves a line of 128, and 65536 tokens of 8 heads of
-// 128 features took 193 us (1.6 TB/s) instead of 78 (3.9 TB/s,
-// where a copy of 2 GiB moves 4.8).
+// 128 features took 193 us instead of 48 (6.3 TB/s; stores alone of as much reach
+// 6.8). The codes of a value sub-vector lie side by side for the tokens of a page,
+// not for the token's other sub-vectors: read byte by byte they made it 79.
 #include "kv_device.h"
 
 namespace lloyd {
@@ -43,7 +44,8 @@ typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 16;
 constexpr int kTokens = 16;          // of a wave's step
 
-// A workgroup takes one head of the keys or the values, and a run of the tokens.
+// A workgroup takes one head of the keys or the values, of whose tokens the
+// workgroups together go through one stretch after the other.
 // A step of a wave is 16 tokens, their rows' runs of 16 bytes in order over its
 // lanes: each store covers whole rows, and past the caches, for the rows are as
 // large as those and not read here again.
@@ -52,13 +54,13 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
 {
     constexpr int S = D / SUB, per = 8 / SUB;            // codes of a row, of a run
     constexpr int runs = D / 32;                         // of a lane
+    constexpr int eights = 2 * S;                        // of codes, in a step of the values
     __shared__ KvEntry<SUB> book[S][256];
+    __shared__ uint64_t turn[kWaves][eights];            // [sub-vector][token] of a step
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = (int)(blockIdx.x % c.heads);
     const bool values = blockIdx.x / c.heads % 2;
-    const int64_t steps = (t.tokens + kTokens - 1) / kTokens;
-    const int64_t part = blockIdx.x / c.heads / 2;
-    const int64_t from = steps * part / parts, to = steps * (part + 1) / parts;
+    const int64_t steps = (t.tokens + kTokens - 1) / kTokens, stride = (int64_t)parts * kWaves;
     const uint16_t *const centres = (values ? c.v_centres : c.k_centres) + (int64_t)h * S * c.K * SUB;
     if (c.K == 256) {
         uint4 *const dst = reinterpret_cast<uint4 *>(&book[0][0]);
@@ -79,37 +81,69 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
     // run i of the lane: of token (64 i + lane) / (D / 8) of the step
     const auto token_of = [&](int i) { return (i * kWave + lane) / (D / 8); };
     const auto run_of = [&](int i) { return (i * kWave + lane) % (D / 8); };
-    // the slots of the next step's tokens are asked for a step ahead
+    // The slots of the next step's tokens are asked for a step ahead: keys, those of
+    // the lane's runs; values, that of token lane % 16.
     int64_t next[runs];
     const auto ask = [&](int64_t step) {
 #pragma unroll
         for (int i = 0; i < runs; ++i) {
-            const int64_t tok = step * kTokens + token_of(i);
-            next[i] = step < to && tok < t.tokens ? t.slots[tok] : (int64_t)-1;
+            const int64_t tok = step * kTokens + (values ? lane & 15 : token_of(i));
+            if (i && values) break;
+            next[i] = tok < t.tokens ? t.slots[tok] : (int64_t)-1;
         }
     };
-    ask(from + wave);
-    for (int64_t step = from + wave; step < to; step += kWaves) {
+    const int64_t begin = (int64_t)(blockIdx.x / c.heads / 2) * kWaves + wave;
+    ask(begin);
+    for (int64_t step = begin; step < steps; step += stride) {
         uint32_t codes[runs];
         bool live[runs];
+        uint32_t page, off;
+        bool in_rows = false;
+        if (values) {
+            // do both eights of tokens lie side by side, on a page each?
+            const int64_t first = __shfl(next[0], lane & 8);
+            in_rows = __all(kv_slot(c, first, &page, &off) &&
+                            off + 8 <= 1u << c.page_log2 && next[0] == first + (lane & 7));
+        }
+        if (in_rows) {
+            // eight codes of a sub-vector to a load, turned in LDS
+            kv_slot(c, __shfl(next[0], (lane & 1) * 8), &page, &off);
+            const uint8_t *const v = c.v_codes + kv_head(c, page, h, S) + off;
 #pragma unroll
-        for (int i = 0; i < runs; ++i) {
-            uint32_t page, off;
-            live[i] = kv_slot(c, next[i], &page, &off);
-            codes[i] = 0;
-            if (!live[i]) continue;
-            const int64_t head = kv_head(c, page, h, S);
-            const int s = run_of(i) * per;
-            if (values) {
-                const uint8_t *const v = c.v_codes + head + off + ((unsigned)s << c.page_log2);
+            for (int i = 0; i < eights; i += kWave)
+                if (i + lane < eights)
+                    __builtin_memcpy(&turn[wave][i + lane],
+                                     v + ((unsigned)((i + lane) >> 1) << c.page_log2), 8);
+            kv_wave_order();
+            const uint8_t *const turned = reinterpret_cast<const uint8_t *>(turn[wave]);
 #pragma unroll
-                for (int x = 0; x < per; ++x) codes[i] |= (uint32_t)v[x << c.page_log2] << (8 * x);
-            } else {
-                __builtin_memcpy(&codes[i],
-                                 __builtin_assume_aligned(c.k_codes + head + off * S + s, per), per);
+            for (int i = 0; i < runs; ++i) {
+                live[i] = true;
+                codes[i] = 0;
+#pragma unroll
+                for (int x = 0; x < per; ++x)
+                    codes[i] |= (uint32_t)turned[(run_of(i) * per + x) * kTokens + token_of(i)] << (8 * x);
+            }
+            kv_wave_order();
+        } else {
+#pragma unroll
+            for (int i = 0; i < runs; ++i) {
+                live[i] = kv_slot(c, values ? __shfl(next[0], token_of(i)) : next[i], &page, &off);
+                codes[i] = 0;
+                if (!live[i]) continue;
+                const int64_t head = kv_head(c, page, h, S);
+                const int s = run_of(i) * per;
+                if (values) {
+                    const uint8_t *const v = c.v_codes + head + off + ((unsigned)s << c.page_log2);
+#pragma unroll
+                    for (int x = 0; x < per; ++x) codes[i] |= (uint32_t)v[x << c.page_log2] << (8 * x);
+                } else {
+                    __builtin_memcpy(&codes[i],
+                                     __builtin_assume_aligned(c.k_codes + head + off * S + s, per), per);
+                }
             }
         }
-        ask(step + kWaves);
+        ask(step + stride);
 #pragma unroll
         for (int i = 0; i < runs; ++i) {
             KvEntry<8> row{};
@@ -134,11 +168,11 @@ hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
 {
     // Centres from LDS from 2^18 sub-vectors on, whose lookups in the L2 take longer
     // than fetching the centres does: 8 heads of 128 features, sub-vectors of 4,
-    // 1024 tokens (2^18) 5.3 us from the L2 and 5.7 from LDS, 2048 8.5 and 6.3; one
-    // head, 8192 tokens (2^18) 4.5 and 5.8, 16384 7.0 and 6.4; 8 heads of 64,
-    // sub-vectors of 2, 1024 tokens (2^18) 4.9 and 4.3; 8 of 128 in 8, 1024 (2^17) 3.8
-    // and 4.7, 2048 (2^18) 5.6 and 5.0. A workgroup has 128 tokens or more, two to a
-    // CU at most.
+    // 512 tokens (2^17) 3.9 us from the L2 and 4.6 from LDS, 1024 5.3 and 4.7; one
+    // head, 8192 tokens (2^18) 4.6 and 4.7, 16384 6.1 and 5.2; 8 heads of 64,
+    // sub-vectors of 2, 512 (2^17) 3.5 and 4.2, 1024 5.0 and 4.1; 8 of 128 in 8, 1024
+    // (2^17) 3.9 and 4.5, 2048 5.9 and 5.1; in 2, 512 (2^18) 4.8 and 6.2, 1024 6.5 and
+    // 6.5. A workgroup has 128 tokens or more, two to a CU at most.
     const int64_t kinds = 2 * c.heads, units = t.tokens * c.heads * (c.dim / SUB);
     if (units >= (int64_t)1 << 18) {
         const int64_t most = (2 * kCUs + kinds - 1) / kinds, enough = (t.tokens + 127) / 128;

@@ -192,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
     const int tiles = (c.K + 31) >> 5;
     // columns of the norms' product: ones for the three parts, T for its 1
     const bool takes_norm = FP16 ? !up : up;
-    __builtin_amdgcn_wave_barrier();                     // a wave's LDS is its own, in order
+    kv_wave_order();
 
     uint8_t *const codes = values ? c.v_codes + ((uint32_t)s << c.page_log2) : c.k_codes + s;
     const uint32_t code_step = values ? 1 : S;           // from token to token of a page

@@ -326,6 +326,46 @@ def test_read(heads, dim, sub, K, dtype, n, page):
         assert (o[:, :, dim:] == 7.0).all()
 
 
+READ_RUNS = [
+    # heads, dim, sub, K, dtype, tokens, page, first place
+    (32, 128, 4, 256, FP, 5003, 64, 0),
+    (8, 128, 4, 256, BF, 1031, 8, 0),
+    (64, 64, 2, 256, BF, 1030, 16, 8),
+    (40, 64, 8, 250, BF, 2047, 32, 3),
+    (64, 96, 8, 31, FP, 1500, 16, 5),
+    (33, 96, 2, 256, FP, 1024, 128, 1),
+    (32, 96, 4, 200, BF, 1999, 1024, 7),
+    (48, 64, 4, 256, FP, 1201, 8, 4),
+    (64, 128, 2, 255, BF, 1111, 16, 0),
+    (64, 128, 8, 256, BF, 513, 64, 9),
+]
+
+
+@pytest.mark.parametrize("heads,dim,sub,K,dtype,n,page,place", READ_RUNS)
+def test_read_of_contexts(heads, dim, sub, K, dtype, n, page, place):
+    """Tokens side by side on pages in any order, up to the last of the cache, some
+    of them left out or elsewhere, from places that are on no boundary."""
+    pages = -(-(n + place) // page)
+    cache = make_cache(heads, dim, sub, K, dtype, pages, page, seed=n)
+    g = torch.Generator().manual_seed(2)
+    pos = torch.arange(place, place + n)
+    slots = torch.randperm(pages, generator=g)[pos // page] * page + pos % page
+    odd = torch.randint(0, n, (5,), generator=g)
+    slots[odd] = torch.tensor([-1, pages * page, 0, pages * page - 1, -2 ** 63])
+    slots[n - 1] = pages * page - 1
+    slots[16:24] = torch.arange(pages * page - 8, pages * page)
+    slots[24:32] = torch.arange(7, -1, -1)
+    slots[32:40] = torch.arange(-4, 4)
+    k, v = km.kmeans_kv_read(cache, slots.to(DEV))
+    live = (slots >= 0) & (slots < pages * page)
+    kc, vc = codes_at(cache, torch.where(live, slots, 0))
+    h, s = torch.arange(heads)[:, None], torch.arange(dim // sub)
+    for got, codes, c in ((k, kc, cache.k_centres), (v, vc, cache.v_centres)):
+        want = c.cpu()[h, s, torch.from_numpy(codes).long()].reshape(n, heads, dim)
+        want[~live] = 0
+        assert torch.equal(got.cpu(), want)
+
+
 def test_codes_past_the_centres_are_zeros():
     cache = make_cache(2, 64, 4, 20, BF, 4, 16)
     cache.k_codes[1, 0, 3, 2] = 20
