@@ -19,9 +19,9 @@
 // A wave keeps the 256 centres of one sub-vector as matrix operands in its
 // registers and takes 32 tokens a step. A lane then has 128 scores, at half an
 // instruction each (the maximum of three), 16 groups at 2, and 4 distances at some
-// 17: about 290 vector instructions and 8 matrix products a step, which add up on
+// 17: about 280 vector instructions and 8 matrix products a step, which add up on
 // gfx950 and bound it. 4096 tokens of 8 heads of 128 features in sub-vectors of 4,
-// keys and values (2.1 million sub-vectors, 537 million distances): 40 us, 13.4
+// keys and values (2.1 million sub-vectors, 537 million distances): 38 us, 14
 // distances a picosecond, where all of them on the vector ALU took 153. A few tokens
 // are better off with the latter (kFew below).
 #include "kv_device.h"
@@ -91,11 +91,12 @@ __device__ inline void evaluate(const Operand<SUB> *centre, int row, const float
         d[k] = kv_distance(x, y);
     }
     const float least = fminf(fminf(d[0], d[1]), fminf(d[2], d[3]));
-    const int j = row + (d[0] == least ? 0 : d[1] == least ? 1 : d[2] == least ? 2 : 3);
-    if (least < near || (least == near && j < code)) {   // not for a NaN
-        near = least;
-        code = j;
-    }
+    int j = d[2] == least ? 2 : 3;
+    j = d[1] == least ? 1 : j;
+    j = row + (d[0] == least ? 0 : j);
+    const bool nearer = (least < near) | ((least == near) & (j < code));     // not for a NaN
+    near = nearer ? least : near;
+    code = nearer ? j : code;
 }
 
 // A workgroup takes kWaves sub-vectors of one head of the keys or the values, one
@@ -259,16 +260,18 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
         // both lanes of a token evaluate half of a group's 8 centres each
         float near = INFINITY;
         int code = 0;
-        while (__any(open)) {
-            if (open) {
-                const int bit = __builtin_ctz(open);
-                open &= open - 1;
-                evaluate<FP16>(centre, (~bit & 15) * 16 + (bit >> 4) * 4 + up * 8, x, near, code);
-            }
-        }
+        do {                                             // a token has one at least
+            const int bit = open ? __builtin_ctz(open) : 0;      // done: some group, not taken
+            float there = near;
+            int row = code;
+            evaluate<FP16>(centre, (~bit & 15) * 16 + (bit >> 4) * 4 + up * 8, x, there, row);
+            near = open ? there : near;
+            code = open ? row : code;
+            open &= open - 1;
+        } while (__any(open));
         const float near2 = __shfl_xor(near, 32);
         const int code2 = __shfl_xor(code, 32);
-        if (near2 < near || (near2 == near && code2 < code)) code = code2;
+        code = (near2 < near) | ((near2 == near) & (code2 < code)) ? code2 : code;
         uint32_t page, off;
         if (up || first + col >= tokens || !kv_slot(c, slot, &page, &off)) continue;
         codes[kv_head(c, page, h, S) + off * code_step] = (uint8_t)code;
