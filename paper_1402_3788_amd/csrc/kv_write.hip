@@ -73,6 +73,15 @@ __device__ inline f16v product(bool fp16, const Operand<SUB> &a, const Operand<S
 
 __device__ inline uint32_t bf16_bits(float x) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x); }
 
+// Of two values of every lane: the lower lanes' x with their y in the upper lanes,
+// and the upper lanes' x in the lower lanes with their y.
+__device__ inline void halves(uint32_t x, uint32_t y, uint32_t *lower, uint32_t *upper)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    *lower = both[0];
+    *upper = both[1];
+}
+
 // The nearest of 4 centres from `row` on to x, if it is nearer than `near` or as
 // near and lower in number.
 template <bool FP16, int SUB>
@@ -138,58 +147,54 @@ __global__ __launch_bounds__(kThreads, 4) void kv_write_kernel(KvCache c, KvToke
 
     // Operands, tile n: centres 32 n + col. bf16: one product, the lower lanes'
     // values are the centre, the upper ones' the three parts of -|c|^2 / 2; fp16:
-    // a product for each. Places from K on: zeros and a norm that never wins, and
-    // in LDS no number, whose distance never does.
+    // a product for each, the upper lanes' zeros. Places from K on: zeros and a norm
+    // that never wins, and in LDS no number, whose distance never does. A lane
+    // works one centre out for two tiles, those of the upper lanes the second's:
+    // lanes and halves are swapped into place.
     Operand<SUB> a[8];
     Operand<4> norm_of[FP16 ? 8 : 1];
     float big = 0.f;
-    KvEntry<SUB> given[8];                               // all asked for before one is waited for
+    KvEntry<SUB> given[4];                               // all asked for before one is waited for
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
-        given[n] = kv_load<SUB>(centres + min(n * 32 + col, c.K - 1) * SUB);
+    for (int p = 0; p < 4; ++p)
+        given[p] = kv_load<SUB>(centres + min(p * kWave + lane, c.K - 1) * SUB);
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-        const int j = n * 32 + col;
-        Operand<SUB> op{};
+    for (int p = 0; p < 4; ++p) {
+        const bool real = p * kWave + lane < c.K;
+        float y[SUB], norm = 0.f;
+        kv_unpack<FP16>(given[p], y);
+#pragma unroll
+        for (int i = 0; i < SUB; ++i) norm = __builtin_fmaf(y[i], y[i], norm);
+        big = fmaxf(big, norm);
+        const float n0 = -0.5f * norm;
+        const uint32_t hi = bf16_bits(n0);
+        const float n1 = n0 - __uint_as_float(hi << 16);
+        const uint32_t mid = bf16_bits(n1);
+        Operand<SUB> op{}, kept{};
         Operand<4> rec{};
-        rec.w[0] = 0xFF7Fu;                              // bf16, as all of the record
-        KvEntry<SUB> e;
+        rec.w[0] = hi | mid << 16;
+        rec.w[1] = bf16_bits(n1 - __uint_as_float(mid << 16)) | 0x3F800000u;
+        const bool finite = norm < INFINITY;             // else every group is evaluated
+        rec.w[0] = real ? finite ? rec.w[0] : 0u : 0xFF7Fu;      // bf16, as all of the record
+        rec.w[1] = real && finite ? rec.w[1] : 0u;
 #pragma unroll
-        for (int i = 0; i < SUB / 2; ++i) e.w[i] = 0x7FFF7FFFu;
-        if (j < c.K) {
-            e = given[n];
-            float y[SUB], norm = 0.f;
-            kv_unpack<FP16>(e, y);
-#pragma unroll
-            for (int i = 0; i < SUB; ++i) norm = __builtin_fmaf(y[i], y[i], norm);
-            big = fmaxf(big, norm);
-            const float n0 = -0.5f * norm;
-            const uint32_t hi = bf16_bits(n0);
-            const float n1 = n0 - __uint_as_float(hi << 16);
-            const uint32_t mid = bf16_bits(n1);
-            rec.w[0] = hi | mid << 16;
-            rec.w[1] = bf16_bits(n1 - __uint_as_float(mid << 16)) | 0x3F800000u;
-            if (!(norm < INFINITY)) rec.w[0] = rec.w[1] = 0;     // every group is evaluated
-#pragma unroll
-            for (int i = 0; i < SUB / 2; ++i) op.w[i] = e.w[i];
+        for (int i = 0; i < SUB / 2; ++i) {
+            op.w[i] = real ? given[p].w[i] : 0u;
+            kept.w[i] = real ? given[p].w[i] : 0x7FFF7FFFu;
         }
-        if (!up) {
-            Operand<SUB> o{};
+        centre[p * kWave + lane] = kept;
+        constexpr int words = sizeof(op) / 4;
 #pragma unroll
-            for (int i = 0; i < SUB / 2; ++i) o.w[i] = e.w[i];
-            centre[j] = o;
-        }
+        for (int i = 0; i < words; ++i)
+            halves(op.w[i], !FP16 && i < 2 ? rec.w[i] : 0u, &a[2 * p].w[i], &a[2 * p + 1].w[i]);
         if constexpr (FP16) {
-            norm_of[n] = rec;
-        } else if (up) {
-            op = Operand<SUB>{};
-            op.w[0] = rec.w[0];
-            op.w[1] = rec.w[1];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                halves(rec.w[i], 0u, &norm_of[2 * p].w[i], &norm_of[2 * p + 1].w[i]);
         }
-        a[n] = op;
     }
 #pragma unroll
-    for (int d = 16; d; d /= 2) big = fmaxf(big, __shfl_xor(big, d));
+    for (int d = 32; d; d /= 2) big = fmaxf(big, __shfl_xor(big, d));
     const int tiles = (c.K + 31) >> 5;
     // columns of the norms' product: ones for the three parts, T for its 1
     const bool takes_norm = FP16 ? !up : up;
