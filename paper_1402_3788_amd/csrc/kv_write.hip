@@ -21,7 +21,7 @@
 // instruction each (the maximum of three), 16 groups at 2, and 4 distances at some
 // 17: about 280 vector instructions and 8 matrix products a step, which add up on
 // gfx950 and bound it. 4096 tokens of 8 heads of 128 features in sub-vectors of 4,
-// keys and values (2.1 million sub-vectors, 537 million distances): 38 us, 14
+// keys and values (2.1 million sub-vectors, 537 million distances): 36 us, 15
 // distances a picosecond, where all of them on the vector ALU took 153. A few tokens
 // are better off with the latter (kFew below).
 #include "kv_device.h"
@@ -36,11 +36,12 @@ constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kTokens = 32;          // tokens of a wave's step, columns of the product
 
 // Sub-vectors up to which all distances are taken on the vector ALU: 8 heads of 128
-// features in sub-vectors of 4, 1 token (512 of them) 2.8 us and 5.1 with the
-// screen, 16 tokens 4.9 and 5.4, 24 tokens (12288) 5.2 and 5.4, 32 tokens 6.0 and 5.5;
-// 8 of 128 in 8, 32 tokens (8192) 5.3 and 5.8, 64 6.9 and 5.9; 8 of 64 in 2, 24 tokens
-// (12288) 5.1 and 5.5, 32 5.7 and 5.5; 1 of 128 in 4, 64 tokens (4096) 3.6 and 5.3.
-constexpr int kFew = 12288;
+// features in sub-vectors of 4, 1 token (512 of them) 2.9 us and 3.9 with the
+// screen, 8 tokens (4096) 3.7 and 3.9, 12 4.4 and 4.1, 24 5.5 and 4.1; 8 of 128 in 8,
+// 16 tokens (4096) 4.0 and 4.1, 24 4.8 and 4.4; 4 of 64 in 2, 16 tokens (4096) 3.6
+// and 4.1, 24 4.1 and 4.0; 8 of 128 in 2, 4 tokens (4096) 3.5 and 3.9, 8 4.8 and 4.2;
+// 1 of 128 in 4, 64 tokens (4096) 3.6 and 4.0, 128 5.0 and 4.1.
+constexpr int kFew = 4096;
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4v __attribute__((ext_vector_type(4)));
@@ -361,11 +362,11 @@ hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
     }
     const int64_t steps = (t.tokens + kTokens - 1) / kTokens;
     // Workgroups to a CU: a wave's start (256 centres read, eight operands made)
-    // takes about as long as a step, so where each CU has few steps, three. 1021
-    // tokens, 3 and 6: 8 heads of 128 in 8 (8 steps a CU) 10.4 and 12.6 us, 4 of 64
-    // in 2 (8) 9.7 and 11.1, 8 of 128 in 4 (16) 15.1 and 15.3, in 2 (32) 23.2 and
-    // 22.6; 4096, 8 of 128 in 4 (64) 43.1 and 39.6.
-    const int64_t each = steps * kinds <= 24 * kCUs ? 3 : 6;
+    // takes nearly as long as a step, so where each CU has few steps, three. 1021
+    // tokens, 3 and 6: 8 heads of 128 in 8 (8 steps a CU) 9.0 and 9.8 us, 4 of 64 in 2
+    // (8) 8.0 and 8.8, 8 of 128 in 4 (16) 13.4 and 13.0, in 2 (32) 21.1 and 20.0; 4096,
+    // 1 of 128 in 4 (8) 6.7 and 7.9, 8 (64) 39.5 and 36.4.
+    const int64_t each = steps * kinds <= 12 * kCUs ? 3 : 6;
     const int64_t most = (each * kCUs + kinds - 1) / kinds;
     const unsigned y = (unsigned)(steps < most ? steps : most);
     if (c.fp16)
