@@ -21,16 +21,16 @@
 // (Codes below). The values' rows are features: four features of eight positions,
 // looked up, are turned in registers.
 //
-// On gfx950 a SIMD's vector instructions and matrix products add up, and their sum
-// bounds the kernel: per tile and wave 178 of the former (32 to find the keys'
-// centres in LDS, 48 to find and turn the values', some 55 for the weights, the
-// rest loads ahead) and 16 of the latter, 85 % of all cycles, against 60 % of LDS
-// (a random key lookup of a wave takes 7 cycles instead of 4; the values' rows are
-// laid out to be free of conflicts). 64 sequences of 8192 to 16384 positions, 8
-// heads of 128 features in sub-vectors of 4, 64 query heads: 111 us, 3.4 TB/s of
-// codes (a copy moves 4.8; with the loads of codes left out it takes 101), of which
-// 6 are the centres and the joining in the workgroup; the joining launch takes 5
-// more. Sub-vectors of 2, with twice the bytes: 4.4 TB/s.
+// A SIMD's vector instructions (63 % of its cycles) and matrix products (21 %) bound
+// the kernel: per tile and wave 178 of the former (32 to find the keys' centres in
+// LDS, 48 to find and turn the values', some 55 for the weights, the rest loads
+// ahead) and 16 of the latter, against 60 % of LDS (a random key lookup of a wave
+// takes 7 cycles instead of 4; the values' rows are laid out to be free of
+// conflicts). 64 sequences of 8192 to 16384 positions, 8 heads of 128 features in
+// sub-vectors of 4, 64 query heads: 111 us, 3.4 TB/s of codes (a copy moves 4.8; with
+// the loads of codes left out it takes 101), of which 6 are the centres and the
+// joining in the workgroup; the joining launch takes 5 more. Sub-vectors of 2, with
+// twice the bytes: 4.4 TB/s.
 #include "kv_device.h"
 
 #include <type_traits>

@@ -19,11 +19,12 @@
 // A wave keeps the 256 centres of one sub-vector as matrix operands in its
 // registers and takes 32 tokens a step. A lane then has 128 scores, at half an
 // instruction each (the maximum of three), 16 groups at 2, and 4 distances at some
-// 17: about 280 vector instructions and 8 matrix products a step, which add up on
-// gfx950 and bound it. 4096 tokens of 8 heads of 128 features in sub-vectors of 4,
-// keys and values (2.1 million sub-vectors, 537 million distances): 36 us, 15
-// distances a picosecond, where all of them on the vector ALU took 153. A few tokens
-// are better off with the latter (kFew below).
+// 17: about 250 vector instructions and 8 matrix products a step. The former take
+// 97 % of a SIMD's cycles and bound it, most of the latter run beside them. 4096
+// tokens of 8 heads of 128 features in sub-vectors of 4, keys and values (2.1 million
+// sub-vectors, 537 million distances): 36 us, 15 distances a picosecond, where all of
+// them on the vector ALU took 153. A few tokens are better off with the latter (kFew
+// below).
 #include "kv_device.h"
 
 #include <type_traits>
