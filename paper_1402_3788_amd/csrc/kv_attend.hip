@@ -85,23 +85,18 @@ __device__ inline uint32_t pack2(float a, float b)
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
 }
 
-// x cut off to the 16-bit type, where mask is all ones; 0 where it is 0. (Below
-// the least normal number of fp16 the cut leaves more bits than fp16 has there,
-// less than 2^-24 that neither part takes up.)
-template <bool FP16>
+// x cut off to fp16, where mask is all ones; 0 where it is 0. (Below the least
+// normal number of fp16 the cut leaves more bits than fp16 has there, less than
+// 2^-24 that neither part takes up.)
 __device__ inline float cut(float x, uint32_t mask)
 {
-    return __uint_as_float(__float_as_uint(x) & (FP16 ? 0xFFFFE000u : 0xFFFF0000u) & mask);
+    return __uint_as_float(__float_as_uint(x) & 0xFFFFE000u & mask);
 }
 
-// Two numbers cut off to the 16-bit type.
-template <bool FP16>
+// Two numbers cut off to fp16.
 __device__ inline uint32_t cut2(float a, float b)
 {
-    if constexpr (FP16)
-        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
-    else
-        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
 }
 
 // Sizes of one form of the kernel.
@@ -476,6 +471,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     const float scale = fabsf(a.scale_log2);
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;     // the scale's sign, for the queries
     const uint32_t low_parts = r >= 8 ? ~0u : 0u;        // lanes whose columns take them
+    // the byte selection that makes the first of two bf16 an fp32 number there, else 0
+    const uint32_t low_byte = r >= 8 ? 0x01000C0Cu : 0x0C0C0C0Cu;
 
     const auto load_q = [&](int b) {
 #pragma unroll
@@ -663,18 +660,30 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 z[i] = __builtin_amdgcn_exp2f(z[i]);
                 l += z[i];
             }
-            // each weight as the sum of two 16-bit numbers, both cut off and not
-            // rounded: one alone (8 bits of bf16) would cost as much of the result
-            // as its own final rounding
+            // Each weight as the sum of two 16-bit numbers. One alone (8 bits of bf16)
+            // would cost as much of the result as its own final rounding. Of bf16 both
+            // are rounded to nearest: cut off, 16 bits would leave every weight too
+            // small, 8e-6 of it on average, beside a sum l that has all of it (three
+            // parts, 24 bits, change the outputs no further and take 8 % longer). Of
+            // fp16 they are cut, which leaves 2^-21 at most.
             u4v p, p_lo;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float z0 = z[2 * i], z1 = z[2 * i + 1];
-                if constexpr (WIDE) {
-                    p[i] = cut2<FP16>(z0, z1);
-                    p_lo[i] = cut2<FP16>(z0 - cut<FP16>(z0, ~0u), z1 - cut<FP16>(z1, ~0u));
+                if constexpr (FP16 && WIDE) {
+                    p[i] = cut2(z0, z1);
+                    p_lo[i] = cut2(z0 - cut(z0, ~0u), z1 - cut(z1, ~0u));
+                } else if constexpr (FP16) {
+                    p[i] = cut2(z0 - cut(z0, low_parts), z1 - cut(z1, low_parts));
+                } else if constexpr (WIDE) {
+                    p[i] = pack2<FP16>(z0, z1);
+                    p_lo[i] = pack2<FP16>(z0 - __uint_as_float(p[i] << 16),
+                                          z1 - __uint_as_float(p[i] & 0xFFFF0000u));
                 } else {
-                    p[i] = cut2<FP16>(z0 - cut<FP16>(z0, low_parts), z1 - cut<FP16>(z1, low_parts));
+                    const uint32_t high = pack2<FP16>(z0, z1);
+                    p[i] = pack2<FP16>(
+                        z0 - __uint_as_float(__builtin_amdgcn_perm(0u, high, low_byte)),
+                        z1 - __uint_as_float(high & low_parts & 0xFFFF0000u));
                 }
             }
             // values: rows are features, columns queries
