@@ -17,7 +17,8 @@ Entry points (same names as the C ABI):
     kmeans_workspace_bytes(n, M, K, flags=0), kmeans_init_workspace_bytes(n, M, K),
     kmeans_strerror(code)
 and, from kv.py, a key-value cache in K-means codes: KVCodes, kmeans_kv_write,
-kmeans_kv_read, kmeans_kv_attend.
+kmeans_kv_read, kmeans_kv_attend (their usual calls through a module in C++,
+_kv_call, where that is built; the same calls through ctypes where not).
 """
 from __future__ import annotations
 

@@ -3,7 +3,8 @@
 // take there, checks, outputs and the library's call, is 4 to 7 us of the host's
 // time in Python beyond the launches' own, as much as the small calls take on the
 // GPU; here it is about 1. Anything else, errors in the arguments among it, is
-// answered by None, and kv.py goes through it step by step.
+// answered by None, and kv.py goes through it step by step, as it does with all
+// calls where this module is not there.
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
@@ -145,4 +146,13 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_call", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__kv_call() { return PyModule_Create(&module); }
+// torch_version: the torch whose headers this was built with; kv.py takes no other.
+PyMODINIT_FUNC PyInit__kv_call()
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", KV_TORCH) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

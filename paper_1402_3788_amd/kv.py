@@ -13,20 +13,27 @@ from __future__ import annotations
 
 import ctypes
 import math
+import warnings
 
 import torch
 
 from . import KmeansError, KMEANS_EUNSUPPORTED, _lib
 
+# The usual calls in C++. Without it, or with one built for another torch, every
+# call takes the steps below: the same results, 4 to 7 us later.
 try:
     from . import _kv_call as _fast
+    _without = None
+    if getattr(_fast, "torch_version", None) != str(torch.__version__):
+        _fast, _without = None, f"it was not built for torch {torch.__version__}"
 except ImportError as e:
-    raise ImportError("_kv_call.so is not built; run `python paper_1402_3788_amd/build.py`") from e
+    _fast, _without = None, str(e)
 
 # a tenth of the time of torch.cuda.current_stream and current_device, which
 # small calls would mostly consist of
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}      # KMEANS_KV_BF16, KMEANS_KV_FP16
 
@@ -52,9 +59,10 @@ def _bind():
     _lib.kmeans_kv_attend.argtypes = [d, p, i64, i64, i32, i32, p, i64, i64, p, p, ctypes.c_float,
                                       p, i64, i64, p, p, sz, p]
     _lib.kmeans_kv_attend.restype = ctypes.c_int
-    _fast.bind(*(ctypes.cast(f, ctypes.c_void_p).value
-                 for f in (_lib.kmeans_kv_write, _lib.kmeans_kv_read,
-                           _lib.kmeans_kv_attend_workspace_bytes, _lib.kmeans_kv_attend)))
+    if _fast is not None:
+        _fast.bind(*(ctypes.cast(f, ctypes.c_void_p).value
+                     for f in (_lib.kmeans_kv_write, _lib.kmeans_kv_read,
+                               _lib.kmeans_kv_attend_workspace_bytes, _lib.kmeans_kv_attend)))
 
 
 _bind()
@@ -97,6 +105,10 @@ class KVCodes:
         # the library says what it takes; it looks at no pointer here
         if not self.attend_workspace_bytes(1, heads, 1):
             raise KmeansError("KVCodes", KMEANS_EUNSUPPORTED)
+        if _fast is None:
+            warnings.warn("_kv_call cannot be used, the cache's calls take 4 to 7 us longer "
+                          f"(`python paper_1402_3788_amd/build.py` builds it): {_without}",
+                          RuntimeWarning, stacklevel=2)
 
     @classmethod
     def empty(cls, k_centres, v_centres, pages: int, page: int):
@@ -177,7 +189,7 @@ def kmeans_kv_write(cache: KVCodes, k: torch.Tensor, v: torch.Tensor, slots: tor
     """Encodes the tokens k, v ([n, heads, dim]) into the slots of `slots` (int64
     [n]; page number * page + place). A token whose slot is negative or past
     the cache is left out."""
-    if _current_device() == cache.index:
+    if _fast is not None and _current_device() == cache.index:
         rc = _fast.write(cache._at, cache.k_centres, _raw_stream(cache.index), k, v, slots)
         if rc == 0:
             return
@@ -198,7 +210,7 @@ def kmeans_kv_read(cache: KVCodes, slots: torch.Tensor, out=None):
     """The keys and values in the slots of `slots` (int64 [n]), as the centres
     that their codes name: (k, v), each [n, heads, dim]; zeros for a slot that
     is not in the cache. `out` may supply both tensors."""
-    if out is None and _current_device() == cache.index:
+    if _fast is not None and out is None and _current_device() == cache.index:
         got = _fast.read(cache._at, cache.k_centres, _raw_stream(cache.index), slots)
         if type(got) is tuple:
             return got
@@ -232,7 +244,8 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
     (cache.attend_workspace_bytes)."""
     if scale is None:
         scale = 1.0 / math.sqrt(cache.dim)
-    if out is None and lse is None and ws is None and _current_device() == cache.index:
+    if (_fast is not None and out is None and lse is None and ws is None
+            and _current_device() == cache.index):
         got = _fast.attend(cache._at, cache.k_centres, _raw_stream(cache.index), q, table, lengths,
                            scale, starts)
         if type(got) is tuple:
