@@ -131,6 +131,12 @@ class KVCodes:
         return nbytes
 
 
+def _strides(t):
+    """t's strides; 0 for a dimension of one, whose stride leads nowhere and may
+    be any number."""
+    return tuple(s if n > 1 else 0 for n, s in zip(t.shape[:2], t.stride())) + t.stride()[2:]
+
+
 def _rows(cache, t, what):
     """t as the library takes it, [n, heads, dim] with its features contiguous
     and its rows on 16 bytes (a copy where it is not), its address, its shape
@@ -145,7 +151,7 @@ def _rows(cache, t, what):
         t = t.contiguous()
         if t.data_ptr() & 15:
             t = t.clone()
-        a, b, c = t.stride()
+        a, b, c = _strides(t)
         at = t.data_ptr()
     return t, at, t.shape, a, b
 
@@ -159,6 +165,8 @@ def _target(cache, t, shape, what):
             and t.dtype is cache.dtype and t.get_device() == cache.index):
         raise ValueError(f"{what} must be {tuple(shape)} of the cache's type on its GPU")
     a, b, c = t.stride()
+    if (a | b) & 7:
+        a, b, c = _strides(t)
     if c != 1 or (a | b) & 7 or t.data_ptr() & 15 or (a == 0 and shape[0] > 1) \
             or (b == 0 and shape[1] > 1):
         raise ValueError(f"{what} needs contiguous features, rows on 16 bytes, and no two "

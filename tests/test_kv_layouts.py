@@ -1,0 +1,72 @@
+"""Strides of the key-value cache's tensors, as the binding hands them to the
+library: on the host, without a GPU, and in calls."""
+import types
+
+import pytest
+import torch
+
+import paper_1402_3788_amd as km
+from paper_1402_3788_amd import kv
+
+BF = torch.bfloat16
+HOST = types.SimpleNamespace(dtype=BF, index=-1, device=torch.device("cpu"), dim=64)
+
+
+def one_token():
+    """One of several tokens whose rows are an odd length apart."""
+    return torch.arange(4 * 516).to(BF).view(4, 516)[:, :512].unflatten(1, (8, 64))[2:3]
+
+
+def one_head():
+    return torch.arange(6 * 75).to(BF).view(6, 75)[:, None, 8:72].transpose(0, 1)[:, :1]
+
+
+@pytest.mark.parametrize("make", [one_token, one_head])
+def test_the_stride_of_a_single_row_is_of_no_account(make):
+    """Such a tensor is contiguous, so that copying it changes no stride."""
+    t = make()
+    assert t.is_contiguous() and any(s % 8 for s in t.stride())
+    got, at, shape, a, b = kv._rows(HOST, t, "t")
+    assert shape == t.shape and a % 8 == 0 and b % 8 == 0
+    assert torch.equal(got.reshape(shape), t) and at == got.data_ptr()
+    assert (a == 0 or shape[0] > 1) and (b == 0 or shape[1] > 1)
+
+
+def test_an_output_of_a_single_row():
+    wide = torch.zeros(4, 520, dtype=BF)
+    at = (-wide.data_ptr() // 2) % 8
+    t = wide.view(-1)[at:].as_strided((1, 8, 64), (516, 64, 1))
+    got, _, a, b = kv._target(HOST, t, (1, 8, 64), "t")
+    assert got is t and a % 8 == 0 and b == 64
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("make", [one_token, one_head])
+def test_calls_with_single_rows(make):
+    dev = torch.device("cuda:0")
+    src = make()
+    wide = src.untyped_storage().nbytes() // 2
+    # the same layout on the GPU
+    t = torch.randn(wide, generator=torch.Generator().manual_seed(0)).to(BF).to(dev).as_strided(
+        src.shape, src.stride(), src.storage_offset())
+    assert any(s % 8 for s in t.stride())
+    n, heads, dim = t.shape
+    centres = torch.randn(heads, dim // 4, 256, 4, device=dev).to(BF)
+    caches = [km.KVCodes.empty(centres, centres, 2, 16) for _ in range(2)]
+    slots = torch.arange(3, 3 + n, device=dev)
+    plain = torch.empty(n, heads, dim, device=dev, dtype=BF).copy_(t)
+    for cache, x in zip(caches, (t, plain)):
+        km.kmeans_kv_write(cache, x, x, slots)
+    assert torch.equal(caches[0].k_codes, caches[1].k_codes)
+    assert torch.equal(caches[0].v_codes, caches[1].v_codes)
+    want = km.kmeans_kv_read(caches[0], slots)
+    out = [torch.zeros(wide + 16, device=dev, dtype=BF).as_strided(t.shape, t.stride())
+           for _ in range(2)]
+    km.kmeans_kv_read(caches[0], slots, out=out)
+    for a, b in zip(out, want):
+        assert torch.equal(a, b)
+    table = torch.zeros(n, 1, dtype=torch.int32, device=dev)
+    lengths = torch.full((n,), 9, dtype=torch.int32, device=dev)
+    want = km.kmeans_kv_attend(caches[0], plain, table, lengths)
+    for a, b in zip(km.kmeans_kv_attend(caches[0], t, table, lengths, out=out[0]), want):
+        assert torch.equal(a, b)
