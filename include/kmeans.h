@@ -317,7 +317,7 @@ int kmeans_kv_write(const kmeans_kv_t *kv, const void *k, int64_t k_token, int64
 /*
  * Reads tokens back: k and v ([tokens][heads][dim], DEVICE) receive the centres
  * that the codes in slots[t] name, zeros where the slot is negative or past
- * the cache. tokens = 0 is KMEANS_OK. Asynchronous on `stream`.
+ * the cache. No two elements of k and v lie in one place. tokens = 0 is KMEANS_OK. Asynchronous on `stream`.
  */
 int kmeans_kv_read(const kmeans_kv_t *kv, const int64_t *slots, int64_t tokens, void *k,
                    int64_t k_token, int64_t k_head, void *v, int64_t v_token, int64_t v_head,
@@ -344,7 +344,8 @@ size_t kmeans_kv_attend_workspace_bytes(const kmeans_kv_t *kv, int32_t seqs, int
  * whose z is above -infinity: out = 0, lse = -infinity. Entries of table whose
  * pages hold no such position are not read. A length is taken as at most
  * table_pages * page, a negative start as 0; an entry outside [0, pages) is
- * taken as some page of the cache. out and lse overlap nothing that is read.
+ * taken as some page of the cache. out and lse overlap nothing that is read, and
+ * no two of their elements lie in one place.
  * 1 <= seqs <= 4096 (0 is KMEANS_OK), seqs * q_heads < 2^24, table_pages * page
  * <= 2^30, and seqs * table_pages * page / 32 < 2^31. scale is finite. Scores,
  * their maximum and sum and the output are held in fp32; a weight

@@ -156,6 +156,23 @@ def _rows(cache, t, what):
     return t, at, t.shape, a, b
 
 
+def _apart(n, a, heads, b, dim):
+    """Whether rows of dim features, n of them a apart for each of the heads b apart,
+    have no element in common."""
+    if n == 0 or heads == 0:
+        return True
+    (n, a), (heads, b) = sorted(((n, a), (heads, b)), key=lambda x: x[1] if x[0] > 1 else 0)
+    if n == 1:
+        return heads == 1 or b >= dim
+    if a < dim:
+        return False
+    if (n - 1) * a + dim <= b:                  # one run of rows ends before the next
+        return True
+    # runs that lie among each other: the rows next to j b of the first run
+    return all(j * b - i * a >= dim and (i + 1 == n or (i + 1) * a - j * b >= dim)
+               for j in range(1, heads) for i in (min(j * b // a, n - 1),))
+
+
 def _target(cache, t, shape, what):
     """An output that the caller gave, or a new one; its address and strides."""
     if t is None:
@@ -167,8 +184,7 @@ def _target(cache, t, shape, what):
     a, b, c = t.stride()
     if (a | b) & 7:
         a, b, c = _strides(t)
-    if c != 1 or (a | b) & 7 or t.data_ptr() & 15 or (a == 0 and shape[0] > 1) \
-            or (b == 0 and shape[1] > 1):
+    if c != 1 or (a | b) & 7 or t.data_ptr() & 15 or not _apart(shape[0], a, shape[1], b, shape[2]):
         raise ValueError(f"{what} needs contiguous features, rows on 16 bytes, and no two "
                          "elements in one place")
     return t, t.data_ptr(), a, b

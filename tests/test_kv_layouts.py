@@ -40,6 +40,35 @@ def test_an_output_of_a_single_row():
     assert got is t and a % 8 == 0 and b == 64
 
 
+OUTPUTS = [
+    # tokens, heads, strides of both
+    (3, 2, 128, 64), (3, 2, 64, 192), (3, 2, 136, 64), (1, 2, 0, 64), (3, 1, 64, 0),
+    (3, 2, 128, 56), (3, 2, 120, 64), (3, 2, 64, 184), (3, 2, 64, 64), (2, 3, 64, 128),
+    (3, 2, 128, 192), (3, 2, 128, 256), (3, 2, 128, 320), (4, 3, 192, 256), (5, 4, 256, 320),
+    (3, 2, 0, 64), (3, 2, 128, 0), (3, 2, 8, 640), (2, 2, 64, 8), (100, 2, 128, 12864),
+]
+
+
+@pytest.mark.parametrize("n,heads,a,b", OUTPUTS)
+def test_outputs_hold_no_two_elements_in_one_place(n, heads, a, b):
+    at = (torch.arange(n)[:, None, None] * a + torch.arange(heads)[:, None] * b
+          + torch.arange(64)).flatten()
+    alone = at.unique().numel() == at.numel()
+    room = torch.zeros(int(at.max()) + 9, dtype=BF)
+    t = room[(-room.data_ptr() // 2) % 8:].as_strided((n, heads, 64), (a, b, 1))
+    if alone:
+        assert kv._target(HOST, t, (n, heads, 64), "t")[0] is t
+    else:
+        with pytest.raises(ValueError, match="one place"):
+            kv._target(HOST, t, (n, heads, 64), "t")
+
+
+def test_outputs_of_no_tokens():
+    for stride in ((0, 0, 1), (8, 8, 1), (128, 64, 1)):
+        t = torch.zeros(0, 2, 64, dtype=BF).as_strided((0, 2, 64), stride)
+        assert kv._target(HOST, t, (0, 2, 64), "t")[0] is t
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("make", [one_token, one_head])
 def test_calls_with_single_rows(make):
