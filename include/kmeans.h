@@ -317,7 +317,8 @@ int kmeans_kv_write(const kmeans_kv_t *kv, const void *k, int64_t k_token, int64
 /*
  * Reads tokens back: k and v ([tokens][heads][dim], DEVICE) receive the centres
  * that the codes in slots[t] name, zeros where the slot is negative or past
- * the cache. No two elements of k and v lie in one place. tokens = 0 is KMEANS_OK. Asynchronous on `stream`.
+ * the cache. No two elements of k and v lie in one place. tokens = 0 is
+ * KMEANS_OK. Asynchronous on `stream`.
  */
 int kmeans_kv_read(const kmeans_kv_t *kv, const int64_t *slots, int64_t tokens, void *k,
                    int64_t k_token, int64_t k_head, void *v, int64_t v_token, int64_t v_head,

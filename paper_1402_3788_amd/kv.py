@@ -159,6 +159,8 @@ def _rows(cache, t, what):
 def _apart(n, a, heads, b, dim):
     """Whether rows of dim features, n of them a apart for each of the heads b apart,
     have no element in common."""
+    if heads * b <= a and b >= dim:             # the usual ones
+        return True
     if n == 0 or heads == 0:
         return True
     (n, a), (heads, b) = sorted(((n, a), (heads, b)), key=lambda x: x[1] if x[0] > 1 else 0)
