@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -110,6 +111,8 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor &centres = THPVariable_Unpack(a[1]);
     const at::Tensor *q = rows(a[3], centres, kv), *table = plain(a[4], centres, at::kInt, 2);
     if (!q || !table) Py_RETURN_NONE;
+    if ((q->requires_grad() && c10::GradMode::is_enabled()) || q->_fw_grad(0).defined())
+        Py_RETURN_NONE;
     const int64_t seqs = q->size(0), q_heads = q->size(1), width = table->size(1);
     if (table->size(0) != seqs || width == 0 || table->stride(1) != 1) Py_RETURN_NONE;
     const at::Tensor *lengths = ints(a[5], centres, at::kInt, seqs), *starts = nullptr;

@@ -7,7 +7,9 @@
                      lse=None, ws=None) -> (out, lse)
 
 Everything runs on the current stream of the cache's device; no call waits for
-it or reads device data back.
+it or reads device data back. No call carries a gradient: keys and values are
+written as constants, the codes and centres are constants, and a query or an
+output that needs a gradient is refused (torch.no_grad() says that it does not).
 """
 from __future__ import annotations
 
@@ -16,6 +18,7 @@ import math
 import warnings
 
 import torch
+from torch.autograd import forward_ad
 
 from . import KmeansError, KMEANS_EUNSUPPORTED, _lib
 
@@ -131,6 +134,14 @@ class KVCodes:
         return nbytes
 
 
+def _no_gradient(t, what):
+    """Refuses a tensor whose gradient the caller would miss without a word."""
+    if (t.requires_grad and torch.is_grad_enabled()) or (
+            forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None):
+        raise ValueError(f"{what} needs a gradient, which these calls do not carry: detach it, "
+                         "or call them under torch.no_grad()")
+
+
 def _strides(t):
     """t's strides; 0 for a dimension of one, whose stride leads nowhere and may
     be any number."""
@@ -183,6 +194,7 @@ def _target(cache, t, shape, what):
     if not (isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape)
             and t.dtype is cache.dtype and t.get_device() == cache.index):
         raise ValueError(f"{what} must be {tuple(shape)} of the cache's type on its GPU")
+    _no_gradient(t, what)
     a, b, c = t.stride()
     if (a | b) & 7:
         a, b, c = _strides(t)
@@ -279,6 +291,7 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
         if got is not None:
             raise KmeansError("kmeans_kv_attend", got)
     q, qp, shape, qa, qb = _rows(cache, q, "q")
+    _no_gradient(q, "q")
     seqs, q_heads, dim = shape
     if q_heads < 1 or q_heads % cache.heads:
         raise ValueError(f"q must have a multiple of {cache.heads} heads")
@@ -303,6 +316,8 @@ def kmeans_kv_attend(cache: KVCodes, q: torch.Tensor, table: torch.Tensor, lengt
               and lse.is_contiguous() and lse.get_device() == cache.index):
         raise ValueError(f"lse must be a contiguous float32 [{seqs}, {q_heads}] tensor on the "
                          "cache's GPU")
+    else:
+        _no_gradient(lse, "lse")
     width = table.shape[1]
     if width == 0 or seqs == 0:         # no position anywhere
         return out.zero_(), lse.fill_(-math.inf)
