@@ -79,7 +79,21 @@ class KVCodes:
     v_codes               [pages, heads, dim / sub, page], uint8
 
     all contiguous on one GPU. The tensors are kept, not copied: what is written
-    to them is what the calls see."""
+    to them is what the calls see. Other tensors, or other sizes, are another
+    KVCodes: these attributes cannot be set."""
+
+    _KEPT = frozenset(("k_centres", "v_centres", "k_codes", "v_codes", "pages", "page", "heads",
+                       "dim", "sub", "K", "dtype", "device", "index"))
+
+    def __setattr__(self, name, value):
+        # the library has their addresses and sizes; an operation in place, which ends
+        # by setting what was there, is none of this
+        if name in self._KEPT and self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} of a KVCodes cannot be set: make another")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{name} of a KVCodes cannot be deleted")
 
     def __init__(self, k_centres, v_centres, k_codes, v_codes):
         tensors = (k_centres, v_centres, k_codes, v_codes)
