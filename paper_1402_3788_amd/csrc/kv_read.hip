@@ -166,15 +166,19 @@ __global__ __launch_bounds__(kWaves * kWave) void kv_read_kernel(KvCache c, KvTo
 template <int SUB>
 hipError_t launch(const KvCache &c, const KvTokens &t, hipStream_t s)
 {
-    // Centres from LDS from 2^18 sub-vectors on, whose lookups in the L2 take longer
-    // than fetching the centres does: 8 heads of 128 features, sub-vectors of 4,
-    // 512 tokens (2^17) 3.9 us from the L2 and 4.6 from LDS, 1024 5.3 and 4.7; one
-    // head, 8192 tokens (2^18) 4.6 and 4.7, 16384 6.1 and 5.2; 8 heads of 64,
-    // sub-vectors of 2, 512 (2^17) 3.5 and 4.2, 1024 5.0 and 4.1; 8 of 128 in 8, 1024
-    // (2^17) 3.9 and 4.5, 2048 5.9 and 5.1; in 2, 512 (2^18) 4.8 and 6.2, 1024 6.5 and
-    // 6.5. A workgroup has 128 tokens or more, two to a CU at most.
-    const int64_t kinds = 2 * c.heads, units = t.tokens * c.heads * (c.dim / SUB);
-    if (units >= (int64_t)1 << 18) {
+    // Centres from LDS where their lookups in the L2 take longer than fetching them,
+    // 512 bytes a feature to a workgroup, does. For sub-vectors of up to 32 a row (a
+    // head of a token) that is from 2^18 of them on, above that, where a workgroup
+    // also has more of them to place, from 2^13 rows. From the L2 and from LDS, us, at
+    // half the limit and at it (dim in sub, heads): 128 in 4, 8 3.8 4.6, 5.2 4.8; 128
+    // in 4, 1 3.6 4.7, 4.5 4.8; 96 in 4, 5 4.0 4.6, 5.0 4.8; 64 in 4, 8 4.0 3.7, 5.2
+    // 4.2; 64 in 2, 8 3.6 4.1, 5.0 4.4; 128 in 8, 8 4.0 4.6, 5.8 5.4; 96 in 8, 8 4.1
+    // 4.8, 5.8 5.4; 64 in 8, 3 3.7 4.2, 5.6 4.5; and with the second limit 128 in 2, 8
+    // 5.0 6.3, 7.4 6.6; 128 in 2, 2 4.9 6.1, 6.9 6.4; 96 in 2, 8 (at 2^18 and 2^19
+    // sub-vectors, 2^18.6 its limit) 5.1 5.6, 7.6 5.9. A workgroup has 128 tokens or
+    // more, two to a CU at most.
+    const int64_t kinds = 2 * c.heads, rows = t.tokens * c.heads, units = rows * (c.dim / SUB);
+    if (units >= (int64_t)1 << 18 && rows >= (int64_t)1 << 13) {
         const int64_t most = (2 * kCUs + kinds - 1) / kinds, enough = (t.tokens + 127) / 128;
         const int parts = (int)(most < enough ? most : enough);
         const dim3 grid((unsigned)(parts * kinds)), block(kWaves * kWave);
