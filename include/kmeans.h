@@ -348,13 +348,12 @@ size_t kmeans_kv_attend_workspace_bytes(const kmeans_kv_t *kv, int32_t seqs, int
  * taken as some page of the cache. out and lse overlap nothing that is read, and
  * no two of their elements lie in one place.
  * 1 <= seqs <= 4096 (0 is KMEANS_OK), seqs * q_heads < 2^24, table_pages * page
- * <= 2^30, and seqs * table_pages * page / 32 < 2^31. scale is finite. Scores,
- * their maximum and sum and the output are held in fp32; a weight
- * exp(z_i - max) enters the product with the values as the sum of two 16-bit
- * numbers: of bf16 each rounded to nearest, 2^-17 of the weight at most; of fp16
- * each cut off, 2^-21 of it and 2^-31 of the largest. The same inputs give the
- * same bits.
- * Asynchronous on `stream`.
+ * <= 2^30, and seqs * table_pages * page / 32 < 2^31. |scale| <= 2.35e38
+ * (KMEANS_EINVAL otherwise: it is taken to base 2). Scores, their maximum and sum
+ * and the output are held in fp32; a weight exp(z_i - max) enters the product with
+ * the values as the sum of two 16-bit numbers: of bf16 each rounded to nearest,
+ * 2^-17 of the weight at most; of fp16 each cut off, 2^-21 of it and 2^-31 of the
+ * largest. The same inputs give the same bits. Asynchronous on `stream`.
  */
 int kmeans_kv_attend(const kmeans_kv_t *kv, const void *q, int64_t q_seq, int64_t q_head,
                      int32_t seqs, int32_t q_heads, const int32_t *table, int64_t table_stride,

@@ -131,7 +131,8 @@ int kmeans_kv_attend(const kmeans_kv_t *kv, const void *q, int64_t q_seq, int64_
 {
     int rc = check_cache(kv);
     if (rc || (rc = check_attend(kv, seqs, q_heads, table_pages))) return rc;
-    if (!isfinite(scale)) return KMEANS_EINVAL;
+    const float scale_log2 = scale * 1.44269504088896341f;
+    if (!isfinite(scale_log2)) return KMEANS_EINVAL;
     if (seqs == 0) return KMEANS_OK;
     if (!q || !out || !table || !lengths || !aligned16(q) || !aligned16(out))
         return KMEANS_EINVAL;
@@ -153,7 +154,7 @@ int kmeans_kv_attend(const kmeans_kv_t *kv, const void *q, int64_t q_seq, int64_
     a.table_pages = (int)table_pages;
     a.lengths = lengths;
     a.starts = starts;
-    a.scale_log2 = scale * 1.44269504088896341f;
+    a.scale_log2 = scale_log2;
     a.out = static_cast<uint16_t *>(out);
     a.out_seq = out_seq;
     a.out_head = out_head;
