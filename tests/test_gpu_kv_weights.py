@@ -31,10 +31,10 @@ def bound():
     bits: errors that do not lean to one side add up as their squares do, 6
     standard deviations of them (uniform ones, each over its whole range). Each
     exponential and its argument, of at most 1.45, to 2^-22; 13 tiles' sums, joined,
-    to 2^-22 of what they add up; the output itself to 2^-9."""
+    to 2^-22 of what they add up; the output itself to 2^-8."""
     total = LOSSY.sum() + N_ONES
     off = 6 * 2.0 ** -17 / math.sqrt(3) * math.sqrt((LOSSY ** 2).sum())
-    return (off + 2.0 ** -22 * LOSSY.sum() + 2.0 ** -22 * total) / total + 2.0 ** -9 * abs(wanted())
+    return (off + 2.0 ** -22 * LOSSY.sum() + 2.0 ** -22 * total) / total + 2.0 ** -8 * abs(wanted())
 
 
 def cut(x):
