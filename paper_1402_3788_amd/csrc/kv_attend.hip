@@ -588,7 +588,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                 return p >= sp.start && p < sp.len;
             };
             // All centres of the tile are asked for before any is waited for: a
-            // lookup takes far longer than its turn, and a SIMD has two waves.
+            // lookup takes far longer than its turn, and a SIMD has but three waves
+            // (four with dim = 64).
             KvEntry<SUB> ke[2][F::SL];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -721,7 +722,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             for (; t < end; ++t) {
                 // The SIMD's waves take turns at the highest priority: the oldest
                 // would have it always, end first and leave the last ones to
-                // run alone.
+                // run alone. There are three turns; of four waves (dim = 64) two
+                // share one.
                 if (turn == 0) __builtin_amdgcn_s_setprio(2);
                 else if (turn == 1) __builtin_amdgcn_s_setprio(1);
                 else __builtin_amdgcn_s_setprio(0);
