@@ -21,16 +21,16 @@
 // (Codes below). The values' rows are features: four features of eight positions,
 // looked up, are turned in registers.
 //
-// A SIMD's vector instructions (63 % of its cycles) and matrix products (21 %) bound
-// the kernel: per tile and wave 178 of the former (32 to find the keys' centres in
-// LDS, 48 to find and turn the values', some 55 for the weights, the rest loads
-// ahead) and 16 of the latter, against 60 % of LDS (a random key lookup of a wave
-// takes 7 cycles instead of 4; the values' rows are laid out to be free of
-// conflicts). 64 sequences of 8192 to 16384 positions, 8 heads of 128 features in
-// sub-vectors of 4, 64 query heads: 111 us, 3.4 TB/s of codes (a copy moves 4.8; with
-// the loads of codes left out it takes 101), of which 6 are the centres and the
-// joining in the workgroup; the joining launch takes 5 more. Sub-vectors of 2, with
-// twice the bytes: 4.4 TB/s.
+// 64 sequences of 8192 to 16384 positions, 8 heads of 128 features in sub-vectors of
+// 4, 64 query heads: 112 us, 3.5 TB/s of codes (a copy moves 4.8; with the loads of
+// codes left out it took 101 of then 111), and the joining launch 5 more. Of a SIMD's
+// cycles there vector instructions, 193 a tile and wave with the 16 matrix products
+// among them, take 67 %, the products themselves are under way in 21 %; LDS is active
+// in 60 % of a CU's (61 % of that bank conflicts, of the random lookups of keys: the
+// values' rows are laid out to be free of them). None of them is a limit alone: the
+// three waves of a SIMD are issuing for 36 % of their time, ready but not issuing
+// for 26 %, and waiting for loads, LDS or a barrier for 39 %. A tile more to every
+// wave costs 1.4 us; a launch with one each takes 11 to 13.
 #include "kv_device.h"
 
 #include <type_traits>
