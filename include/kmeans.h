@@ -361,6 +361,152 @@ int kmeans_kv_attend(const kmeans_kv_t *kv, const void *q, int64_t q_seq, int64_
                      float scale, void *out, int64_t out_seq, int64_t out_head, float *lse,
                      void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Serving from the cache: queries and keys turned by their positions before the
+ * keys are encoded (kmeans_kv_rotate), attention of many new tokens of every
+ * sequence (kmeans_kv_attend_tokens), the weight that attention gave to every cached
+ * position (kmeans_kv_weigh), and the eviction of the positions that got little
+ * (kmeans_kv_evict).
+ */
+#define KMEANS_KV_INTERLEAVED (1u << 0) /* pairs (2i, 2i + 1); else (i, i + half)      */
+#define KMEANS_KV_INVERSE     (1u << 1) /* by the negative angle                      */
+
+typedef struct kmeans_kv_turn {
+    const int64_t *positions;    /* [tokens], DEVICE, any sign                          */
+    const double *frequencies;   /* [half], DEVICE: radians to a position               */
+    int64_t tokens;              /* 0 to 2^31 - 1                                       */
+    int32_t dim;                 /* features of a head: a multiple of 8, 8 to 512       */
+    int32_t half;                /* pairs that are turned, 0 to dim / 2                 */
+    int32_t type;                /* KMEANS_KV_BF16 or KMEANS_KV_FP16                    */
+    uint32_t flags;
+    float amplitude;             /* of the turned features, finite                      */
+} kmeans_kv_turn_t;
+
+/*
+ * Rotary positions. q and k are [tokens][heads][dim] with contiguous features and
+ * strides in elements, multiples of 8, from 16-byte aligned addresses; k_heads (or
+ * q_heads) may be 0. Of token t, pair i = (a, b) of every head becomes
+ *   (A (a cos w - b sin w), A (a sin w + b cos w)),   w = positions[t] * frequencies[i],
+ * with A the amplitude and -w with KMEANS_KV_INVERSE; features from 2 half on are
+ * copied. The call with KMEANS_KV_INVERSE takes the gradients of the outputs to
+ * those of the inputs. w is formed in fp64 and reduced to one turn there; the rest is
+ * fp32, rounded once. q_out and k_out may be q and k themselves, with the same
+ * strides; otherwise they overlap nothing that is read, and no two of their elements
+ * lie in one place. tokens = 0 is KMEANS_OK. Asynchronous on `stream`.
+ */
+int kmeans_kv_rotate(const kmeans_kv_turn_t *turn, const void *q, int64_t q_token, int64_t q_head,
+                     int32_t q_heads, void *q_out, int64_t q_out_token, int64_t q_out_head,
+                     const void *k, int64_t k_token, int64_t k_head, int32_t k_heads, void *k_out,
+                     int64_t k_out_token, int64_t k_out_head, void *stream);
+
+/*
+ * The new tokens of a call and how they score the cached positions. Sequence b has
+ * the tokens [bounds[b], bounds[b + 1]) of the call's (cut to [0, tokens)); they are
+ * the last of its lengths[b] positions: token t of it stands at
+ *   p = lengths[b] - bounds[b + 1] + t
+ * (below 0: it sees nothing but what a prefix gives). The new tokens are in the cache
+ * already. Token t sees the positions i with
+ *   max(0, starts[t], p - window + 1) <= i < min(lengths[b], max(p + 1, prefixes[b])),
+ * without the terms that are not given, and scores one in query head h by
+ *   z = scale * (q . k_i),  with a cap z = cap * tanh(z / cap),  with slopes
+ *   z = z - slopes[h] * |p - i|.
+ * starts are what documents in one sequence, padding before it and other masks
+ * leave, prefixes what every token sees.
+ */
+typedef struct kmeans_kv_tokens {
+    const int32_t *bounds;       /* [seqs + 1], DEVICE, ascending                       */
+    const int32_t *table;        /* [seqs][table_pages], DEVICE, as of kmeans_kv_attend */
+    int64_t table_stride, table_pages;
+    const int32_t *lengths;      /* [seqs], DEVICE: cached positions, new ones included */
+    const int32_t *starts;       /* [tokens], DEVICE, or NULL                           */
+    const int32_t *prefixes;     /* [seqs], DEVICE, or NULL                             */
+    const float *slopes;         /* [q_heads], DEVICE, or NULL; finite                  */
+    int64_t tokens;              /* rows of q                                           */
+    int32_t seqs;                /* 0 to 4096; seqs * heads < 2^18                      */
+    int32_t q_heads;             /* a multiple of the cache's heads, up to 128 to each  */
+    int32_t window;              /* 0: none                                             */
+    float scale;
+    float cap;                   /* 0: none                                             */
+} kmeans_kv_tokens_t;
+
+/* Bytes of device workspace that kmeans_kv_attend_tokens needs; 0 for arguments it
+ * refuses. Pure host computation; no pointer is looked at but whether starts is NULL. */
+size_t kmeans_kv_attend_tokens_workspace_bytes(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t);
+
+/*
+ * Attention of the new tokens over the cache. q and out are [tokens][q_heads][dim] of the
+ * cache's type, strides as of kmeans_kv_attend, lse fp32 [tokens][q_heads] (NULL: not
+ * wanted). Over the positions that a token sees:
+ *   out = sum_i exp(z_i - lse) v_i,   lse = log sum_i exp(z_i);
+ * none, or none whose z is above -infinity: out = 0, lse = -infinity. Tokens outside
+ * every sequence are left as they were; one in several sequences (bounds that descend)
+ * gets the result of either. A length is taken as at most table_pages * page; an entry
+ * of table outside [0, pages) is taken as some page of the cache, and those of pages that
+ * no token of the sequence sees are not read. out and lse overlap nothing that is read,
+ * and no two of their elements lie in one place.
+ * tokens * q_heads < 2^30, table_pages * page <= 2^30, |scale| <= 2.35e38, cap finite,
+ * 0 or so large that scale / cap is finite (KMEANS_EINVAL otherwise). Scores, their maximum
+ * and sum and the output are held in fp32; a weight enters the product with the values as
+ * one or two 16-bit numbers, off by at most half a step of the cache's type. The same
+ * inputs give the same bits. Asynchronous on `stream`.
+ */
+int kmeans_kv_attend_tokens(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t, const void *q,
+                            int64_t q_token, int64_t q_head, void *out, int64_t out_token,
+                            int64_t out_head, float *lse, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/*
+ * What the new tokens' attention gave to every cached position of a key-value head,
+ *   weights[b][h][i] = sum over its new tokens t and the query heads g of h of exp(z - lse[t][g]),
+ * from the lse that kmeans_kv_attend_tokens or kmeans_kv_attend returned (fp32
+ * [tokens][q_heads], contiguous; a row of -infinity counts for nothing). weights is fp32
+ * [seqs][heads][positions], contiguous in the last, other strides in elements; positions
+ * from `positions` on are left out. With add == 0 every element is written, with 1 the sums
+ * are added to what is there. No two rows overlap. Limits as of kmeans_kv_attend_tokens;
+ * positions up to 2^30. The same inputs give the same bits. Asynchronous on `stream`.
+ */
+int kmeans_kv_weigh(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t, const void *q,
+                    int64_t q_token, int64_t q_head, const float *lse, float *weights,
+                    int64_t weights_seq, int64_t weights_head, int64_t positions, int32_t add,
+                    void *stream);
+
+/* What kmeans_kv_evict keeps, of rows of [seqs][heads]. */
+typedef struct kmeans_kv_evict {
+    const int32_t *table;        /* [seqs][table_pages], DEVICE                         */
+    int64_t table_stride, table_pages;
+    const int32_t *lengths;      /* [seqs], DEVICE                                      */
+    const float *weights;        /* [seqs][heads][positions], DEVICE                    */
+    int64_t weights_seq, weights_head;
+    int64_t positions;           /* of a row of weights; those past it weigh 0          */
+    int32_t seqs;                /* 0 to 4096; seqs * heads < 2^18                      */
+    int32_t keep;                /* positions that are left, 1 to 2^30                  */
+    int32_t recent, first;       /* of them, the last and first of the sequence,        */
+                                 /* recent + first <= keep                              */
+    const int32_t *to;           /* [seqs][to_pages], DEVICE: pages that take what is   */
+    int64_t to_stride, to_pages; /* kept; NULL: the table's own                         */
+} kmeans_kv_evict_t;
+
+/*
+ * Brings every sequence of more than `keep` positions down to `keep`. Each head of it
+ * keeps the last `recent` and the first `first` and, of those between, the ones of the
+ * largest weight: ties go to the lowest position, a NaN is below all numbers. What is kept
+ * stays in its order: place j of the sequence takes the codes, key and value, of kept
+ * position kept[b][h][j] (int32 [seqs][heads][keep], contiguous; -1 past the last).
+ * lengths_out[b] = min(lengths[b], keep). weights_out ([seqs][heads][positions], strides of
+ * its own) gets the kept positions' weights, in order, and zeros after them. lengths_out may
+ * be lengths, weights_out may be weights with the same strides. A sequence of up to `keep`
+ * positions keeps them all (with `to`, its codes are copied). Heads keep different
+ * positions, so that a place stands for no one position of the sequence any more: slopes,
+ * windows and starts of later calls count places.
+ * Sequences share no page that is written to; pages of `to` are no pages of table, and have
+ * room for min(keep, table_pages * page) positions (KMEANS_EINVAL otherwise). What would go to
+ * an entry of `to`, or of table in its place, outside [0, pages) is left out. Asynchronous on
+ * `stream`.
+ */
+int kmeans_kv_evict(const kmeans_kv_t *kv, const kmeans_kv_evict_t *e, int32_t *kept,
+                    int32_t *lengths_out, float *weights_out, int64_t out_seq, int64_t out_head,
+                    void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -355,3 +355,6 @@ def ctl_reruns(ws: torch.Tensor) -> int:
 
 
 from .kv import KVCodes, kmeans_kv_attend, kmeans_kv_read, kmeans_kv_write  # noqa: E402,F401
+from .kv_serve import (kmeans_kv_attend_tokens,  # noqa: E402,F401
+                       kmeans_kv_attend_tokens_workspace_bytes, kmeans_kv_evict, kmeans_kv_rotate,
+                       kmeans_kv_weigh)
