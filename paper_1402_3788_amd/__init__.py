@@ -49,7 +49,8 @@ EXPORTED = ("kmeans_workspace_bytes", "kmeans_strerror", "kmeans_assign", "kmean
             "kmeans_centroid_workspace_bytes", "kmeans_centroid",
             "kmeans_diameter_workspace_bytes", "kmeans_diameter", "kmeans_run_noalloc",
             "kmeans_kv_write", "kmeans_kv_read", "kmeans_kv_attend_workspace_bytes",
-            "kmeans_kv_attend")
+            "kmeans_kv_attend", "kmeans_kv_rotate", "kmeans_kv_attend_tokens_workspace_bytes",
+            "kmeans_kv_attend_tokens", "kmeans_kv_weigh", "kmeans_kv_evict")
 
 
 class KmeansTiming(ctypes.Structure):
