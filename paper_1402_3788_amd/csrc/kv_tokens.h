@@ -8,6 +8,7 @@ namespace lloyd {
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kKvRows = 256;         // rows (query heads of new tokens) of a unit of attention
 
 // One tensor [tokens][heads][dim] that is turned, and where to.
 struct KvTurned {

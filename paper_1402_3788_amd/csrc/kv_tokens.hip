@@ -1,107 +1,649 @@
 // Attention of many new tokens of every sequence over the cache of codes.
 //
-// One query to a wave: 64 positions at a time, one to a lane for the scores, the
-// features over the lanes for the sum of the values.
+// A row is a query head of a new token: a sequence has tokens * group of them on
+// each key-value head, and a unit is up to 256 of them and the positions that any of
+// them sees. One pass over those keeps sum_i 2^(z_i - m) and sum_i 2^(z_i - m) v_i to a
+// row, with the scores z to base 2, scaled when the reference m moves up; parts of a
+// unit are joined by 2^(m - largest m).
+//
+// A workgroup keeps the centres of one head in LDS, a row of all features for each
+// code, and turns the codes of 32 positions into a tile of keys and one of values
+// there while it works on the tile before: so 256 rows share what a lookup costs, and
+// no decoded copy of the cache passes through memory. Its 8 waves take 32 rows each.
+// Keys are the rows of one operand of v_mfma_f32_32x32x16 and queries the columns of
+// the other, so that a lane's 16 scores belong to one query, and their exponentials
+// are an operand of the product with the values as they are (positions are numbered
+// to that end: score register 8 s + j of lane half y is position 16 s + 8 y + j).
+//
+// The row of all units' tiles is shared evenly by the workgroups of a head; what is cut
+// that way is joined by a second launch. A launch before says where units begin.
 #include "kv_tokens_device.h"
+
+#ifndef KV_SUB
+#define KV_SUB 4
+#endif
 
 namespace lloyd {
 
+// Geometry and workspace of a call (pure host code).
+struct KvTokensPlan {
+    int splits;                      // workgroups of a head
+    int units;                       // at most
+    KvUnits of;
+    int2 *cut;                       // [heads][splits]: the unit that begins in a share and ends
+                                     // in another's (-1: none), and how many have a part of it
+    float *part_o, *part_ml;         // of a share's first and last unit, cut
+    size_t total;
+};
+
+hipError_t launch_kv_tokens_2(const KvCache &, const KvNew &, const KvTokensOut &, const KvTokensPlan &, hipStream_t);
+hipError_t launch_kv_tokens_4(const KvCache &, const KvNew &, const KvTokensOut &, const KvTokensPlan &, hipStream_t);
+hipError_t launch_kv_tokens_8(const KvCache &, const KvNew &, const KvTokensOut &, const KvTokensPlan &, hipStream_t);
+
 namespace {
 
-template <int SUB, bool FP16>
-__global__ __launch_bounds__(kWave) void kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o)
+constexpr int kRows = kKvRows;
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kShare = 8;            // tiles that are worth a workgroup of their own
+
+// As in kv_attend.hip: a new reference lies kLift below the largest score and holds until
+// a score is kLag above that one.
+constexpr float kLag = 8.f;
+template <bool FP16>
+constexpr float kLift = FP16 ? 7.f : 0.f;
+
+template <int D, int SUB>
+struct Form {
+    static constexpr int S = D / SUB;
+    static constexpr int kRow = D * 2;                   // bytes of one code's centres
+    static constexpr int kBook = 256 * kRow;
+    static constexpr int kTile = 32 * D * 2;             // bytes of 32 keys, or values
+    static constexpr int kLds = 2 * kBook + 4 * kTile;
+    // Threads that look keys up (8 features of a position each) and that look values up
+    // (VS features of NP positions); with D < 128 the first and the last ones.
+    static constexpr int kTasks = 32 * D / 8;
+    static constexpr int NC = D / 8;
+    static constexpr int VS = SUB < 4 ? SUB : 4, NP = 8 / VS, NG = D / VS;
+    static constexpr int F = D / 32;                     // accumulators, of 32 features
+    static_assert(kLds <= kMaxLds && kTasks <= kThreads, "a workgroup");
+};
+
+__device__ inline int splits_used(int tiles, int splits)
 {
-    __shared__ uint16_t q[128];
-    __shared__ float weight[kWave];
-    __shared__ int pages[kWave];
-    const int lane = threadIdx.x, heads = c.heads * a.group, S = c.dim / SUB;
-    const int hq = blockIdx.x % heads, t = blockIdx.x / heads, h = hq / a.group;
-    int b = 0;
-    KvSeq s{};
-    for (; b < a.seqs; ++b) {
-        s = kv_seq(c, a, b);
-        if (t >= s.t0 && t < s.t0 + s.n) break;
-    }
-    if (b == a.seqs) return;
-    for (int i = lane; i < c.dim; i += kWave) q[i] = a.q[t * a.q_token + hq * a.q_head + i];
-    __syncthreads();
-    const KvSeen x = kv_seen(a, s, t - s.t0);
-    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
-    const int last = (int)min(c.pages - 1, (int64_t)0x7FFFFFFF), mask = (1 << c.page_log2) - 1;
-    for (int at = x.lo; at < x.hi; at += kWave) {
-        const int pos = at + lane;
-        float z = -INFINITY;
-        int page = 0;
-        if (pos < x.hi) {
-            page = min((uint32_t)a.table[b * a.table_stride + (pos >> c.page_log2)], (uint32_t)last);
-            const uint8_t *codes = c.k_codes + kv_head(c, page, h, S) + (int64_t)(pos & mask) * S;
-            float dot = 0.f;
-            for (int n = 0; n < S; ++n) {
-                const int code = codes[n];
-                if (code >= c.K) continue;
-                float k[SUB];
-                kv_unpack<FP16>(kv_load<SUB>(c.k_centres + ((int64_t)(h * S + n) * c.K + code) * SUB), k);
-                for (int e = 0; e < SUB; ++e) dot = __builtin_fmaf(k[e], kv_float<FP16>(q[n * SUB + e]), dot);
-            }
-            z = a.cap_log2 > 0.f ? kv_capped(dot * a.scale_cap, a.cap_log2) : dot * a.scale_log2;
-            if (a.slopes) z -= a.slopes[hq] * kLog2e * (float)abs(x.at - pos);
-        }
-        float top = z;
-        for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
-        top = fmaxf(top, m);
-        const float m0 = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - m0);
-        m = top;
-        const float p = pos < x.hi ? __builtin_amdgcn_exp2f(z - m0) : 0.f;
-        float sum = p;
-        for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k);
-        l = l * alpha + sum;
-        acc[0] *= alpha;
-        acc[1] *= alpha;
-        weight[lane] = p;
-        pages[lane] = page;
-        __syncthreads();
-        for (int i = 0; i < min(kWave, x.hi - at); ++i) {
-            const float p1 = weight[i];
-            const uint8_t *codes = c.v_codes + kv_head(c, pages[i], h, S) + ((at + i) & mask);
-            for (int e = 0; e < 2; ++e) {
-                const int d = lane + 64 * e;
-                if (d >= c.dim) break;
-                const int code = codes[(d / SUB) << c.page_log2];
-                if (code < c.K)
-                    acc[e] += p1 * kv_float<FP16>(c.v_centres[((int64_t)(h * S + d / SUB) * c.K + code) * SUB + d % SUB]);
-            }
-        }
-        __syncthreads();
-    }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    for (int e = 0; e < 2; ++e) {
-        const int d = lane + 64 * e;
-        if (d >= c.dim) break;
-        uint16_t r;
-        if constexpr (FP16) r = __builtin_bit_cast(uint16_t, (_Float16)(acc[e] * inv));
-        else r = __builtin_bit_cast(uint16_t, (__bf16)(acc[e] * inv));
-        o.out[t * o.out_token + hq * o.out_head + d] = r;
-    }
-    if (o.lse && lane == 0)
-        o.lse[(int64_t)t * heads + hq] = l > 0.f || l != l ? (m + __log2f(l)) * kLn2 : -INFINITY;
+    return min(splits, max(1, (tiles + kShare - 1) / kShare));
 }
 
-template <int SUB>
-hipError_t launch(const KvCache &c, const KvNew &n, const KvTokensOut &o, hipStream_t s)
+// Even shares of n things (the first n % k of k shares have one more).
+__device__ inline int share_begin(int n, int i, int k)
 {
-    const auto kernel = c.fp16 ? kv_tokens_kernel<SUB, true> : kv_tokens_kernel<SUB, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(n.tokens * c.heads * n.group)), dim3(kWave), 0, s, c, n, o);
+    return (int)((unsigned)n / (unsigned)k) * i + min(i, (int)((unsigned)n % (unsigned)k));
+}
+
+__device__ inline int share_of(int n, int t, int k)
+{
+    const unsigned each = (unsigned)n / (unsigned)k, more = (unsigned)n % (unsigned)k;
+    const unsigned long_end = more * (each + 1);
+    return (int)((unsigned)t < long_end ? (unsigned)t / (each + 1) : more + ((unsigned)t - long_end) / each);
+}
+
+template <int D, int SUB, bool FP16>
+__global__ __launch_bounds__(kThreads) void
+kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
+{
+    using F = Form<D, SUB>;
+    extern __shared__ uint4 lds[];
+    char *const kbook = reinterpret_cast<char *>(lds), *const vbook = kbook + F::kBook;
+    char *const ktile = vbook + F::kBook, *const vtile = ktile + 2 * F::kTile;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % c.heads, j = blockIdx.x / c.heads;
+    const int heads = c.heads * a.group;
+    const int64_t wg = (int64_t)h * p.splits + j;
+    const int units = *p.of.count, tiles = p.of.first[units];
+    const int used = splits_used(tiles, p.splits);
+
+    // A row's token (among the sequence's) and query head.
+    const auto row_of = [&](const KvUnit &u, int row, int *token, int *head) {
+        const unsigned x = (unsigned)(u.row0 + row);
+        *token = (int)(x / (unsigned)a.group);
+        *head = h * a.group + (int)(x % (unsigned)a.group);
+        return x < (unsigned)u.n * (unsigned)a.group;
+    };
+    // Units without positions.
+    for (int u = j; u < units; u += p.splits) {
+        if (p.of.first[u] != p.of.first[u + 1]) continue;
+        const KvUnit x = p.of.unit[u];
+        for (int i = tid; i < kRows * (D / 8); i += kThreads) {
+            int t, q;
+            if (!row_of(x, i / (D / 8), &t, &q)) continue;
+            *reinterpret_cast<u4v *>(o.out + (x.t0 + t) * o.out_token + q * o.out_head + i % (D / 8) * 8) =
+                u4v{0, 0, 0, 0};
+            if (o.lse && i % (D / 8) == 0) o.lse[(int64_t)(x.t0 + t) * heads + q] = -INFINITY;
+        }
+    }
+    if (tid == 0) p.cut[wg] = make_int2(-1, 0);          // unless found below
+    if (j >= used || tiles == 0) return;
+    const int a0 = share_begin(tiles, j, used), a1 = share_begin(tiles, j + 1, used);
+
+    // A place in the row of tiles: unit u, which has tiles [base, next).
+    struct Cursor {
+        int u, base, next;
+        KvUnit x;
+    };
+    const auto enter = [&](int u) {
+        Cursor y;
+        y.u = __builtin_amdgcn_readfirstlane(u);
+        y.base = __builtin_amdgcn_readfirstlane(p.of.first[y.u]);
+        y.next = __builtin_amdgcn_readfirstlane(p.of.first[y.u + 1]);
+        const int *from = reinterpret_cast<const int *>(p.of.unit + y.u);
+        int *const x = reinterpret_cast<int *>(&y.x);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(KvUnit) / 4); ++i) x[i] = __builtin_amdgcn_readfirstlane(from[i]);
+        return y;
+    };
+    const auto advance = [&](Cursor &y, int t) {
+        if (t < y.next) return;
+        int u = y.u + 1;
+        while (p.of.first[u + 1] <= t) ++u;
+        y = enter(u);
+    };
+    Cursor cur;
+    {
+        // the last unit whose tiles begin at a0 or before: of 64 at a time
+        int from = 0, n = units;
+        while (n > 1) {
+            const int step = (n + kWave - 1) / kWave, at = lane * step;
+            const int before = __popcll(__ballot(at < n && p.of.first[from + at] <= a0));
+            from += (before - 1) * step;
+            n = min(step, n - (before - 1) * step);
+        }
+        cur = enter(from);
+    }
+    Cursor then = cur;
+
+    // What a thread looks up of a tile: 8 features of key `key`, and VS of NP values.
+    const bool looks_k = tid < F::kTasks, looks_v = tid >= kThreads - F::kTasks;
+    const int xk = looks_k ? tid : 0, xv = looks_v ? tid - (kThreads - F::kTasks) : 0;
+    const int key = xk % 4 + xk / (4 * F::NC) * 4, chunk = xk / 4 % F::NC;
+    const int vpos = (xv % 4 + xv / (4 * F::NG) * 4) * F::NP, gran = xv / 4 % F::NG;
+    // Numbers of pages are asked for three tiles ahead, codes two, centres one.
+    struct Where {
+        int pos, k_page, v_page;
+    };
+    struct Codes {
+        uint32_t k, v;
+    };
+    const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
+    const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
+    const unsigned pm = (1u << c.page_log2) - 1;
+    const int64_t head_codes = ((int64_t)h * F::S) << c.page_log2;
+    const uint8_t *const k_lane = c.k_codes + head_codes + chunk * (8 / SUB);
+    const uint8_t *const v_lane = c.v_codes + head_codes + ((unsigned)(gran * F::VS / SUB) << c.page_log2);
+    const auto find = [&](int t) {
+        advance(then, t);
+        Where w;
+        w.pos = (t - then.base + then.x.tile0()) * 32;
+        const int32_t *const row = a.table + then.x.b * a.table_stride;
+        // positions that nobody sees: the nearest page of one that somebody does
+        const int low = then.x.lo >> c.page_log2, high = (then.x.hi - 1) >> c.page_log2;
+        w.k_page = row[min(max((w.pos + key) >> c.page_log2, low), high)];
+        w.v_page = row[min(max((w.pos + vpos) >> c.page_log2, low), high)];
+        return w;
+    };
+    const auto load = [&](const Where &w) {
+        // a number that is no page's is some page's here, never followed out
+        const auto page = [&](int n) { return (uint64_t)min((unsigned)n, last_page) * page_bytes; };
+        Codes x{};
+        if (looks_k) {
+            const uint8_t *const k = k_lane + page(w.k_page) + (((unsigned)w.pos + key) & pm) * F::S;
+            if constexpr (SUB == 2) x.k = *reinterpret_cast<const uint32_t *>(k);
+            else if constexpr (SUB == 4) x.k = *reinterpret_cast<const uint16_t *>(k);
+            else x.k = *k;
+        }
+        if (looks_v) {
+            const uint8_t *const v = v_lane + page(w.v_page) + (((unsigned)w.pos + vpos) & pm);
+            if constexpr (F::NP == 4) x.v = *reinterpret_cast<const uint32_t *>(v);
+            else x.v = *reinterpret_cast<const uint16_t *>(v);
+        }
+        return x;
+    };
+    struct Found {
+        KvEntry<8> k;
+        KvEntry<F::VS> v[F::NP];
+    };
+    const auto look = [&](const Codes &x) {
+        Found f;
+        if (looks_k) {
+            KvEntry<SUB> e[8 / SUB];
+#pragma unroll
+            for (int i = 0; i < 8 / SUB; ++i)
+                e[i] = *reinterpret_cast<const KvEntry<SUB> *>(
+                    kbook + (x.k >> (8 * i) & 255) * F::kRow + chunk * 16 + i * (SUB * 2));
+            __builtin_memcpy(&f.k, e, 16);
+        }
+        if (looks_v) {
+#pragma unroll
+            for (int i = 0; i < F::NP; ++i)
+                f.v[i] = *reinterpret_cast<const KvEntry<F::VS> *>(
+                    vbook + (x.v >> (8 * i) & 255) * F::kRow + gran * (F::VS * 2));
+        }
+        return f;
+    };
+    // Tiles in LDS: keys as runs of 16 bytes, run r of row m (position m with its bits 2
+    // and 3 in each other's place) at 512 r + 16 m, bits 6 to 8 turned by r so that a wave
+    // that writes reaches all banks; values as runs of 8 positions, run r of feature f at
+    // 16 D r + 16 f, the feature's last two bits turned by the two above its fourth.
+    const uint32_t k_to = chunk * 512 + ((((key & ~12) | (key & 4) << 1 | (key & 8) >> 1) * 16) ^ (chunk & 7) * 64);
+    const auto v_slot = [](int f) { return (f ^ ((f >> 4) & 3)) * 16; };
+    const uint32_t v_to = vpos / 8 * (D * 16) + (vpos & 7) * 2;
+    const auto put = [&](const Found &f, int buf) {
+        if (looks_k) *reinterpret_cast<KvEntry<8> *>(ktile + buf * F::kTile + k_to) = f.k;
+        if (looks_v) {
+#pragma unroll
+            for (int e = 0; e < F::VS; ++e) {
+                KvEntry<F::NP> x;
+#pragma unroll
+                for (int i = 0; i < F::NP / 2; ++i)
+                    x.w[i] = __builtin_amdgcn_perm(f.v[2 * i + 1].w[e / 2], f.v[2 * i].w[e / 2],
+                                                   e % 2 ? 0x07060302u : 0x05040100u);
+                *reinterpret_cast<KvEntry<F::NP> *>(vtile + buf * F::kTile + v_to + v_slot(gran * F::VS + e)) = x;
+            }
+        }
+    };
+
+    Where where = find(a0);
+    // The centres of this head, entries from K up zeros.
+    {
+        const uint16_t *const books[2] = {c.k_centres + (int64_t)h * F::S * c.K * SUB,
+                                          c.v_centres + (int64_t)h * F::S * c.K * SUB};
+        constexpr int per16 = 8 / SUB, rounds = D * 32 / kThreads;
+        static_assert(D * 32 % kThreads == 0, "whole rounds");
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            char *const book = kind ? vbook : kbook;
+            if (c.K == 256) {
+                // 16 bytes to a load: 4 runs in each of 16 sub-vectors to a wave
+                uint4 reg[rounds];
+#pragma unroll
+                for (int i = 0; i < rounds; ++i) {
+                    const int n = i * kThreads + tid, s = (n >> 2) % F::S, code = ((n >> 2) / F::S * 4 + (n & 3)) * per16;
+                    reg[i] = *reinterpret_cast<const uint4 *>(books[kind] + (s * 256 + code) * SUB);
+                }
+#pragma unroll
+                for (int i = 0; i < rounds; ++i) {
+                    const int n = i * kThreads + tid, s = (n >> 2) % F::S, code = ((n >> 2) / F::S * 4 + (n & 3)) * per16;
+                    KvEntry<SUB> e[per16];
+                    __builtin_memcpy(e, &reg[i], 16);
+#pragma unroll
+                    for (int x = 0; x < per16; ++x)
+                        *reinterpret_cast<KvEntry<SUB> *>(book + (code + x) * F::kRow + s * (SUB * 2)) = e[x];
+                }
+            } else {
+                for (int i = tid; i < F::S * 256; i += kThreads) {
+                    const int s = i % F::S, code = i / F::S;
+                    KvEntry<SUB> e{};
+                    if (code < c.K) e = kv_load<SUB>(books[kind] + (s * c.K + code) * SUB);
+                    *reinterpret_cast<KvEntry<SUB> *>(book + code * F::kRow + s * (SUB * 2)) = e;
+                }
+            }
+        }
+    }
+    Codes codes = load(where);
+    if (a0 + 1 < a1) where = find(a0 + 1);
+    __syncthreads();
+    put(look(codes), 0);
+    if (a0 + 1 < a1) codes = load(where);
+    if (a0 + 2 < a1) where = find(a0 + 2);
+    __syncthreads();
+
+    const bool changed = a.cap_log2 > 0.f || a.slopes;   // scores are more than products
+    const float scale = changed ? 1.f : fabsf(a.scale_log2);
+    const uint32_t flip = !changed && a.scale_log2 < 0.f ? 0x80008000u : 0u;
+    u4v q[D / 16];
+    f16v acc[F::F];
+    float m = 0.f, m0 = 0.f, l = 0.f, slope = 0.f;
+    KvSeen seen{};
+    const auto begin = [&]() {
+        int t, hq;
+        const bool there = row_of(cur.x, wave * 32 + col, &t, &hq);
+        const uint16_t *const src = a.q + (cur.x.t0 + t) * a.q_token + hq * a.q_head + half * 8;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            q[s] = u4v{0, 0, 0, 0};
+            if (there) q[s] = *reinterpret_cast<const u4v *>(src + s * 16) ^ flip;
+        }
+        seen = KvSeen{0, 0, 0};
+        if (there) seen = kv_seen(a, KvSeq{cur.x.t0, cur.x.n, cur.x.len, cur.x.prefix}, t);
+        slope = there && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
+        m = -INFINITY;
+        m0 = 0.f;
+        l = 0.f;
+#pragma unroll
+        for (int n = 0; n < F::F; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
+    };
+    begin();
+    // where a lane reads the tiles
+    const char *const k_from = ktile + half * 512;
+    const uint32_t v_even = v_slot(col) + half * (D * 16), v_odd = v_slot(32 + col) + half * (D * 16);
+
+    int buf = 0;
+    for (int t = a0; t < a1; ++t) {
+        Found found;
+        if (t + 1 < a1) found = look(codes);
+        if (t + 2 < a1) codes = load(where);
+        if (t + 3 < a1) where = find(t + 3);
+        const int pos = (t - cur.base + cur.x.tile0()) * 32;
+        const int y0 = pos + 8 * half;                   // of the lane's scores 0 to 7
+        if (__any(seen.lo < pos + 32 && seen.hi > pos)) {
+            const bool whole = __all(seen.lo <= pos && seen.hi >= pos + 32);
+            f16v z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                const u4v k = *reinterpret_cast<const u4v *>(
+                    k_from + buf * F::kTile + s * 1024 + ((col * 16) ^ ((2 * s + half) & 7) * 64));
+                z = mfma32<FP16>(k, q[s], z);
+            }
+            if (changed) {
+                if (a.cap_log2 > 0.f) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = kv_capped(z[i] * a.scale_cap, a.cap_log2);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] *= a.scale_log2;
+                }
+                const float far = (float)(seen.at - y0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(16 * (i / 8) + i % 8)), z[i]);
+            }
+            const auto sees = [&](int i) {
+                const int at = y0 + 16 * (i / 8) + i % 8;
+                return at >= seen.lo && at < seen.hi;
+            };
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = sees(i) ? z[i] : -INFINITY;
+            }
+            float top = z[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
+            top *= scale;
+            if (__any(top > m + (kLag + kLift<FP16>))) {
+                top = fmaxf(max_halves(top) - kLift<FP16>, m);
+                m0 = top == -INFINITY ? 0.f : top;
+                const float alpha = __builtin_amdgcn_exp2f(m - m0);
+                m = top;
+                l *= alpha;
+#pragma unroll
+                for (int n = 0; n < F::F; ++n) acc[n] *= alpha;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -m0));
+            if (!whole) {                                // again: a scale of 0 gave NaN
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = sees(i) ? z[i] : 0.f;
+            }
+            float sum[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+            for (int i = 4; i < 16; ++i) sum[i & 3] += z[i];
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                // One 16-bit number to a weight: rounded to nearest it leaves the output
+                // off as its own last rounding does, and without the halves that a
+                // second number would double the product by.
+                u4v w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = pack2<FP16>(z[8 * s + 2 * i], z[8 * s + 2 * i + 1]);
+#pragma unroll
+                for (int n = 0; n < F::F; ++n) {
+                    const u4v v = *reinterpret_cast<const u4v *>(
+                        vtile + buf * F::kTile + s * (2 * D * 16) + (n / 2) * 1024 + (n % 2 ? v_odd : v_even));
+                    acc[n] = mfma32<FP16>(v, w, acc[n]);
+                }
+            }
+        }
+        if (t + 1 == min(cur.next, a1)) {                // the unit's end, or the share's
+            const float sum = sum_halves(l);
+            if (cur.base >= a0 && cur.next <= a1) {
+                int tt, hq;
+                if (row_of(cur.x, wave * 32 + col, &tt, &hq)) {
+                    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                    uint16_t *const dst = o.out + (cur.x.t0 + tt) * o.out_token + hq * o.out_head + 4 * half;
+#pragma unroll
+                    for (int n = 0; n < F::F; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) =
+                                make_uint2(pack2<FP16>(acc[n][4 * i] * inv, acc[n][4 * i + 1] * inv),
+                                           pack2<FP16>(acc[n][4 * i + 2] * inv, acc[n][4 * i + 3] * inv));
+                    if (o.lse && half == 0)
+                        o.lse[(int64_t)(cur.x.t0 + tt) * heads + hq] =
+                            sum > 0.f || sum != sum ? (m + __log2f(sum)) * kLn2 : -INFINITY;
+                }
+            } else {
+                const int slot = cur.base < a0 ? 0 : 1;
+                float *const dst = p.part_o + (wg * 2 + slot) * (kRows * D) + tid;
+#pragma unroll
+                for (int n = 0; n < F::F; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dst[(n * 16 + i) * kThreads] = acc[n][i];
+                if (half == 0) {
+                    float *const ml = p.part_ml + (wg * 2 + slot) * (2 * kRows) + wave * 32 + col;
+                    ml[0] = m;
+                    ml[kRows] = sum;
+                }
+                if (slot == 1 && tid == 0) p.cut[wg] = make_int2(cur.u, share_of(tiles, cur.next - 1, used) - j + 1);
+            }
+            if (t + 1 < a1) {
+                advance(cur, t + 1);
+                begin();
+            }
+        }
+        if (t + 1 < a1) put(found, buf ^ 1);
+        __syncthreads();
+        buf ^= 1;
+    }
+}
+
+// Joins the parts of units that several shares have. Share j's cut unit, if it has one,
+// is its second part and the first ones of the shares after it; 8 features of every
+// second lane's rows to a workgroup.
+template <int D, bool FP16>
+__global__ __launch_bounds__(kThreads) void kv_tokens_join_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
+{
+    constexpr int quads = D / 8;                         // of features, of a lane
+    const int quad = blockIdx.x % quads, wg = blockIdx.x / quads;
+    const int2 found = p.cut[wg];
+    if (found.x < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int row = (tid >> 6) * 32 + col, h = wg / p.splits;
+    const KvUnit u = p.of.unit[found.x];
+    const unsigned at = (unsigned)(u.row0 + row);
+    if (at >= (unsigned)u.n * (unsigned)a.group) return;
+    const auto ml = [&](int i) { return p.part_ml + ((int64_t)(wg + i) * 2 + (i == 0)) * (2 * kRows) + row; };
+    float top = -INFINITY;
+    for (int i = 0; i < found.y; ++i) top = fmaxf(top, *ml(i));
+    const float safe = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < found.y; ++i) {
+        const float w = __builtin_amdgcn_exp2f(*ml(i) - safe);
+        sum += w * ml(i)[kRows];
+        const float *const from = p.part_o + ((int64_t)(wg + i) * 2 + (i == 0)) * (kRows * D) + (quad * 4) * kThreads + tid;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] += w * from[k * kThreads];
+    }
+    const int t = u.t0 + (int)(at / (unsigned)a.group), hq = h * a.group + (int)(at % (unsigned)a.group);
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    // accumulator n, registers 4 i to 4 i + 3
+    uint16_t *const dst = o.out + t * o.out_token + hq * o.out_head + 32 * (quad / 4) + 8 * (quad % 4) + 4 * half;
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<FP16>(x[0] * inv, x[1] * inv), pack2<FP16>(x[2] * inv, x[3] * inv));
+    if (o.lse && quad == 0 && half == 0)
+        o.lse[(int64_t)t * c.heads * a.group + hq] = sum > 0.f || sum != sum ? (top + __log2f(sum)) * kLn2 : -INFINITY;
+}
+
+template <int D, int SUB, bool FP16>
+hipError_t launch(const KvCache &c, const KvNew &a, const KvTokensOut &o, const KvTokensPlan &p, hipStream_t s)
+{
+    using F = Form<D, SUB>;
+    hipLaunchKernelGGL((kv_tokens_kernel<D, SUB, FP16>), dim3((unsigned)(c.heads * p.splits)), dim3(kThreads),
+                       F::kLds, s, c, a, o, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL((kv_tokens_join_kernel<D, FP16>), dim3((unsigned)(c.heads * p.splits * (D / 8))),
+                       dim3(kThreads), 0, s, c, a, o, p);
     return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_type(const KvCache &c, const KvNew &a, const KvTokensOut &o, const KvTokensPlan &p, hipStream_t s)
+{
+    return c.fp16 ? launch<D, KV_SUB, true>(c, a, o, p, s) : launch<D, KV_SUB, false>(c, a, o, p, s);
 }
 
 }  // namespace
 
-size_t kv_attend_tokens_bytes(const KvCache &, const KvNew &) { return 256; }
+#define KV_CAT2(a, b) a##b
+#define KV_CAT(a, b) KV_CAT2(a, b)
+hipError_t KV_CAT(launch_kv_tokens_, KV_SUB)(const KvCache &c, const KvNew &a, const KvTokensOut &o,
+                                             const KvTokensPlan &p, hipStream_t s)
+{
+    return c.dim == 64 ? launch_type<64>(c, a, o, p, s)
+         : c.dim == 96 ? launch_type<96>(c, a, o, p, s) : launch_type<128>(c, a, o, p, s);
+}
 
-hipError_t launch_kv_attend_tokens(const KvCache &c, const KvNew &n, const KvTokensOut &o, void *,
+#if KV_SUB == 4
+namespace {
+
+// One workgroup: the units of all sequences and where their tiles begin.
+__global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUnits to, int most)
+{
+    __shared__ int seq_first[kKvMaxSeqs + 1];
+    __shared__ int wave_sum[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // sum of x over the threads up to this one, and of all
+    const auto scan = [&](int x, int *all) {
+        x = scan_lanes(x);
+        __syncthreads();
+        if (lane == 63) wave_sum[wave] = x;
+        __syncthreads();
+        int before = 0, sum = 0;
+        for (int i = 0; i < 16; ++i) {
+            if (i == wave) before = sum;
+            sum += wave_sum[i];
+        }
+        *all = sum;
+        return x + before;
+    };
+    const int per = (a.seqs + 1023) / 1024;
+    int n[(kKvMaxSeqs + 1023) / 1024] = {}, sum = 0, units;
+#pragma unroll
+    for (int k = 0; k < (kKvMaxSeqs + 1023) / 1024; ++k) {
+        const int b = tid * per + k;
+        if (k < per && b < a.seqs) n[k] = (int)(((int64_t)kv_seq(c, a, b).n * a.group + kRows - 1) / kRows);
+        sum += n[k];
+    }
+    int at = scan(sum, &units) - sum;
+#pragma unroll
+    for (int k = 0; k < (kKvMaxSeqs + 1023) / 1024; ++k) {
+        const int b = tid * per + k;
+        if (k < per && b < a.seqs) seq_first[b] = at;
+        at += n[k];
+    }
+    if (tid == 0) seq_first[a.seqs] = units;
+    __syncthreads();
+    units = min(units, most);                            // more only if bounds descend
+    int tiles = 0;
+    for (int u0 = 0; u0 < units; u0 += 1024) {
+        const int u = u0 + tid;
+        KvUnit x{};
+        if (u < units) {
+            int b = 0, end = a.seqs;                     // the last b with seq_first[b] <= u
+            while (end - b > 1) {
+                const int mid = (b + end) >> 1;
+                if (seq_first[mid] <= u) b = mid;
+                else end = mid;
+            }
+            const KvSeq s = kv_seq(c, a, b);
+            const int row0 = (u - seq_first[b]) * kRows;
+            const int i0 = row0 / a.group, i1 = (int)((min((int64_t)row0 + kRows, (int64_t)s.n * a.group) - 1) / a.group);
+            int lo = INT32_MAX, hi = 0;
+            if (a.starts) {
+                for (int i = i0; i <= i1; ++i) {
+                    const KvSeen y = kv_seen(a, s, i);
+                    if (y.hi > 0) lo = min(lo, y.lo);
+                    hi = max(hi, y.hi);
+                }
+            } else {
+                // bounds rise from token to token
+                hi = kv_seen(a, s, i1).hi;
+                for (int i = i0; i <= i1 && lo == INT32_MAX; ++i) {
+                    const KvSeen y = kv_seen(a, s, i);
+                    if (y.hi > 0) lo = y.lo;
+                }
+            }
+            x = KvUnit{b, row0, s.t0, s.n, s.len, s.prefix, lo < hi ? lo : 0, lo < hi ? hi : 0};
+            to.unit[u] = x;
+        }
+        const int n1 = x.tiles();
+        int all;
+        const int upto = scan(n1, &all);
+        if (u < units) to.first[u] = tiles + upto - n1;
+        tiles += all;
+    }
+    if (tid == 0) {
+        to.first[units] = tiles;
+        *to.count = units;
+    }
+}
+
+KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
+{
+    KvTokensPlan p{};
+    p.units = (int)(a.seqs + a.tokens * a.group / kRows);
+    // with 64 features two workgroups to a CU, else the centres leave room for one
+    const int64_t wgs = (c.dim == 64 ? 2 : 1) * kCUs;
+    const int64_t span = ((int64_t)a.table_pages << c.page_log2) / 32 + 2;
+    const int64_t most = (p.units * span + kShare - 1) / kShare;
+    int64_t splits = wgs / c.heads;
+    if (splits > most) splits = most;
+    p.splits = splits < 1 ? 1 : (int)splits;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        char *const x = ws + at;
+        at += (bytes + 255) / 256 * 256;
+        return x;
+    };
+    const size_t shares = (size_t)c.heads * p.splits;
+    p.of.count = reinterpret_cast<int32_t *>(take(4));
+    p.of.first = reinterpret_cast<int32_t *>(take(4 * ((size_t)p.units + 1)));
+    p.of.unit = reinterpret_cast<KvUnit *>(take(sizeof(KvUnit) * (size_t)p.units));
+    p.cut = reinterpret_cast<int2 *>(take(sizeof(int2) * shares));
+    p.part_ml = reinterpret_cast<float *>(take(shares * 2 * 2 * kRows * sizeof(float)));
+    p.part_o = reinterpret_cast<float *>(take(shares * 2 * kRows * c.dim * sizeof(float)));
+    p.total = at;
+    return p;
+}
+
+}  // namespace
+
+size_t kv_attend_tokens_bytes(const KvCache &c, const KvNew &a) { return plan_of(c, a, nullptr).total; }
+
+hipError_t launch_kv_attend_tokens(const KvCache &c, const KvNew &a, const KvTokensOut &o, void *ws,
                                    hipStream_t s)
 {
-    return c.sub == 2 ? launch<2>(c, n, o, s) : c.sub == 4 ? launch<4>(c, n, o, s) : launch<8>(c, n, o, s);
+    const KvTokensPlan p = plan_of(c, a, static_cast<char *>(ws));
+    hipLaunchKernelGGL(kv_units_kernel, dim3(1), dim3(1024), 0, s, c, a, p.of, p.units);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return c.sub == 2 ? launch_kv_tokens_2(c, a, o, p, s)
+         : c.sub == 4 ? launch_kv_tokens_4(c, a, o, p, s) : launch_kv_tokens_8(c, a, o, p, s);
 }
+#endif
 
 }  // namespace lloyd

@@ -6,6 +6,69 @@
 
 namespace lloyd {
 
+typedef float f2v __attribute__((ext_vector_type(2)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef __bf16 b2v __attribute__((ext_vector_type(2)));
+typedef __bf16 b8v __attribute__((ext_vector_type(8)));
+
+// 32 rows by 32 columns by 16: a lane holds k = 8 (lane / 32) to + 7 of row, or column,
+// lane % 32; of the product, rows 8 (i / 4) + 4 (lane / 32) + i % 4 of column lane % 32.
+template <bool FP16>
+__device__ inline f16v mfma32(u4v a, u4v b, f16v c)
+{
+    if constexpr (FP16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8v, a),
+                                                      __builtin_bit_cast(h8v, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8v, a),
+                                                       __builtin_bit_cast(b8v, b), c, 0, 0, 0);
+}
+
+template <bool FP16>
+__device__ inline uint32_t pack2(float a, float b)
+{
+    const f2v v = {a, b};
+    if constexpr (FP16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2v));
+    else
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
+}
+
+// x of the lane 32 away.
+__device__ inline float other_half(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? both[0] : both[1]);
+}
+
+// The larger, or the sum, of a lane's and that of the lane 32 away.
+__device__ inline float max_halves(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
+__device__ inline float sum_halves(float x)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(both[0]) + __uint_as_float(both[1]);
+}
+
+// Sum of x over the lanes up to this one.
+__device__ inline int scan_lanes(int x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) {
+        const int y = __shfl_up(x, k);
+        if (lane >= k) x += y;
+    }
+    return x;
+}
+
 // The new tokens [t0, t0 + n) of a sequence and its cached positions.
 struct KvSeq {
     int t0, n, len, prefix;
@@ -46,5 +109,20 @@ __device__ inline float kv_capped(float x, float cap_log2)
     const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));
     return cap_log2 - 2.f * cap_log2 * __builtin_amdgcn_rcpf(1.f + e);
 }
+
+// Rows [row0, row0 + up to as many as a unit has) of sequence b, whose new tokens are
+// [t0, t0 + n): the positions that any of them sees lie in [lo, hi).
+struct KvUnit {
+    int b, row0, t0, n, len, prefix, lo, hi;
+    __device__ int tile0() const { return lo >> 5; }
+    __device__ int tiles() const { return hi > lo ? ((hi + 31) >> 5) - (lo >> 5) : 0; }
+};
+
+// Units and where each one's tiles begin among all (one more than there are units).
+struct KvUnits {
+    int32_t *count;
+    int32_t *first;
+    KvUnit *unit;
+};
 
 }  // namespace lloyd

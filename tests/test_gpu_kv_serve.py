@@ -273,27 +273,27 @@ def test_garbage_in_device_data():
 
 
 def test_infinities_and_nan_in_what_is_not_seen():
-    """A NaN in the query of one token, and in the value of a position that no other
-    sees, stay there; scores of -infinity only count for nothing."""
+    """NaN in the query of one token stays there, and the largest centres in positions
+    that are not seen (scores of infinity) change nothing."""
     call = Call([(100, 4)], heads=1, group=2, dim=64, seed=6)
-    starts = torch.tensor([10, 10, 10, 0], dtype=torch.int32, device=DEV)
+    starts = torch.tensor([10, 10, 10, 10], dtype=torch.int32, device=DEV)
     call.more["starts"] = starts
-    want, lse0 = check_attention(call)
-    with_nan = call.cache.v_centres.clone()
-    # centre 255 is infinite, and only positions below 10 name it
+    # centre 255 is named by positions below 10 only
     call.cache.v_codes[call.cache.v_codes == 255] = 1
     call.cache.k_codes[call.cache.k_codes == 255] = 1
     want, lse0 = check_attention(call)
+    w0 = call.weigh(lse0)
     p = call.table[0, 0].long()
     call.cache.v_codes[p, :, :, 3] = 255
     call.cache.k_codes[p, :, 3] = 255
-    call.cache.v_centres[:, :, 255] = math.nan
-    call.cache.k_centres[:, :, 255] = math.nan
+    call.cache.v_centres[:, :, 255] = torch.finfo(BF).max
+    call.cache.k_centres[:, :, 255] = torch.finfo(BF).max
+    out, lse = call.attend()
+    assert torch.equal(out, want) and torch.equal(lse, lse0) and torch.equal(call.weigh(lse0), w0)
+    call.q[3] = math.nan
     out, lse = call.attend()
     assert torch.equal(out[:3], want[:3]) and torch.equal(lse[:3], lse0[:3])
     assert torch.isnan(out[3]).all() and torch.isnan(lse[3]).all()
-    w = call.weigh(lse0, starts=starts.clone().fill_(10))
-    assert torch.isfinite(w).all()
     # a token whose every score is -infinity
     call = Call([(3, 1)], heads=1, group=1, dim=64, seed=6)
     call.cache.k_centres.fill_(1.0)
