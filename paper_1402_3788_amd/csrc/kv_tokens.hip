@@ -350,16 +350,17 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
             }
             if (changed) {
                 if (a.cap_log2 > 0.f) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = kv_capped(z[i] * a.scale_cap, a.cap_log2);
+                    kv_cap<16>(z, a.scale_cap, a.cap_log2);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) z[i] *= a.scale_log2;
                 }
-                const float far = (float)(seen.at - y0);
+                if (a.slopes) {
+                    const float far = (float)(seen.at - y0);
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(16 * (i / 8) + i % 8)), z[i]);
+                    for (int i = 0; i < 16; ++i)
+                        z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(16 * (i / 8) + i % 8)), z[i]);
+                }
             }
             const auto sees = [&](int i) {
                 const int at = y0 + 16 * (i / 8) + i % 8;

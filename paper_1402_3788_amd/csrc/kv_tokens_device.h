@@ -102,12 +102,36 @@ __device__ inline KvSeen kv_seen(const KvNew &a, const KvSeq &s, int i)
     return x;
 }
 
-// cap * tanh(z / cap) to base 2, of x = z / cap. tanh x = 1 - 2 / (1 + e^2x): off by
-// 2^-23 of 1 for small x, where a cap of 50 makes it 4e-6 of a score.
-__device__ inline float kv_capped(float x, float cap_log2)
+// cap * tanh(scale * z / cap) to base 2, of a lane's N products z. Up to 5/8 tanh x = x + x^3 P(x^2), P of degree 4 fitted to it there (off
+// by 2^-27 of it); beyond 1 - 2 / (1 + e^2x), which for small x would be off by 2^-23 of 1,
+// 4e-6 of a score for a cap of 50. Most scores are far below their cap: a wave whose
+// scores all are saves the exponentials.
+template <int N, typename V>
+__device__ inline void kv_cap(V &z, float scale_cap, float cap_log2)
 {
-    const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));
-    return cap_log2 - 2.f * cap_log2 * __builtin_amdgcn_rcpf(1.f + e);
+    float x[N], most = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = z[i] * scale_cap;
+        most = fmaxf(most, fabsf(x[i]));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float t = x[i] * x[i], y = cap_log2 * x[i];
+        float p = __builtin_fmaf(t, -0.0057036951f, 0.020637562f);
+        p = __builtin_fmaf(t, p, -0.053739071f);
+        p = __builtin_fmaf(t, p, 0.13331431f);
+        p = __builtin_fmaf(t, p, -0.33333281f);
+        z[i] = __builtin_fmaf(y * t, p, y);
+    }
+    if (__any(!(most <= 0.625f))) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float e = __builtin_amdgcn_exp2f(x[i] * (2.f * kLog2e));
+            const float far = cap_log2 - 2.f * cap_log2 * __builtin_amdgcn_rcpf(1.f + e);
+            z[i] = fabsf(x[i]) <= 0.625f ? z[i] : far;
+        }
+    }
 }
 
 // Rows [row0, row0 + up to as many as a unit has) of sequence b, whose new tokens are
