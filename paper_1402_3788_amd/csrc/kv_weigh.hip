@@ -13,8 +13,9 @@ namespace lloyd {
 
 namespace {
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 12;
 constexpr int kThreads = kWaves * kWave;
+constexpr int kSeqs = 1024;          // sequences that are kept in LDS
 
 
 template <int D, int SUB>
@@ -33,13 +34,14 @@ __device__ inline void load_codes(uint32_t (&dst)[(N + 3) / 4], const uint8_t *s
 }
 
 template <int D, int SUB, bool FP16>
-__global__ __launch_bounds__(kThreads, 4) void kv_weigh_kernel(KvCache c, KvNew a, KvWeigh w, int splits)
+__global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, KvWeigh w, int splits)
 {
     using F = Form<D, SUB>;
     extern __shared__ uint4 lds[];
     char *const book = reinterpret_cast<char *>(lds);
-    int *const first = reinterpret_cast<int *>(book + F::kBook);         // [seqs + 1]
-    __shared__ int wave_sum[kWaves];
+    int64_t *const first = reinterpret_cast<int64_t *>(book + F::kBook); // [seqs + 1]
+    __shared__ int64_t wave_sum[kWaves];
+    __shared__ KvSeq seqs[kSeqs];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % c.heads, j = blockIdx.x / c.heads;
@@ -50,8 +52,8 @@ __global__ __launch_bounds__(kThreads, 4) void kv_weigh_kernel(KvCache c, KvNew 
     const uint16_t *const from = c.k_centres + (int64_t)h * F::S * c.K * SUB;
     if (c.K == 256) {
 #pragma unroll
-        for (int i = 0; i < D * 32 / kThreads; ++i)
-            __builtin_amdgcn_global_load_lds(
+        for (int i = 0; i < (D * 32 + kThreads - 1) / kThreads; ++i)
+            if (i * kThreads + (wave << 6) < D * 32) __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void *)(reinterpret_cast<const char *>(from) + (i * kThreads + tid) * 16),
                 (__attribute__((address_space(3))) void *)(book + (i * kThreads + (wave << 6)) * 16), 16, 0, 0);
     } else {
@@ -61,46 +63,60 @@ __global__ __launch_bounds__(kThreads, 4) void kv_weigh_kernel(KvCache c, KvNew 
             reinterpret_cast<KvEntry<SUB> *>(book)[i] = e;
         }
     }
-    // A sequence's tiles, and where each one's begin among all. One without new tokens has
-    // none, and a window leaves out those before it.
+    // A sequence's tiles, and where the work on each one's begins in all of it. One without
+    // new tokens has none, and a window leaves out those before it. A tile's work is that
+    // of looking its keys up, some two blocks of rows, and that of each block.
     const int span = (int)min(w.positions, (int64_t)a.table_pages << c.page_log2);
     const auto tile0_of = [&](const KvSeq &s) {
         return a.window ? max(s.len - s.n - a.window + 1, 0) >> 5 : 0;
     };
-    const auto tiles_of = [&](int b) {
-        const KvSeq s = kv_seq(c, a, b);
+    const auto tiles_of = [&](const KvSeq &s) {
         return s.n ? max(((min(s.len, span) + 31) >> 5) - tile0_of(s), 0) : 0;
     };
-    int tiles;
+    const auto work_of = [&](const KvSeq &s) { return 2 + (s.n * a.group + 31) / 32; };
+    int64_t all;
     {
         const int per = (a.seqs + kThreads - 1) / kThreads;
-        int sum = 0;
-        for (int k = 0; k < per; ++k)
-            if (tid * per + k < a.seqs) sum += tiles_of(tid * per + k);
-        const int upto = scan_lanes(sum);
+        int64_t sum = 0;
+        for (int k = 0; k < per; ++k) {
+            const int b = tid * per + k;
+            if (b >= a.seqs) break;
+            const KvSeq s = kv_seq(c, a, b);
+            sum += (int64_t)tiles_of(s) * work_of(s);
+            if (b < kSeqs) seqs[b] = s;
+        }
+        int64_t upto = sum;
+#pragma unroll
+        for (int k = 1; k < kWave; k *= 2) {
+            const int64_t y = __shfl_up(upto, k);
+            if (lane >= k) upto += y;
+        }
         if (lane == 63) wave_sum[wave] = upto;
         __syncthreads();
-        int at = upto - sum;
-        tiles = 0;
+        int64_t at = upto - sum;
+        all = 0;
         for (int i = 0; i < kWaves; ++i) {
             if (i < wave) at += wave_sum[i];
-            tiles += wave_sum[i];
+            all += wave_sum[i];
         }
         for (int k = 0; k < per; ++k) {
             const int b = tid * per + k;
             if (b >= a.seqs) break;
+            const KvSeq s = per == 1 && b < kSeqs ? seqs[b] : kv_seq(c, a, b);
             first[b] = at;
-            at += tiles_of(b);
+            at += (int64_t)tiles_of(s) * work_of(s);
         }
-        if (tid == 0) first[a.seqs] = tiles;
+        if (tid == 0) first[a.seqs] = all;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the centres
     __syncthreads();
+    const auto seq_of = [&](int b) { return b < kSeqs ? seqs[b] : kv_seq(c, a, b); };
     // What no tile covers.
     if (!w.add) {
         for (int b = j; b < a.seqs; b += splits) {
             float *const to = w.weights + b * w.weights_seq + wrow;
-            const int n = first[b + 1] - first[b], tile0 = n ? tile0_of(kv_seq(c, a, b)) : 0;
+            const KvSeq s = seq_of(b);
+            const int n = tiles_of(s), tile0 = n ? tile0_of(s) : 0;
             for (int i = tid; i < tile0 * 32; i += kThreads) to[i] = 0.f;
             for (int64_t i = (int64_t)(tile0 + n) * 32 + tid; i < w.positions; i += kThreads) to[i] = 0.f;
         }
@@ -110,107 +126,172 @@ __global__ __launch_bounds__(kThreads, 4) void kv_weigh_kernel(KvCache c, KvNew 
     const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
     const unsigned pm = (1u << c.page_log2) - 1;
     const uint8_t *const lane_codes = c.k_codes + (((int64_t)h * F::S) << c.page_log2) + half * F::H;
-    const bool changed = a.cap_log2 > 0.f || a.slopes;
-    const int step = kWaves * splits;
-
-    // Tile t: its sequence, and a lane's position and page.
-    struct Where {
-        int b, pos, page;
+    // A wave's share: the tiles whose work begins in an even share of all.
+    const int64_t shares = (int64_t)kWaves * splits, share = (int64_t)j * kWaves + wave;
+    const int64_t work0 = all / shares * share + min(share, all % shares);
+    const int64_t work1 = all / shares * (share + 1) + min(share + 1, all % shares);
+    // A place among the tiles: tile t of a sequence's n.
+    struct Place {
+        int b, t, n, work;
+        int64_t first;
+        KvSeq s;
     };
-    const auto find = [&](int t, int b) {
-        Where x;
-        // the last sequence whose tiles begin at t or before: of 64 after b at a time
+    const auto enter = [&](int b) {
+        Place x;
+        x.b = __builtin_amdgcn_readfirstlane(b);
+        const KvSeq s = seq_of(x.b);
+        x.s.t0 = __builtin_amdgcn_readfirstlane(s.t0);
+        x.s.n = __builtin_amdgcn_readfirstlane(s.n);
+        x.s.len = __builtin_amdgcn_readfirstlane(s.len);
+        x.s.prefix = __builtin_amdgcn_readfirstlane(s.prefix);
+        x.first = first[x.b];
+        x.t = 0;
+        x.n = tiles_of(x.s);
+        x.work = work_of(x.s);
+        return x;
+    };
+    // Whether there is a tile at x that is the wave's, or one in a sequence after it.
+    const auto settle = [&](Place &x) {
+        while (x.t >= x.n) {
+            // the next sequence that has tiles: of 64 at a time
+            int b = x.b + 1;
+            for (;;) {
+                const int n = b + lane;
+                const uint64_t some = __ballot(n < a.seqs && first[min(n, a.seqs)] < first[min(n + 1, a.seqs)]);
+                if (some) {
+                    b += __builtin_ctzll(some);
+                    break;
+                }
+                b += kWave;
+                if (b >= a.seqs) return false;
+            }
+            x = enter(b);
+        }
+        return x.first + (int64_t)x.t * x.work < work1;
+    };
+    // A lane's page of the tile at x.
+    struct Where {
+        int pos, page;
+    };
+    const auto find = [&](const Place &x) {
+        Where y;
+        y.pos = (x.t + tile0_of(x.s)) * 32;
+        y.page = a.table[x.b * a.table_stride + (min(y.pos + col, x.s.len - 1) >> c.page_log2)];
+        return y;
+    };
+    const auto load = [&](uint32_t (&codes)[(F::H + 3) / 4], const Where &y) {
+        load_codes<F::H>(codes, lane_codes + (uint64_t)min((unsigned)y.page, last_page) * page_bytes +
+                                    (((unsigned)y.pos + col) & pm) * F::S);
+    };
+    if (work0 >= work1) return;
+    Place now;
+    {
+        // the sequence in whose tiles work0 lies: the last that begins at it or before
+        int b = 0;
         for (;;) {
             const int n = b + 1 + lane;
-            const int more = __popcll(__ballot(n < a.seqs && first[min(n, a.seqs)] <= t));
+            const int more = __popcll(__ballot(n < a.seqs && first[min(n, a.seqs)] <= work0));
             b += more;
             if (more < kWave) break;
         }
-        x.b = __builtin_amdgcn_readfirstlane(b);
-        const KvSeq s = kv_seq(c, a, x.b);
-        x.pos = (t - __builtin_amdgcn_readfirstlane(first[x.b]) + tile0_of(s)) * 32;
-        x.page = a.table[x.b * a.table_stride + (min(x.pos + col, s.len - 1) >> c.page_log2)];
-        return x;
-    };
-    const auto load = [&](uint32_t (&codes)[(F::H + 3) / 4], const Where &x) {
-        load_codes<F::H>(codes, lane_codes + (uint64_t)min((unsigned)x.page, last_page) * page_bytes +
-                                    (((unsigned)x.pos + col) & pm) * F::S);
-    };
-    int t = j * kWaves + wave;
-    if (t >= tiles) return;
-    Where now = find(t, 0), next = now;
+        now = enter(b);
+        now.t = (int)((work0 - now.first + now.work - 1) / now.work);
+    }
+    if (!settle(now)) return;
+    Place next = now;
+    Where at = find(now), ahead = at;
     uint32_t codes[(F::H + 3) / 4];
-    load(codes, now);
-    if (t + step < tiles) next = find(t + step, now.b);
-    for (; t < tiles; t += step) {
+    load(codes, at);
+    ++next.t;
+    bool more = settle(next);
+    if (more) ahead = find(next);
+    u4v q[D / 16];
+    KvSeen seen{0, 0, 0};
+    float base = 0.f, slope = 0.f;
+    // The 32 rows from r0 on.
+    const auto begin = [&](const KvSeq &s, int r0) {
+        const int row = r0 + col, tok = (int)((unsigned)row / (unsigned)a.group);
+        const int hq = h * a.group + (int)((unsigned)row % (unsigned)a.group);
+        const bool there = row < s.n * a.group;
+        seen = KvSeen{0, 0, 0};
+        base = INFINITY;
+        slope = 0.f;
+        if (there) {
+            seen = kv_seen(a, s, tok);
+            base = w.lse[(int64_t)(s.t0 + tok) * heads + hq] * kLog2e;
+            if (base == -INFINITY) seen.lo = seen.hi = 0;
+            if (a.slopes) slope = a.slopes[hq] * kLog2e;
+        }
+        const uint16_t *const src = a.q + (s.t0 + tok) * a.q_token + hq * a.q_head + half * (D / 2);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            q[i] = u4v{0, 0, 0, 0};
+            if (there) q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
+        }
+    };
+    int loaded = -1;                                     // the sequence whose only rows are in q
+    for (;;) {
         // the keys: a lane has features [half D / 2, + D / 2) of position col
         u4v k[D / 16];
         {
             KvEntry<SUB> e[F::H];
-            const char *const at = book + half * (F::H * 512 * SUB);
+            const char *const from = book + half * (F::H * 512 * SUB);
 #pragma unroll
             for (int n = 0; n < F::H; ++n)
                 e[n] = *reinterpret_cast<const KvEntry<SUB> *>(
-                    at + n * (512 * SUB) + (codes[n / 4] >> (8 * (n % 4)) & 255) * (2 * SUB));
+                    from + n * (512 * SUB) + (codes[n / 4] >> (8 * (n % 4)) & 255) * (2 * SUB));
             __builtin_memcpy(k, e, sizeof(k));
         }
-        const Where x = now;
-        now = next;
-        if (t + step < tiles) load(codes, now);
-        if (t + 2 * step < tiles) next = find(t + 2 * step, now.b);
-
-        const KvSeq s = kv_seq(c, a, x.b);
+        const int b = now.b, pos = at.pos;
+        const KvSeq s = now.s;
+        const bool last = !more;
+        if (more) {
+            load(codes, ahead);
+            at = ahead;
+            now = next;
+            ++next.t;
+            more = settle(next);
+            if (more) ahead = find(next);
+        }
         const int rows = s.n * a.group;
         float sum[16] = {};
         for (int r0 = 0; r0 < rows; r0 += 32) {
-            const int row = r0 + col;
-            const int tok = (int)((unsigned)row / (unsigned)a.group), hq = h * a.group + (int)((unsigned)row % (unsigned)a.group);
-            KvSeen seen{0, 0, 0};
-            float lse = INFINITY;
-            if (row < rows) {
-                seen = kv_seen(a, s, tok);
-                lse = w.lse[(int64_t)(s.t0 + tok) * heads + hq];
-                if (lse == -INFINITY) seen.lo = seen.hi = 0;
-            }
-            if (!__any(seen.lo < x.pos + 32 && seen.hi > x.pos)) continue;
-            const bool whole = __all(seen.lo <= x.pos && seen.hi >= x.pos + 32);
-            u4v q[D / 16];
-            const uint16_t *const src = a.q + (s.t0 + tok) * a.q_token + hq * a.q_head + half * (D / 2);
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                q[i] = u4v{0, 0, 0, 0};
-                if (row < rows) q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
-            }
+            if (loaded != b) begin(s, r0);
+            loaded = rows <= 32 ? b : -1;
+            if (!__any(seen.lo < pos + 32 && seen.hi > pos)) continue;
+            const bool whole = __all(seen.lo <= pos && seen.hi >= pos + 32);
             f16v z;
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) z = mfma32<FP16>(k[i], q[i], z);
-            const int y0 = x.pos + 4 * half;             // score i is position y0 + 8 (i / 4) + i % 4
+            const int y0 = pos + 4 * half;               // score i is position y0 + 8 (i / 4) + i % 4
             float scale = a.scale_log2;
-            if (changed) {
-                if (a.cap_log2 > 0.f) {
-                    kv_cap<16>(z, a.scale_cap, a.cap_log2);
-                    scale = 1.f;
-                }
-                if (a.slopes && row < rows) {
-                    const float slope = a.slopes[hq] * kLog2e, far = (float)(seen.at - y0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale);
-                    scale = 1.f;
-                }
+            if (a.cap_log2 > 0.f) {
+                kv_cap<16>(z, a.scale_cap, a.cap_log2);
+                scale = 1.f;
             }
-            const float base = lse * kLog2e;
+            if (a.slopes) {
+                const float far = (float)(seen.at - y0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -base));
-                const int at = y0 + 8 * (i / 4) + i % 4;
-                sum[i] += whole || (at >= seen.lo && at < seen.hi) ? e : 0.f;
+                for (int i = 0; i < 16; ++i)
+                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale);
+                scale = 1.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -base));
+            if (whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] += z[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int p = y0 + 8 * (i / 4) + i % 4;
+                    sum[i] += p >= seen.lo && p < seen.hi ? z[i] : 0.f;
+                }
             }
         }
-        // Over the lanes of a half, halving what each holds: in the end the even lanes have
-        // position 16 bit 4 + 8 bit 3 + 2 bit 2 + bit 1 of theirs (of a sum's place i).
+        // Over the lanes of a half, halving what each holds.
         int place = 0;
 #pragma unroll
         for (int n = 8, m = 16; n >= 1; n /= 2, m /= 2) {
@@ -223,11 +304,12 @@ __global__ __launch_bounds__(kThreads, 4) void kv_weigh_kernel(KvCache c, KvNew 
             place += up ? n : 0;
         }
         sum[0] += __shfl_xor(sum[0], 1);
-        const int pos = x.pos + 4 * half + 8 * (place / 4) + place % 4;
-        if (!(lane & 1) && pos < w.positions) {
-            float *const to = w.weights + x.b * w.weights_seq + wrow + pos;
+        const int p = pos + 4 * half + 8 * (place / 4) + place % 4;
+        if (!(lane & 1) && p < w.positions) {
+            float *const to = w.weights + b * w.weights_seq + wrow + p;
             *to = w.add ? *to + sum[0] : sum[0];
         }
+        if (last) break;
     }
 }
 
@@ -237,10 +319,10 @@ hipError_t launch(const KvCache &c, const KvNew &a, const KvWeigh &w, hipStream_
     const auto kernel = c.fp16 ? kv_weigh_kernel<D, SUB, true> : kv_weigh_kernel<D, SUB, false>;
     const int64_t span = (int64_t)a.table_pages << c.page_log2;
     const int64_t tiles = a.seqs * (((span < w.positions ? span : w.positions) + 31) / 32);
-    int64_t splits = 2 * kCUs / c.heads;                 // two workgroups to a CU
+    int64_t splits = kCUs / c.heads;                     // one workgroup to a CU
     if (splits > (tiles + kWaves - 1) / kWaves) splits = (tiles + kWaves - 1) / kWaves;
     if (splits < 1) splits = 1;
-    const size_t lds = Form<D, SUB>::kBook + (a.seqs + 1) * sizeof(int);
+    const size_t lds = Form<D, SUB>::kBook + (a.seqs + 1) * sizeof(int64_t);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(c.heads * splits)), dim3(kThreads), lds, s, c, a, w,
                        (int)splits);
     return hipGetLastError();
