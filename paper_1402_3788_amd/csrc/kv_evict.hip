@@ -12,10 +12,11 @@ namespace lloyd {
 
 namespace {
 
-constexpr int kPick = 1024;          // threads that pick
+constexpr int kPick = 512;           // threads that pick
 constexpr int kPickWaves = kPick / kWave;
-constexpr int kMove = 256;           // threads that move, and places of a tile
-constexpr int kParts = 4;            // shares of a token's codes, each moved on its own
+constexpr int kMove = 256;           // threads that move
+constexpr int kSpan = 768;           // positions between a tile's first and last that LDS holds
+constexpr int kParts = 4;            // shares of a value's codes, in place each moved on its own
 
 // Weights as whole numbers of the same order; NaN below all.
 __device__ inline uint32_t order_of(float w)
@@ -30,12 +31,123 @@ __device__ inline int length_of(const KvCache &c, const KvEvict &e, int b)
     return min(max(e.lengths[b], 0), e.table_pages << c.page_log2);
 }
 
+// How many of a row's weights a thread holds; longer rows are read again in each pass.
+constexpr int kHeld = 32;
+
+struct PickLds {
+    int counts[2048];
+    int wave_sum[kPickWaves], wave_eq[kPickWaves];
+    int found[2];
+};
+
+// The positions [from, to) of a row, wave after wave and in each 64 at a time: f(i,
+// whether i is in the row, the order of its weight).
+template <int HELD, typename G, typename F>
+__device__ inline void each_of(int from, int to, const uint32_t (&held)[HELD ? HELD : 1], const G &order_at, const F &f)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int each = ((to - from + kPick - 1) / kPick) * kWave, w0 = from + wave * each;
+    if constexpr (HELD) {
+#pragma unroll
+        for (int r = 0; r < HELD; ++r) {
+            const int i = w0 + r * kWave + lane;
+            if (r * kWave < each && w0 + r * kWave < to) f(i, i < to, held[r]);
+        }
+    } else {
+        for (int i = w0 + lane; i - lane < min(w0 + each, to); i += kWave) {
+            const bool in = i < min(w0 + each, to);
+            f(i, in, in ? order_at(i) : 0u);
+        }
+    }
+}
+
+// Writes the `left` (at least 1) positions of [from, to) with the largest weights, in order.
+template <int HELD, typename G>
+__device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *out, const G &order_at)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t held[HELD ? HELD : 1];
+    if constexpr (HELD) {
+        const int each = ((to - from + kPick - 1) / kPick) * kWave, i0 = from + wave * each + lane;
+#pragma unroll
+        for (int r = 0; r < HELD; ++r)
+            held[r] = r * kWave < each && i0 + r * kWave < to ? order_at(i0 + r * kWave) : 0u;
+    }
+    uint32_t last = 0, mask = 0;                         // the bits known of the last one
+#pragma unroll 1
+    for (int digit = 0; digit < 3; ++digit) {
+        // 11, 11 and 10 bits: the first has an octave's four quarters apart, so that
+        // lanes seldom count the same value
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
+        const uint32_t bins = digit == 2 ? 1023u : 2047u;
+        reinterpret_cast<int4 *>(lds.counts)[tid] = make_int4(0, 0, 0, 0);
+        __syncthreads();
+        each_of<HELD>(from, to, held, order_at, [&](int, bool in, uint32_t u) {
+            if (in && (u & mask) == last) atomicAdd(&lds.counts[u >> shift & bins], 1);
+        });
+        __syncthreads();
+        // thread t has bins 4 t to 4 t + 3; how many lie above those
+        const int4 n4 = reinterpret_cast<const int4 *>(lds.counts)[tid];
+        const int n[4] = {n4.x, n4.y, n4.z, n4.w}, own = n4.x + n4.y + n4.z + n4.w;
+        int above = own;
+#pragma unroll
+        for (int k = 1; k < kWave; k *= 2) {
+            const int x = __shfl_down(above, k);
+            if (lane + k < kWave) above += x;
+        }
+        if (lane == 0) lds.wave_sum[wave] = above;
+        __syncthreads();
+        above -= own;
+#pragma unroll
+        for (int k = 1; k < kPickWaves; ++k) above += k > wave ? lds.wave_sum[k] : 0;
+        if (above < left && above + own >= left) {
+#pragma unroll
+            for (int k = 3; k >= 0; --k) {
+                if (above < left && above + n[k] >= left) {
+                    lds.found[0] = 4 * tid + k;
+                    lds.found[1] = left - above;
+                }
+                above += n[k];
+            }
+        }
+        __syncthreads();
+        last |= (uint32_t)lds.found[0] << shift;
+        mask |= bins << shift;
+        left = lds.found[1];
+    }
+    // All above `last`, and the first `left` of those alike.
+    int gt = 0, eq = 0;
+    each_of<HELD>(from, to, held, order_at, [&](int, bool in, uint32_t u) {
+        gt += __popcll(__ballot(in && u > last));
+        eq += __popcll(__ballot(in && u == last));
+    });
+    if (lane == 0) {
+        lds.wave_sum[wave] = gt;
+        lds.wave_eq[wave] = eq;
+    }
+    __syncthreads();
+    int alike = 0, at = 0;
+#pragma unroll
+    for (int k = 0; k < kPickWaves - 1; ++k) {
+        at += k < wave ? lds.wave_sum[k] : 0;
+        alike += k < wave ? lds.wave_eq[k] : 0;
+    }
+    at += min(alike, left);
+    const uint64_t below = (1ull << lane) - 1;
+    each_of<HELD>(from, to, held, order_at, [&](int i, bool in, uint32_t u) {
+        const uint64_t same = __ballot(in && u == last);
+        const bool take = in && (u > last || (u == last && alike + __popcll(same & below) < left));
+        const uint64_t taken = __ballot(take);
+        if (take) out[at + __popcll(taken & below)] = i;
+        at += __popcll(taken);
+        alike += __popcll(same);
+    });
+}
+
 __global__ __launch_bounds__(kPick) void kv_pick_kernel(KvCache c, KvEvict e)
 {
-    __shared__ int counts[256];
-    __shared__ int found[2];
-    __shared__ int wave_gt[kPickWaves], wave_eq[kPickWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ PickLds lds;
+    const int tid = threadIdx.x;
     const int b = blockIdx.x / c.heads, h = blockIdx.x % c.heads;
     const int n = length_of(c, e, b);
     int32_t *const kept = e.kept + ((int64_t)b * c.heads + h) * e.keep;
@@ -44,191 +156,223 @@ __global__ __launch_bounds__(kPick) void kv_pick_kernel(KvCache c, KvEvict e)
         return;
     }
     const float *const w = e.weights + b * e.weights_seq + h * e.weights_head;
-    const int from = e.first, to = n - e.recent;         // picked among these
     const auto order_at = [&](int i) { return i < e.positions ? order_of(w[i]) : order_of(0.f); };
-    int left = e.keep - e.first - e.recent;              // still to be picked
-    uint32_t last = 0, mask = 0;                         // the bits known of the last one
+    const int from = e.first, to = n - e.recent, left = e.keep - e.first - e.recent;
     for (int j = tid; j < e.first; j += kPick) kept[j] = j;
     for (int j = tid; j < e.recent; j += kPick) kept[e.keep - e.recent + j] = to + j;
     if (left == 0) return;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) counts[tid] = 0;
-        __syncthreads();
-        for (int i = from + tid; i < to; i += kPick) {
-            const uint32_t u = order_at(i);
-            if ((u & mask) == last) atomicAdd(&counts[u >> shift & 255], 1);
-        }
-        __syncthreads();
-        if (wave == 0) {
-            // bins 4 lane to 4 lane + 3, and how many lie in the lanes above
-            const int4 n4 = reinterpret_cast<const int4 *>(counts)[lane];
-            int above = n4.x + n4.y + n4.z + n4.w;
-            const int own = above;
-            for (int k = 1; k < kWave; k *= 2) {
-                const int x = __shfl_down(above, k);
-                if (lane + k < kWave) above += x;
-            }
-            above -= own;
-            const int bins[4] = {n4.x, n4.y, n4.z, n4.w};
-            for (int k = 3; k >= 0; --k) {
-                if (above < left && above + bins[k] >= left) {
-                    found[0] = 4 * lane + k;
-                    found[1] = left - above;
-                }
-                above += bins[k];
-            }
-        }
-        __syncthreads();
-        last |= (uint32_t)found[0] << shift;
-        mask |= 255u << shift;
-        left = found[1];
-        __syncthreads();
-    }
-    // All above `last`, and the first `left` of those alike.
-    const int each = ((to - from + kPick - 1) / kPick) * kWave;
-    const int w0 = min(from + wave * each, to), w1 = min(w0 + each, to);
-    int gt = 0, eq = 0;
-    for (int i = w0; i < w1; i += kWave) {
-        const uint32_t u = i + lane < w1 ? order_at(i + lane) : 0;
-        gt += __popcll(__ballot(i + lane < w1 && u > last));
-        eq += __popcll(__ballot(i + lane < w1 && u == last));
-    }
-    if (lane == 0) {
-        wave_gt[wave] = gt;
-        wave_eq[wave] = eq;
-    }
-    __syncthreads();
-    int alike = 0, at = e.first;
-    for (int k = 0; k < wave; ++k) {
-        at += wave_gt[k];
-        alike += wave_eq[k];
-    }
-    at += min(alike, left);
-    for (int i = w0; i < w1; i += kWave) {
-        const uint32_t u = i + lane < w1 ? order_at(i + lane) : 0;
-        const uint64_t below = (1ull << lane) - 1;
-        const uint64_t same = __ballot(i + lane < w1 && u == last);
-        const bool take = i + lane < w1 &&
-                          (u > last || (u == last && alike + __popcll(same & below) < left));
-        const uint64_t taken = __ballot(take);
-        if (take) kept[at + __popcll(taken & below)] = i + lane;
-        at += __popcll(taken);
-        alike += __popcll(same);
-    }
+    if (to - from <= kHeld / 8 * kPick)
+        pick<kHeld / 8>(lds, from, to, left, kept + e.first, order_at);
+    else if (to - from <= kHeld / 2 * kPick)
+        pick<kHeld / 2>(lds, from, to, left, kept + e.first, order_at);
+    else if (to - from <= kHeld * kPick)
+        pick<kHeld>(lds, from, to, left, kept + e.first, order_at);
+    else
+        pick<0>(lds, from, to, left, kept + e.first, order_at);
 }
 
-// Part 0: the weights; 1 to kParts: keys' codes; then the values'. A workgroup takes
-// every step-th tile of its part, in place all of them.
+// What a workgroup moves: weights, keys' codes or values' codes of a head of a sequence; out
+// of place one tile of places, in place all tiles one after the other (of a share of the
+// sub-vectors, for values). Each thread asks for all that it moves of a tile before it
+// waits: the way from a kept position over the table to the codes is three trips to
+// memory, and bytes under way are what the card's rate takes.
+struct MoveGrid {
+    int weights, keys, values;       // workgroups of a row
+    __host__ __device__ int all() const { return weights + keys + values; }
+};
+
 template <int S>
-__global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, int tiles, int step)
+constexpr int kRun = S % 16 == 0 ? 16 : S % 8 == 0 ? 8 : 4;      // bytes of a key's codes to a thread
+constexpr int kHold = 8;             // weights, or runs, of a thread
+constexpr int kFloats = kMove * kHold;                           // places of a tile of weights
+template <int S>
+constexpr int kKeys = kMove * kHold / (S / kRun<S>);             // of keys
+constexpr int kValues = 256;                                     // of values
+
+template <int N>
+struct BytesOf {
+    typedef uint32_t type __attribute__((ext_vector_type(N / 4)));
+};
+template <>
+struct BytesOf<4> {
+    typedef uint32_t type;
+};
+template <int N>
+using Bytes = typename BytesOf<N>::type;
+
+template <int S, bool IN_PLACE>
+__global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, MoveGrid grid)
 {
-    constexpr int words = (S / 4 + kParts - 1) / kParts; // of a key's codes, to a part
-    constexpr int subs = (S + kParts - 1) / kParts;      // of a value's
-    constexpr int runs = (kMove / 8 * subs + kMove - 1) / kMove;
-    __shared__ int32_t s_page[kMove];
-    __shared__ int32_t s_off[kMove];
-    const int tid = threadIdx.x;
-    const int part = blockIdx.x % (2 * kParts + 1), bh = blockIdx.x / (2 * kParts + 1) % (c.heads * e.seqs);
-    const int tile0 = blockIdx.x / (2 * kParts + 1) / (c.heads * e.seqs);
-    const int b = bh / c.heads, h = bh % c.heads;
+    const int tid = threadIdx.x, rows = c.heads * e.seqs;
+    const int bh = blockIdx.x % rows, b = bh / c.heads, h = bh % c.heads;
+    int part = blockIdx.x / rows;
     const int m = min(length_of(c, e, b), e.keep);
     const int32_t *const kept = e.kept + (int64_t)bh * e.keep;
-    if (part == 0) {
-        const float *const in = e.weights + b * e.weights_seq + h * e.weights_head;
-        float *const out = e.weights_out + b * e.out_seq + h * e.out_head;
-        for (int tile = tile0; tile < tiles; tile += step) {
-            const int64_t j = (int64_t)tile * kMove + tid;
-            float x = 0.f;
-            if (j < m) {
-                const int i = kept[j];
-                if (i < e.positions) x = in[i];
-            }
-            __syncthreads();
-            if (j < e.positions) out[j] = x;
-        }
-        if (tile0 == 0 && h == 0 && tid == 0) e.lengths_out[b] = m;
-        return;
-    }
-    if (m == 0 || (e.in_place && kept[m - 1] == m - 1)) return;      // all where they are
     const uint32_t last = (uint32_t)min(c.pages - 1, (int64_t)0x7FFFFFFF);
     const int mask = (1 << c.page_log2) - 1;
     const int32_t *const table = e.table + b * e.table_stride, *const to = e.to + b * e.to_stride;
-    for (int tile = tile0; tile < tiles && tile * kMove < m; tile += step) {
-        const int j0 = tile * kMove;
-        __syncthreads();
-        if (j0 + tid < m) {
-            const int i = kept[j0 + tid];
-            s_page[tid] = (int)min((uint32_t)table[i >> c.page_log2], last);
-            s_off[tid] = i & mask;
+    if (part < grid.weights) {
+        const float *const in = e.weights + b * e.weights_seq + h * e.weights_head;
+        float *const out = e.weights_out + b * e.out_seq + h * e.out_head;
+        if (part == 0 && h == 0 && tid == 0) e.lengths_out[b] = m;
+        for (int64_t j0 = (int64_t)part * kFloats + tid; j0 - tid < e.positions; j0 += (int64_t)grid.weights * kFloats) {
+            int i[kHold];
+            float x[kHold];
+#pragma unroll
+            for (int k = 0; k < kHold; ++k) i[k] = j0 + k * kMove < m ? kept[j0 + k * kMove] : INT32_MAX;
+#pragma unroll
+            for (int k = 0; k < kHold; ++k) x[k] = i[k] < e.positions ? in[i[k]] : 0.f;
+            if (IN_PLACE) __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kHold; ++k)
+                if (j0 + k * kMove < e.positions) out[j0 + k * kMove] = x[k];
         }
-        __syncthreads();
-        if (part <= kParts) {
-            const int w0 = (part - 1) * words;
-            const int j = j0 + tid;
-            uint32_t x[words];
-            if (j < m) {
-                const uint8_t *src = c.k_codes + kv_head(c, s_page[tid], h, S) + (int64_t)s_off[tid] * S;
+        return;
+    }
+    if (m == 0 || (IN_PLACE && kept[m - 1] == m - 1)) return;        // all where they are
+    part -= grid.weights;
+    if (part < grid.keys) {
+        constexpr int runs = S / kRun<S>;
+        for (int j0 = part * kKeys<S>; j0 < m; j0 += grid.keys * kKeys<S>) {
+            int i[kHold], goal[kHold], page[kHold];
+            Bytes<kRun<S>> x[kHold];
 #pragma unroll
-                for (int k = 0; k < words; ++k)
-                    if (w0 + k < S / 4) x[k] = reinterpret_cast<const uint32_t *>(src)[w0 + k];
+            for (int k = 0; k < kHold; ++k) {
+                const int j = min(j0 + (k * kMove + tid) / runs, m - 1);
+                i[k] = kept[j];
+                goal[k] = to[j >> c.page_log2];
             }
-            if (e.in_place) __syncthreads();
-            if (j < m) {
-                const uint32_t page = (uint32_t)to[j >> c.page_log2];
-                if (page <= last) {
-                    uint8_t *dst = c.k_codes + kv_head(c, page, h, S) + (int64_t)(j & mask) * S;
 #pragma unroll
-                    for (int k = 0; k < words; ++k)
-                        if (w0 + k < S / 4) reinterpret_cast<uint32_t *>(dst)[w0 + k] = x[k];
+            for (int k = 0; k < kHold; ++k) page[k] = table[i[k] >> c.page_log2];
+#pragma unroll
+            for (int k = 0; k < kHold; ++k)
+                x[k] = *reinterpret_cast<const Bytes<kRun<S>> *>(
+                    c.k_codes + kv_head(c, min((uint32_t)page[k], last), h, S) + (i[k] & mask) * S +
+                    (k * kMove + tid) % runs * kRun<S>);
+            if (IN_PLACE) __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kHold; ++k) {
+                const int j = j0 + (k * kMove + tid) / runs;
+                if (j < m && (uint32_t)goal[k] <= last)
+                    *reinterpret_cast<Bytes<kRun<S>> *>(c.k_codes + kv_head(c, goal[k], h, S) + (j & mask) * S +
+                                                        (k * kMove + tid) % runs * kRun<S>) = x[k];
+            }
+        }
+        return;
+    }
+    part -= grid.keys;
+    // Values: what lies between the tile's first and last position comes to LDS by whole
+    // words, 8 positions of a sub-vector each, where single bytes are picked: picked from
+    // memory they took 142 us instead of TODO for 64 contexts of 8192 brought to half. Where
+    // little is kept they come from memory.
+    constexpr int shares = IN_PLACE ? kParts : 1, subs = (S + shares - 1) / shares;
+    constexpr int wide = 32, high = kMove / wide;        // a thread's words and sub-vectors: every 32nd and 8th
+    constexpr int words = kSpan / 8 / wide, turns = (subs + high - 1) / high;
+    constexpr int row = kSpan + 4;                       // bytes of a sub-vector's in LDS
+    __shared__ uint32_t s_codes[subs * row / 4];
+    __shared__ int32_t s_table[kSpan / 8 + 1];
+    const int p0 = IN_PLACE ? part * subs : 0, p1 = min(p0 + subs, S);
+    const int lane = tid % wide, sub0 = p0 + tid / wide;
+    for (int j0 = IN_PLACE ? 0 : part * kValues; j0 < m; j0 += (IN_PLACE ? 1 : grid.values) * kValues) {
+        const int j = j0 + lane * 8;                     // the thread's places
+        int at[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) at[y] = kept[min(j + y, m - 1)];
+        const uint32_t goal = j < m ? (uint32_t)to[j >> c.page_log2] : ~0u;
+        const int i0 = kept[j0] & ~7, end = kept[min(j0 + kValues, m) - 1] + 1;
+        uint64_t x[turns];
+        if (end - i0 <= kSpan) {
+            const int page0 = i0 >> c.page_log2;
+            if (tid <= ((end - 1) >> c.page_log2) - page0) s_table[tid] = table[page0 + tid];
+            __syncthreads();
+            uint64_t w[turns * words];
+#pragma unroll
+            for (int k = 0; k < words; ++k) {
+                const int i = min(i0 + (lane + k * wide) * 8, (end - 1) & ~7);
+                const uint32_t page = (uint32_t)s_table[(i >> c.page_log2) - page0];
+                const uint8_t *const from = c.v_codes + kv_head(c, min(page, last), h, S) + (i & mask);
+#pragma unroll
+                for (int n = 0; n < turns; ++n)
+                    w[k * turns + n] = *reinterpret_cast<const uint64_t *>(
+                        from + ((int64_t)min(sub0 + n * high, p1 - 1) << c.page_log2));
+            }
+#pragma unroll
+            for (int k = 0; k < words; ++k)
+#pragma unroll
+                for (int n = 0; n < turns; ++n)
+                    if (i0 + (lane + k * wide) * 8 < end && sub0 + n * high < p1) {
+                        uint32_t *const dst = s_codes + ((sub0 - p0 + n * high) * row + (lane + k * wide) * 8) / 4;
+                        dst[0] = (uint32_t)w[k * turns + n];
+                        dst[1] = (uint32_t)(w[k * turns + n] >> 32);
+                    }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < turns; ++n) {
+                const uint8_t *const from = reinterpret_cast<const uint8_t *>(s_codes) +
+                                            min(sub0 - p0 + n * high, p1 - p0 - 1) * row - i0;
+                uint32_t lo = 0, hi = 0;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    lo |= (uint32_t)from[at[y]] << (8 * y);
+                    hi |= (uint32_t)from[at[y + 4]] << (8 * y);
                 }
+                x[n] = (uint64_t)hi << 32 | lo;
             }
         } else {
-            const int s0 = (part - 1 - kParts) * subs;
-            uint64_t x[runs];
+            const uint8_t *from[8];
 #pragma unroll
-            for (int k = 0; k < runs; ++k) {
-                const int u = k * kMove + tid, sub = s0 + u / (kMove / 8), g = u % (kMove / 8) * 8;
-                x[k] = 0;
-                if (u >= kMove / 8 * subs || sub >= S || j0 + g >= m) continue;
+            for (int y = 0; y < 8; ++y)
+                from[y] = c.v_codes + kv_head(c, min((uint32_t)table[at[y] >> c.page_log2], last), h, S) + (at[y] & mask);
 #pragma unroll
-                for (int y = 0; y < 8; ++y)
-                    if (j0 + g + y < m)
-                        x[k] |= (uint64_t)c.v_codes[kv_head(c, s_page[g + y], h, S) +
-                                                    ((int64_t)sub << c.page_log2) + s_off[g + y]]
-                                << (8 * y);
-            }
-            if (e.in_place) __syncthreads();
+            for (int n = 0; n < turns; ++n) {
+                const int64_t sub = (int64_t)min(sub0 + n * high, p1 - 1) << c.page_log2;
+                uint32_t lo = 0, hi = 0;
 #pragma unroll
-            for (int k = 0; k < runs; ++k) {
-                const int u = k * kMove + tid, sub = s0 + u / (kMove / 8), g = u % (kMove / 8) * 8;
-                const int j = j0 + g;
-                if (u >= kMove / 8 * subs || sub >= S || j >= m) continue;
-                const uint32_t page = (uint32_t)to[j >> c.page_log2];
-                if (page > last) continue;
-                uint8_t *dst = c.v_codes + kv_head(c, page, h, S) + ((int64_t)sub << c.page_log2) + (j & mask);
-                if (j + 8 <= m)
-                    *reinterpret_cast<uint64_t *>(dst) = x[k];
-                else
-                    for (int y = 0; y < m - j; ++y) dst[y] = (uint8_t)(x[k] >> (8 * y));
+                for (int y = 0; y < 4; ++y) {
+                    lo |= (uint32_t)from[y][sub] << (8 * y);
+                    hi |= (uint32_t)from[y + 4][sub] << (8 * y);
+                }
+                x[n] = (uint64_t)hi << 32 | lo;
             }
         }
+        if (IN_PLACE) __syncthreads();                   // all read; LDS is done with, too
+        if (goal <= last) {
+            uint8_t *const dst = c.v_codes + kv_head(c, goal, h, S) + (j & mask);
+#pragma unroll
+            for (int n = 0; n < turns; ++n) {
+                if (sub0 + n * high >= p1) continue;
+                uint8_t *const out = dst + ((int64_t)(sub0 + n * high) << c.page_log2);
+                if (j + 8 <= m)
+                    *reinterpret_cast<uint64_t *>(out) = x[n];
+                else
+                    for (int y = 0; y < m - j; ++y) out[y] = (uint8_t)(x[n] >> (8 * y));
+            }
+        }
+        if (!IN_PLACE) __syncthreads();
     }
 }
 
 template <int S>
 void move(const KvCache &c, const KvEvict &e, hipStream_t s)
 {
-    // places that any sequence can have, and those of a row of weights
-    int64_t most = (int64_t)e.table_pages << c.page_log2;
-    if (most > e.keep) most = e.keep;
-    if (most < e.positions) most = e.positions;
-    const int tiles = (int)((most + kMove - 1) / kMove);
-    const int64_t rows = (int64_t)c.heads * e.seqs * (2 * kParts + 1);
-    // out of place a workgroup to a tile, up to some 2^22 of them
-    int64_t step = e.in_place ? 1 : ((int64_t)1 << 22) / rows;
-    step = step < 1 ? 1 : step > tiles ? tiles : step;
-    hipLaunchKernelGGL((kv_move_kernel<S>), dim3((unsigned)(rows * step)), dim3(kMove), 0, s, c, e,
-                       tiles, (int)step);
+    const int64_t rows = (int64_t)c.heads * e.seqs;
+    MoveGrid grid{1, 1, kParts};
+    if (!e.in_place) {
+        // a workgroup to a tile, up to some 2^22 in all
+        int64_t most = (int64_t)e.table_pages << c.page_log2;
+        if (most > e.keep) most = e.keep;
+        const int64_t room = ((int64_t)1 << 22) / (3 * rows);
+        const auto tiles = [&](int64_t n, int tile) {
+            n = (n + tile - 1) / tile;
+            return (int)(n > room ? room : n < 1 ? 1 : n);
+        };
+        grid = MoveGrid{tiles(e.positions, kFloats), tiles(most, kKeys<S>), tiles(most, kValues)};
+    }
+    const dim3 blocks((unsigned)(rows * grid.all()));
+    if (e.in_place)
+        hipLaunchKernelGGL((kv_move_kernel<S, true>), blocks, dim3(kMove), 0, s, c, e, grid);
+    else
+        hipLaunchKernelGGL((kv_move_kernel<S, false>), blocks, dim3(kMove), 0, s, c, e, grid);
 }
 
 }  // namespace
