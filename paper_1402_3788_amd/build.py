@@ -43,6 +43,8 @@ SOURCES = ([("kmeans_api.hip", [], "kmeans_api.o"), ("lloyd_ctl.hip", [], "lloyd
               for f in ("api", "write", "read", "serve_api", "rotate", "weigh", "evict")]
            + [(f"kv_{f}.hip", [f"-DKV_SUB={sub}"], f"kv_{f}_sub{sub}.o")
               for f in ("attend", "tokens") for sub in (2, 4, 8)]
+           + [("kv_attend.hip", [f"-DKV_SUB={sub}", "-DKV_FEW=1"], f"kv_few_sub{sub}.o")
+              for sub in (2, 4, 8)]
            + [(f, [f"-DLLOYD_PART={p}", *UNIT_FLAGS.get(f, [])], f.replace(".hip", f"_part{p}.o"))
               for f in ("lloyd_tile.hip", "lloyd_lane.hip", "lloyd_lane_mfma.hip")
               for p in range(PARTS)])

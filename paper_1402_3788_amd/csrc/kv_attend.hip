@@ -32,15 +32,22 @@
 // for 26 %, and waiting for loads, LDS or a barrier for 39 %. A tile more to every
 // wave costs 1.4 us; a launch with one each takes 11 to 13.
 #include "kv_device.h"
+#include "kv_few.h"
 
 #include <type_traits>
 
 #ifndef KV_SUB
 #define KV_SUB 4
 #endif
+#ifndef KV_FEW
+#define KV_FEW 0
+#endif
 
 namespace lloyd {
 
+hipError_t launch_kv_few_2(const KvCache &, const KvFew &, const KvFewPlan &, hipStream_t);
+hipError_t launch_kv_few_4(const KvCache &, const KvFew &, const KvFewPlan &, hipStream_t);
+hipError_t launch_kv_few_8(const KvCache &, const KvFew &, const KvFewPlan &, hipStream_t);
 hipError_t launch_kv_attend_2(const KvCache &, const KvAttend &, const KvAttendPlan &, hipStream_t);
 hipError_t launch_kv_attend_4(const KvCache &, const KvAttend &, const KvAttendPlan &, hipStream_t);
 hipError_t launch_kv_attend_8(const KvCache &, const KvAttend &, const KvAttendPlan &, hipStream_t);
@@ -57,12 +64,6 @@ template <bool FP16>
 constexpr float kLift = FP16 ? 7.f : 0.f;
 
 typedef float f4v __attribute__((ext_vector_type(4)));
-typedef _Float16 h2v __attribute__((ext_vector_type(2)));
-typedef _Float16 h8v __attribute__((ext_vector_type(8)));
-typedef uint32_t u4v __attribute__((ext_vector_type(4)));
-typedef __bf16 b2v __attribute__((ext_vector_type(2)));
-typedef __bf16 b8v __attribute__((ext_vector_type(8)));
-typedef float f2v __attribute__((ext_vector_type(2)));
 
 template <bool FP16>
 __device__ inline f4v mfma(u4v a, u4v b, f4v c)
@@ -73,16 +74,6 @@ __device__ inline f4v mfma(u4v a, u4v b, f4v c)
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8v, a),
                                                        __builtin_bit_cast(b8v, b), c, 0, 0, 0);
-}
-
-template <bool FP16>
-__device__ inline uint32_t pack2(float a, float b)
-{
-    const f2v v = {a, b};
-    if constexpr (FP16)
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2v));
-    else
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
 }
 
 // x cut off to fp16, where mask is all ones; 0 where it is 0. (Below the least
@@ -141,7 +132,7 @@ struct Span {
     __device__ int tiles() const { return len > start ? ((len + 31) >> 5) - (start >> 5) : 0; }
 };
 
-__device__ inline Span span_of(const KvCache &c, const KvAttend &a, int b)
+[[maybe_unused]] __device__ inline Span span_of(const KvCache &c, const KvAttend &a, int b)
 {
     const int cap = a.table_pages << c.page_log2;
     Span s;
@@ -265,12 +256,18 @@ __device__ inline int wave_scan(int x)
 // WIDE: more than 8 queries, so that the high and the low parts of the weights
 // are operands of their own. Else the queries stand twice in the 16 columns,
 // the first eight of which take the high parts and the others the low ones.
-template <int D, int SUB, bool FP16, bool WIDE>
+//
+// A is KvAttend, or KvFew for few new tokens of every sequence: then what is said of a
+// sequence here holds for a unit, up to 8 or 16 (WIDE) query heads of its new tokens,
+// each of which sees positions of its own.
+template <int D, int SUB, bool FP16, bool WIDE, typename A>
 __global__ __launch_bounds__((Form<D, SUB>::kThreads)) void
-kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
+kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
 {
     using F = Form<D, SUB>;
     constexpr int W = F::kWaves;
+    constexpr bool FEW = std::is_same_v<A, KvFew>;
+    constexpr int kUnits = F::kSpans * sizeof(Span) / sizeof(KvUnit);    // kept in LDS
     extern __shared__ uint4 lds[];
     // the values first: their addresses below 2^16 fit the offset of a load
     char *const vbook = reinterpret_cast<char *>(lds);
@@ -280,6 +277,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     int *const tag = reinterpret_cast<int *>(ml + 4 * W);
     int *const wave_sum = tag + 2 * W;
     Span *const spans = reinterpret_cast<Span *>(wave_sum + W);          // [kSpans]
+    KvUnit *const units = reinterpret_cast<KvUnit *>(spans);             // [kUnits]
     int *const first = reinterpret_cast<int *>(spans + F::kSpans);       // [seqs + 1]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -287,7 +285,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     const int h = blockIdx.x % c.heads;
     const int qb = blockIdx.x / c.heads % qblocks;
     const int j = blockIdx.x / c.heads / qblocks;
-    const int nq = min(kKvQueries, a.group - qb * kKvQueries);
+    // of a sequence, of which a unit may have fewer
+    const int nq = FEW ? kv_few_rows(WIDE) : min(kKvQueries, a.group - qb * kKvQueries);
     const int rq = WIDE ? r : r & 7;                     // the lane's query
     const int64_t wg = ((int64_t)qb * c.heads + h) * splits + j;
     float *const part_o = a.part_o + wg * (W + 2) * F::kEntry;
@@ -296,11 +295,44 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 
     // Where each sequence's tiles begin in the row of all tiles. Up to 64
     // sequences every wave has them in its lanes, and looks nothing up later.
-    const bool in_lanes = a.seqs <= kWave;
-    int tiles;
+    bool in_lanes = a.seqs <= kWave;
+    int tiles, seqs = a.seqs;
     Span my_span{0, 0};
     int my_first = 0, my_next = 0;
-    if (in_lanes) {
+    if constexpr (FEW) {
+        in_lanes = a.in_lanes;
+        if (in_lanes) {
+            // the lanes' sequences, then the lanes' units
+            KvSeq s{};
+            if (lane < a.seqs) s = kv_seq(c, a, lane);
+            const int upto = wave_scan((s.n * a.group + nq - 1) / nq);
+            seqs = __builtin_amdgcn_readlane(upto, 63);
+            int b = 0;
+            for (int i = 0; i < a.seqs; ++i) b += __builtin_amdgcn_readlane(upto, i) <= lane;
+            const int before = __shfl(upto, max(b - 1, 0));
+            const KvSeq of{__shfl(s.t0, b & 63), __shfl(s.n, b & 63), __shfl(s.len, b & 63),
+                           __shfl(s.prefix, b & 63)};
+            KvUnit x{};
+            if (lane < seqs) x = kv_unit(a, of, b, (lane - (b ? before : 0)) * nq, nq);
+            const int n = x.tiles();
+            my_span = Span{x.lo, x.hi};
+            my_next = wave_scan(n);
+            my_first = my_next - n;
+            tiles = __builtin_amdgcn_readlane(my_next, 63);
+            if (lane < seqs) {
+                first[lane] = my_first;
+                units[lane] = x;
+                if (blockIdx.x == 0 && wave == 0) a.units.unit[lane] = x;        // for the joining launch
+            }
+            if (lane == 0) first[seqs] = tiles;
+        } else {
+            seqs = *a.units.count;
+            for (int i = tid; i <= seqs; i += F::kThreads) first[i] = a.units.first[i];
+            for (int i = tid; i < min(seqs, kUnits); i += F::kThreads) units[i] = a.units.unit[i];
+            tiles = a.units.first[seqs];
+            __syncthreads();
+        }
+    } else if (in_lanes) {
         if (lane < a.seqs) my_span = span_of(c, a, lane);
         const int n = my_span.tiles();
         my_next = wave_scan(n);
@@ -340,21 +372,49 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         __syncthreads();
     }
     const int used = splits_used(tiles, splits, W);
+    const auto unit_of = [&](int u) {
+        if constexpr (FEW) return u < kUnits ? units[u] : a.units.unit[u];
+        else return KvUnit{};
+    };
+    // Where query q of sequence b has its output, and its logarithm among all.
+    struct Row {
+        int64_t out, lse;
+    };
+    const auto row_of = [&](int b, int q) {
+        if constexpr (FEW) {
+            const KvUnit x = unit_of(b);
+            const int row = x.row0 + q, token = x.t0 + row / a.group, head = h * a.group + row % a.group;
+            return Row{token * a.out_token + head * a.out_head, (int64_t)token * c.heads * a.group + head};
+        } else {
+            const int head = h * a.group + qb * kKvQueries + q;
+            return Row{b * a.out_seq + head * a.out_head, (int64_t)b * c.heads * a.group + head};
+        }
+    };
+    const auto rows_of = [&](int b) {
+        if constexpr (FEW) return unit_of(b).rows(a.group, nq);
+        else return nq;
+    };
     const auto empty = [&](int b) {
-        for (int i = tid; i < nq * D; i += F::kThreads)
-            a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + i / D) * a.out_head + i % D] = 0;
-        if (a.lse && tid < nq)
-            a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + tid] = -INFINITY;
+        if constexpr (FEW) {
+            const int n = rows_of(b);
+            for (int i = tid; i < n * D; i += F::kThreads) a.out[row_of(b, i / D).out + i % D] = 0;
+            if (a.lse && tid < n) a.lse[row_of(b, tid).lse] = -INFINITY;
+        } else {
+            for (int i = tid; i < nq * D; i += F::kThreads)
+                a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + i / D) * a.out_head + i % D] = 0;
+            if (a.lse && tid < nq)
+                a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + tid] = -INFINITY;
+        }
     };
     // Sequences without positions.
     if (in_lanes) {
-        uint64_t none = __ballot(lane < a.seqs && my_first == my_next);
+        uint64_t none = __ballot(lane < seqs && my_first == my_next);
         for (; none; none &= none - 1) {
             const int b = __builtin_ctzll(none);
             if (b % splits == j) empty(b);
         }
     } else {
-        for (int b = j; b < a.seqs; b += splits)
+        for (int b = j; b < seqs; b += splits)
             if (first[b] == first[b + 1]) empty(b);
     }
     if (tid == 0) a.shared[wg] = KvShared{-1, 0};        // unless found below
@@ -364,12 +424,11 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 
     // Final output of query q, feature d of sequence b.
     const auto put = [&](int b, int q, int d, float x) {
-        a.out[b * a.out_seq + (h * a.group + qb * kKvQueries + q) * a.out_head + d] =
-            (uint16_t)pack2<FP16>(x, 0.f);
+        a.out[row_of(b, q).out + d] = (uint16_t)pack2<FP16>(x, 0.f);
     };
     const auto put_lse = [&](int b, int q, float m, float l) {
         if (a.lse)
-            a.lse[(int64_t)b * c.heads * a.group + h * a.group + qb * kKvQueries + q] =
+            a.lse[row_of(b, q).lse] =
                 l > 0.f || l != l ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
     };
 
@@ -385,13 +444,21 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     struct Cursor {
         int b, base, next;
         Span sp;
+        int of;                  // the sequence that unit b belongs to
     };
     const auto enter = [&](int b) {
         Cursor x;
         x.b = __builtin_amdgcn_readfirstlane(b);
         x.base = __builtin_amdgcn_readfirstlane(first[x.b]);
         x.next = __builtin_amdgcn_readfirstlane(first[x.b + 1]);
-        const Span s = x.b < F::kSpans ? spans[x.b] : span_of(c, a, x.b);
+        Span s;
+        if constexpr (FEW) {
+            const KvUnit *const u = x.b < kUnits ? units + x.b : a.units.unit + x.b;
+            s = Span{u->lo, u->hi};
+            x.of = __builtin_amdgcn_readfirstlane(u->b);
+        } else {
+            s = x.b < F::kSpans ? spans[x.b] : span_of(c, a, x.b);
+        }
         x.sp.start = __builtin_amdgcn_readfirstlane(s.start);
         x.sp.len = __builtin_amdgcn_readfirstlane(s.len);
         return x;
@@ -421,7 +488,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         y.pos = (t - x.base + x.sp.tile0()) * 32;
         y.low = x.sp.start >> c.page_log2 << 2;
         y.high = (x.sp.len - 1) >> c.page_log2 << 2;
-        y.row = reinterpret_cast<const char *>(a.table + x.b * a.table_stride);
+        y.row = reinterpret_cast<const char *>(a.table + (FEW ? x.of : x.b) * a.table_stride);
         return y;
     };
     const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
@@ -468,8 +535,13 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
         for (int hh = 0; hh < F::NH; ++hh) load_bytes<8>(cd.v[hh], v + v_step(hh));
     };
-    const float scale = fabsf(a.scale_log2);
-    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;     // the scale's sign, for the queries
+    bool changed = false;        // scores are more than products
+    if constexpr (FEW) changed = a.cap_log2 > 0.f || a.slopes;
+    const float scale = changed ? 1.f : fabsf(a.scale_log2);
+    const uint32_t flip = !changed && a.scale_log2 < 0.f ? 0x80008000u : 0u;     // the scale's sign, for the queries
+    // what the lane's query of a unit sees, and its slope
+    [[maybe_unused]] KvSeen view{0, 0, 0};
+    [[maybe_unused]] float slope = 0.f;
     const uint32_t low_parts = r >= 8 ? ~0u : 0u;        // lanes whose columns take them
     // the byte selection that makes the first of two bf16 an fp32 number there, else 0
     const uint32_t low_byte = r >= 8 ? 0x01000C0Cu : 0x0C0C0C0Cu;
@@ -477,7 +549,20 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     const auto load_q = [&](int b) {
 #pragma unroll
         for (int st = 0; st < D / 32; ++st) q[st] = u4v{0, 0, 0, 0};
-        if (rq < nq) {
+        if constexpr (FEW) {
+            const KvUnit x = unit_of(b);
+            view = KvSeen{0, 0, 0};
+            slope = 0.f;
+            if (rq < x.rows(a.group, nq)) {
+                const int t = (x.row0 + rq) / a.group, head = h * a.group + (x.row0 + rq) % a.group;
+                const uint16_t *src = a.q + (x.t0 + t) * a.q_token + head * a.q_head + g * (D / 4);
+#pragma unroll
+                for (int st = 0; st < D / 32; ++st)
+                    q[st] = *reinterpret_cast<const u4v *>(src + st * 8);
+                view = kv_seen(a, KvSeq{x.t0, x.n, x.len, x.prefix}, t);
+                if (a.slopes) slope = a.slopes[head] * kLog2e;
+            }
+        } else if (rq < nq) {
             const uint16_t *src = a.q + b * a.q_seq +
                                   (h * a.group + qb * kKvQueries + rq) * a.q_head + g * (D / 4);
 #pragma unroll
@@ -497,15 +582,16 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
     Where where{};
     if (a0 < a1) {
         if (in_lanes) {
-            cur.b = (int)__popcll(__ballot(lane < a.seqs && my_next <= a0));
+            cur.b = (int)__popcll(__ballot(lane < seqs && my_next <= a0));
             cur.base = __builtin_amdgcn_readlane(my_first, cur.b);
             cur.next = __builtin_amdgcn_readlane(my_next, cur.b);
             cur.sp.start = __builtin_amdgcn_readlane(my_span.start, cur.b);
             cur.sp.len = __builtin_amdgcn_readlane(my_span.len, cur.b);
+            if constexpr (FEW) cur.of = __builtin_amdgcn_readfirstlane(units[cur.b].b);
         } else {
             // the last b with first[b] <= a0: of every 64th, then of the 64
-            const int block = __popcll(__ballot(first[min((lane + 1) * kWave, a.seqs)] <= a0));
-            const int b = min(block * kWave + lane + 1, a.seqs);
+            const int block = __popcll(__ballot(first[min((lane + 1) * kWave, seqs)] <= a0));
+            const int b = min(block * kWave + lane + 1, seqs);
             cur = enter(block * kWave + __popcll(__ballot(first[b] <= a0)));
         }
         then = cur;
@@ -582,10 +668,16 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
         // is masked in branches of its own, which most tiles skip.
         const auto step = [&](int t, int pos) {
             const Span &sp = cur.sp;
-            const bool partial = pos < sp.start || pos + 32 > sp.len;
+            bool partial = pos < sp.start || pos + 32 > sp.len;
+            if constexpr (FEW) partial = !__all(pos >= view.lo && pos + 32 <= view.hi);
             const auto seen = [&](int i) {
                 const int p = pos + 8 * g + i;
                 return p >= sp.start && p < sp.len;
+            };
+            const auto sees = [&](int i) {               // the lane's query
+                const int p = pos + 8 * g + i;
+                if constexpr (FEW) return p >= view.lo && p < view.hi;
+                else return seen(i);
             };
             // All centres of the tile are asked for before any is waited for: a
             // lookup takes far longer than its turn, and a SIMD has but three waves
@@ -631,9 +723,22 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
                                               0x0C0C0000u | (4 + (x & 3)) << 8));
             __builtin_amdgcn_sched_barrier(0);
             if (t + 1 < a1) load_v(coming);
+            if constexpr (FEW) {
+                if (a.cap_log2 > 0.f) {
+                    kv_cap<8>(z, a.scale_cap, a.cap_log2);
+                } else if (changed) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[i] *= a.scale_log2;
+                }
+                if (a.slopes) {
+                    const float far = (float)(view.at - pos - 8 * g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[i] = __builtin_fmaf(-slope, fabsf(far - (float)i), z[i]);
+                }
+            }
             if (partial) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] = seen(i) ? z[i] : -INFINITY;
+                for (int i = 0; i < 8; ++i) z[i] = sees(i) ? z[i] : -INFINITY;
             }
             float top = fmaxf(z[0], z[1]);
 #pragma unroll
@@ -654,7 +759,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             for (int i = 0; i < 8; ++i) z[i] = __builtin_fmaf(z[i], scale, -m0);
             if (partial) {                                // again: a scale of 0 gave NaN
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] = seen(i) ? z[i] : -INFINITY;
+                for (int i = 0; i < 8; ++i) z[i] = sees(i) ? z[i] : -INFINITY;
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -741,10 +846,8 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             }
             if (piece == cur.base && end == cur.next) {  // the whole sequence
                 const float inv = lw > 0.f || lw != lw ? 1.f / lw : 0.f;
-                if (r < nq) {
-                    uint16_t *const dst =
-                        here(a.out + b * a.out_seq +
-                             (h * a.group + qb * kKvQueries + r) * a.out_head + 4 * g * F::VS);
+                if (r < rows_of(b)) {
+                    uint16_t *const dst = here(a.out + row_of(b, r).out + 4 * g * F::VS);
 #pragma unroll
                     for (int n = 0; n < F::NV; ++n)
 #pragma unroll
@@ -819,7 +922,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
             if (!in) continue;
             weight[e][qq] = w;
             weight[e][16 + qq] = lw;
-            if (e != lead || qq >= nq) continue;
+            if (e != lead || qq >= rows_of(b)) continue;
             if (at >= w0 && end <= w1) {
                 put_lse(b, qq, top, lw);
             } else {
@@ -872,7 +975,7 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 #pragma unroll
         for (int i = 0; i < mine; ++i) {
             const int at = i * F::kThreads + tid, d = F::feature(at);
-            if (qq < nq && at < F::kEntry) {
+            if (qq < rows_of(b) && at < F::kEntry) {
                 if (!whole)
                     part_o[(W + slot) * F::kEntry + at] = o[i];
                 else if (d < D)
@@ -890,15 +993,16 @@ kv_attend_kernel(KvCache c, KvAttend a, int splits, int qblocks)
 // of the shares after it. It takes 256 of the outputs, one to a thread, and asks
 // for the parts and for what weighs them at once: this launch is a chain of two
 // trips to memory.
-template <int D, int SUB, bool FP16>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int splits)
+template <int D, int SUB, bool FP16, typename A>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, A a, int splits)
 {
     using F = Form<D, SUB>;
+    constexpr bool FEW = std::is_same_v<A, KvFew>;
     constexpr int chunks = F::kEntry / 256, batch = 8;
     const int x = blockIdx.x % chunks * 256 + threadIdx.x;
     const int j = blockIdx.x / chunks % (splits - 1), hq = blockIdx.x / chunks / (splits - 1);
     const int h = hq % c.heads, qb = hq / c.heads;
-    const int nq = min(kKvQueries, a.group - qb * kKvQueries);
+    int nq = FEW ? 0 : min(kKvQueries, a.group - qb * kKvQueries);
     const int64_t wg = (int64_t)hq * splits + j;
     const int tid = threadIdx.x, q = tid & 15;
     const auto part = [&](int i) {                       // of this thread's output
@@ -956,10 +1060,16 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
     float lw = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) lw += s_sum[i * 16 + q];
+    int token = b, head = h * a.group + qb * kKvQueries + q;
+    if constexpr (FEW) {
+        const KvUnit u = a.units.unit[b];
+        nq = u.rows(a.group, a.rows);
+        token = u.t0 + (u.row0 + q) / a.group;
+        head = h * a.group + (u.row0 + q) % a.group;
+    }
     if (q >= nq) return;
-    const int head = h * a.group + qb * kKvQueries + q;
     if (x < 16 && a.lse)
-        a.lse[(int64_t)b * c.heads * a.group + head] =
+        a.lse[(int64_t)token * c.heads * a.group + head] =
             lw > 0.f || lw != lw ? (top + __log2f(lw)) * 0.69314718055994531f : -INFINITY;
     const int d = F::feature(x);
     if (d >= D) return;
@@ -976,66 +1086,95 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvCache c, KvAttend a, int
         for (int k = 0; k < batch; ++k)
             if (i + k < n) o += weight[(i + k) * 16 + q] * now[k];
     }
-    a.out[b * a.out_seq + head * a.out_head + d] =
+    int64_t stride;
+    if constexpr (FEW) stride = a.out_token;
+    else stride = a.out_seq;
+    a.out[token * stride + head * a.out_head + d] =
         (uint16_t)pack2<FP16>(lw > 0.f || lw != lw ? o / lw : 0.f, 0.f);
 }
 
-template <int D, int SUB, bool FP16>
-hipError_t launch(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hipStream_t s)
+template <int D, int SUB, bool FP16, bool WIDE, typename A>
+hipError_t launch(const KvCache &c, const A &a, int splits, int qblocks, int seqs, hipStream_t s)
 {
     using F = Form<D, SUB>;
-    const size_t lds = F::lds_bytes(a.seqs);
-    const unsigned grid = (unsigned)c.heads * p.qblocks * p.splits;
-    if (a.group > kKvQueries / 2)
-        hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16, true>), dim3(grid), dim3(F::kThreads), lds,
-                           s, c, a, p.splits, p.qblocks);
-    else
-        hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16, false>), dim3(grid), dim3(F::kThreads), lds,
-                           s, c, a, p.splits, p.qblocks);
+    const unsigned grid = (unsigned)c.heads * qblocks * splits;
+    hipLaunchKernelGGL((kv_attend_kernel<D, SUB, FP16, WIDE, A>), dim3(grid), dim3(F::kThreads),
+                       F::lds_bytes(seqs), s, c, a, splits, qblocks);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits == 1) return e;
-    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16>),
-                       dim3((unsigned)c.heads * p.qblocks * (p.splits - 1) * (F::kEntry / 256)), dim3(256), 0,
-                       s, c, a, p.splits);
+    if (e != hipSuccess || splits == 1) return e;
+    hipLaunchKernelGGL((kv_join_kernel<D, SUB, FP16, A>),
+                       dim3((unsigned)c.heads * qblocks * (splits - 1) * (F::kEntry / 256)), dim3(256), 0,
+                       s, c, a, splits);
     return hipGetLastError();
 }
 
-template <int D>
-hipError_t launch_type(const KvCache &c, const KvAttend &a, const KvAttendPlan &p, hipStream_t s)
+template <int D, bool WIDE, typename A>
+hipError_t launch_type(const KvCache &c, const A &a, int splits, int qblocks, int seqs, hipStream_t s)
 {
-    return c.fp16 ? launch<D, KV_SUB, true>(c, a, p, s) : launch<D, KV_SUB, false>(c, a, p, s);
+    return c.fp16 ? launch<D, KV_SUB, true, WIDE>(c, a, splits, qblocks, seqs, s)
+                  : launch<D, KV_SUB, false, WIDE>(c, a, splits, qblocks, seqs, s);
 }
+
+template <bool WIDE, typename A>
+hipError_t launch_dim(const KvCache &c, const A &a, int splits, int qblocks, int seqs, hipStream_t s)
+{
+    return c.dim == 64 ? launch_type<64, WIDE>(c, a, splits, qblocks, seqs, s)
+         : c.dim == 96 ? launch_type<96, WIDE>(c, a, splits, qblocks, seqs, s)
+                       : launch_type<128, WIDE>(c, a, splits, qblocks, seqs, s);
+}
+
+#if KV_SUB == 2
+// Workgroups of a head and block of queries: one to a CU, for the centres fill its LDS,
+// and no more than leave each wave a tile.
+int splits_of(const KvCache &c, int qblocks, int64_t tiles)
+{
+    int64_t splits = (int64_t)kCUs / (c.heads * qblocks);
+    const int waves = kv_waves(c.dim);
+    if (splits > (tiles + waves - 1) / waves) splits = (tiles + waves - 1) / waves;
+    return splits < 1 ? 1 : (int)splits;
+}
+
+// Floats of a wave's accumulators.
+size_t entry_of(const KvCache &c)
+{
+    const int gran = c.sub < 4 ? c.sub : 4;
+    return (size_t)((c.dim / gran + 15) / 16 * gran) * 256;
+}
+#endif
 
 }  // namespace
 
 #define KV_CAT2(a, b) a##b
 #define KV_CAT(a, b) KV_CAT2(a, b)
+#if KV_FEW
+hipError_t KV_CAT(launch_kv_few_, KV_SUB)(const KvCache &c, const KvFew &a, const KvFewPlan &p,
+                                          hipStream_t s)
+{
+    return p.wide ? launch_dim<true>(c, a, p.splits, 1, p.units, s)
+                  : launch_dim<false>(c, a, p.splits, 1, p.units, s);
+}
+#else
 hipError_t KV_CAT(launch_kv_attend_, KV_SUB)(const KvCache &c, const KvAttend &a,
                                              const KvAttendPlan &p, hipStream_t s)
 {
-    return c.dim == 64 ? launch_type<64>(c, a, p, s)
-         : c.dim == 96 ? launch_type<96>(c, a, p, s) : launch_type<128>(c, a, p, s);
+    return a.group > kKvQueries / 2 ? launch_dim<true>(c, a, p.splits, p.qblocks, a.seqs, s)
+                                    : launch_dim<false>(c, a, p.splits, p.qblocks, a.seqs, s);
 }
+#endif
 
-#if KV_SUB == 2
+#if KV_SUB == 2 && !KV_FEW
 KvAttendPlan plan_kv_attend(const KvCache &c, int seqs, int group, int64_t table_pages)
 {
     KvAttendPlan p{};
     p.qblocks = (group + kKvQueries - 1) / kKvQueries;
     const int64_t span = table_pages << c.page_log2;
-    const int64_t tiles = seqs * ((span + kKvTile - 1) / kKvTile);
-    // one workgroup to a CU: the centres fill its LDS
-    int64_t splits = (int64_t)kCUs / (c.heads * p.qblocks);
-    const int waves = kv_waves(c.dim);
-    if (splits > (tiles + waves - 1) / waves) splits = (tiles + waves - 1) / waves;
-    p.splits = splits < 1 ? 1 : (int)splits;
-    const int gran = c.sub < 4 ? c.sub : 4;
-    const size_t entry = (size_t)((c.dim / gran + 15) / 16 * gran) * 256 * sizeof(float);
+    p.splits = splits_of(c, p.qblocks, seqs * ((span + kKvTile - 1) / kKvTile));
+    const size_t entry = entry_of(c) * sizeof(float);
     const size_t wgs = (size_t)c.heads * p.qblocks * p.splits;
     const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     p.shared_off = 0;
     p.part_o_off = up(wgs * sizeof(KvShared));
-    p.part_ml_off = p.part_o_off + wgs * (waves + 2) * entry;
+    p.part_ml_off = p.part_o_off + wgs * (kv_waves(c.dim) + 2) * entry;
     p.total = p.part_ml_off + up(wgs * 64 * sizeof(float));
     return p;
 }
@@ -1045,6 +1184,60 @@ hipError_t launch_kv_attend(const KvCache &c, const KvAttend &a, const KvAttendP
 {
     return c.sub == 2 ? launch_kv_attend_2(c, a, p, s)
          : c.sub == 4 ? launch_kv_attend_4(c, a, p, s) : launch_kv_attend_8(c, a, p, s);
+}
+#endif
+
+#if KV_SUB == 2 && KV_FEW
+KvFewPlan plan_kv_few(const KvCache &c, const KvNew &n)
+{
+    KvFewPlan p{};
+    const int64_t rows = n.tokens * n.group;
+    // what fits half the columns takes half the products (and twice the queries' registers)
+    p.wide = rows > 8 * (int64_t)n.seqs;
+    const int64_t units = n.seqs + rows / kv_few_rows(p.wide);
+    p.units = units > kKvMaxFew ? kKvMaxFew + 1 : (int)units;
+    p.in_lanes = n.seqs <= kWave && units <= kWave;
+    const int64_t span = ((int64_t)n.table_pages << c.page_log2) / kKvTile + 1;
+    p.splits = splits_of(c, 1, units * span);
+    const size_t wgs = (size_t)c.heads * p.splits;
+    p.total = 0;
+    for (size_t x : {sizeof(int32_t), sizeof(int32_t) * (p.units + 1), sizeof(KvUnit) * p.units,
+                     sizeof(KvShared) * wgs, wgs * 64 * sizeof(float),
+                     wgs * (kv_waves(c.dim) + 2) * entry_of(c) * sizeof(float)})
+        p.total += (x + 255) / 256 * 256;
+    return p;
+}
+
+hipError_t launch_kv_few(const KvCache &c, const KvNew &n, const KvTokensOut &o, const KvFewPlan &p,
+                         void *ws, hipStream_t s)
+{
+    char *at = static_cast<char *>(ws);
+    const auto take = [&](size_t bytes) {
+        char *const x = at;
+        at += (bytes + 255) / 256 * 256;
+        return x;
+    };
+    const size_t wgs = (size_t)c.heads * p.splits;
+    KvFew a{};
+    static_cast<KvNew &>(a) = n;
+    a.out = o.out;
+    a.out_token = o.out_token;
+    a.out_head = o.out_head;
+    a.lse = o.lse;
+    a.in_lanes = p.in_lanes;
+    a.rows = kv_few_rows(p.wide);
+    a.units.count = reinterpret_cast<int32_t *>(take(sizeof(int32_t)));
+    a.units.first = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * (p.units + 1)));
+    a.units.unit = reinterpret_cast<KvUnit *>(take(sizeof(KvUnit) * p.units));
+    a.shared = reinterpret_cast<KvShared *>(take(sizeof(KvShared) * wgs));
+    a.part_ml = reinterpret_cast<float *>(take(wgs * 64 * sizeof(float)));
+    a.part_o = reinterpret_cast<float *>(take(0));
+    if (!p.in_lanes) {
+        const hipError_t e = launch_kv_units(c, n, a.units, kv_few_rows(p.wide), p.units, s);
+        if (e != hipSuccess) return e;
+    }
+    return c.sub == 2 ? launch_kv_few_2(c, a, p, s)
+         : c.sub == 4 ? launch_kv_few_4(c, a, p, s) : launch_kv_few_8(c, a, p, s);
 }
 #endif
 

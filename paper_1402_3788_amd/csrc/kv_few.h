@@ -1,0 +1,41 @@
+// Few new tokens of every sequence: what the attention of one new token (kv_attend.hip)
+// takes in the place of its sequences.
+#pragma once
+
+#include "kv_tokens_device.h"
+
+namespace lloyd {
+
+// Query heads of new tokens (rows) of a unit.
+constexpr int kv_few_rows(bool wide) { return wide ? 16 : 8; }
+constexpr int kKvMaxFew = 4096;      // units at most
+
+struct KvFew : KvNew {
+    uint16_t *out;
+    int64_t out_token, out_head;
+    float *lse;
+    KvUnits units;
+    int rows;                        // of a unit
+    bool in_lanes;                   // up to 64 units: each workgroup works them out, one writes them
+    // workspace
+    KvShared *shared;
+    float *part_o, *part_ml;
+};
+
+struct KvFewPlan {
+    bool wide;
+    int splits;                      // workgroups of a head
+    int units;                       // at most
+    bool in_lanes;                   // up to 64 sequences and units: no launch that works them out
+    size_t total;                    // workspace
+};
+
+KvFewPlan plan_kv_few(const KvCache &c, const KvNew &n);
+hipError_t launch_kv_few(const KvCache &c, const KvNew &n, const KvTokensOut &o, const KvFewPlan &p,
+                         void *ws, hipStream_t s);
+
+// Writes the units of `rows` rows of a call, `most` of them at most.
+hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, int rows, int most,
+                           hipStream_t s);
+
+}  // namespace lloyd

@@ -17,7 +17,7 @@
 //
 // The row of all units' tiles is shared evenly by the workgroups of a head; what is cut
 // that way is joined by a second launch. A launch before says where units begin.
-#include "kv_tokens_device.h"
+#include "kv_few.h"
 
 #ifndef KV_SUB
 #define KV_SUB 4
@@ -522,7 +522,7 @@ hipError_t KV_CAT(launch_kv_tokens_, KV_SUB)(const KvCache &c, const KvNew &a, c
 namespace {
 
 // One workgroup: the units of all sequences and where their tiles begin.
-__global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUnits to, int most)
+__global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUnits to, int rows, int most)
 {
     __shared__ int seq_first[kKvMaxSeqs + 1];
     __shared__ int wave_sum[16];
@@ -546,7 +546,7 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
 #pragma unroll
     for (int k = 0; k < (kKvMaxSeqs + 1023) / 1024; ++k) {
         const int b = tid * per + k;
-        if (k < per && b < a.seqs) n[k] = (int)(((int64_t)kv_seq(c, a, b).n * a.group + kRows - 1) / kRows);
+        if (k < per && b < a.seqs) n[k] = (kv_seq(c, a, b).n * a.group + rows - 1) / rows;
         sum += n[k];
     }
     int at = scan(sum, &units) - sum;
@@ -571,24 +571,7 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
                 else end = mid;
             }
             const KvSeq s = kv_seq(c, a, b);
-            const int row0 = (u - seq_first[b]) * kRows;
-            const int i0 = row0 / a.group, i1 = (int)((min((int64_t)row0 + kRows, (int64_t)s.n * a.group) - 1) / a.group);
-            int lo = INT32_MAX, hi = 0;
-            if (a.starts) {
-                for (int i = i0; i <= i1; ++i) {
-                    const KvSeen y = kv_seen(a, s, i);
-                    if (y.hi > 0) lo = min(lo, y.lo);
-                    hi = max(hi, y.hi);
-                }
-            } else {
-                // bounds rise from token to token
-                hi = kv_seen(a, s, i1).hi;
-                for (int i = i0; i <= i1 && lo == INT32_MAX; ++i) {
-                    const KvSeen y = kv_seen(a, s, i);
-                    if (y.hi > 0) lo = y.lo;
-                }
-            }
-            x = KvUnit{b, row0, s.t0, s.n, s.len, s.prefix, lo < hi ? lo : 0, lo < hi ? hi : 0};
+            x = kv_unit(a, s, b, (u - seq_first[b]) * rows, rows);
             to.unit[u] = x;
         }
         const int n1 = x.tiles();
@@ -602,6 +585,8 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
         *to.count = units;
     }
 }
+
+constexpr int kFewRows = 32;         // of a sequence on average, up to which units are of few
 
 KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 {
@@ -633,14 +618,32 @@ KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 
 }  // namespace
 
-size_t kv_attend_tokens_bytes(const KvCache &c, const KvNew &a) { return plan_of(c, a, nullptr).total; }
+hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, int rows, int most,
+                           hipStream_t s)
+{
+    hipLaunchKernelGGL(kv_units_kernel, dim3(1), dim3(1024), 0, s, c, n, to, rows, most);
+    return hipGetLastError();
+}
+
+// Whether a unit is of few rows: every sequence has few on average.
+static bool few(const KvCache &c, const KvNew &a, const KvFewPlan &p)
+{
+    return a.tokens * a.group <= kFewRows * (int64_t)a.seqs && p.units <= kKvMaxFew;
+}
+
+size_t kv_attend_tokens_bytes(const KvCache &c, const KvNew &a)
+{
+    const KvFewPlan p = plan_kv_few(c, a);
+    return few(c, a, p) ? p.total : plan_of(c, a, nullptr).total;
+}
 
 hipError_t launch_kv_attend_tokens(const KvCache &c, const KvNew &a, const KvTokensOut &o, void *ws,
                                    hipStream_t s)
 {
+    const KvFewPlan f = plan_kv_few(c, a);
+    if (few(c, a, f)) return launch_kv_few(c, a, o, f, ws, s);
     const KvTokensPlan p = plan_of(c, a, static_cast<char *>(ws));
-    hipLaunchKernelGGL(kv_units_kernel, dim3(1), dim3(1024), 0, s, c, a, p.of, p.units);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kv_units(c, a, p.of, kRows, p.units, s);
     if (e != hipSuccess) return e;
     return c.sub == 2 ? launch_kv_tokens_2(c, a, o, p, s)
          : c.sub == 4 ? launch_kv_tokens_4(c, a, o, p, s) : launch_kv_tokens_8(c, a, o, p, s);

@@ -140,7 +140,30 @@ struct KvUnit {
     int b, row0, t0, n, len, prefix, lo, hi;
     __device__ int tile0() const { return lo >> 5; }
     __device__ int tiles() const { return hi > lo ? ((hi + 31) >> 5) - (lo >> 5) : 0; }
+    __device__ int rows(int group, int most) const { return min(n * group - row0, most); }
 };
+
+// The unit of up to `rows` rows of sequence b from row0 on.
+__device__ inline KvUnit kv_unit(const KvNew &a, const KvSeq &s, int b, int row0, int rows)
+{
+    const int i0 = row0 / a.group, i1 = (min(row0 + rows, s.n * a.group) - 1) / a.group;
+    int lo = INT32_MAX, hi = 0;
+    if (a.starts) {
+        for (int i = i0; i <= i1; ++i) {
+            const KvSeen y = kv_seen(a, s, i);
+            if (y.hi > 0) lo = min(lo, y.lo);
+            hi = max(hi, y.hi);
+        }
+    } else {
+        // bounds rise from token to token
+        hi = kv_seen(a, s, i1).hi;
+        for (int i = i0; i <= i1 && lo == INT32_MAX; ++i) {
+            const KvSeen y = kv_seen(a, s, i);
+            if (y.hi > 0) lo = y.lo;
+        }
+    }
+    return KvUnit{b, row0, s.t0, s.n, s.len, s.prefix, lo < hi ? lo : 0, lo < hi ? hi : 0};
+}
 
 // Units and where each one's tiles begin among all (one more than there are units).
 struct KvUnits {
