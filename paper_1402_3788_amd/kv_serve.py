@@ -22,6 +22,7 @@ import math
 import torch
 
 from . import KmeansError, KMEANS_EUNSUPPORTED, _lib
+from . import kv as _kv
 from .kv import (KVCodes, _TYPES, _apart, _call, _current_device, _Desc, _ints, _no_gradient,
                  _raw_stream, _rows, _strides, _target)
 
@@ -71,6 +72,12 @@ def _bind():
     _lib.kmeans_kv_weigh.restype = ctypes.c_int
     _lib.kmeans_kv_evict.argtypes = [d, ctypes.POINTER(_Evict), p, p, p, i64, i64, p]
     _lib.kmeans_kv_evict.restype = ctypes.c_int
+    if _kv._fast is not None:
+        _kv._fast.bind_serve(*(ctypes.cast(f, ctypes.c_void_p).value
+                               for f in (_lib.kmeans_kv_rotate,
+                                         _lib.kmeans_kv_attend_tokens_workspace_bytes,
+                                         _lib.kmeans_kv_attend_tokens, _lib.kmeans_kv_weigh,
+                                         _lib.kmeans_kv_evict)))
 
 
 _bind()
@@ -111,6 +118,15 @@ def kmeans_kv_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.T
 
     Returns the turned tensors (q, k). `out` may supply them, among them q and k
     themselves."""
+    flags = (_INTERLEAVED if interleaved else 0) | (_INVERSE if inverse else 0)
+    if _kv._fast is not None and out is None:
+        index = _current_device()
+        got = _kv._fast.rotate(index, _raw_stream(index), q, k, positions, frequencies, flags,
+                               amplitude)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            raise KmeansError("kmeans_kv_rotate", got)
     if not (isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 3 and q.dtype in _TYPES):
         raise ValueError("q must be a bfloat16 or float16 [tokens, heads, dim] tensor on a GPU")
     like = _Like(q)
@@ -147,8 +163,7 @@ def kmeans_kv_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.T
     if 2 * frequencies.shape[0] > like.dim:
         raise ValueError("more features are turned than a head has")
     turn = _Turn(positions.data_ptr(), frequencies.data_ptr(), tokens, like.dim,
-                 frequencies.shape[0], _TYPES[q.dtype],
-                 (_INTERLEAVED if interleaved else 0) | (_INVERSE if inverse else 0), amplitude)
+                 frequencies.shape[0], _TYPES[q.dtype], flags, amplitude)
     _here(like.index, like.device, _lib.kmeans_kv_rotate, "kmeans_kv_rotate", turn, *args)
     return tuple(got)
 
@@ -178,8 +193,6 @@ def _new_tokens(cache, q, bounds, table, lengths, scale, cap, slopes, window, pr
     if slopes is not None:
         slopes = _ints(cache, slopes, torch.float32, q_heads, "slopes")
         _no_gradient(slopes, "slopes")
-    if scale is None:
-        scale = 1.0 / math.sqrt(cache.dim)
     if not 0 <= window < 1 << 31:
         raise ValueError("window must be a number of positions, or 0")
     t = _Tokens(bounds.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1],
@@ -228,6 +241,16 @@ def kmeans_kv_attend_tokens(cache: KVCodes, q: torch.Tensor, bounds: torch.Tenso
     the sum of the scores' exponentials (-inf, with out 0, where nothing is seen).
     Tokens outside every sequence are not written. `out` and `lse` may supply the
     tensors, `ws` the workspace (kmeans_kv_attend_tokens_workspace_bytes)."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.dim)
+    if (_kv._fast is not None and out is None and lse is None and ws is None
+            and _current_device() == cache.index):
+        got = _kv._fast.attend_tokens(cache._at, cache.k_centres, _raw_stream(cache.index), q, bounds,
+                                      table, lengths, scale, cap, slopes, window, prefixes, starts)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            raise KmeansError("kmeans_kv_attend_tokens", got)
     t, q, qp, qa, qb, _keep = _new_tokens(cache, q, bounds, table, lengths, scale, cap, slopes,
                                           window, prefixes, starts)
     shape = q.shape
@@ -288,6 +311,15 @@ def kmeans_kv_weigh(cache: KVCodes, q: torch.Tensor, lse: torch.Tensor, bounds: 
     others   as of kmeans_kv_attend_tokens
 
     Returns weights."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(cache.dim)
+    if _kv._fast is not None and weights is None and _current_device() == cache.index:
+        got = _kv._fast.weigh(cache._at, cache.k_centres, _raw_stream(cache.index), q, bounds, table,
+                              lengths, lse, scale, cap, slopes, window, prefixes, starts)
+        if type(got) is tuple:
+            return got[0]
+        if got is not None:
+            raise KmeansError("kmeans_kv_weigh", got)
     t, q, qp, qa, qb, _keep = _new_tokens(cache, q, bounds, table, lengths, scale, cap, slopes,
                                           window, prefixes, starts)
     if not (isinstance(lse, torch.Tensor) and lse.dtype is torch.float32
@@ -327,6 +359,13 @@ def kmeans_kv_evict(cache: KVCodes, weights: torch.Tensor, table: torch.Tensor,
     stay as they are. Returns (kept, lengths, weights): kept int32 [seqs, heads, keep], the
     positions in their order, -1 past the last; weights those of the kept positions, then
     zeros."""
+    if _kv._fast is not None and _current_device() == cache.index:
+        got = _kv._fast.evict(cache._at, cache.k_centres, _raw_stream(cache.index), weights, table,
+                              lengths, keep, recent, first, to)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            raise KmeansError("kmeans_kv_evict", got)
     lengths = _ints(cache, lengths, torch.int32, None, "lengths") if to is not None else lengths
     if to is None and not (isinstance(lengths, torch.Tensor) and lengths.dtype is torch.int32
                            and lengths.get_device() == cache.index and lengths.dim() == 1
