@@ -87,65 +87,97 @@ __device__ inline int share_of(int n, int t, int k)
     return (int)((unsigned)t < long_end ? (unsigned)t / (each + 1) : more + ((unsigned)t - long_end) / each);
 }
 
-template <int D, int SUB, bool FP16>
-__global__ __launch_bounds__(kThreads) void
-kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
+struct KvTokensArgs {
+    KvCache c;
+    KvNew a;
+    KvTokensOut o;
+    KvTokensPlan p;
+};
+
+// The kernel's arguments where they lie in memory: for what a loop needs seldom, read there
+// each time, which would else be kept in scalar registers through it, more than there are.
+__device__ inline const KvTokensArgs &seldom()
+{
+    auto p = (const __attribute__((address_space(4))) KvTokensArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const KvTokensArgs *)p;
+}
+
+// All waves' LDS accesses before it are done behind it; loads from memory stay under way,
+// which __syncthreads() would wait for.
+__device__ inline void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// ONE_PAGE: pages of 32 tokens or more, so that a tile lies on one.
+template <int D, int SUB, bool FP16, bool ONE_PAGE>
+__global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
 {
     using F = Form<D, SUB>;
+    const KvCache &c = args.c;
+    const KvNew &a = args.a;
+    const KvTokensPlan &p = args.p;
     extern __shared__ uint4 lds[];
     char *const kbook = reinterpret_cast<char *>(lds), *const vbook = kbook + F::kBook;
     char *const ktile = vbook + F::kBook, *const vtile = ktile + 2 * F::kTile;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % c.heads, j = blockIdx.x / c.heads;
-    const int heads = c.heads * a.group;
-    const int64_t wg = (int64_t)h * p.splits + j;
     const int units = *p.of.count, tiles = p.of.first[units];
     const int used = splits_used(tiles, p.splits);
 
-    // A row's token (among the sequence's) and query head.
+    // A row's token (among all) and query head.
     const auto row_of = [&](const KvUnit &u, int row, int *token, int *head) {
-        const unsigned x = (unsigned)(u.row0 + row);
-        *token = (int)(x / (unsigned)a.group);
-        *head = h * a.group + (int)(x % (unsigned)a.group);
-        return x < (unsigned)u.n * (unsigned)a.group;
+        const unsigned group = (unsigned)seldom().a.group, x = (unsigned)(u.row0 + row);
+        *token = u.t0 + (int)(x / group);
+        *head = h * group + (int)(x % group);
+        return x < (unsigned)u.n * group;
     };
     // Units without positions.
     for (int u = j; u < units; u += p.splits) {
         if (p.of.first[u] != p.of.first[u + 1]) continue;
         const KvUnit x = p.of.unit[u];
+        const KvTokensOut &o = args.o;
         for (int i = tid; i < kRows * (D / 8); i += kThreads) {
             int t, q;
             if (!row_of(x, i / (D / 8), &t, &q)) continue;
-            *reinterpret_cast<u4v *>(o.out + (x.t0 + t) * o.out_token + q * o.out_head + i % (D / 8) * 8) =
-                u4v{0, 0, 0, 0};
-            if (o.lse && i % (D / 8) == 0) o.lse[(int64_t)(x.t0 + t) * heads + q] = -INFINITY;
+            *reinterpret_cast<u4v *>(o.out + t * o.out_token + q * o.out_head + i % (D / 8) * 8) = u4v{0, 0, 0, 0};
+            if (o.lse && i % (D / 8) == 0) o.lse[(int64_t)t * c.heads * a.group + q] = -INFINITY;
         }
     }
-    if (tid == 0) p.cut[wg] = make_int2(-1, 0);          // unless found below
+    if (tid == 0) p.cut[(int64_t)h * p.splits + j] = make_int2(-1, 0);   // unless found below
     if (j >= used || tiles == 0) return;
     const int a0 = share_begin(tiles, j, used), a1 = share_begin(tiles, j + 1, used);
 
-    // A place in the row of tiles: unit u, which has tiles [base, next).
+    // A place in the row of tiles: unit u, which has tiles [base, next), the first of which is
+    // tile tile0 of its sequence; the entries of that one's row of the table that may be read.
     struct Cursor {
-        int u, base, next;
-        KvUnit x;
+        int u, base, next, tile0, low, high;
+        const int32_t *row;
     };
     const auto enter = [&](int u) {
+        const KvUnits &of = seldom().p.of;
+        const KvNew &n = seldom().a;
         Cursor y;
         y.u = __builtin_amdgcn_readfirstlane(u);
-        y.base = __builtin_amdgcn_readfirstlane(p.of.first[y.u]);
-        y.next = __builtin_amdgcn_readfirstlane(p.of.first[y.u + 1]);
-        const int *from = reinterpret_cast<const int *>(p.of.unit + y.u);
-        int *const x = reinterpret_cast<int *>(&y.x);
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(KvUnit) / 4); ++i) x[i] = __builtin_amdgcn_readfirstlane(from[i]);
+        y.base = __builtin_amdgcn_readfirstlane(of.first[y.u]);
+        y.next = __builtin_amdgcn_readfirstlane(of.first[y.u + 1]);
+        const KvUnit &x = of.unit[y.u];
+        const int lo = __builtin_amdgcn_readfirstlane(x.lo), hi = __builtin_amdgcn_readfirstlane(x.hi);
+        y.tile0 = lo >> 5;
+        y.low = lo >> c.page_log2;
+        y.high = (hi - 1) >> c.page_log2;
+        y.row = n.table + __builtin_amdgcn_readfirstlane(x.b) * n.table_stride;
         return y;
     };
     const auto advance = [&](Cursor &y, int t) {
         if (t < y.next) return;
+        const int32_t *const first = seldom().p.of.first;
         int u = y.u + 1;
-        while (p.of.first[u + 1] <= t) ++u;
+        while (first[u + 1] <= t) ++u;
         y = enter(u);
     };
     Cursor cur;
@@ -163,13 +195,13 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
     Cursor then = cur;
 
     // What a thread looks up of a tile: 8 features of key `key`, and VS of NP values.
-    const bool looks_k = tid < F::kTasks, looks_v = tid >= kThreads - F::kTasks;
+    constexpr bool all_look = F::kTasks == kThreads;
+    const bool looks_k = all_look || tid < F::kTasks, looks_v = all_look || tid >= kThreads - F::kTasks;
     const int xk = looks_k ? tid : 0, xv = looks_v ? tid - (kThreads - F::kTasks) : 0;
     const int key = xk % 4 + xk / (4 * F::NC) * 4, chunk = xk / 4 % F::NC;
     const int vpos = (xv % 4 + xv / (4 * F::NG) * 4) * F::NP, gran = xv / 4 % F::NG;
-    // Numbers of pages are asked for three tiles ahead, codes two, centres one.
     struct Where {
-        int pos, k_page, v_page;
+        int pos, k_page, v_page;     // ONE_PAGE: k_page of both
     };
     struct Codes {
         uint32_t k, v;
@@ -178,31 +210,41 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
     const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
     const unsigned pm = (1u << c.page_log2) - 1;
     const int64_t head_codes = ((int64_t)h * F::S) << c.page_log2;
-    const uint8_t *const k_lane = c.k_codes + head_codes + chunk * (8 / SUB);
-    const uint8_t *const v_lane = c.v_codes + head_codes + ((unsigned)(gran * F::VS / SUB) << c.page_log2);
+    const uint8_t *const k_head = c.k_codes + head_codes, *const v_head = c.v_codes + head_codes;
+    const unsigned k_lane = chunk * (8 / SUB), v_lane = (unsigned)(gran * F::VS / SUB) << c.page_log2;
+    const unsigned k_whole = k_lane + key * F::S, v_whole = v_lane + vpos;
     const auto find = [&](int t) {
         advance(then, t);
         Where w;
-        w.pos = (t - then.base + then.x.tile0()) * 32;
-        const int32_t *const row = a.table + then.x.b * a.table_stride;
-        // positions that nobody sees: the nearest page of one that somebody does
-        const int low = then.x.lo >> c.page_log2, high = (then.x.hi - 1) >> c.page_log2;
-        w.k_page = row[min(max((w.pos + key) >> c.page_log2, low), high)];
-        w.v_page = row[min(max((w.pos + vpos) >> c.page_log2, low), high)];
+        w.pos = (t - then.base + then.tile0) * 32;
+        if constexpr (ONE_PAGE) {
+            w.k_page = then.row[w.pos >> c.page_log2];
+        } else {
+            // positions that nobody sees: the nearest page of one that somebody does
+            w.k_page = then.row[min(max((w.pos + key) >> c.page_log2, then.low), then.high)];
+            w.v_page = then.row[min(max((w.pos + vpos) >> c.page_log2, then.low), then.high)];
+        }
         return w;
     };
     const auto load = [&](const Where &w) {
         // a number that is no page's is some page's here, never followed out
         const auto page = [&](int n) { return (uint64_t)min((unsigned)n, last_page) * page_bytes; };
         Codes x{};
+        const uint8_t *k, *v;
+        if constexpr (ONE_PAGE) {
+            const uint64_t at = page(__builtin_amdgcn_readfirstlane(w.k_page));
+            k = k_head + at + ((unsigned)w.pos & pm) * F::S + k_whole;
+            v = v_head + at + ((unsigned)w.pos & pm) + v_whole;
+        } else {
+            k = k_head + page(w.k_page) + (((unsigned)w.pos + key) & pm) * F::S + k_lane;
+            v = v_head + page(w.v_page) + (((unsigned)w.pos + vpos) & pm) + v_lane;
+        }
         if (looks_k) {
-            const uint8_t *const k = k_lane + page(w.k_page) + (((unsigned)w.pos + key) & pm) * F::S;
             if constexpr (SUB == 2) x.k = *reinterpret_cast<const uint32_t *>(k);
             else if constexpr (SUB == 4) x.k = *reinterpret_cast<const uint16_t *>(k);
             else x.k = *k;
         }
         if (looks_v) {
-            const uint8_t *const v = v_lane + page(w.v_page) + (((unsigned)w.pos + vpos) & pm);
             if constexpr (F::NP == 4) x.v = *reinterpret_cast<const uint32_t *>(v);
             else x.v = *reinterpret_cast<const uint16_t *>(v);
         }
@@ -212,21 +254,21 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
         KvEntry<8> k;
         KvEntry<F::VS> v[F::NP];
     };
-    const auto look = [&](const Codes &x) {
+    const auto look = [&](uint32_t k, uint32_t v) {
         Found f;
         if (looks_k) {
             KvEntry<SUB> e[8 / SUB];
 #pragma unroll
             for (int i = 0; i < 8 / SUB; ++i)
                 e[i] = *reinterpret_cast<const KvEntry<SUB> *>(
-                    kbook + (x.k >> (8 * i) & 255) * F::kRow + chunk * 16 + i * (SUB * 2));
+                    kbook + (k >> (8 * i) & 255) * F::kRow + chunk * 16 + i * (SUB * 2));
             __builtin_memcpy(&f.k, e, 16);
         }
         if (looks_v) {
 #pragma unroll
             for (int i = 0; i < F::NP; ++i)
                 f.v[i] = *reinterpret_cast<const KvEntry<F::VS> *>(
-                    vbook + (x.v >> (8 * i) & 255) * F::kRow + gran * (F::VS * 2));
+                    vbook + (v >> (8 * i) & 255) * F::kRow + gran * (F::VS * 2));
         }
         return f;
     };
@@ -237,19 +279,18 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
     const uint32_t k_to = chunk * 512 + ((((key & ~12) | (key & 4) << 1 | (key & 8) >> 1) * 16) ^ (chunk & 7) * 64);
     const auto v_slot = [](int f) { return (f ^ ((f >> 4) & 3)) * 16; };
     const uint32_t v_to = vpos / 8 * (D * 16) + (vpos & 7) * 2;
-    const auto put = [&](const Found &f, int buf) {
+    const auto put_k = [&](const Found &f, int buf) {
         if (looks_k) *reinterpret_cast<KvEntry<8> *>(ktile + buf * F::kTile + k_to) = f.k;
-        if (looks_v) {
+    };
+    // feature e of the granule's
+    const auto put_v = [&](const Found &f, int buf, int e) {
+        if (!looks_v) return;
+        KvEntry<F::NP> x;
 #pragma unroll
-            for (int e = 0; e < F::VS; ++e) {
-                KvEntry<F::NP> x;
-#pragma unroll
-                for (int i = 0; i < F::NP / 2; ++i)
-                    x.w[i] = __builtin_amdgcn_perm(f.v[2 * i + 1].w[e / 2], f.v[2 * i].w[e / 2],
-                                                   e % 2 ? 0x07060302u : 0x05040100u);
-                *reinterpret_cast<KvEntry<F::NP> *>(vtile + buf * F::kTile + v_to + v_slot(gran * F::VS + e)) = x;
-            }
-        }
+        for (int i = 0; i < F::NP / 2; ++i)
+            x.w[i] = __builtin_amdgcn_perm(f.v[2 * i + 1].w[e / 2], f.v[2 * i].w[e / 2],
+                                           e % 2 ? 0x07060302u : 0x05040100u);
+        *reinterpret_cast<KvEntry<F::NP> *>(vtile + buf * F::kTile + v_to + v_slot(gran * F::VS + e)) = x;
     };
 
     Where where = find(a0);
@@ -289,33 +330,52 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
             }
         }
     }
+    // On its turn for tile t a wave looks up the keys of t + 2 and the values of t + 1. Codes
+    // are asked for a tile before, numbers of pages two.
+    int ahead = a0;                                      // the tile that `codes` are of
+    uint32_t v_codes = 0;                                // of the tile before
     Codes codes = load(where);
     if (a0 + 1 < a1) where = find(a0 + 1);
+    // Behind the share's last tile these go on with that one's, which nobody reads.
+    const auto step = [&]() {
+        v_codes = codes.v;
+        codes = load(where);
+        if (++ahead + 1 < a1) where = find(ahead + 1);
+    };
     __syncthreads();
-    put(look(codes), 0);
-    if (a0 + 1 < a1) codes = load(where);
-    if (a0 + 2 < a1) where = find(a0 + 2);
+    put_k(look(codes.k, 0), 0);
+    step();
+    {
+        const Found f = look(codes.k, v_codes);
+        put_k(f, 1);
+#pragma unroll
+        for (int e = 0; e < F::VS; ++e) put_v(f, 0, e);
+        step();
+    }
     __syncthreads();
 
     const bool changed = a.cap_log2 > 0.f || a.slopes;   // scores are more than products
     const float scale = changed ? 1.f : fabsf(a.scale_log2);
-    const uint32_t flip = !changed && a.scale_log2 < 0.f ? 0x80008000u : 0u;
     u4v q[D / 16];
     f16v acc[F::F];
     float m = 0.f, m0 = 0.f, l = 0.f, slope = 0.f;
     KvSeen seen{};
     const auto begin = [&]() {
+        const KvTokensArgs &all = seldom();
+        const KvNew &n = all.a;
+        const KvUnit u = all.p.of.unit[cur.u];
+        const uint32_t flip = !changed && n.scale_log2 < 0.f ? 0x80008000u : 0u;
         int t, hq;
-        const bool there = row_of(cur.x, wave * 32 + col, &t, &hq);
-        const uint16_t *const src = a.q + (cur.x.t0 + t) * a.q_token + hq * a.q_head + half * 8;
+        const bool there = row_of(u, wave * 32 + col, &t, &hq);
+        const uint16_t *const src = n.q + t * n.q_token + hq * n.q_head + half * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
             q[s] = u4v{0, 0, 0, 0};
             if (there) q[s] = *reinterpret_cast<const u4v *>(src + s * 16) ^ flip;
         }
         seen = KvSeen{0, 0, 0};
-        if (there) seen = kv_seen(a, KvSeq{cur.x.t0, cur.x.n, cur.x.len, cur.x.prefix}, t);
-        slope = there && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
+        if (there) seen = kv_seen(n, KvSeq{u.t0, u.n, u.len, u.prefix}, t - u.t0);
+        slope = there && n.slopes ? n.slopes[hq] * kLog2e : 0.f;
         m = -INFINITY;
         m0 = 0.f;
         l = 0.f;
@@ -324,130 +384,180 @@ kv_tokens_kernel(KvCache c, KvNew a, KvTokensOut o, KvTokensPlan p)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
     };
-    begin();
-    // where a lane reads the tiles
-    const char *const k_from = ktile + half * 512;
-    const uint32_t v_even = v_slot(col) + half * (D * 16), v_odd = v_slot(32 + col) + half * (D * 16);
-
-    int buf = 0;
-    for (int t = a0; t < a1; ++t) {
-        Found found;
-        if (t + 1 < a1) found = look(codes);
-        if (t + 2 < a1) codes = load(where);
-        if (t + 3 < a1) where = find(t + 3);
-        const int pos = (t - cur.base + cur.x.tile0()) * 32;
-        const int y0 = pos + 8 * half;                   // of the lane's scores 0 to 7
-        if (__any(seen.lo < pos + 32 && seen.hi > pos)) {
-            const bool whole = __all(seen.lo <= pos && seen.hi >= pos + 32);
-            f16v z;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = 0.f;
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                const u4v k = *reinterpret_cast<const u4v *>(
-                    k_from + buf * F::kTile + s * 1024 + ((col * 16) ^ ((2 * s + half) & 7) * 64));
-                z = mfma32<FP16>(k, q[s], z);
-            }
-            if (changed) {
-                if (a.cap_log2 > 0.f) {
-                    kv_cap<16>(z, a.scale_cap, a.cap_log2);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] *= a.scale_log2;
-                }
-                if (a.slopes) {
-                    const float far = (float)(seen.at - y0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(16 * (i / 8) + i % 8)), z[i]);
-                }
-            }
-            const auto sees = [&](int i) {
-                const int at = y0 + 16 * (i / 8) + i % 8;
-                return at >= seen.lo && at < seen.hi;
-            };
-            if (!whole) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = sees(i) ? z[i] : -INFINITY;
-            }
-            float top = z[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
-            top *= scale;
-            if (__any(top > m + (kLag + kLift<FP16>))) {
-                top = fmaxf(max_halves(top) - kLift<FP16>, m);
-                m0 = top == -INFINITY ? 0.f : top;
-                const float alpha = __builtin_amdgcn_exp2f(m - m0);
-                m = top;
-                l *= alpha;
-#pragma unroll
-                for (int n = 0; n < F::F; ++n) acc[n] *= alpha;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -m0));
-            if (!whole) {                                // again: a scale of 0 gave NaN
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = sees(i) ? z[i] : 0.f;
-            }
-            float sum[4] = {z[0], z[1], z[2], z[3]};
-#pragma unroll
-            for (int i = 4; i < 16; ++i) sum[i & 3] += z[i];
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                // One 16-bit number to a weight: rounded to nearest it leaves the output
-                // off as its own last rounding does, and without the halves that a
-                // second number would double the product by.
-                u4v w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = pack2<FP16>(z[8 * s + 2 * i], z[8 * s + 2 * i + 1]);
-#pragma unroll
-                for (int n = 0; n < F::F; ++n) {
-                    const u4v v = *reinterpret_cast<const u4v *>(
-                        vtile + buf * F::kTile + s * (2 * D * 16) + (n / 2) * 1024 + (n % 2 ? v_odd : v_even));
-                    acc[n] = mfma32<FP16>(v, w, acc[n]);
-                }
-            }
-        }
-        if (t + 1 == min(cur.next, a1)) {                // the unit's end, or the share's
-            const float sum = sum_halves(l);
-            if (cur.base >= a0 && cur.next <= a1) {
-                int tt, hq;
-                if (row_of(cur.x, wave * 32 + col, &tt, &hq)) {
-                    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-                    uint16_t *const dst = o.out + (cur.x.t0 + tt) * o.out_token + hq * o.out_head + 4 * half;
-#pragma unroll
-                    for (int n = 0; n < F::F; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) =
-                                make_uint2(pack2<FP16>(acc[n][4 * i] * inv, acc[n][4 * i + 1] * inv),
-                                           pack2<FP16>(acc[n][4 * i + 2] * inv, acc[n][4 * i + 3] * inv));
-                    if (o.lse && half == 0)
-                        o.lse[(int64_t)(cur.x.t0 + tt) * heads + hq] =
-                            sum > 0.f || sum != sum ? (m + __log2f(sum)) * kLn2 : -INFINITY;
-                }
-            } else {
-                const int slot = cur.base < a0 ? 0 : 1;
-                float *const dst = p.part_o + (wg * 2 + slot) * (kRows * D) + tid;
+    // The end of the unit, or of the share.
+    const auto finish = [&]() {
+        const KvTokensArgs &all = seldom();
+        const KvTokensOut &o = all.o;
+        const float sum = sum_halves(l);
+        if (cur.base >= a0 && cur.next <= a1) {
+            int t, hq;
+            if (row_of(all.p.of.unit[cur.u], wave * 32 + col, &t, &hq)) {
+                const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                uint16_t *const dst = o.out + t * o.out_token + hq * o.out_head + 4 * half;
 #pragma unroll
                 for (int n = 0; n < F::F; ++n)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) dst[(n * 16 + i) * kThreads] = acc[n][i];
-                if (half == 0) {
-                    float *const ml = p.part_ml + (wg * 2 + slot) * (2 * kRows) + wave * 32 + col;
-                    ml[0] = m;
-                    ml[kRows] = sum;
-                }
-                if (slot == 1 && tid == 0) p.cut[wg] = make_int2(cur.u, share_of(tiles, cur.next - 1, used) - j + 1);
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) =
+                            make_uint2(pack2<FP16>(acc[n][4 * i] * inv, acc[n][4 * i + 1] * inv),
+                                       pack2<FP16>(acc[n][4 * i + 2] * inv, acc[n][4 * i + 3] * inv));
+                if (o.lse && half == 0)
+                    o.lse[(int64_t)t * all.c.heads * all.a.group + hq] =
+                        sum > 0.f || sum != sum ? (m + __log2f(sum)) * kLn2 : -INFINITY;
             }
+        } else {
+            const int64_t wg = (int64_t)h * all.p.splits + j;
+            const int slot = cur.base < a0 ? 0 : 1;
+            float *const dst = all.p.part_o + (wg * 2 + slot) * (kRows * D) + tid;
+#pragma unroll
+            for (int n = 0; n < F::F; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dst[(n * 16 + i) * kThreads] = acc[n][i];
+            if (half == 0) {
+                float *const ml = all.p.part_ml + (wg * 2 + slot) * (2 * kRows) + wave * 32 + col;
+                ml[0] = m;
+                ml[kRows] = sum;
+            }
+            if (slot == 1 && tid == 0) all.p.cut[wg] = make_int2(cur.u, share_of(tiles, cur.next - 1, used) - j + 1);
+        }
+    };
+
+    // Operand n of the products: of a tile's keys, and of its values (a step of 16 positions
+    // after the other, all features of each).
+    const char *const k_from = ktile + half * 512;
+    const uint32_t v_even = v_slot(col) + half * (D * 16), v_odd = v_slot(32 + col) + half * (D * 16);
+    const auto key_at = [&](int buf, int n) {
+        return *reinterpret_cast<const u4v *>(
+            k_from + buf * F::kTile + n * 1024 + ((col * 16) ^ ((2 * n + half) & 7) * 64));
+    };
+    const auto value_at = [&](int buf, int n) {
+        const int s = n / F::F, f = n % F::F;
+        return *reinterpret_cast<const u4v *>(vtile + buf * F::kTile + s * (2 * D * 16) + f / 2 * 1024 +
+                                              (f % 2 ? v_odd : v_even));
+    };
+    const auto scores = [&](int buf) {
+        f16v z;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) z = mfma32<FP16>(key_at(buf, n), q[n], z);
+        return z;
+    };
+
+    // The scores of tile t + 1 are under way on the matrix cores while the vector ALU works
+    // out the weights of tile t, and the product with its values while the next tiles are
+    // written: one after the other a wave would wait for each. LDS is asked long before:
+    // all keys, then a value for each key that is done with.
+    begin();
+    f16v z = scores(0);
+    lds_barrier();                                       // the keys of a0 make room for those of a0 + 2
+    int buf = 0;
+    for (int t = a0; t < a1; ++t) {
+        const bool same = t + 1 < min(cur.next, a1);     // the unit, and the share, go on
+        // operands of the next tile's scores, then of this one's values, four of them ahead
+        constexpr int N = D / 16, slots = 4;
+        static_assert(N >= slots, "operands ahead");
+        u4v kv[slots];
+        const auto operand = [&](int n) { return n < N ? key_at(buf ^ 1, n) : value_at(buf, n - N); };
+#pragma unroll
+        for (int n = 0; n < slots; ++n) kv[n] = operand(n);
+        const Found found = look(codes.k, v_codes);
+        step();
+        const int pos = (t - cur.base + cur.tile0) * 32;
+        const int y0 = pos + 8 * half;                   // of the lane's scores 0 to 7
+        const bool whole = __ballot(seen.lo <= pos && seen.hi >= pos + 32) == ~0ull;
+        const auto sees = [&](int i) {
+            const int at = y0 + 16 * (i / 8) + i % 8;
+            return at >= seen.lo && at < seen.hi;
+        };
+        if (changed) {
+            if (a.cap_log2 > 0.f) {
+                kv_cap<16>(z, a.scale_cap, a.cap_log2);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] *= a.scale_log2;
+            }
+            if (a.slopes) {
+                const float far = (float)(seen.at - y0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(16 * (i / 8) + i % 8)), z[i]);
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = sees(i) ? z[i] : -INFINITY;
+        }
+        float top = z[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
+        top *= scale;
+        if (__any(top > m + (kLag + kLift<FP16>))) {
+            top = fmaxf(max_halves(top) - kLift<FP16>, m);
+            m0 = top == -INFINITY ? 0.f : top;
+            const float alpha = __builtin_amdgcn_exp2f(m - m0);
+            m = top;
+            l *= alpha;
+#pragma unroll
+            for (int n = 0; n < F::F; ++n) acc[n] *= alpha;
+        }
+        // One 16-bit number to a weight: rounded to nearest it leaves the output off as its
+        // own last rounding does, and without the halves that a second number would double
+        // the product by.
+        u4v weight[2];
+        float sum[2] = {0.f, 0.f};
+        const auto weigh = [&](int i) {                  // scores i and i + 1
+            float w[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                w[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i + k], scale, -m0));
+                if (!whole && !sees(i + k)) w[k] = 0.f;  // again: a scale of 0 gave NaN
+                sum[k] += w[k];
+            }
+            weight[i / 8][i % 8 / 2] = pack2<FP16>(w[0], w[1]);
+        };
+        f16v next;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next[i] = 0.f;
+        if (whole) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                next = mfma32<FP16>(kv[n % slots], q[n], next);
+                kv[n % slots] = operand(n + slots);
+#pragma unroll
+                for (int i = n * 8 / N; i < (n + 1) * 8 / N; ++i) weigh(2 * i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                next = mfma32<FP16>(kv[n % slots], q[n], next);
+                kv[n % slots] = operand(n + slots);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) weigh(i);
+        }
+        l += sum[0] + sum[1];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            acc[n % F::F] = mfma32<FP16>(kv[(N + n) % slots], weight[n / F::F], acc[n % F::F]);
+            if (n + slots < N) kv[(N + n) % slots] = operand(N + n + slots);
+            if (n == 0) put_k(found, buf);
+            else if (n <= F::VS) put_v(found, buf ^ 1, n - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = N - 1; e < F::VS; ++e) put_v(found, buf ^ 1, e);
+        if (!same) {
+            finish();
             if (t + 1 < a1) {
                 advance(cur, t + 1);
                 begin();
+                next = scores(buf ^ 1);
             }
         }
-        if (t + 1 < a1) put(found, buf ^ 1);
-        __syncthreads();
+        z = next;
+        lds_barrier();
         buf ^= 1;
     }
 }
@@ -492,8 +602,9 @@ template <int D, int SUB, bool FP16>
 hipError_t launch(const KvCache &c, const KvNew &a, const KvTokensOut &o, const KvTokensPlan &p, hipStream_t s)
 {
     using F = Form<D, SUB>;
-    hipLaunchKernelGGL((kv_tokens_kernel<D, SUB, FP16>), dim3((unsigned)(c.heads * p.splits)), dim3(kThreads),
-                       F::kLds, s, c, a, o, p);
+    const KvTokensArgs args{c, a, o, p};
+    const auto kernel = c.page_log2 >= 5 ? kv_tokens_kernel<D, SUB, FP16, true> : kv_tokens_kernel<D, SUB, FP16, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(c.heads * p.splits)), dim3(kThreads), F::kLds, s, args);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL((kv_tokens_join_kernel<D, FP16>), dim3((unsigned)(c.heads * p.splits * (D / 8))),
