@@ -19,6 +19,8 @@
 // that way is joined by a second launch. A launch before says where units begin.
 #include "kv_few.h"
 
+#include <type_traits>
+
 #ifndef KV_SUB
 #define KV_SUB 4
 #endif
@@ -112,6 +114,31 @@ __device__ inline void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
+// 4, 8 or 16 bytes at a byte of LDS, `more` bytes on.
+template <int N>
+struct LdsWords {
+    typedef uint32_t type __attribute__((ext_vector_type(N / 4)));
+};
+template <>
+struct LdsWords<4> {
+    typedef uint32_t type;
+};
+
+template <typename T>
+__device__ inline T lds_get(uint32_t at, int more = 0)
+{
+    typedef const __attribute__((address_space(3))) typename LdsWords<sizeof(T)>::type *P;
+    return __builtin_bit_cast(T, *(P)((const __attribute__((address_space(3))) char *)(uintptr_t)at + more));
+}
+
+template <typename T>
+__device__ inline void lds_put(uint32_t at, int more, const T &x)
+{
+    typedef typename LdsWords<sizeof(T)>::type W;
+    typedef __attribute__((address_space(3))) W *P;
+    *(P)((__attribute__((address_space(3))) char *)(uintptr_t)at + more) = __builtin_bit_cast(W, x);
+}
+
 // ONE_PAGE: pages of 32 tokens or more, so that a tile lies on one.
 template <int D, int SUB, bool FP16, bool ONE_PAGE>
 __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
@@ -120,9 +147,8 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
     const KvCache &c = args.c;
     const KvNew &a = args.a;
     const KvTokensPlan &p = args.p;
-    extern __shared__ uint4 lds[];
-    char *const kbook = reinterpret_cast<char *>(lds), *const vbook = kbook + F::kBook;
-    char *const ktile = vbook + F::kBook, *const vtile = ktile + 2 * F::kTile;
+    // the kernel has no LDS but its dynamic one, which so begins at 0
+    constexpr uint32_t kbook = 0, vbook = F::kBook, ktile = 2 * F::kBook, vtile = ktile + 2 * F::kTile;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % c.heads, j = blockIdx.x / c.heads;
@@ -233,8 +259,10 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         const uint8_t *k, *v;
         if constexpr (ONE_PAGE) {
             const uint64_t at = page(__builtin_amdgcn_readfirstlane(w.k_page));
-            k = k_head + at + ((unsigned)w.pos & pm) * F::S + k_whole;
-            v = v_head + at + ((unsigned)w.pos & pm) + v_whole;
+            const uint8_t *const k_tile = k_head + (at + ((unsigned)w.pos & pm) * F::S);
+            const uint8_t *const v_tile = v_head + (at + ((unsigned)w.pos & pm));
+            k = k_tile + k_whole;
+            v = v_tile + v_whole;
         } else {
             k = k_head + page(w.k_page) + (((unsigned)w.pos + key) & pm) * F::S + k_lane;
             v = v_head + page(w.v_page) + (((unsigned)w.pos + vpos) & pm) + v_lane;
@@ -260,15 +288,13 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
             KvEntry<SUB> e[8 / SUB];
 #pragma unroll
             for (int i = 0; i < 8 / SUB; ++i)
-                e[i] = *reinterpret_cast<const KvEntry<SUB> *>(
-                    kbook + (k >> (8 * i) & 255) * F::kRow + chunk * 16 + i * (SUB * 2));
+                e[i] = lds_get<KvEntry<SUB>>((k >> (8 * i) & 255) * F::kRow + (kbook + chunk * 16), i * (SUB * 2));
             __builtin_memcpy(&f.k, e, 16);
         }
         if (looks_v) {
 #pragma unroll
             for (int i = 0; i < F::NP; ++i)
-                f.v[i] = *reinterpret_cast<const KvEntry<F::VS> *>(
-                    vbook + (v >> (8 * i) & 255) * F::kRow + gran * (F::VS * 2));
+                f.v[i] = lds_get<KvEntry<F::VS>>((v >> (8 * i) & 255) * F::kRow + (vbook + gran * (F::VS * 2)));
         }
         return f;
     };
@@ -276,11 +302,14 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
     // and 3 in each other's place) at 512 r + 16 m, bits 6 to 8 turned by r so that a wave
     // that writes reaches all banks; values as runs of 8 positions, run r of feature f at
     // 16 D r + 16 f, the feature's last two bits turned by the two above its fourth.
-    const uint32_t k_to = chunk * 512 + ((((key & ~12) | (key & 4) << 1 | (key & 8) >> 1) * 16) ^ (chunk & 7) * 64);
+    const uint32_t k_to = ktile + chunk * 512 + ((((key & ~12) | (key & 4) << 1 | (key & 8) >> 1) * 16) ^ (chunk & 7) * 64);
     const auto v_slot = [](int f) { return (f ^ ((f >> 4) & 3)) * 16; };
-    const uint32_t v_to = vpos / 8 * (D * 16) + (vpos & 7) * 2;
+    uint32_t v_to[F::VS];
+#pragma unroll
+    for (int e = 0; e < F::VS; ++e)
+        v_to[e] = vtile + vpos / 8 * (D * 16) + (vpos & 7) * 2 + v_slot(gran * F::VS + e);
     const auto put_k = [&](const Found &f, int buf) {
-        if (looks_k) *reinterpret_cast<KvEntry<8> *>(ktile + buf * F::kTile + k_to) = f.k;
+        if (looks_k) lds_put(k_to, buf * F::kTile, f.k);
     };
     // feature e of the granule's
     const auto put_v = [&](const Found &f, int buf, int e) {
@@ -290,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         for (int i = 0; i < F::NP / 2; ++i)
             x.w[i] = __builtin_amdgcn_perm(f.v[2 * i + 1].w[e / 2], f.v[2 * i].w[e / 2],
                                            e % 2 ? 0x07060302u : 0x05040100u);
-        *reinterpret_cast<KvEntry<F::NP> *>(vtile + buf * F::kTile + v_to + v_slot(gran * F::VS + e)) = x;
+        lds_put(v_to[e], buf * F::kTile, x);
     };
 
     Where where = find(a0);
@@ -302,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         static_assert(D * 32 % kThreads == 0, "whole rounds");
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
-            char *const book = kind ? vbook : kbook;
+            const uint32_t book = kind ? vbook : kbook;
             if (c.K == 256) {
                 // 16 bytes to a load: 4 runs in each of 16 sub-vectors to a wave
                 uint4 reg[rounds];
@@ -318,14 +347,14 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
                     __builtin_memcpy(e, &reg[i], 16);
 #pragma unroll
                     for (int x = 0; x < per16; ++x)
-                        *reinterpret_cast<KvEntry<SUB> *>(book + (code + x) * F::kRow + s * (SUB * 2)) = e[x];
+                        lds_put(book + (code + x) * F::kRow + s * (SUB * 2), 0, e[x]);
                 }
             } else {
                 for (int i = tid; i < F::S * 256; i += kThreads) {
                     const int s = i % F::S, code = i / F::S;
                     KvEntry<SUB> e{};
                     if (code < c.K) e = kv_load<SUB>(books[kind] + (s * c.K + code) * SUB);
-                    *reinterpret_cast<KvEntry<SUB> *>(book + code * F::kRow + s * (SUB * 2)) = e;
+                    lds_put(book + code * F::kRow + s * (SUB * 2), 0, e);
                 }
             }
         }
@@ -354,7 +383,8 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
     }
     __syncthreads();
 
-    const bool changed = a.cap_log2 > 0.f || a.slopes;   // scores are more than products
+    // scores are more than products (times 0, -infinity in an unseen place would be NaN)
+    const bool changed = a.cap_log2 > 0.f || a.slopes || a.scale_log2 == 0.f;
     const float scale = changed ? 1.f : fabsf(a.scale_log2);
     u4v q[D / 16];
     f16v acc[F::F];
@@ -424,16 +454,14 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
 
     // Operand n of the products: of a tile's keys, and of its values (a step of 16 positions
     // after the other, all features of each).
-    const char *const k_from = ktile + half * 512;
-    const uint32_t v_even = v_slot(col) + half * (D * 16), v_odd = v_slot(32 + col) + half * (D * 16);
-    const auto key_at = [&](int buf, int n) {
-        return *reinterpret_cast<const u4v *>(
-            k_from + buf * F::kTile + n * 1024 + ((col * 16) ^ ((2 * n + half) & 7) * 64));
-    };
+    uint32_t k_from[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) k_from[n] = ktile + half * 512 + ((col * 16) ^ (2 * n + half) * 64);
+    const uint32_t v_even = vtile + v_slot(col) + half * (D * 16), v_odd = vtile + v_slot(32 + col) + half * (D * 16);
+    const auto key_at = [&](int buf, int n) { return lds_get<u4v>(k_from[n % 4], buf * F::kTile + n * 1024); };
     const auto value_at = [&](int buf, int n) {
         const int s = n / F::F, f = n % F::F;
-        return *reinterpret_cast<const u4v *>(vtile + buf * F::kTile + s * (2 * D * 16) + f / 2 * 1024 +
-                                              (f % 2 ? v_odd : v_even));
+        return lds_get<u4v>(f % 2 ? v_odd : v_even, buf * F::kTile + s * (2 * D * 16) + f / 2 * 1024);
     };
     const auto scores = [&](int buf) {
         f16v z;
@@ -448,11 +476,9 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
     // out the weights of tile t, and the product with its values while the next tiles are
     // written: one after the other a wave would wait for each. LDS is asked long before:
     // all keys, then a value for each key that is done with.
-    begin();
-    f16v z = scores(0);
-    lds_barrier();                                       // the keys of a0 make room for those of a0 + 2
-    int buf = 0;
-    for (int t = a0; t < a1; ++t) {
+    // Tile t, whose keys' and values' buffer B is: the scores z of it, those of t + 1 in next.
+    const auto turn = [&](auto B, int t, f16v &z, f16v &next) {
+        constexpr int buf = decltype(B)::value;
         const bool same = t + 1 < min(cur.next, a1);     // the unit, and the share, go on
         // operands of the next tile's scores, then of this one's values, four of them ahead
         constexpr int N = D / 16, slots = 4;
@@ -466,10 +492,6 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         const int pos = (t - cur.base + cur.tile0) * 32;
         const int y0 = pos + 8 * half;                   // of the lane's scores 0 to 7
         const bool whole = __ballot(seen.lo <= pos && seen.hi >= pos + 32) == ~0ull;
-        const auto sees = [&](int i) {
-            const int at = y0 + 16 * (i / 8) + i % 8;
-            return at >= seen.lo && at < seen.hi;
-        };
         if (changed) {
             if (a.cap_log2 > 0.f) {
                 kv_cap<16>(z, a.scale_cap, a.cap_log2);
@@ -486,7 +508,10 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         }
         if (!whole) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = sees(i) ? z[i] : -INFINITY;
+            for (int i = 0; i < 16; ++i) {
+                const int at = y0 + 16 * (i / 8) + i % 8;
+                z[i] = at >= seen.lo && at < seen.hi ? z[i] : -INFINITY;
+            }
         }
         float top = z[0];
 #pragma unroll
@@ -511,31 +536,19 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 w[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i + k], scale, -m0));
-                if (!whole && !sees(i + k)) w[k] = 0.f;  // again: a scale of 0 gave NaN
                 sum[k] += w[k];
             }
             weight[i / 8][i % 8 / 2] = pack2<FP16>(w[0], w[1]);
         };
-        f16v next;
 #pragma unroll
         for (int i = 0; i < 16; ++i) next[i] = 0.f;
-        if (whole) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                next = mfma32<FP16>(kv[n % slots], q[n], next);
-                kv[n % slots] = operand(n + slots);
+        for (int n = 0; n < N; ++n) {
+            next = mfma32<FP16>(kv[n % slots], q[n], next);
+            kv[n % slots] = operand(n + slots);
 #pragma unroll
-                for (int i = n * 8 / N; i < (n + 1) * 8 / N; ++i) weigh(2 * i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                next = mfma32<FP16>(kv[n % slots], q[n], next);
-                kv[n % slots] = operand(n + slots);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) weigh(i);
+            for (int i = n * 8 / N; i < (n + 1) * 8 / N; ++i) weigh(2 * i);
+            __builtin_amdgcn_sched_barrier(0);
         }
         l += sum[0] + sum[1];
 #pragma unroll
@@ -556,9 +569,17 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
                 next = scores(buf ^ 1);
             }
         }
-        z = next;
         lds_barrier();
-        buf ^= 1;
+    };
+    begin();
+    f16v z[2];
+    z[0] = scores(0);
+    lds_barrier();                                       // the keys of a0 make room for those of a0 + 2
+    for (int t = a0;;) {
+        turn(std::integral_constant<int, 0>{}, t, z[0], z[1]);
+        if (++t == a1) break;
+        turn(std::integral_constant<int, 1>{}, t, z[1], z[0]);
+        if (++t == a1) break;
     }
 }
 
@@ -703,11 +724,9 @@ KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 {
     KvTokensPlan p{};
     p.units = (int)(a.seqs + a.tokens * a.group / kRows);
-    // with 64 features two workgroups to a CU, else the centres leave room for one
-    const int64_t wgs = (c.dim == 64 ? 2 : 1) * kCUs;
     const int64_t span = ((int64_t)a.table_pages << c.page_log2) / 32 + 2;
     const int64_t most = (p.units * span + kShare - 1) / kShare;
-    int64_t splits = wgs / c.heads;
+    int64_t splits = kCUs / c.heads;                     // one workgroup to a CU: registers allow no more
     if (splits > most) splits = most;
     p.splits = splits < 1 ? 1 : (int)splits;
     size_t at = 0;
