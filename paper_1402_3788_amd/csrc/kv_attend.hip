@@ -305,15 +305,19 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
             // the lanes' sequences, then the lanes' units
             KvSeq s{};
             if (lane < a.seqs) s = kv_seq(c, a, lane);
-            const int upto = wave_scan((s.n * a.group + nq - 1) / nq);
-            seqs = __builtin_amdgcn_readlane(upto, 63);
-            int b = 0;
-            for (int i = 0; i < a.seqs; ++i) b += __builtin_amdgcn_readlane(upto, i) <= lane;
-            const int before = __shfl(upto, max(b - 1, 0));
-            const KvSeq of{__shfl(s.t0, b & 63), __shfl(s.n, b & 63), __shfl(s.len, b & 63),
-                           __shfl(s.prefix, b & 63)};
+            int b = lane, before = lane;
+            if (__any(lane < a.seqs && (unsigned)(s.n * a.group - 1) >= (unsigned)nq)) {
+                const int upto = wave_scan((s.n * a.group + nq - 1) / nq);
+                seqs = __builtin_amdgcn_readlane(upto, 63);
+                b = 0;
+                for (int i = 0; i < a.seqs; ++i) b += __builtin_amdgcn_readlane(upto, i) <= lane;
+                before = __shfl(upto, max(b - 1, 0));
+                if (b == 0) before = 0;
+                s = KvSeq{__shfl(s.t0, b & 63), __shfl(s.n, b & 63), __shfl(s.len, b & 63),
+                          __shfl(s.prefix, b & 63)};
+            }                                            // else a unit to every sequence
             KvUnit x{};
-            if (lane < seqs) x = kv_unit(a, of, b, (lane - (b ? before : 0)) * nq, nq);
+            if (lane < seqs) x = kv_unit(a, s, b, (lane - before) * nq, nq);
             const int n = x.tiles();
             my_span = Span{x.lo, x.hi};
             my_next = wave_scan(n);

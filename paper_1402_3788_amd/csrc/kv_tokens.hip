@@ -691,20 +691,48 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
     if (tid == 0) seq_first[a.seqs] = units;
     __syncthreads();
     units = min(units, most);                            // more only if bounds descend
+    const auto seq_of = [&](int u) {
+        int b = 0, end = a.seqs;                         // the last b with seq_first[b] <= u
+        while (end - b > 1) {
+            const int mid = (b + end) >> 1;
+            if (seq_first[mid] <= u) b = mid;
+            else end = mid;
+        }
+        return b;
+    };
+    if (a.starts) {
+        // what a token sees says nothing of the next one's: a unit's over the lanes of a wave
+        for (int u = wave; u < units; u += 16) {
+            const int b = seq_of(u), row0 = (u - seq_first[b]) * rows;
+            const KvSeq s = kv_seq(c, a, b);
+            const int i1 = (min(row0 + rows, s.n * a.group) - 1) / a.group;
+            int lo = INT32_MAX, hi = 0;
+            for (int i = row0 / a.group + lane; i <= i1; i += kWave) {
+                const KvSeen y = kv_seen(a, s, i);
+                if (y.hi > 0) lo = min(lo, y.lo);
+                hi = max(hi, y.hi);
+            }
+            for (int k = 1; k < kWave; k *= 2) {
+                lo = min(lo, __shfl_xor(lo, k));
+                hi = max(hi, __shfl_xor(hi, k));
+            }
+            if (lane == 0)
+                to.unit[u] = KvUnit{b, row0, s.t0, s.n, s.len, s.prefix, lo < hi ? lo : 0, lo < hi ? hi : 0};
+        }
+        __syncthreads();
+    }
     int tiles = 0;
     for (int u0 = 0; u0 < units; u0 += 1024) {
         const int u = u0 + tid;
         KvUnit x{};
         if (u < units) {
-            int b = 0, end = a.seqs;                     // the last b with seq_first[b] <= u
-            while (end - b > 1) {
-                const int mid = (b + end) >> 1;
-                if (seq_first[mid] <= u) b = mid;
-                else end = mid;
+            if (a.starts) {
+                x = to.unit[u];
+            } else {
+                const int b = seq_of(u);
+                x = kv_unit(a, kv_seq(c, a, b), b, (u - seq_first[b]) * rows, rows);
+                to.unit[u] = x;
             }
-            const KvSeq s = kv_seq(c, a, b);
-            x = kv_unit(a, s, b, (u - seq_first[b]) * rows, rows);
-            to.unit[u] = x;
         }
         const int n1 = x.tiles();
         int all;
