@@ -13,7 +13,7 @@ namespace lloyd {
 
 namespace {
 
-constexpr int kWaves = 12;
+constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kSeqs = 1024;          // sequences that are kept in LDS
 
@@ -31,6 +31,25 @@ __device__ inline void load_codes(uint32_t (&dst)[(N + 3) / 4], const uint8_t *s
     constexpr int align = N % 16 == 0 ? 16 : N % 8 == 0 ? 8 : N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
     dst[(N - 1) / 4] = 0;
     __builtin_memcpy(dst, __builtin_assume_aligned(src, align), N);
+}
+
+// x of another lane of the row of 16.
+template <int DPP>
+__device__ inline float moved(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), DPP, 0xF, 0xF, true));
+}
+
+// The lanes of which `up` holds keep sums N to 2 N - 1, the others the first N, and get
+// what the lane that DPP names has of them.
+template <int N, int DPP>
+__device__ inline void fold(float (&sum)[16], bool up)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float mine = up ? sum[i + N] : sum[i], theirs = up ? sum[i] : sum[i + N];
+        sum[i] = mine + moved<DPP>(theirs);
+    }
 }
 
 template <int D, int SUB, bool FP16>
@@ -205,31 +224,45 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     ++next.t;
     bool more = settle(next);
     if (more) ahead = find(next);
-    u4v q[D / 16];
-    KvSeen seen{0, 0, 0};
-    float base = 0.f, slope = 0.f;
-    // The 32 rows from r0 on.
-    const auto begin = [&](const KvSeq &s, int r0) {
-        const int row = r0 + col, tok = (int)((unsigned)row / (unsigned)a.group);
-        const int hq = h * a.group + (int)((unsigned)row % (unsigned)a.group);
-        const bool there = row < s.n * a.group;
-        seen = KvSeen{0, 0, 0};
-        base = INFINITY;
-        slope = 0.f;
+    // 32 rows: a lane has half the features of row `col` of them, what that sees and its
+    // logarithm, and the number of its token and head in the sequence.
+    struct Rows {
+        u4v q[D / 16];
+        KvSeen seen;
+        float base, slope;
+    };
+    Rows cur, coming;
+    int loaded = -1;                                     // the sequence whose only rows are in cur
+    const int tokens32 = 32 / a.group, heads32 = 32 % a.group;
+    int tok = 0, hd = 0;                                 // of the next block's row
+    // the sequence's first rows come next
+    const auto rewind = [&]() {
+        tok = (int)((unsigned)col / (unsigned)a.group);
+        hd = (int)((unsigned)col % (unsigned)a.group);
+    };
+    const auto begin = [&](Rows &x, const KvSeq &s) {
+        const bool there = tok < s.n;
+        const int hq = h * a.group + hd;
+        x.seen = KvSeen{0, 0, 0};
+        x.base = INFINITY;
+        x.slope = 0.f;
         if (there) {
-            seen = kv_seen(a, s, tok);
-            base = w.lse[(int64_t)(s.t0 + tok) * heads + hq] * kLog2e;
-            if (base == -INFINITY) seen.lo = seen.hi = 0;
-            if (a.slopes) slope = a.slopes[hq] * kLog2e;
+            x.seen = kv_seen(a, s, tok);
+            x.base = w.lse[(int64_t)(s.t0 + tok) * heads + hq] * kLog2e;
+            if (x.base == -INFINITY) x.seen.lo = x.seen.hi = 0;
+            if (a.slopes) x.slope = a.slopes[hq] * kLog2e;
         }
-        const uint16_t *const src = a.q + (s.t0 + tok) * a.q_token + hq * a.q_head + half * (D / 2);
+        // behind the last row: some row, whose weights are exp(-infinity)
+        const uint16_t *const src = a.q + (s.t0 + min(tok, s.n - 1)) * a.q_token + hq * a.q_head + half * (D / 2);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            q[i] = u4v{0, 0, 0, 0};
-            if (there) q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
+        for (int i = 0; i < D / 16; ++i) x.q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
+        tok += tokens32;
+        hd += heads32;
+        if (hd >= a.group) {
+            hd -= a.group;
+            ++tok;
         }
     };
-    int loaded = -1;                                     // the sequence whose only rows are in q
     for (;;) {
         // the keys: a lane has features [half D / 2, + D / 2) of position col
         u4v k[D / 16];
@@ -253,18 +286,16 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             more = settle(next);
             if (more) ahead = find(next);
         }
-        const int rows = s.n * a.group;
         float sum[16] = {};
-        for (int r0 = 0; r0 < rows; r0 += 32) {
-            if (loaded != b) begin(s, r0);
-            loaded = rows <= 32 ? b : -1;
-            if (!__any(seen.lo < pos + 32 && seen.hi > pos)) continue;
-            const bool whole = __all(seen.lo <= pos && seen.hi >= pos + 32);
+        const auto block = [&](const Rows &x) {
+            const KvSeen seen = x.seen;
+            if (!__any(seen.lo < pos + 32 && seen.hi > pos)) return;
+            const bool whole = __ballot(seen.lo <= pos && seen.hi >= pos + 32) == ~0ull;
             f16v z;
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) z = mfma32<FP16>(k[i], q[i], z);
+            for (int i = 0; i < D / 16; ++i) z = mfma32<FP16>(k[i], x.q[i], z);
             const int y0 = pos + 4 * half;               // score i is position y0 + 8 (i / 4) + i % 4
             float scale = a.scale_log2;
             if (a.cap_log2 > 0.f) {
@@ -275,11 +306,11 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
                 const float far = (float)(seen.at - y0);
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale);
+                    z[i] = __builtin_fmaf(-x.slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale);
                 scale = 1.f;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -base));
+            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -x.base));
             if (whole) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum[i] += z[i];
@@ -290,20 +321,35 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
                     sum[i] += p >= seen.lo && p < seen.hi ? z[i] : 0.f;
                 }
             }
+        };
+        // a block's rows are asked for while the one before is worked on; a single block's stay
+        const int rows = s.n * a.group;
+        if (loaded != b) {
+            rewind();
+            begin(cur, s);
         }
-        // Over the lanes of a half, halving what each holds.
-        int place = 0;
-#pragma unroll
-        for (int n = 8, m = 16; n >= 1; n /= 2, m /= 2) {
-            const bool up = lane & m;
-#pragma unroll
-            for (int i = 0; i < n; ++i) {
-                const float mine = up ? sum[i + n] : sum[i], theirs = up ? sum[i] : sum[i + n];
-                sum[i] = mine + __shfl_xor(theirs, m);
-            }
-            place += up ? n : 0;
+        loaded = rows <= 32 ? b : -1;
+#pragma unroll 1
+        for (int r0 = 32;; r0 += 32) {
+            const bool two = r0 < rows;
+            if (two) begin(coming, s);
+            block(cur);
+            if (!two) break;
+            cur = coming;
         }
-        sum[0] += __shfl_xor(sum[0], 1);
+        // Over the 32 lanes of a half, halving what each holds (rows of 16 exchange, then
+        // lanes 8, 7, 2 and 1 away): place i of the sums in the end is 8 bit 4 + 4 bit 3 +
+        // 2 bit 2 + bit 1 of the lane.
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum[i]), __float_as_uint(sum[i + 8]), false, false);
+            sum[i] = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+        }
+        fold<4, 0x128>(sum, lane & 8);                   // row_ror:8
+        fold<2, 0x141>(sum, lane & 4);                   // row_half_mirror
+        fold<1, 0x4E>(sum, lane & 2);                    // quad_perm:[2,3,0,1]
+        sum[0] += moved<0xB1>(sum[0]);                   // quad_perm:[1,0,3,2]
+        const int place = (lane & 16) / 2 + (lane & 8) / 2 + (lane & 4) / 2 + (lane & 2) / 2;
         const int p = pos + 4 * half + 8 * (place / 4) + place % 4;
         if (!(lane & 1) && p < w.positions) {
             float *const to = w.weights + b * w.weights_seq + wrow + p;
