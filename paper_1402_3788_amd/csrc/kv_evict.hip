@@ -18,12 +18,11 @@ constexpr int kMove = 256;           // threads that move
 constexpr int kSpan = 768;           // positions between a tile's first and last that LDS holds
 constexpr int kParts = 4;            // shares of a value's codes, in place each moved on its own
 
-// Weights as whole numbers of the same order; NaN below all.
+// Weights as whole numbers of the same order; NaN, 1, below all. 0 is no weight's.
 __device__ inline uint32_t order_of(float w)
 {
-    if (w != w) return 0;
     const uint32_t u = __float_as_uint(w + 0.f);         // -0 is 0
-    return u >> 31 ? ~u : u | 0x80000000u;
+    return w != w ? 1u : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 __device__ inline int length_of(const KvCache &c, const KvEvict &e, int b)
@@ -40,8 +39,8 @@ struct PickLds {
     int found[2];
 };
 
-// The positions [from, to) of a row, wave after wave and in each 64 at a time: f(i,
-// whether i is in the row, the order of its weight).
+// The positions [from, to) of a row, wave after wave and in each 64 at a time: f(i, the
+// order of its weight), of 64 whole ones that may go beyond `to`, where that is 0.
 template <int HELD, typename G, typename F>
 __device__ inline void each_of(int from, int to, const uint32_t (&held)[HELD ? HELD : 1], const G &order_at, const F &f)
 {
@@ -51,12 +50,11 @@ __device__ inline void each_of(int from, int to, const uint32_t (&held)[HELD ? H
 #pragma unroll
         for (int r = 0; r < HELD; ++r) {
             const int i = w0 + r * kWave + lane;
-            if (r * kWave < each && w0 + r * kWave < to) f(i, i < to, held[r]);
+            if (r * kWave < each && w0 + r * kWave < to) f(i, held[r]);
         }
     } else {
         for (int i = w0 + lane; i - lane < min(w0 + each, to); i += kWave) {
-            const bool in = i < min(w0 + each, to);
-            f(i, in, in ? order_at(i) : 0u);
+            f(i, i < min(w0 + each, to) ? order_at(i) : 0u);
         }
     }
 }
@@ -82,8 +80,16 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
         const uint32_t bins = digit == 2 ? 1023u : 2047u;
         reinterpret_cast<int4 *>(lds.counts)[tid] = make_int4(0, 0, 0, 0);
         __syncthreads();
-        each_of<HELD>(from, to, held, order_at, [&](int, bool in, uint32_t u) {
-            if (in && (u & mask) == last) atomicAdd(&lds.counts[u >> shift & bins], 1);
+        each_of<HELD>(from, to, held, order_at, [&](int, uint32_t u) {
+            // many weights may be alike: what the first lane counts is counted at once for all
+            const bool counts = (u & mask) == last;
+            const uint64_t some = __ballot(counts);
+            if (!some) return;
+            const int lead = __builtin_ctzll(some), bin = (int)(u >> shift & bins);
+            const int of = __builtin_amdgcn_readlane(bin, lead);
+            const uint64_t alike = __ballot(counts && bin == of);
+            if (lane == lead) atomicAdd(&lds.counts[of], __popcll(alike));
+            if (counts && bin != of) atomicAdd(&lds.counts[bin], 1);
         });
         __syncthreads();
         // thread t has bins 4 t to 4 t + 3; how many lie above those
@@ -117,9 +123,9 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
     }
     // All above `last`, and the first `left` of those alike.
     int gt = 0, eq = 0;
-    each_of<HELD>(from, to, held, order_at, [&](int, bool in, uint32_t u) {
-        gt += __popcll(__ballot(in && u > last));
-        eq += __popcll(__ballot(in && u == last));
+    each_of<HELD>(from, to, held, order_at, [&](int, uint32_t u) {
+        gt += __popcll(__ballot(u > last));
+        eq += __popcll(__ballot(u == last));
     });
     if (lane == 0) {
         lds.wave_sum[wave] = gt;
@@ -134,9 +140,9 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
     }
     at += min(alike, left);
     const uint64_t below = (1ull << lane) - 1;
-    each_of<HELD>(from, to, held, order_at, [&](int i, bool in, uint32_t u) {
-        const uint64_t same = __ballot(in && u == last);
-        const bool take = in && (u > last || (u == last && alike + __popcll(same & below) < left));
+    each_of<HELD>(from, to, held, order_at, [&](int i, uint32_t u) {
+        const uint64_t same = __ballot(u == last);
+        const bool take = u > last || (u == last && alike + __popcll(same & below) < left);
         const uint64_t taken = __ballot(take);
         if (take) out[at + __popcll(taken & below)] = i;
         at += __popcll(taken);
