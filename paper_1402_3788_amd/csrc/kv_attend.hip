@@ -729,7 +729,7 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
             if (t + 1 < a1) load_v(coming);
             if constexpr (FEW) {
                 if (a.cap_log2 > 0.f) {
-                    kv_cap<8>(z, a.scale_cap, a.cap_log2);
+                    kv_cap<8>(z, a);
                 } else if (changed) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) z[i] *= a.scale_log2;

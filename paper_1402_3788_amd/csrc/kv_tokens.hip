@@ -494,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         const bool whole = __ballot(seen.lo <= pos && seen.hi >= pos + 32) == ~0ull;
         if (changed) {
             if (a.cap_log2 > 0.f) {
-                kv_cap<16>(z, a.scale_cap, a.cap_log2);
+                kv_cap<16>(z, a);
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) z[i] *= a.scale_log2;
@@ -542,6 +542,8 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
         };
 #pragma unroll
         for (int i = 0; i < 16; ++i) next[i] = 0.f;
+        // the wave that has its products to give goes first
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             next = mfma32<FP16>(kv[n % slots], q[n], next);
@@ -551,6 +553,7 @@ __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)
             __builtin_amdgcn_sched_barrier(0);
         }
         l += sum[0] + sum[1];
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             acc[n % F::F] = mfma32<FP16>(kv[(N + n) % slots], weight[n / F::F], acc[n % F::F]);

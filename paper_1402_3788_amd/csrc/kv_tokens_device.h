@@ -102,22 +102,23 @@ __device__ inline KvSeen kv_seen(const KvNew &a, const KvSeq &s, int i)
     return x;
 }
 
-// cap * tanh(scale * z / cap) to base 2, of a lane's N products z. Up to 5/8 tanh x = x + x^3 P(x^2), P of degree 4 fitted to it there (off
-// by 2^-27 of it); beyond 1 - 2 / (1 + e^2x), which for small x would be off by 2^-23 of 1,
-// 4e-6 of a score for a cap of 50. Most scores are far below their cap: a wave whose
-// scores all are saves the exponentials.
+// cap * tanh(scale * z / cap) to base 2, of a lane's N products z. With x = scale * z / cap,
+// up to 5/8 tanh x = x + x^3 P(x^2), P of degree 4 fitted to it there (off by 2^-27 of it);
+// beyond 1 - 2 / (1 + e^2x), which for small x would be off by 2^-23 of 1, 4e-6 of a score for
+// a cap of 50. Most scores are far below their cap: a wave whose scores all are saves the
+// exponentials.
 template <int N, typename V>
-__device__ inline void kv_cap(V &z, float scale_cap, float cap_log2)
+__device__ inline void kv_cap(V &z, const KvNew &a)
 {
     float x[N], most = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        x[i] = z[i] * scale_cap;
+        x[i] = z[i] * a.scale_cap;
         most = fmaxf(most, fabsf(x[i]));
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float t = x[i] * x[i], y = cap_log2 * x[i];
+        const float t = x[i] * x[i], y = a.cap_log2 * x[i];
         float p = __builtin_fmaf(t, -0.0057036951f, 0.020637562f);
         p = __builtin_fmaf(t, p, -0.053739071f);
         p = __builtin_fmaf(t, p, 0.13331431f);
@@ -128,7 +129,7 @@ __device__ inline void kv_cap(V &z, float scale_cap, float cap_log2)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float e = __builtin_amdgcn_exp2f(x[i] * (2.f * kLog2e));
-            const float far = cap_log2 - 2.f * cap_log2 * __builtin_amdgcn_rcpf(1.f + e);
+            const float far = a.cap_log2 - 2.f * a.cap_log2 * __builtin_amdgcn_rcpf(1.f + e);
             z[i] = fabsf(x[i]) <= 0.625f ? z[i] : far;
         }
     }

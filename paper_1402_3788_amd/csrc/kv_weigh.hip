@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             const int y0 = pos + 4 * half;               // score i is position y0 + 8 (i / 4) + i % 4
             float scale = a.scale_log2;
             if (a.cap_log2 > 0.f) {
-                kv_cap<16>(z, a.scale_cap, a.cap_log2);
+                kv_cap<16>(z, a);
                 scale = 1.f;
             }
             if (a.slopes) {
