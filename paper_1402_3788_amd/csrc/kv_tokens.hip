@@ -114,31 +114,6 @@ __device__ inline void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-// 4, 8 or 16 bytes at a byte of LDS, `more` bytes on.
-template <int N>
-struct LdsWords {
-    typedef uint32_t type __attribute__((ext_vector_type(N / 4)));
-};
-template <>
-struct LdsWords<4> {
-    typedef uint32_t type;
-};
-
-template <typename T>
-__device__ inline T lds_get(uint32_t at, int more = 0)
-{
-    typedef const __attribute__((address_space(3))) typename LdsWords<sizeof(T)>::type *P;
-    return __builtin_bit_cast(T, *(P)((const __attribute__((address_space(3))) char *)(uintptr_t)at + more));
-}
-
-template <typename T>
-__device__ inline void lds_put(uint32_t at, int more, const T &x)
-{
-    typedef typename LdsWords<sizeof(T)>::type W;
-    typedef __attribute__((address_space(3))) W *P;
-    *(P)((__attribute__((address_space(3))) char *)(uintptr_t)at + more) = __builtin_bit_cast(W, x);
-}
-
 // ONE_PAGE: pages of 32 tokens or more, so that a tile lies on one.
 template <int D, int SUB, bool FP16, bool ONE_PAGE>
 __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)

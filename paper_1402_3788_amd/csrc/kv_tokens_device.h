@@ -37,11 +37,29 @@ __device__ inline uint32_t pack2(float a, float b)
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2v));
 }
 
-// x of the lane 32 away.
-__device__ inline float other_half(float x)
+// 4, 8 or 16 bytes at a byte of LDS, `more` bytes on.
+template <int N>
+struct LdsWords {
+    typedef uint32_t type __attribute__((ext_vector_type(N / 4)));
+};
+template <>
+struct LdsWords<4> {
+    typedef uint32_t type;
+};
+
+template <typename T>
+__device__ inline T lds_get(uint32_t at, int more = 0)
 {
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float((threadIdx.x & 32) ? both[0] : both[1]);
+    typedef const __attribute__((address_space(3))) typename LdsWords<sizeof(T)>::type *P;
+    return __builtin_bit_cast(T, *(P)((const __attribute__((address_space(3))) char *)(uintptr_t)at + more));
+}
+
+template <typename T>
+__device__ inline void lds_put(uint32_t at, int more, const T &x)
+{
+    typedef typename LdsWords<sizeof(T)>::type W;
+    typedef __attribute__((address_space(3))) W *P;
+    *(P)((__attribute__((address_space(3))) char *)(uintptr_t)at + more) = __builtin_bit_cast(W, x);
 }
 
 // The larger, or the sum, of a lane's and that of the lane 32 away.

@@ -9,12 +9,15 @@
 // they bound it, for many the exponentials do.
 #include "kv_tokens_device.h"
 
+#include <type_traits>
+
 namespace lloyd {
 
 namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
+constexpr int kAhead = 4;            // tiles whose codes are under way to a wave
 constexpr int kSeqs = 1024;          // sequences that are kept in LDS
 
 
@@ -31,6 +34,16 @@ __device__ inline void load_codes(uint32_t (&dst)[(N + 3) / 4], const uint8_t *s
     constexpr int align = N % 16 == 0 ? 16 : N % 8 == 0 ? 8 : N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
     dst[(N - 1) / 4] = 0;
     __builtin_memcpy(dst, __builtin_assume_aligned(src, align), N);
+}
+
+// base + code n times the size of an entry; base has no bits below 256 entries.
+template <int SUB>
+__device__ inline uint32_t code_at(const uint32_t *w, int n, uint32_t base)
+{
+    constexpr int shift = SUB == 2 ? 2 : SUB == 4 ? 3 : 4;
+    const int low = 8 * (n & 3);
+    const uint32_t at = low < shift ? w[n >> 2] << (shift - low) : w[n >> 2] >> (low - shift);
+    return (at & (255u << shift)) | base;
 }
 
 // x of another lane of the row of 16.
@@ -57,10 +70,11 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
 {
     using F = Form<D, SUB>;
     extern __shared__ uint4 lds[];
+    // the kernel has no LDS but its dynamic one, which so begins at 0
     char *const book = reinterpret_cast<char *>(lds);
-    int64_t *const first = reinterpret_cast<int64_t *>(book + F::kBook); // [seqs + 1]
-    __shared__ int64_t wave_sum[kWaves];
-    __shared__ KvSeq seqs[kSeqs];
+    KvSeq *const seqs = reinterpret_cast<KvSeq *>(book + F::kBook);      // [kSeqs]
+    unsigned *const wave_sum = reinterpret_cast<unsigned *>(seqs + kSeqs);       // [kWaves]
+    unsigned *const first = wave_sum + kWaves;                           // [seqs + 1]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % c.heads, j = blockIdx.x / c.heads;
@@ -92,46 +106,45 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     const auto tiles_of = [&](const KvSeq &s) {
         return s.n ? max(((min(s.len, span) + 31) >> 5) - tile0_of(s), 0) : 0;
     };
-    const auto work_of = [&](const KvSeq &s) { return 2 + (s.n * a.group + 31) / 32; };
-    int64_t all;
+    const auto work_of = [&](const KvSeq &s) { return 2u + (unsigned)(s.n * a.group + 31) / 32; };
+    // (all of it below 2^32: ten times what the entry point lets be 2^28)
+    unsigned all;
     {
         const int per = (a.seqs + kThreads - 1) / kThreads;
-        int64_t sum = 0;
+        unsigned sum = 0;
         for (int k = 0; k < per; ++k) {
             const int b = tid * per + k;
             if (b >= a.seqs) break;
             const KvSeq s = kv_seq(c, a, b);
-            sum += (int64_t)tiles_of(s) * work_of(s);
+            sum += (unsigned)tiles_of(s) * work_of(s);
             if (b < kSeqs) seqs[b] = s;
         }
-        int64_t upto = sum;
-#pragma unroll
-        for (int k = 1; k < kWave; k *= 2) {
-            const int64_t y = __shfl_up(upto, k);
-            if (lane >= k) upto += y;
-        }
+        const unsigned upto = (unsigned)scan_lanes((int)sum);
         if (lane == 63) wave_sum[wave] = upto;
         __syncthreads();
-        int64_t at = upto - sum;
+        unsigned at = upto - sum;
         all = 0;
+#pragma unroll
         for (int i = 0; i < kWaves; ++i) {
-            if (i < wave) at += wave_sum[i];
-            all += wave_sum[i];
+            const unsigned x = wave_sum[i];
+            at += i < wave ? x : 0u;
+            all += x;
         }
         for (int k = 0; k < per; ++k) {
             const int b = tid * per + k;
             if (b >= a.seqs) break;
             const KvSeq s = per == 1 && b < kSeqs ? seqs[b] : kv_seq(c, a, b);
             first[b] = at;
-            at += (int64_t)tiles_of(s) * work_of(s);
+            at += (unsigned)tiles_of(s) * work_of(s);
         }
         if (tid == 0) first[a.seqs] = all;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the centres
     __syncthreads();
     const auto seq_of = [&](int b) { return b < kSeqs ? seqs[b] : kv_seq(c, a, b); };
-    // What no tile covers.
-    if (!w.add) {
+    // What no tile covers, for the waves that have done their share.
+    const auto clear = [&]() {
+        if (w.add) return;
         for (int b = j; b < a.seqs; b += splits) {
             float *const to = w.weights + b * w.weights_seq + wrow;
             const KvSeq s = seq_of(b);
@@ -139,21 +152,23 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             for (int i = tid; i < tile0 * 32; i += kThreads) to[i] = 0.f;
             for (int64_t i = (int64_t)(tile0 + n) * 32 + tid; i < w.positions; i += kThreads) to[i] = 0.f;
         }
-    }
+    };
 
     const unsigned page_bytes = (unsigned)(c.heads * F::S) << c.page_log2;
     const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
     const unsigned pm = (1u << c.page_log2) - 1;
     const uint8_t *const lane_codes = c.k_codes + (((int64_t)h * F::S) << c.page_log2) + half * F::H;
     // A wave's share: the tiles whose work begins in an even share of all.
-    const int64_t shares = (int64_t)kWaves * splits, share = (int64_t)j * kWaves + wave;
-    const int64_t work0 = all / shares * share + min(share, all % shares);
-    const int64_t work1 = all / shares * (share + 1) + min(share + 1, all % shares);
-    // A place among the tiles: tile t of a sequence's n.
+    const unsigned shares = kWaves * splits, share = j * kWaves + wave;
+    all = __builtin_amdgcn_readfirstlane(all);
+    const unsigned each = all / shares, over = all - each * shares;
+    const unsigned work0 = each * share + min(share, over), work1 = work0 + each + (share < over);
+    // A place among the tiles: tile t of sequence b, of which the wave's are those up to
+    // `end` of its n.
     struct Place {
-        int b, t, n, work;
-        int64_t first;
+        int b, t, end, n, tile0;
         KvSeq s;
+        const int32_t *row;
     };
     const auto enter = [&](int b) {
         Place x;
@@ -163,15 +178,21 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         x.s.n = __builtin_amdgcn_readfirstlane(s.n);
         x.s.len = __builtin_amdgcn_readfirstlane(s.len);
         x.s.prefix = __builtin_amdgcn_readfirstlane(s.prefix);
-        x.first = first[x.b];
-        x.t = 0;
+        x.row = a.table + x.b * a.table_stride;
         x.n = tiles_of(x.s);
-        x.work = work_of(x.s);
+        x.tile0 = tile0_of(x.s);
+        const unsigned from = __builtin_amdgcn_readfirstlane(first[x.b]), work = work_of(x.s);
+        const auto tiles_before = [&](unsigned to) {     // that begin there
+            return to <= from ? 0 : to - from >= x.n * work ? x.n : (int)((to - from + work - 1) / work);
+        };
+        x.t = tiles_before(work0);
+        x.end = tiles_before(work1);
         return x;
     };
     // Whether there is a tile at x that is the wave's, or one in a sequence after it.
     const auto settle = [&](Place &x) {
-        while (x.t >= x.n) {
+        while (x.t >= x.end) {
+            if (x.end < x.n) return false;
             // the next sequence that has tiles: of 64 at a time
             int b = x.b + 1;
             for (;;) {
@@ -186,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             }
             x = enter(b);
         }
-        return x.first + (int64_t)x.t * x.work < work1;
+        return true;
     };
     // A lane's page of the tile at x.
     struct Where {
@@ -194,15 +215,15 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     };
     const auto find = [&](const Place &x) {
         Where y;
-        y.pos = (x.t + tile0_of(x.s)) * 32;
-        y.page = a.table[x.b * a.table_stride + (min(y.pos + col, x.s.len - 1) >> c.page_log2)];
+        y.pos = (x.t + x.tile0) * 32;
+        y.page = x.row[(unsigned)min(y.pos + col, x.s.len - 1) >> c.page_log2];
         return y;
     };
     const auto load = [&](uint32_t (&codes)[(F::H + 3) / 4], const Where &y) {
         load_codes<F::H>(codes, lane_codes + (uint64_t)min((unsigned)y.page, last_page) * page_bytes +
                                     (((unsigned)y.pos + col) & pm) * F::S);
     };
-    if (work0 >= work1) return;
+    if (work0 >= work1) return clear();
     Place now;
     {
         // the sequence in whose tiles work0 lies: the last that begins at it or before
@@ -214,16 +235,29 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             if (more < kWave) break;
         }
         now = enter(b);
-        now.t = (int)((work0 - now.first + now.work - 1) / now.work);
     }
-    if (!settle(now)) return;
+    if (!settle(now)) return clear();
+    // Codes are asked for kAhead tiles before they are looked up, numbers of pages twice as
+    // many; behind the last tile, some tile's again.
     Place next = now;
-    Where at = find(now), ahead = at;
-    uint32_t codes[(F::H + 3) / 4];
-    load(codes, at);
-    ++next.t;
-    bool more = settle(next);
-    if (more) ahead = find(next);
+    bool more = true;
+    Where where[kAhead]{};
+    uint32_t codes[kAhead][(F::H + 3) / 4];
+    const auto find_next = [&](Where &x) {
+        if (!more) return;
+        x = find(next);
+        ++next.t;
+        more = settle(next);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        if (i) where[i] = where[i - 1];
+        find_next(where[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load(codes[i], where[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) find_next(where[i]);
     // 32 rows: a lane has half the features of row `col` of them, what that sees and its
     // logarithm, and the number of its token and head in the sequence.
     struct Rows {
@@ -263,29 +297,22 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             ++tok;
         }
     };
-    for (;;) {
+    // The tile at `now`, whose codes are codes[I]. False: it was the last.
+    const auto turn = [&](auto I) {
+        constexpr int slot = decltype(I)::value;
         // the keys: a lane has features [half D / 2, + D / 2) of position col
         u4v k[D / 16];
         {
             KvEntry<SUB> e[F::H];
-            const char *const from = book + half * (F::H * 512 * SUB);
 #pragma unroll
             for (int n = 0; n < F::H; ++n)
-                e[n] = *reinterpret_cast<const KvEntry<SUB> *>(
-                    from + n * (512 * SUB) + (codes[n / 4] >> (8 * (n % 4)) & 255) * (2 * SUB));
+                e[n] = lds_get<KvEntry<SUB>>(code_at<SUB>(codes[slot], n, half * (F::H * 512 * SUB)), n * (512 * SUB));
             __builtin_memcpy(k, e, sizeof(k));
         }
-        const int b = now.b, pos = at.pos;
+        load(codes[slot], where[slot]);
+        find_next(where[slot]);
+        const int b = now.b, pos = (now.t + now.tile0) * 32;
         const KvSeq s = now.s;
-        const bool last = !more;
-        if (more) {
-            load(codes, ahead);
-            at = ahead;
-            now = next;
-            ++next.t;
-            more = settle(next);
-            if (more) ahead = find(next);
-        }
         float sum[16] = {};
         const auto block = [&](const Rows &x) {
             const KvSeen seen = x.seen;
@@ -322,20 +349,24 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
                 }
             }
         };
-        // a block's rows are asked for while the one before is worked on; a single block's stay
+        // A block's rows are asked for while the one before is worked on, behind the last one
+        // the first again, for the next tile; a single block's stay.
         const int rows = s.n * a.group;
         if (loaded != b) {
             rewind();
             begin(cur, s);
-        }
-        loaded = rows <= 32 ? b : -1;
+            loaded = b;
+            __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0), or the compiler waits below,
+        }                                                // where codes are under way
 #pragma unroll 1
         for (int r0 = 32;; r0 += 32) {
-            const bool two = r0 < rows;
-            if (two) begin(coming, s);
+            if (rows > 32) {
+                if (r0 >= rows) rewind();
+                begin(coming, s);
+            }
             block(cur);
-            if (!two) break;
-            cur = coming;
+            if (rows > 32) cur = coming;
+            if (r0 >= rows) break;
         }
         // Over the 32 lanes of a half, halving what each holds (rows of 16 exchange, then
         // lanes 8, 7, 2 and 1 away): place i of the sums in the end is 8 bit 4 + 4 bit 3 +
@@ -355,8 +386,12 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             float *const to = w.weights + b * w.weights_seq + wrow + p;
             *to = w.add ? *to + sum[0] : sum[0];
         }
-        if (last) break;
-    }
+        ++now.t;
+        return settle(now);
+    };
+    while (turn(std::integral_constant<int, 0>{}) && turn(std::integral_constant<int, 1>{}) &&
+           turn(std::integral_constant<int, 2>{}) && turn(std::integral_constant<int, 3>{})) {}
+    clear();
 }
 
 template <int D, int SUB>
@@ -365,10 +400,10 @@ hipError_t launch(const KvCache &c, const KvNew &a, const KvWeigh &w, hipStream_
     const auto kernel = c.fp16 ? kv_weigh_kernel<D, SUB, true> : kv_weigh_kernel<D, SUB, false>;
     const int64_t span = (int64_t)a.table_pages << c.page_log2;
     const int64_t tiles = a.seqs * (((span < w.positions ? span : w.positions) + 31) / 32);
-    int64_t splits = kCUs / c.heads;                     // one workgroup to a CU
+    int64_t splits = kCUs / c.heads;
     if (splits > (tiles + kWaves - 1) / kWaves) splits = (tiles + kWaves - 1) / kWaves;
     if (splits < 1) splits = 1;
-    const size_t lds = Form<D, SUB>::kBook + (a.seqs + 1) * sizeof(int64_t);
+    const size_t lds = Form<D, SUB>::kBook + kSeqs * sizeof(KvSeq) + (kWaves + a.seqs + 1) * sizeof(unsigned);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(c.heads * splits)), dim3(kThreads), lds, s, c, a, w,
                        (int)splits);
     return hipGetLastError();
