@@ -5,8 +5,7 @@
 // the 256 values of each, then writes the kept positions in order. The second moves:
 // what goes to place j comes from a position of at least j, so that in place a tile of
 // places may be written once all of it, and of the tiles before, has been read.
-#include "kv_device.h"
-#include "kv_tokens.h"
+#include "kv_tokens_device.h"
 
 namespace lloyd {
 
@@ -194,6 +193,7 @@ constexpr int kFloats = kMove * kHold;                           // places of a 
 template <int S>
 constexpr int kKeys = kMove * kHold / (S / kRun<S>);             // of keys
 constexpr int kValues = 256;                                     // of values
+constexpr int kResident = 4;         // workgroups of a CU that move values
 
 template <int N>
 struct BytesOf {
@@ -206,6 +206,17 @@ struct BytesOf<4> {
 template <int N>
 using Bytes = typename BytesOf<N>::type;
 
+typedef uint32_t Four __attribute__((ext_vector_type(4)));
+
+// Byte y of word n to byte n of word y.
+__device__ inline Four turned(Four a)
+{
+    const uint32_t b0 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400), b1 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400);
+    const uint32_t b2 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602), b3 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602);
+    return Four{__builtin_amdgcn_perm(b1, b0, 0x05040100), __builtin_amdgcn_perm(b1, b0, 0x07060302),
+                __builtin_amdgcn_perm(b3, b2, 0x05040100), __builtin_amdgcn_perm(b3, b2, 0x07060302)};
+}
+
 template <int S, bool IN_PLACE>
 __global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, MoveGrid grid)
 {
@@ -217,7 +228,9 @@ __global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, Mo
     const uint32_t last = (uint32_t)min(c.pages - 1, (int64_t)0x7FFFFFFF);
     const int mask = (1 << c.page_log2) - 1;
     const int32_t *const table = e.table + b * e.table_stride, *const to = e.to + b * e.to_stride;
-    if (part < grid.weights) {
+    // values, whose workgroups take longest, come first
+    if (part >= grid.values + grid.keys) {
+        part -= grid.values + grid.keys;
         const float *const in = e.weights + b * e.weights_seq + h * e.weights_head;
         float *const out = e.weights_out + b * e.out_seq + h * e.out_head;
         if (part == 0 && h == 0 && tid == 0) e.lengths_out[b] = m;
@@ -225,9 +238,12 @@ __global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, Mo
             int i[kHold];
             float x[kHold];
 #pragma unroll
-            for (int k = 0; k < kHold; ++k) i[k] = j0 + k * kMove < m ? kept[j0 + k * kMove] : INT32_MAX;
+            for (int k = 0; k < kHold; ++k) i[k] = m ? kept[min(j0 + k * kMove, (int64_t)m - 1)] : 0;
 #pragma unroll
-            for (int k = 0; k < kHold; ++k) x[k] = i[k] < e.positions ? in[i[k]] : 0.f;
+            for (int k = 0; k < kHold; ++k) x[k] = in[min((int64_t)i[k], e.positions - 1)];
+#pragma unroll
+            for (int k = 0; k < kHold; ++k)
+                if (j0 + k * kMove >= m || i[k] >= e.positions) x[k] = 0.f;
             if (IN_PLACE) __syncthreads();
 #pragma unroll
             for (int k = 0; k < kHold; ++k)
@@ -236,8 +252,8 @@ __global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, Mo
         return;
     }
     if (m == 0 || (IN_PLACE && kept[m - 1] == m - 1)) return;        // all where they are
-    part -= grid.weights;
-    if (part < grid.keys) {
+    if (part >= grid.values) {
+        part -= grid.values;
         constexpr int runs = S / kRun<S>;
         for (int j0 = part * kKeys<S>; j0 < m; j0 += grid.keys * kKeys<S>) {
             int i[kHold], goal[kHold], page[kHold];
@@ -266,95 +282,135 @@ __global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, Mo
         }
         return;
     }
-    part -= grid.keys;
-    // Values: what lies between the tile's first and last position comes to LDS by whole
-    // words, 8 positions of a sub-vector each, where single bytes are picked: picked from
-    // memory they took 142 us instead of TODO for 64 contexts of 8192 brought to half. Where
-    // little is kept they come from memory.
-    constexpr int shares = IN_PLACE ? kParts : 1, subs = (S + shares - 1) / shares;
-    constexpr int wide = 32, high = kMove / wide;        // a thread's words and sub-vectors: every 32nd and 8th
-    constexpr int words = kSpan / 8 / wide, turns = (subs + high - 1) / high;
-    constexpr int row = kSpan + 4;                       // bytes of a sub-vector's in LDS
-    __shared__ uint32_t s_codes[subs * row / 4];
-    __shared__ int32_t s_table[kSpan / 8 + 1];
-    const int p0 = IN_PLACE ? part * subs : 0, p1 = min(p0 + subs, S);
-    const int lane = tid % wide, sub0 = p0 + tid / wide;
-    for (int j0 = IN_PLACE ? 0 : part * kValues; j0 < m; j0 += (IN_PLACE ? 1 : grid.values) * kValues) {
-        const int j = j0 + lane * 8;                     // the thread's places
-        int at[8];
+    // Values: what lies between the tile's first and last position comes to LDS, a thread's
+    // 8 positions of 4 sub-vectors at a time, laid out anew as one word to a position, and
+    // is picked there by words, which are laid out back. Where little is kept it comes from
+    // memory by single bytes.
+    constexpr int groups = S / 4, shares = IN_PLACE ? kParts : 1, most = (groups + shares - 1) / shares;
+    constexpr int wide = 32, high = kMove / wide;        // a thread's positions and groups: every 32nd 8 and 8th
+    constexpr int words = kSpan / 8 / wide, turns = (most + high - 1) / high;
+    constexpr int row = kSpan + 4;                       // words of a group's in LDS
+    __shared__ __attribute__((aligned(16))) uint32_t s_codes[most * row];
+    const int g0 = IN_PLACE ? part * most : 0, g1 = min(g0 + most, groups);
+    if (g0 >= g1) return;
+    // a wave has 64 positions of all groups: what it asks for at once lies on few pages
+    const int lane = tid / kWave * 8 + tid % 8, mine = g0 + tid / 8 % high;
+    // A tile at place j0: what the thread keeps of it, where it goes, and between which
+    // positions all lie. The next tile's is asked for while this one's codes are under way.
+    struct Tile {
+        int at[8], i0, end;
+        uint32_t goal, page[words];
+    };
+    const auto find = [&](Tile &x, int j0) {
+        const int j = j0 + lane * 8;
+        if (j + 8 <= m) {
+            __builtin_memcpy(x.at, kept + j, sizeof(x.at));
+        } else {
 #pragma unroll
-        for (int y = 0; y < 8; ++y) at[y] = kept[min(j + y, m - 1)];
-        const uint32_t goal = j < m ? (uint32_t)to[j >> c.page_log2] : ~0u;
-        const int i0 = kept[j0] & ~7, end = kept[min(j0 + kValues, m) - 1] + 1;
-        uint64_t x[turns];
+            for (int y = 0; y < 8; ++y) x.at[y] = kept[min(j + y, m - 1)];
+        }
+        x.goal = j < m ? (uint32_t)to[j >> c.page_log2] : ~0u;
+        x.i0 = kept[j0] & ~7;
+        x.end = kept[min(j0 + kValues, m) - 1] + 1;
+    };
+    const auto find_pages = [&](Tile &x) {
+#pragma unroll
+        for (int k = 0; k < words; ++k)
+            x.page[k] = min((uint32_t)table[min(x.i0 + (lane + k * wide) * 8, x.end - 1) >> c.page_log2], last);
+    };
+    const int step = (IN_PLACE ? 1 : grid.values) * kValues;
+    int j0 = IN_PLACE ? 0 : part * kValues;
+    if (j0 >= m) return;
+    Tile now, next;
+    find(now, j0);
+    find_pages(now);
+    for (;;) {
+        const int j = j0 + lane * 8;                     // the thread's places
+        const int i0 = now.i0, end = now.end, (&at)[8] = now.at;
+        const bool more = j0 + step < m;
+        Four x[turns][2];                                // of a group: places 0 to 3, 4 to 7
         if (end - i0 <= kSpan) {
-            const int page0 = i0 >> c.page_log2;
-            if (tid <= ((end - 1) >> c.page_log2) - page0) s_table[tid] = table[page0 + tid];
-            __syncthreads();
-            uint64_t w[turns * words];
+            uint64_t w[words][turns][4];
 #pragma unroll
             for (int k = 0; k < words; ++k) {
                 const int i = min(i0 + (lane + k * wide) * 8, (end - 1) & ~7);
-                const uint32_t page = (uint32_t)s_table[(i >> c.page_log2) - page0];
-                const uint8_t *const from = c.v_codes + kv_head(c, min(page, last), h, S) + (i & mask);
+                const uint8_t *const from = c.v_codes + kv_head(c, now.page[k], h, S) + (i & mask);
 #pragma unroll
                 for (int n = 0; n < turns; ++n)
-                    w[k * turns + n] = *reinterpret_cast<const uint64_t *>(
-                        from + ((int64_t)min(sub0 + n * high, p1 - 1) << c.page_log2));
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        w[k][n][y] = *reinterpret_cast<const uint64_t *>(
+                            from + ((unsigned)(min(mine + n * high, g1 - 1) + y * groups) << c.page_log2));
             }
+            find(next, more ? j0 + step : j0);
 #pragma unroll
             for (int k = 0; k < words; ++k)
 #pragma unroll
-                for (int n = 0; n < turns; ++n)
-                    if (i0 + (lane + k * wide) * 8 < end && sub0 + n * high < p1) {
-                        uint32_t *const dst = s_codes + ((sub0 - p0 + n * high) * row + (lane + k * wide) * 8) / 4;
-                        dst[0] = (uint32_t)w[k * turns + n];
-                        dst[1] = (uint32_t)(w[k * turns + n] >> 32);
+                for (int n = 0; n < turns; ++n) {
+                    // (where there is nothing more, what is there again)
+                    Four *const dst = reinterpret_cast<Four *>(s_codes + (min(mine + n * high, g1 - 1) - g0) * row + (lane + k * wide) * 8);
+                    Four part0, part1;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        part0[y] = (uint32_t)w[k][n][y];
+                        part1[y] = (uint32_t)(w[k][n][y] >> 32);
                     }
-            __syncthreads();
+                    dst[0] = turned(part0);
+                    dst[1] = turned(part1);
+                }
+            lds_barrier();
 #pragma unroll
             for (int n = 0; n < turns; ++n) {
-                const uint8_t *const from = reinterpret_cast<const uint8_t *>(s_codes) +
-                                            min(sub0 - p0 + n * high, p1 - p0 - 1) * row - i0;
-                uint32_t lo = 0, hi = 0;
+                const uint32_t *const from = s_codes + min(mine - g0 + n * high, g1 - g0 - 1) * row - i0;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    lo |= (uint32_t)from[at[y]] << (8 * y);
-                    hi |= (uint32_t)from[at[y + 4]] << (8 * y);
-                }
-                x[n] = (uint64_t)hi << 32 | lo;
+                for (int y = 0; y < 8; ++y) x[n][y / 4][y % 4] = from[at[y]];
+                x[n][0] = turned(x[n][0]);
+                x[n][1] = turned(x[n][1]);
             }
         } else {
+            find(next, more ? j0 + step : j0);
             const uint8_t *from[8];
 #pragma unroll
             for (int y = 0; y < 8; ++y)
                 from[y] = c.v_codes + kv_head(c, min((uint32_t)table[at[y] >> c.page_log2], last), h, S) + (at[y] & mask);
 #pragma unroll
-            for (int n = 0; n < turns; ++n) {
-                const int64_t sub = (int64_t)min(sub0 + n * high, p1 - 1) << c.page_log2;
-                uint32_t lo = 0, hi = 0;
+            for (int n = 0; n < turns; ++n)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    lo |= (uint32_t)from[y][sub] << (8 * y);
-                    hi |= (uint32_t)from[y + 4][sub] << (8 * y);
+                for (int z = 0; z < 4; ++z) {
+                    const unsigned sub = (unsigned)(min(mine + n * high, g1 - 1) + z * groups) << c.page_log2;
+                    uint32_t lo = 0, hi = 0;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        lo |= (uint32_t)from[y][sub] << (8 * y);
+                        hi |= (uint32_t)from[y + 4][sub] << (8 * y);
+                    }
+                    x[n][0][z] = lo;
+                    x[n][1][z] = hi;
                 }
-                x[n] = (uint64_t)hi << 32 | lo;
-            }
+            if (IN_PLACE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
-        if (IN_PLACE) __syncthreads();                   // all read; LDS is done with, too
-        if (goal <= last) {
-            uint8_t *const dst = c.v_codes + kv_head(c, goal, h, S) + (j & mask);
+        find_pages(next);
+        lds_barrier();                                   // all read; LDS is done with, too
+        if (now.goal <= last) {
+            uint8_t *const dst = c.v_codes + kv_head(c, now.goal, h, S) + (j & mask);
 #pragma unroll
             for (int n = 0; n < turns; ++n) {
-                if (sub0 + n * high >= p1) continue;
-                uint8_t *const out = dst + ((int64_t)(sub0 + n * high) << c.page_log2);
-                if (j + 8 <= m)
-                    *reinterpret_cast<uint64_t *>(out) = x[n];
-                else
-                    for (int y = 0; y < m - j; ++y) out[y] = (uint8_t)(x[n] >> (8 * y));
+                if (mine + n * high >= g1) continue;
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    uint8_t *const out = dst + ((unsigned)(mine + n * high + z * groups) << c.page_log2);
+                    const uint64_t bytes = (uint64_t)x[n][1][z] << 32 | x[n][0][z];
+                    if (j + 8 <= m)
+                        *reinterpret_cast<uint64_t *>(out) = bytes;
+                    else
+#pragma unroll 1
+                        for (int y = 0; y < m - j; ++y) out[y] = (uint8_t)(bytes >> (8 * y));
+                }
             }
         }
-        if (!IN_PLACE) __syncthreads();
+        if (!more) break;
+        now = next;
+        j0 += step;
     }
 }
 
@@ -373,6 +429,9 @@ void move(const KvCache &c, const KvEvict &e, hipStream_t s)
             return (int)(n > room ? room : n < 1 ? 1 : n);
         };
         grid = MoveGrid{tiles(e.positions, kFloats), tiles(most, kKeys<S>), tiles(most, kValues)};
+        // of values, no more than are at work at once
+        const int64_t values = kResident * kCUs / rows;
+        if (grid.values > values) grid.values = (int)(values < 1 ? 1 : values);
     }
     const dim3 blocks((unsigned)(rows * grid.all()));
     if (e.in_place)

@@ -105,15 +105,6 @@ __device__ inline const KvTokensArgs &seldom()
     return *(const KvTokensArgs *)p;
 }
 
-// All waves' LDS accesses before it are done behind it; loads from memory stay under way,
-// which __syncthreads() would wait for.
-__device__ inline void lds_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // ONE_PAGE: pages of 32 tokens or more, so that a tile lies on one.
 template <int D, int SUB, bool FP16, bool ONE_PAGE>
 __global__ __launch_bounds__(kThreads) void kv_tokens_kernel(KvTokensArgs args)

@@ -62,6 +62,15 @@ __device__ inline void lds_put(uint32_t at, int more, const T &x)
     *(P)((__attribute__((address_space(3))) char *)(uintptr_t)at + more) = __builtin_bit_cast(W, x);
 }
 
+// All waves' LDS accesses before it are done behind it; loads and stores of memory stay
+// under way, which __syncthreads() would wait for.
+__device__ inline void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // The larger, or the sum, of a lane's and that of the lane 32 away.
 __device__ inline float max_halves(float x)
 {
