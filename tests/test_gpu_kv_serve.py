@@ -54,6 +54,14 @@ ROTATE = [
     (3, 7, 10, 512, 256, True, False, 1.0, FP),
     (600, 8, 2, 64, 0, False, False, 3.0, BF),
     (1500, 5, 1, 64, 32, True, False, 1.0, BF),
+    # halves that are no whole runs of 16 bytes, heads that fill no wave
+    (33, 13, 3, 40, 19, False, False, 1.0, FP),
+    (20, 9, 2, 512, 255, False, True, 1.0, BF),
+    (20, 9, 2, 512, 251, True, False, 1.0, FP),
+    (7, 70, 9, 96, 46, False, False, 1.5, BF),
+    (2, 300, 8, 24, 12, False, False, 1.0, FP),
+    (2, 300, 8, 24, 11, True, False, 1.0, BF),
+    (3, 5, 5, 8, 3, False, False, 1.0, BF),
 ]
 
 
@@ -75,6 +83,22 @@ def test_rotate(T, hq, hk, dim, half, inter, inverse, amp, dtype, in_place):
         assert torch.equal(x[..., 2 * half:], old[..., 2 * half:])
         if not in_place:
             assert torch.equal(src, old)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("half", [3, 8, 12, 16])
+def test_rotate_leaves_features_behind_as_they_are(half, inter):
+    """Infinities and NaN there reach no feature that is turned, and stay themselves."""
+    g = torch.Generator().manual_seed(half)
+    q = torch.randn(5, 6, 64, generator=g).to(BF).to(DEV)
+    pos = torch.arange(5).to(DEV)
+    f = torch.rand(half, generator=g, dtype=torch.float64).to(DEV)
+    want = km.kmeans_kv_rotate(q, None, pos, f, interleaved=inter)[0]
+    q[..., 2 * half:] = torch.tensor([float("nan"), float("inf"), -float("inf"), 1.0]).to(BF).to(
+        DEV).repeat(16)[:64 - 2 * half]
+    got = km.kmeans_kv_rotate(q, None, pos, f, interleaved=inter)[0]
+    assert torch.equal(got[..., :2 * half], want[..., :2 * half])
+    assert torch.equal(got[..., 2 * half:].view(torch.int16), q[..., 2 * half:].view(torch.int16))
 
 
 def test_rotate_far_positions_and_gradient():
