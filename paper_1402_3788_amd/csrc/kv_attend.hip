@@ -618,7 +618,7 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
         const int n = i * F::kThreads + tid;
         return ((n >> 2) / F::S * 4 + (n & 3)) * per16;
     };
-    uint4 vreg[rounds];
+    u4v vreg[rounds];                                    // (as uint4, they went to memory)
     if (c.K == 256) {
 #pragma unroll
         for (int i = 0; i < rounds; ++i) {
@@ -628,7 +628,7 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
 #pragma unroll
         for (int i = 0; i < rounds; ++i)
             if (i * F::kThreads + tid < D * 32)
-                vreg[i] = *reinterpret_cast<const uint4 *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
+                vreg[i] = *reinterpret_cast<const u4v *>(vs + (value_s(i) * 256 + value_code(i)) * SUB);
     } else {
         using E = KvEntry<SUB>;
 #pragma unroll 4
@@ -655,12 +655,14 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
 #pragma unroll
         for (int i = 0; i < rounds; ++i) {
             if (i * F::kThreads + tid >= D * 32) break;
-            KvEntry<SUB> e[per16];
-            __builtin_memcpy(e, &vreg[i], 16);
 #pragma unroll
-            for (int x = 0; x < per16; ++x)
+            for (int x = 0; x < per16; ++x) {
+                KvEntry<SUB> e;
+#pragma unroll
+                for (int y = 0; y < SUB / 2; ++y) e.w[y] = vreg[i][x * (SUB / 2) + y];
                 *reinterpret_cast<KvEntry<SUB> *>(vbook + (value_code(i) + x) * F::kRow +
-                                                  value_s(i) * (SUB * 2)) = e[x];
+                                                  value_s(i) * (SUB * 2)) = e;
+            }
         }
     }
     lds_landed();
