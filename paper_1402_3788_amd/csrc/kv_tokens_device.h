@@ -118,15 +118,21 @@ struct KvSeen {
     int lo, hi, at;
 };
 
-__device__ inline KvSeen kv_seen(const KvNew &a, const KvSeq &s, int i)
+// (of token i, whose start is given)
+__device__ inline KvSeen kv_seen(const KvNew &a, const KvSeq &s, int i, int start)
 {
     KvSeen x;
     x.at = s.len - s.n + i;
     x.hi = max(x.at + 1, s.prefix);
-    x.lo = a.starts ? max(a.starts[s.t0 + i], 0) : 0;
+    x.lo = max(start, 0);
     if (a.window) x.lo = max(x.lo, x.at - a.window + 1);
     if (x.lo >= x.hi) x.lo = x.hi = 0;
     return x;
+}
+
+__device__ inline KvSeen kv_seen(const KvNew &a, const KvSeq &s, int i)
+{
+    return kv_seen(a, s, i, a.starts ? a.starts[s.t0 + i] : 0);
 }
 
 // cap * tanh(scale * z / cap) to base 2, of a lane's N products z. With x = scale * z / cap,

@@ -258,12 +258,12 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     for (int i = 0; i < kAhead; ++i) load(codes[i], where[i]);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) find_next(where[i]);
-    // 32 rows: a lane has half the features of row `col` of them, what that sees and its
-    // logarithm, and the number of its token and head in the sequence.
+    // 32 rows as they come from memory: a lane has half the features of row `col` of them,
+    // its token's number in the sequence and start, its logarithm and slope.
     struct Rows {
         u4v q[D / 16];
-        KvSeen seen;
-        float base, slope;
+        int tok, start;
+        float lse, slope;
     };
     Rows cur, coming;
     int loaded = -1;                                     // the sequence whose only rows are in cur
@@ -275,19 +275,14 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         hd = (int)((unsigned)col % (unsigned)a.group);
     };
     const auto begin = [&](Rows &x, const KvSeq &s) {
-        const bool there = tok < s.n;
+        // behind the last row: some row
+        const int64_t t = s.t0 + min(tok, s.n - 1);
         const int hq = h * a.group + hd;
-        x.seen = KvSeen{0, 0, 0};
-        x.base = INFINITY;
-        x.slope = 0.f;
-        if (there) {
-            x.seen = kv_seen(a, s, tok);
-            x.base = w.lse[(int64_t)(s.t0 + tok) * heads + hq] * kLog2e;
-            if (x.base == -INFINITY) x.seen.lo = x.seen.hi = 0;
-            if (a.slopes) x.slope = a.slopes[hq] * kLog2e;
-        }
-        // behind the last row: some row, whose weights are exp(-infinity)
-        const uint16_t *const src = a.q + (s.t0 + min(tok, s.n - 1)) * a.q_token + hq * a.q_head + half * (D / 2);
+        x.tok = tok;
+        x.start = a.starts ? a.starts[t] : 0;
+        x.lse = w.lse[t * heads + hq];
+        x.slope = a.slopes ? a.slopes[hq] : 0.f;
+        const uint16_t *const src = a.q + t * a.q_token + hq * a.q_head + half * (D / 2);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) x.q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
         tok += tokens32;
@@ -315,7 +310,9 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         const KvSeq s = now.s;
         float sum[16] = {};
         const auto block = [&](const Rows &x) {
-            const KvSeen seen = x.seen;
+            KvSeen seen = kv_seen(a, s, x.tok, x.start);
+            const float base = x.lse * kLog2e;
+            if (x.tok >= s.n || base == -INFINITY) seen.lo = seen.hi = 0;
             if (!__any(seen.lo < pos + 32 && seen.hi > pos)) return;
             const bool whole = __ballot(seen.lo <= pos && seen.hi >= pos + 32) == ~0ull;
             f16v z;
@@ -324,20 +321,19 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) z = mfma32<FP16>(k[i], x.q[i], z);
             const int y0 = pos + 4 * half;               // score i is position y0 + 8 (i / 4) + i % 4
-            float scale = a.scale_log2;
-            if (a.cap_log2 > 0.f) {
-                kv_cap<16>(z, a);
-                scale = 1.f;
-            }
+            if (a.cap_log2 > 0.f) kv_cap<16>(z, a);
+            const float scale = a.cap_log2 > 0.f ? 1.f : a.scale_log2;
             if (a.slopes) {
-                const float far = (float)(seen.at - y0);
+                const float far = (float)(seen.at - y0), slope = x.slope * kLog2e;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    z[i] = __builtin_fmaf(-x.slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale);
-                scale = 1.f;
+                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale) - base;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = __builtin_fmaf(z[i], scale, -base);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -x.base));
+            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(z[i]);
             if (whole) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum[i] += z[i];
