@@ -47,7 +47,9 @@ namespace {
 constexpr int kRows = kKvRows;
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
-constexpr int kShare = 8;            // tiles that are worth a workgroup of their own
+// Tiles that are worth a workgroup of their own. bf16, 8 heads of 128: with 3, 8 and 24 in us
+// 42, 38, 46 (256 new tokens behind 500), 47, 47, 52 (behind 2000), 34, 41, 81 (8 prompts of 100).
+constexpr int kShare = 8;
 
 // As in kv_attend.hip: a new reference lies kLift below the largest score and holds until
 // a score is kLag above that one.
@@ -715,7 +717,15 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
     }
 }
 
-constexpr int kFewRows = 32;         // of a sequence on average, up to which units are of few
+// Units of few rows (kv_attend.hip) read the cache once for every 16 rows, units of 256 take
+// longer to begin and cost the same however few of their rows there are. bf16, 8 heads of 128,
+// in us, units of few and of 256: 64 rows of each sequence 23 and 47 (8 of 2000 positions),
+// 32 and 71 (one of 30000), 54 and 62 (64 of 500), 93 and 131 (256 of 300); 128 rows 42 and 48,
+// 49 and 75, 144 and 164 (16 of 8000), but where few positions are cut to many units 54 and 37
+// (32 of 500, 288 units), 88 and 69 (64 of 500, 576 units); 256 rows 60 and 55, 74 and 73.
+constexpr int kFewRows = 64;         // of a sequence on average, up to which units are of few,
+constexpr int kFewMore = 128;        // and where that makes no more than
+constexpr int kFewUnits = 256;       // of them
 
 KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 {
@@ -755,7 +765,9 @@ hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, 
 // Whether a unit is of few rows: every sequence has few on average.
 static bool few(const KvCache &c, const KvNew &a, const KvFewPlan &p)
 {
-    return a.tokens * a.group <= kFewRows * (int64_t)a.seqs && p.units <= kKvMaxFew;
+    const int64_t rows = a.tokens * a.group, seqs = a.seqs;
+    return (rows <= kFewRows * seqs && p.units <= kKvMaxFew) ||
+           (rows <= kFewMore * seqs && p.units <= kFewUnits);
 }
 
 size_t kv_attend_tokens_bytes(const KvCache &c, const KvNew &a)
