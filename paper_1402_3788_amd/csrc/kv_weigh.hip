@@ -66,14 +66,15 @@ __device__ inline void fold(float (&sum)[16], bool up)
 }
 
 template <int D, int SUB, bool FP16>
-__global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, KvWeigh w, int splits)
+__global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, KvWeigh w, int splits, int team)
 {
     using F = Form<D, SUB>;
     extern __shared__ uint4 lds[];
     // the kernel has no LDS but its dynamic one, which so begins at 0
     char *const book = reinterpret_cast<char *>(lds);
     KvSeq *const seqs = reinterpret_cast<KvSeq *>(book + F::kBook);      // [kSeqs]
-    unsigned *const wave_sum = reinterpret_cast<unsigned *>(seqs + kSeqs);       // [kWaves]
+    float *const team_sum = reinterpret_cast<float *>(seqs + kSeqs);     // [2][kWaves][32]
+    unsigned *const wave_sum = reinterpret_cast<unsigned *>(team_sum + 2 * kWaves * 32);      // [kWaves]
     unsigned *const first = wave_sum + kWaves;                           // [seqs + 1]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -106,7 +107,10 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     const auto tiles_of = [&](const KvSeq &s) {
         return s.n ? max(((min(s.len, span) + 31) >> 5) - tile0_of(s), 0) : 0;
     };
-    const auto work_of = [&](const KvSeq &s) { return 2u + (unsigned)(s.n * a.group + 31) / 32; };
+    const int team_rows = 32 * team, rank = team > 1 ? wave : 0;
+    const auto work_of = [&](const KvSeq &s) {
+        return 2u + (unsigned)(s.n * a.group + team_rows - 1) / (unsigned)team_rows;
+    };
     // (all of it below 2^32: ten times what the entry point lets be 2^28)
     unsigned all;
     {
@@ -158,8 +162,8 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     const unsigned last_page = (unsigned)min(c.pages - 1, (int64_t)0x7FFFFFFF);
     const unsigned pm = (1u << c.page_log2) - 1;
     const uint8_t *const lane_codes = c.k_codes + (((int64_t)h * F::S) << c.page_log2) + half * F::H;
-    // A wave's share: the tiles whose work begins in an even share of all.
-    const unsigned shares = kWaves * splits, share = j * kWaves + wave;
+    // A wave's share, or that of a team: the tiles whose work begins in an even share of all.
+    const unsigned shares = team > 1 ? splits : kWaves * splits, share = team > 1 ? j : j * kWaves + wave;
     all = __builtin_amdgcn_readfirstlane(all);
     const unsigned each = all / shares, over = all - each * shares;
     const unsigned work0 = each * share + min(share, over), work1 = work0 + each + (share < over);
@@ -267,12 +271,12 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     };
     Rows cur, coming;
     int loaded = -1;                                     // the sequence whose only rows are in cur
-    const int tokens32 = 32 / a.group, heads32 = 32 % a.group;
+    const int tokens_on = team_rows / a.group, heads_on = team_rows % a.group;
     int tok = 0, hd = 0;                                 // of the next block's row
     // the sequence's first rows come next
     const auto rewind = [&]() {
-        tok = (int)((unsigned)col / (unsigned)a.group);
-        hd = (int)((unsigned)col % (unsigned)a.group);
+        tok = (int)((unsigned)(32 * rank + col) / (unsigned)a.group);
+        hd = (int)((unsigned)(32 * rank + col) % (unsigned)a.group);
     };
     const auto begin = [&](Rows &x, const KvSeq &s) {
         // behind the last row: some row
@@ -285,8 +289,8 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         const uint16_t *const src = a.q + t * a.q_token + hq * a.q_head + half * (D / 2);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) x.q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
-        tok += tokens32;
-        hd += heads32;
+        tok += tokens_on;
+        hd += heads_on;
         if (hd >= a.group) {
             hd -= a.group;
             ++tok;
@@ -355,13 +359,13 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
             __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0), or the compiler waits below,
         }                                                // where codes are under way
 #pragma unroll 1
-        for (int r0 = 32;; r0 += 32) {
-            if (rows > 32) {
+        for (int r0 = 32 * rank + team_rows;; r0 += team_rows) {
+            if (rows > team_rows) {
                 if (r0 >= rows) rewind();
                 begin(coming, s);
             }
             block(cur);
-            if (rows > 32) cur = coming;
+            if (rows > team_rows) cur = coming;
             if (r0 >= rows) break;
         }
         // Over the 32 lanes of a half, halving what each holds (rows of 16 exchange, then
@@ -377,9 +381,23 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         fold<1, 0x4E>(sum, lane & 2);                    // quad_perm:[2,3,0,1]
         sum[0] += moved<0xB1>(sum[0]);                   // quad_perm:[1,0,3,2]
         const int place = (lane & 16) / 2 + (lane & 8) / 2 + (lane & 4) / 2 + (lane & 2) / 2;
-        const int p = pos + 4 * half + 8 * (place / 4) + place % 4;
-        if (!(lane & 1) && p < w.positions) {
-            float *const to = w.weights + b * w.weights_seq + wrow + p;
+        int at = 4 * half + 8 * (place / 4) + place % 4;
+        bool mine = !(lane & 1);
+        if (team > 1) {
+            // (two of them: the first wave reads a tile's while the others write the next)
+            float *const to = team_sum + slot % 2 * (kWaves * 32);
+            if (mine) to[wave * 32 + at] = sum[0];
+            lds_barrier();
+            at = col;
+            mine = wave == 0 && half == 0;
+            if (mine) {
+                sum[0] = to[at];
+#pragma unroll
+                for (int i = 1; i < kWaves; ++i) sum[0] += to[i * 32 + at];
+            }
+        }
+        if (mine && pos + at < w.positions) {
+            float *const to = w.weights + b * w.weights_seq + wrow + pos + at;
             *to = w.add ? *to + sum[0] : sum[0];
         }
         ++now.t;
@@ -396,12 +414,21 @@ hipError_t launch(const KvCache &c, const KvNew &a, const KvWeigh &w, hipStream_
     const auto kernel = c.fp16 ? kv_weigh_kernel<D, SUB, true> : kv_weigh_kernel<D, SUB, false>;
     const int64_t span = (int64_t)a.table_pages << c.page_log2;
     const int64_t tiles = a.seqs * (((span < w.positions ? span : w.positions) + 31) / 32);
-    int64_t splits = kCUs / c.heads;
-    if (splits > (tiles + kWaves - 1) / kWaves) splits = (tiles + kWaves - 1) / kWaves;
-    if (splits < 1) splits = 1;
-    const size_t lds = Form<D, SUB>::kBook + kSeqs * sizeof(KvSeq) + (kWaves + a.seqs + 1) * sizeof(unsigned);
+    const auto over = [](int64_t n, int64_t k) { return (n + k - 1) / k; };
+    const auto splits_of = [&](int64_t n) {
+        const int64_t most = kCUs / c.heads;
+        return n > most ? (most < 1 ? 1 : most) : n < 1 ? 1 : n;
+    };
+    // A tile to a wave, or, of few positions and many rows, to all waves of a workgroup, its
+    // rows shared: what takes fewer turns, were all sequences as long as the table's rows.
+    const int64_t alone = splits_of(over(tiles, kWaves)), together = splits_of(tiles);
+    const int64_t blocks = over(over(a.tokens * a.group, a.seqs), 32);
+    const bool team = over(tiles, together) * (3 + over(blocks, kWaves)) < over(tiles, alone * kWaves) * (2 + blocks);
+    const int64_t splits = team ? together : alone;
+    const size_t lds = Form<D, SUB>::kBook + kSeqs * sizeof(KvSeq) + 2 * kWaves * 32 * sizeof(float) +
+                       (kWaves + a.seqs + 1) * sizeof(unsigned);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(c.heads * splits)), dim3(kThreads), lds, s, c, a, w,
-                       (int)splits);
+                       (int)splits, team ? kWaves : 1);
     return hipGetLastError();
 }
 

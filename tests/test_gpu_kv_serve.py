@@ -236,6 +236,33 @@ def test_every_form(dim, sub, dtype):
         assert ((call.weigh(lse).double() - w).abs() <= d).all()
 
 
+# Rows and positions that are shared out in other ways: to units of few and of many rows, to
+# waves alone and to all of a workgroup.
+SHARES = [
+    ([(100, 41), (33, 20), (0, 0), (64, 64)], dict(dim=64, group=5, heads=1, page=8)),
+    ([(70, 45), (40, 40)], dict(dim=64, sub=8, group=2, heads=128)),
+    ([(50, 20)], dict(dim=64, sub=8, group=4, heads=300)),
+    ([(40, 40)], dict(dim=128, group=8, heads=2)),
+    ([(30, 9)], dict(dim=96, group=128, heads=1, sub=8, dtype=FP)),
+    ([(300, 30)], dict(dim=128, group=4, heads=2)),
+    ([(60 - b % 7, 25) for b in range(40)], dict(dim=64, group=4, heads=1)),
+    ([(60 - b % 7, 16) for b in range(40)], dict(dim=64, group=4, heads=1)),
+]
+
+
+@pytest.mark.parametrize("mode", ["plain", "all"])
+@pytest.mark.parametrize("case", range(len(SHARES)))
+def test_shares(case, mode):
+    sizes, kw = SHARES[case]
+    call = Call(sizes, seed=100 + case, **kw)
+    set_mode(call, mode)
+    _, lse = check_attention(call)
+    w, d = weights_of(call, lse, call.table.shape[1] * call.cache.page)
+    got = call.weigh(lse)
+    assert ((got.double() - w).abs() <= d).all()
+    assert torch.equal(call.weigh(lse), got)
+
+
 def test_long_contexts():
     """Contexts long enough to be shared by many workgroups, with few and many rows."""
     for sizes in ([(9000, 1), (20001, 1)], [(9000, 9)], [(12345, 200)], [(5000, 1), (6000, 150), (33, 33)]):
