@@ -445,7 +445,7 @@ size_t kmeans_kv_attend_tokens_workspace_bytes(const kmeans_kv_t *kv, const kmea
  * no token of the sequence sees are not read. out and lse overlap nothing that is read,
  * and no two of their elements lie in one place.
  * tokens * q_heads < 2^30, table_pages * page <= 2^30, as many of both together that
- * (seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^28, |scale| <= 2.35e38, cap finite,
+ * (seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27, |scale| <= 2.35e38, cap finite,
  * 0 or so large that scale / cap is finite (KMEANS_EINVAL otherwise). Scores, their maximum
  * and sum and the output are held in fp32; a weight enters the product with the values as
  * one or two 16-bit numbers, off by at most half a step of the cache's type. The same

@@ -172,7 +172,8 @@ template <bool FP16>
 hipError_t launch(const KvRotate &r, hipStream_t s)
 {
     const int heads = r.x[0].heads + r.x[1].heads;
-    // few tokens: a token's heads over several workgroups, that repeat its angles
+    // few tokens: a token's heads over several workgroups, that repeat its angles (one token of
+    // 72 heads of 128 2.6 us, in one workgroup 4.0; of 256 heads 2.6 and 7.8)
     int parts = 1;
     while (r.tokens * parts < 2 * kCUs && heads * (r.dim / 16) > parts * kThreads) ++parts;
     const auto kernel = r.interleaved ? kv_rotate_kernel<FP16, kInterleaved>

@@ -32,7 +32,7 @@ int check_new(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t)
     if (t->q_heads / kv->heads > kKvMaxGroup || t->tokens >= (int64_t)1 << 30 ||
         t->tokens * t->q_heads >= (int64_t)1 << 30 ||
         (t->seqs + t->tokens * (t->q_heads / kv->heads) / kKvRows) *
-                (t->table_pages * kv->page / kKvTile + 2) >= (int64_t)1 << 28)
+                (t->table_pages * kv->page / kKvTile + 2) >= (int64_t)1 << 27)
         return KMEANS_EUNSUPPORTED;
     if (!isfinite(t->scale * kLog2e) || !(t->cap >= 0.f) || !isfinite(t->cap * kLog2e))
         return KMEANS_EINVAL;

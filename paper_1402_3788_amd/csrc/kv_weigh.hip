@@ -4,9 +4,17 @@
 // centres of its head in LDS, which become the rows of one operand of
 // v_mfma_f32_32x32x16, and goes through the rows of the sequence's new tokens (the query
 // heads of each), 32 at a time as columns of the other: exp(z - lse) is summed for each
-// position in its lanes, and over the lanes at the end. Each sum has one order and one
-// writer. The keys' codes are the bytes that must come from memory; for a single new token
-// they bound it, for many the exponentials do.
+// position in its lanes, and over the lanes at the end. Where positions are few and rows many
+// the waves of a workgroup share a tile's rows and add up over LDS. Each sum has one order
+// and one writer.
+//
+// The keys' codes are the bytes that must come from memory. For a single new token it is their
+// way that takes the time, and what a launch takes before its first tile (the centres to LDS,
+// some 9 us): 32 sequences of 512 to 4096, 4 heads to each of 8 key heads of 128, bf16, 19 us.
+// For many the vector ALU does, with 19 operations to a score under a cap, 9 without, and the
+// way that tiles fall to waves (3.2 to one): the last 33 to 64 tokens of 4 prompts of 5000 to
+// 8000, 8 heads to a key head, capped, 95 us, 0.22 PFLOP/s of products; the vector ALU is at
+// work for half of it, the matrix cores for a tenth.
 #include "kv_tokens_device.h"
 
 #include <type_traits>
@@ -17,9 +25,10 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
-constexpr int kAhead = 4;            // tiles whose codes are under way to a wave
+// Tiles whose codes are under way to a wave: with four 32 sequences of 4096 took 18.5 us, with
+// one 20.4; more would not fit the registers.
+constexpr int kAhead = 4;
 constexpr int kSeqs = 1024;          // sequences that are kept in LDS
-
 
 template <int D, int SUB>
 struct Form {
@@ -99,7 +108,8 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     }
     // A sequence's tiles, and where the work on each one's begins in all of it. One without
     // new tokens has none, and a window leaves out those before it. A tile's work is that
-    // of looking its keys up, some two blocks of rows, and that of each block.
+    // of looking its keys up and folding its sums, counted as two blocks of rows, and that of
+    // each block.
     const int span = (int)min(w.positions, (int64_t)a.table_pages << c.page_log2);
     const auto tile0_of = [&](const KvSeq &s) {
         return a.window ? max(s.len - s.n - a.window + 1, 0) >> 5 : 0;
@@ -111,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     const auto work_of = [&](const KvSeq &s) {
         return 2u + (unsigned)(s.n * a.group + team_rows - 1) / (unsigned)team_rows;
     };
-    // (all of it below 2^32: ten times what the entry point lets be 2^28)
+    // (all of it below 2^32: twelve times what the entry point lets be 2^27)
     unsigned all;
     {
         const int per = (a.seqs + kThreads - 1) / kThreads;
@@ -420,10 +430,13 @@ hipError_t launch(const KvCache &c, const KvNew &a, const KvWeigh &w, hipStream_
         return n > most ? (most < 1 ? 1 : most) : n < 1 ? 1 : n;
     };
     // A tile to a wave, or, of few positions and many rows, to all waves of a workgroup, its
-    // rows shared: what takes fewer turns, were all sequences as long as the table's rows.
+    // rows shared: what takes less work, were all sequences as long as the table's rows. In us,
+    // alone and shared, 8 heads of 128, bf16: 52 and 69 (4 sequences of 5000, 33 tokens of 8
+    // heads), 121 and 151 (of 8000, 64 tokens), 35 and 29 (of 1000, 128 tokens of 4), 63 and 31
+    // (one of 2000, 256 tokens); of one head of 300 positions, 1000 tokens of 8, 384 and 61.
     const int64_t alone = splits_of(over(tiles, kWaves)), together = splits_of(tiles);
     const int64_t blocks = over(over(a.tokens * a.group, a.seqs), 32);
-    const bool team = over(tiles, together) * (3 + over(blocks, kWaves)) < over(tiles, alone * kWaves) * (2 + blocks);
+    const bool team = over(tiles, together) * (1 + 2 * over(blocks, kWaves)) < over(tiles, alone * kWaves) * (1 + 2 * blocks);
     const int64_t splits = team ? together : alone;
     const size_t lds = Form<D, SUB>::kBook + kSeqs * sizeof(KvSeq) + 2 * kWaves * 32 * sizeof(float) +
                        (kWaves + a.seqs + 1) * sizeof(unsigned);
