@@ -10,11 +10,10 @@
 //
 // The keys' codes are the bytes that must come from memory. For a single new token it is their
 // way that takes the time, and what a launch takes before its first tile (the centres to LDS,
-// some 9 us): 32 sequences of 512 to 4096, 4 heads to each of 8 key heads of 128, bf16, 19 us.
+// some 9 us): 32 sequences of 512 to 4096, 4 heads to each of 8 key heads of 128, bf16, 19.7 us.
 // For many the vector ALU does, with 19 operations to a score under a cap, 9 without, and the
-// way that tiles fall to waves (3.2 to one): the last 33 to 64 tokens of 4 prompts of 5000 to
-// 8000, 8 heads to a key head, capped, 95 us, 0.22 PFLOP/s of products; the vector ALU is at
-// work for half of it, the matrix cores for a tenth.
+// way that tiles fall to waves (some 3 to one): the last 33 to 64 tokens of 4 prompts of 5000
+// to 8000, 8 heads to a key head, capped, 82 us, 0.25 PFLOP/s of products.
 #include "kv_tokens_device.h"
 
 #include <type_traits>
@@ -28,12 +27,21 @@ constexpr int kThreads = kWaves * kWave;
 // Tiles whose codes are under way to a wave: with four 32 sequences of 4096 took 18.5 us, with
 // one 20.4; more would not fit the registers.
 constexpr int kAhead = 4;
-constexpr int kSeqs = 1024;          // sequences that are kept in LDS
+constexpr int kSeqs = 512;           // sequences that are kept in LDS
 
 template <int D, int SUB>
 struct Form {
     static constexpr int S = D / SUB, H = S / 2;         // codes of a key, of a lane's half of it
     static constexpr int kBook = D * 512;                // [S][256][SUB]
+    static constexpr int kRow = D * 2 + 16;              // bytes of a row of queries in LDS: rows that
+    static constexpr int kRows = kWaves * 32 * kRow;     // lanes read at once begin on banks of their own
+    static constexpr size_t lds(int64_t sequences)
+    {
+        return kBook + kRows + kSeqs * sizeof(KvSeq) + 2 * kWaves * 32 * sizeof(float) +
+               (kWaves + sequences + 1) * sizeof(unsigned);
+    }
+    static_assert(kBook + kRows + kSeqs * sizeof(KvSeq) + 2 * kWaves * 32 * sizeof(float) +
+                  (kWaves + kKvMaxSeqs + 1) * sizeof(unsigned) <= kMaxLds, "a workgroup");
 };
 
 // N bytes of codes, in whole words.
@@ -81,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     extern __shared__ uint4 lds[];
     // the kernel has no LDS but its dynamic one, which so begins at 0
     char *const book = reinterpret_cast<char *>(lds);
-    KvSeq *const seqs = reinterpret_cast<KvSeq *>(book + F::kBook);      // [kSeqs]
+    KvSeq *const seqs = reinterpret_cast<KvSeq *>(book + F::kBook + F::kRows);      // [kSeqs]
     float *const team_sum = reinterpret_cast<float *>(seqs + kSeqs);     // [2][kWaves][32]
     unsigned *const wave_sum = reinterpret_cast<unsigned *>(team_sum + 2 * kWaves * 32);      // [kWaves]
     unsigned *const first = wave_sum + kWaves;                           // [seqs + 1]
@@ -272,23 +280,30 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
     for (int i = 0; i < kAhead; ++i) load(codes[i], where[i]);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) find_next(where[i]);
-    // 32 rows as they come from memory: a lane has half the features of row `col` of them,
-    // its token's number in the sequence and start, its logarithm and slope.
+    // 32 rows: a lane has its token's number in the sequence and start, logarithm and slope of
+    // row `col` of them. The queries come from memory 1024 bytes of rows to a load, a block
+    // ahead, and go to LDS, where each lane has its half of a row for the products: a block
+    // takes some 3600 cycles. Loaded as the products take them, 16 bytes of 64 half rows to a
+    // load, it took 5000, half of them waiting for the rows.
     struct Rows {
-        u4v q[D / 16];
         int tok, start;
         float lse, slope;
     };
     Rows cur, coming;
-    int loaded = -1;                                     // the sequence whose only rows are in cur
+    u4v raw[D / 16];                                     // the queries of the coming rows
+    const uint32_t wave_rows = F::kBook + wave * (32 * F::kRow);
+    int loaded = -1;                                     // the sequence whose rows are in LDS
+    int next_row = 0;                                    // the first of those to ask for
     const int tokens_on = team_rows / a.group, heads_on = team_rows % a.group;
     int tok = 0, hd = 0;                                 // of the next block's row
     // the sequence's first rows come next
     const auto rewind = [&]() {
+        next_row = 32 * rank;
         tok = (int)((unsigned)(32 * rank + col) / (unsigned)a.group);
         hd = (int)((unsigned)(32 * rank + col) % (unsigned)a.group);
     };
-    const auto begin = [&](Rows &x, const KvSeq &s) {
+    const auto begin = [&](const KvSeq &s) {
+        Rows &x = coming;
         // behind the last row: some row
         const int64_t t = s.t0 + min(tok, s.n - 1);
         const int hq = h * a.group + hd;
@@ -296,15 +311,30 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         x.start = a.starts ? a.starts[t] : 0;
         x.lse = w.lse[t * heads + hq];
         x.slope = a.slopes ? a.slopes[hq] : 0.f;
-        const uint16_t *const src = a.q + t * a.q_token + hq * a.q_head + half * (D / 2);
+        const uint64_t src = reinterpret_cast<uint64_t>(a.q + t * a.q_token + hq * a.q_head);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x.q[i] = *reinterpret_cast<const u4v *>(src + i * 8);
+        for (int i = 0; i < D / 16; ++i) {
+            const int row = (i * kWave + lane) / (D / 8), chunk = (i * kWave + lane) % (D / 8);
+            const uint32_t lo = __builtin_amdgcn_ds_bpermute(row * 4, (int)(uint32_t)src);
+            const uint32_t hi = __builtin_amdgcn_ds_bpermute(row * 4, (int)(uint32_t)(src >> 32));
+            raw[i] = *(const __attribute__((address_space(1))) u4v *)(((uint64_t)hi << 32 | lo) + chunk * 16);
+        }
         tok += tokens_on;
         hd += heads_on;
         if (hd >= a.group) {
             hd -= a.group;
             ++tok;
         }
+        next_row += team_rows;
+        if (next_row >= s.n * a.group) rewind();         // behind the last: the first, for the next tile
+    };
+    // The rows that begin() asked for are the ones at hand.
+    const auto take = [&]() {
+        cur = coming;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            lds_put(wave_rows + (i * kWave + lane) / (D / 8) * F::kRow + (i * kWave + lane) % (D / 8) * 16, 0, raw[i]);
+        asm volatile("" ::: "memory");                   // a wave's LDS accesses keep their order
     };
     // The tile at `now`, whose codes are codes[I]. False: it was the last.
     const auto turn = [&](auto I) {
@@ -323,60 +353,63 @@ __global__ __launch_bounds__(kThreads) void kv_weigh_kernel(KvCache c, KvNew a, 
         const int b = now.b, pos = (now.t + now.tile0) * 32;
         const KvSeq s = now.s;
         float sum[16] = {};
-        const auto block = [&](const Rows &x) {
+        const int rows = s.n * a.group;
+        if (loaded != b) {
+            loaded = b;
+            rewind();
+            begin(s);
+            __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0), or the compiler waits below,
+            take();                                      // where codes are under way
+            if (rows > team_rows) begin(s);
+        }
+#pragma unroll 1
+        for (int r0 = 32 * rank;; r0 += team_rows) {
+            const Rows x = cur;
             KvSeen seen = kv_seen(a, s, x.tok, x.start);
             const float base = x.lse * kLog2e;
             if (x.tok >= s.n || base == -INFINITY) seen.lo = seen.hi = 0;
-            if (!__any(seen.lo < pos + 32 && seen.hi > pos)) return;
+            const bool any = __any(seen.lo < pos + 32 && seen.hi > pos);
             const bool whole = __ballot(seen.lo <= pos && seen.hi >= pos + 32) == ~0ull;
             f16v z;
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.f;
+            if (any) {
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) z = mfma32<FP16>(k[i], x.q[i], z);
-            const int y0 = pos + 4 * half;               // score i is position y0 + 8 (i / 4) + i % 4
-            if (a.cap_log2 > 0.f) kv_cap<16>(z, a);
-            const float scale = a.cap_log2 > 0.f ? 1.f : a.scale_log2;
-            if (a.slopes) {
-                const float far = (float)(seen.at - y0), slope = x.slope * kLog2e;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale) - base;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = __builtin_fmaf(z[i], scale, -base);
+                for (int i = 0; i < D / 16; ++i)
+                    z = mfma32<FP16>(k[i], lds_get<u4v>(wave_rows + col * F::kRow + half * D, i * 16), z);
+                asm volatile("" ::: "memory");
             }
+            if (rows > team_rows) {
+                take();
+                begin(s);
+            }
+            if (any) {
+                const int y0 = pos + 4 * half;               // score i is position y0 + 8 (i / 4) + i % 4
+                if (a.cap_log2 > 0.f) kv_cap<16>(z, a);
+                const float scale = a.cap_log2 > 0.f ? 1.f : a.scale_log2;
+                if (a.slopes) {
+                    const float far = (float)(seen.at - y0), slope = x.slope * kLog2e;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(z[i]);
-            if (whole) {
+                    for (int i = 0; i < 16; ++i)
+                        z[i] = __builtin_fmaf(-slope, fabsf(far - (float)(8 * (i / 4) + i % 4)), z[i] * scale) - base;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i] += z[i];
-            } else {
+                    for (int i = 0; i < 16; ++i) z[i] = __builtin_fmaf(z[i], scale, -base);
+                }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int p = y0 + 8 * (i / 4) + i % 4;
-                    sum[i] += p >= seen.lo && p < seen.hi ? z[i] : 0.f;
+                for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(z[i]);
+                if (whole) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[i] += z[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int p = y0 + 8 * (i / 4) + i % 4;
+                        sum[i] += p >= seen.lo && p < seen.hi ? z[i] : 0.f;
+                    }
                 }
             }
-        };
-        // A block's rows are asked for while the one before is worked on, behind the last one
-        // the first again, for the next tile; a single block's stay.
-        const int rows = s.n * a.group;
-        if (loaded != b) {
-            rewind();
-            begin(cur, s);
-            loaded = b;
-            __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0), or the compiler waits below,
-        }                                                // where codes are under way
-#pragma unroll 1
-        for (int r0 = 32 * rank + team_rows;; r0 += team_rows) {
-            if (rows > team_rows) {
-                if (r0 >= rows) rewind();
-                begin(coming, s);
-            }
-            block(cur);
-            if (rows > team_rows) cur = coming;
-            if (r0 >= rows) break;
+            if (r0 + team_rows >= rows) break;
         }
         // Over the 32 lanes of a half, halving what each holds (rows of 16 exchange, then
         // lanes 8, 7, 2 and 1 away): place i of the sums in the end is 8 bit 4 + 4 bit 3 +
@@ -431,15 +464,15 @@ hipError_t launch(const KvCache &c, const KvNew &a, const KvWeigh &w, hipStream_
     };
     // A tile to a wave, or, of few positions and many rows, to all waves of a workgroup, its
     // rows shared: what takes less work, were all sequences as long as the table's rows. In us,
-    // alone and shared, 8 heads of 128, bf16: 52 and 69 (4 sequences of 5000, 33 tokens of 8
-    // heads), 121 and 151 (of 8000, 64 tokens), 35 and 29 (of 1000, 128 tokens of 4), 63 and 31
-    // (one of 2000, 256 tokens); of one head of 300 positions, 1000 tokens of 8, 384 and 61.
+    // alone and shared, 8 heads of 128, bf16, measured with the queries not yet over LDS: 52 and
+    // 69 (4 sequences of 5000, 33 tokens of 8 heads), 121 and 151 (of 8000, 64 tokens), 35 and 29
+    // (of 1000, 128 tokens of 4), 63 and 31 (one of 2000, 256 tokens); of one head of 300
+    // positions, 1000 tokens of 8, 384 and 61.
     const int64_t alone = splits_of(over(tiles, kWaves)), together = splits_of(tiles);
     const int64_t blocks = over(over(a.tokens * a.group, a.seqs), 32);
     const bool team = over(tiles, together) * (1 + 2 * over(blocks, kWaves)) < over(tiles, alone * kWaves) * (1 + 2 * blocks);
     const int64_t splits = team ? together : alone;
-    const size_t lds = Form<D, SUB>::kBook + kSeqs * sizeof(KvSeq) + 2 * kWaves * 32 * sizeof(float) +
-                       (kWaves + a.seqs + 1) * sizeof(unsigned);
+    const size_t lds = Form<D, SUB>::lds(a.seqs);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(c.heads * splits)), dim3(kThreads), lds, s, c, a, w,
                        (int)splits, team ? kWaves : 1);
     return hipGetLastError();
