@@ -5,6 +5,7 @@ import math
 
 import pytest
 import torch
+import torch.autograd.forward_ad
 
 import paper_1402_3788_amd as km
 from kv_serve_reference import (BF, DEV, FP, Call, attention, check_attention, evicted, make_cache,
@@ -704,3 +705,145 @@ def test_refusals_of_the_others():
     refused(e, call.cache, w, call.table, n, 30, to=call.table[:, :1])
     refused(e, call.cache, w, call.table, torch.stack((n, n), 1)[:, 0], 5)
     refused(e, call.cache, w[:, :1].expand(2, 2, -1), call.table, n, 5)
+
+
+# ------------------------------------------------------------------ other ways to the calls
+
+def test_same_bits_without_the_call_module(monkeypatch):
+    """The calls that the C++ module makes and those through ctypes are the same."""
+    call = Call([(200, 30), (90, 1), (0, 0)], heads=2, group=2, dim=64, seed=21)
+    set_mode(call, "all")
+    positions = torch.arange(call.q.shape[0], device=DEV)
+    f = torch.rand(20, dtype=torch.float64, device=DEV)
+
+    def everything():
+        q, k = km.kmeans_kv_rotate(call.q, call.q[:, :2], positions, f, interleaved=True, amplitude=1.5)
+        out, lse = call.attend()
+        w = call.weigh(lse)
+        codes = call.cache.k_codes.clone(), call.cache.v_codes.clone()
+        table = torch.arange(6, dtype=torch.int32, device=DEV).view(3, 2)
+        kept, left, ww = km.kmeans_kv_evict(call.cache, w, call.table, call.lengths, 24, recent=5, first=2,
+                                            to=table)
+        moved = call.cache.k_codes.clone(), call.cache.v_codes.clone()
+        for t, x in zip((call.cache.k_codes, call.cache.v_codes), codes):
+            t.copy_(x)
+        return q, k, out, lse, w, kept, left, ww, *moved
+
+    # pages 0 to 5 take what is kept: no sequence may have them
+    used = call.table[call.table >= 0]
+    call.table[call.table >= 0] = used.argsort().argsort().to(torch.int32) + 6
+    pages = 6 + used.numel()
+    old = call.cache
+    call.cache = make_cache(2, 64, 4, 256, BF, pages, old.page, seed=22)
+    want = everything()
+    monkeypatch.setattr(km.kv, "_fast", None)
+    for a, b in zip(everything(), want):
+        assert torch.equal(a, b)
+
+
+def test_calls_that_need_a_gradient():
+    call = Call([(40, 7)], heads=2, group=2, dim=64, seed=23)
+    positions = torch.arange(7, device=DEV)
+    f = torch.rand(8, dtype=torch.float64, device=DEV)
+    out, lse = call.attend()
+    q = call.q
+    fwd = torch.autograd.forward_ad
+    for leaf in (q.clone().requires_grad_(), q.clone().requires_grad_() * 1):
+        call.q = leaf
+        for run in (call.attend, lambda: call.weigh(lse),
+                    lambda: km.kmeans_kv_rotate(leaf, None, positions, f)):
+            with pytest.raises(ValueError, match="gradient"):
+                run()
+        with torch.no_grad():
+            assert torch.equal(call.attend()[0], out)
+    with fwd.dual_level():
+        call.q = fwd.make_dual(q, q)
+        for run in (call.attend, lambda: call.weigh(lse),
+                    lambda: km.kmeans_kv_rotate(call.q, None, positions, f)):
+            with pytest.raises(ValueError, match="gradient"):
+                run()
+    call.q = q
+    w = call.weigh(lse)
+    with pytest.raises(ValueError, match="gradient"):
+        call.weigh(lse, w.clone().requires_grad_())
+    with pytest.raises(ValueError, match="gradient"):
+        call.weigh(lse.clone().requires_grad_())
+    with pytest.raises(ValueError, match="gradient"):
+        km.kmeans_kv_evict(call.cache, w.clone().requires_grad_(), call.table, call.lengths, 8)
+
+
+def test_two_streams_at_once():
+    calls = [Call([(3000, 70), (500, 1)], heads=2, group=4, dim=128, seed=31),
+             Call([(900, 1), (2000, 5)], heads=2, group=4, dim=128, seed=32)]
+    want = []
+    for c in calls:
+        out, lse = c.attend()
+        want.append((out, lse, c.weigh(lse)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = [[], []]
+    for _ in range(10):
+        for c, s, g in zip(calls, streams, got):
+            with torch.cuda.stream(s):
+                out, lse = c.attend()
+                g.append((out, lse, c.weigh(lse)))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for x in g:
+            for a, b in zip(x, w):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("lengths,keep,kind", [
+    # a tile of kept positions that lie far from each other, and near; many heads, whose
+    # workgroups take one tile after the other
+    ([20000, 9000], 300, "ties"), ([1500] * 6, 1400, "ties"), ([700, 20000], 650, "ties"),
+])
+def test_evict_far_and_near(lengths, keep, kind, in_place):
+    for dim, sub in ((64, 8), (128, 2), (96, 8)):
+        run_evict(lengths, keep, 10, 2, None, in_place, dim, sub, 32, heads=3 if len(lengths) < 3 else 80,
+                  kind=kind)
+
+
+def test_offsets_past_32_bits():
+    """The last pages of a cache whose codes are more than 2^32 bytes, and weights whose
+    rows are more than 2^31 elements apart."""
+    heads, dim, sub, page = 8, 128, 2, 64
+    each = heads * page * (dim // sub)
+    pages = (1 << 32) // each + 200
+    g = torch.Generator().manual_seed(41)
+    centres = torch.randn(heads, dim // sub, 256, sub, generator=g).to(BF).to(DEV)
+    cache = km.KVCodes.empty(centres, centres, pages, page)
+    n = 40                                               # pages of a sequence
+    low = torch.arange(n, dtype=torch.int32, device=DEV).view(1, n)
+    high = low + (pages - n)
+    for t in (cache.k_codes, cache.v_codes):
+        t[:n].copy_(torch.randint(0, 256, t[:n].shape, generator=g, dtype=torch.uint8))
+        t[-n:] = t[:n]
+    lengths = torch.tensor([n * page - 5], dtype=torch.int32, device=DEV)
+    for new in (1, 40):
+        q = torch.randn(new, heads * 4, dim, generator=g).to(BF).to(DEV)
+        bounds = torch.tensor([0, new], dtype=torch.int32, device=DEV)
+        want = km.kmeans_kv_attend_tokens(cache, q, bounds, low, lengths)
+        got = km.kmeans_kv_attend_tokens(cache, q, bounds, high, lengths)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        w = km.kmeans_kv_weigh(cache, q, want[1], bounds, low, lengths)
+        assert torch.equal(km.kmeans_kv_weigh(cache, q, want[1], bounds, high, lengths), w)
+    # the same weights to both, in rows far apart
+    room = torch.zeros((1 << 31) + heads * n * page, device=DEV)
+    far = room.as_strided((2, heads, n * page), (1 << 31, n * page, 1))
+    both, two = torch.cat((low, high)), torch.cat((lengths, lengths))
+    km.kmeans_kv_weigh(cache, q.repeat(2, 1, 1), want[1].repeat(2, 1),
+                       torch.tensor([0, 40, 80], dtype=torch.int32, device=DEV), both, two, far)
+    assert torch.equal(far[0], far[1])
+    # one sequence and two share rows out in different ways: sums of the same 160 weights, none
+    # below zero, in two orders, each off by at most 159 roundings of at most the sum
+    assert ((far[0].double() - w[0]).abs() <= 2 * 159 * 2.0 ** -24 * w[0].double()).all()
+    was = far.clone()
+    kept, left, ww = km.kmeans_kv_evict(cache, far, both, two, 1000, recent=30)
+    assert ww is far and left is two and left.tolist() == [1000, 1000]
+    assert torch.equal(kept[0], kept[1]) and torch.equal(far[0], far[1])
+    assert (kept[0].diff(dim=-1) > 0).all() and torch.equal(far[0, :, :1000], was[0].gather(1, kept[0].long()))
+    for t in (cache.k_codes, cache.v_codes):
+        assert torch.equal(t[:n], t[-n:])
