@@ -445,11 +445,13 @@ size_t kmeans_kv_attend_tokens_workspace_bytes(const kmeans_kv_t *kv, const kmea
  * no token of the sequence sees are not read. out and lse overlap nothing that is read,
  * and no two of their elements lie in one place.
  * tokens * q_heads < 2^30, table_pages * page <= 2^30, as many of both together that
- * (seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27, |scale| <= 2.35e38, cap finite,
- * 0 or so large that scale / cap is finite (KMEANS_EINVAL otherwise). Scores, their maximum
+ * (seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27,
+ * |scale| <= 2.35e38, cap finite, 0 or so large that scale / cap is finite
+ * (KMEANS_EINVAL otherwise). Scores, their maximum
  * and sum and the output are held in fp32; a weight enters the product with the values as
  * one or two 16-bit numbers, off by at most half a step of the cache's type. The same
- * inputs give the same bits. Asynchronous on `stream`.
+ * inputs give the same bits; the order of a sequence's sums may depend on what else the
+ * call has. Asynchronous on `stream`.
  */
 int kmeans_kv_attend_tokens(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t, const void *q,
                             int64_t q_token, int64_t q_head, void *out, int64_t out_token,
@@ -464,7 +466,8 @@ int kmeans_kv_attend_tokens(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t, 
  * [seqs][heads][positions], contiguous in the last, other strides in elements; positions
  * from `positions` on are left out. With add == 0 every element is written, with 1 the sums
  * are added to what is there. No two rows overlap. Limits as of kmeans_kv_attend_tokens;
- * positions up to 2^30. The same inputs give the same bits. Asynchronous on `stream`.
+ * positions up to 2^30. The same inputs give the same bits, as above. Asynchronous on
+ * `stream`.
  */
 int kmeans_kv_weigh(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t, const void *q,
                     int64_t q_token, int64_t q_head, const float *lse, float *weights,
