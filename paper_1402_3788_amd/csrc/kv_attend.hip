@@ -312,6 +312,7 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
             if (__any(lane < a.seqs && (unsigned)(s.n * a.group - 1) >= (unsigned)nq)) {
                 const int upto = wave_scan((s.n * a.group + nq - 1) / nq);
                 seqs = __builtin_amdgcn_readlane(upto, 63);
+                if (seqs > kv_most_units(a, nq)) seqs = 0;
                 b = 0;
                 for (int i = 0; i < a.seqs; ++i) b += __builtin_amdgcn_readlane(upto, i) <= lane;
                 before = __shfl(upto, max(b - 1, 0));
@@ -1205,7 +1206,7 @@ KvFewPlan plan_kv_few(const KvCache &c, const KvNew &n)
     // in us, by half and whole columns, 37 and 44 (64 sequences of 2000, 8 rows), 38 and 39 (32
     // of 4096, 4 rows), 30 and 38 (32 of 4096, 8 rows)
     p.wide = rows > 8 * (int64_t)n.seqs;
-    const int64_t units = n.seqs + rows / kv_few_rows(p.wide);
+    const int64_t units = kv_most_units(n, kv_few_rows(p.wide));
     p.units = units > kKvMaxFew ? kKvMaxFew + 1 : (int)units;
     p.in_lanes = n.seqs <= kWave && units <= kWave;
     const int64_t span = ((int64_t)n.table_pages << c.page_log2) / kKvTile + 1;
@@ -1244,7 +1245,7 @@ hipError_t launch_kv_few(const KvCache &c, const KvNew &n, const KvTokensOut &o,
     a.part_ml = reinterpret_cast<float *>(take(wgs * 64 * sizeof(float)));
     a.part_o = reinterpret_cast<float *>(take(0));
     if (!p.in_lanes) {
-        const hipError_t e = launch_kv_units(c, n, a.units, kv_few_rows(p.wide), p.units, s);
+        const hipError_t e = launch_kv_units(c, n, a.units, kv_few_rows(p.wide), s);
         if (e != hipSuccess) return e;
     }
     return c.sub == 2 ? launch_kv_few_2(c, a, p, s)

@@ -6,6 +6,13 @@
 
 namespace lloyd {
 
+// Units of `rows` rows of a call at most, which there is room for. Bounds that descend can
+// make more of the same tokens: then there are none.
+__host__ __device__ inline int64_t kv_most_units(const KvNew &n, int rows)
+{
+    return n.seqs + n.tokens * n.group / rows;
+}
+
 // Query heads of new tokens (rows) of a unit.
 constexpr int kv_few_rows(bool wide) { return wide ? 16 : 8; }
 constexpr int kKvMaxFew = 4096;      // units at most
@@ -34,8 +41,7 @@ KvFewPlan plan_kv_few(const KvCache &c, const KvNew &n);
 hipError_t launch_kv_few(const KvCache &c, const KvNew &n, const KvTokensOut &o, const KvFewPlan &p,
                          void *ws, hipStream_t s);
 
-// Writes the units of `rows` rows of a call, `most` of them at most.
-hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, int rows, int most,
-                           hipStream_t s);
+// Writes the units of `rows` rows of a call.
+hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, int rows, hipStream_t s);
 
 }  // namespace lloyd

@@ -632,10 +632,11 @@ hipError_t KV_CAT(launch_kv_tokens_, KV_SUB)(const KvCache &c, const KvNew &a, c
 namespace {
 
 // One workgroup: the units of all sequences and where their tiles begin.
-__global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUnits to, int rows, int most)
+__global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUnits to, int rows)
 {
     __shared__ int seq_first[kKvMaxSeqs + 1];
     __shared__ int wave_sum[16];
+    __shared__ unsigned long long total;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // sum of x over the threads up to this one, and of all
     const auto scan = [&](int x, int *all) {
@@ -653,11 +654,26 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
     };
     const int per = (a.seqs + 1023) / 1024;
     int n[(kKvMaxSeqs + 1023) / 1024] = {}, sum = 0, units;
+    bool descend = false;
 #pragma unroll
     for (int k = 0; k < (kKvMaxSeqs + 1023) / 1024; ++k) {
         const int b = tid * per + k;
-        if (k < per && b < a.seqs) n[k] = (kv_seq(c, a, b).n * a.group + rows - 1) / rows;
+        if (k < per && b < a.seqs) {
+            n[k] = (kv_seq(c, a, b).n * a.group + rows - 1) / rows;
+            descend |= a.bounds[b] > a.bounds[b + 1];
+        }
         sum += n[k];
+    }
+    if (__syncthreads_or(descend)) {
+        if (tid == 0) total = 0;
+        __syncthreads();
+        atomicAdd(&total, (unsigned long long)sum);
+        __syncthreads();
+        if (total > (unsigned long long)kv_most_units(a, rows)) {
+            sum = 0;
+#pragma unroll
+            for (int k = 0; k < (kKvMaxSeqs + 1023) / 1024; ++k) n[k] = 0;
+        }
     }
     int at = scan(sum, &units) - sum;
 #pragma unroll
@@ -668,7 +684,6 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
     }
     if (tid == 0) seq_first[a.seqs] = units;
     __syncthreads();
-    units = min(units, most);                            // more only if bounds descend
     const auto seq_of = [&](int u) {
         int b = 0, end = a.seqs;                         // the last b with seq_first[b] <= u
         while (end - b > 1) {
@@ -737,7 +752,7 @@ constexpr int kFewUnits = 256;       // of them
 KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 {
     KvTokensPlan p{};
-    p.units = (int)(a.seqs + a.tokens * a.group / kRows);
+    p.units = (int)kv_most_units(a, kRows);
     const int64_t span = ((int64_t)a.table_pages << c.page_log2) / 32 + 2;
     const int64_t most = (p.units * span + kShare - 1) / kShare;
     int64_t splits = kCUs / c.heads;                     // one workgroup to a CU: registers allow no more
@@ -762,10 +777,9 @@ KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 
 }  // namespace
 
-hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, int rows, int most,
-                           hipStream_t s)
+hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, int rows, hipStream_t s)
 {
-    hipLaunchKernelGGL(kv_units_kernel, dim3(1), dim3(1024), 0, s, c, n, to, rows, most);
+    hipLaunchKernelGGL(kv_units_kernel, dim3(1), dim3(1024), 0, s, c, n, to, rows);
     return hipGetLastError();
 }
 
@@ -789,7 +803,7 @@ hipError_t launch_kv_attend_tokens(const KvCache &c, const KvNew &a, const KvTok
     const KvFewPlan f = plan_kv_few(c, a);
     if (few(c, a, f)) return launch_kv_few(c, a, o, f, ws, s);
     const KvTokensPlan p = plan_of(c, a, static_cast<char *>(ws));
-    const hipError_t e = launch_kv_units(c, a, p.of, kRows, p.units, s);
+    const hipError_t e = launch_kv_units(c, a, p.of, kRows, s);
     if (e != hipSuccess) return e;
     return c.sub == 2 ? launch_kv_tokens_2(c, a, o, p, s)
          : c.sub == 4 ? launch_kv_tokens_4(c, a, o, p, s) : launch_kv_tokens_8(c, a, o, p, s);

@@ -324,6 +324,29 @@ def test_garbage_in_device_data():
     assert torch.isfinite(w).all() and (w[1] == 0).all()
 
 
+@pytest.mark.parametrize("seqs,new", [(40, 1), (64, 2), (200, 1), (30, 40), (300, 90)])
+def test_bounds_that_descend(seqs, new):
+    """Bounds that make more rows of the tokens than there are give undefined outputs and
+    touch nothing else: the call's neighbours in memory stay, and so do later calls."""
+    call = Call([(60, new)] * seqs, heads=1, group=4, dim=64, seed=7)
+    T = call.q.shape[0]
+    want, lse0 = call.attend()
+    w0 = call.weigh(lse0)
+    good = call.bounds.clone()
+    n = km.kmeans_kv_attend_tokens_workspace_bytes(call.cache, T, seqs, 4, call.table.shape[1])
+    room = torch.full((n + 4096,), 77, dtype=torch.uint8, device=DEV)
+    out = torch.full((T + 8, 4, 64), 5.0, dtype=BF, device=DEV)
+    for bad in (torch.arange(seqs + 1) % 2 * T, T - good.cpu(), good.cpu().roll(1)):
+        call.bounds.copy_(bad)
+        _, lse = call.attend(out=out[:T], ws=room[:n])
+        assert (room[n:] == 77).all() and (out[T:] == 5).all()
+        w = call.weigh(lse0)
+        assert w.shape == w0.shape
+    call.bounds.copy_(good)
+    out, lse = call.attend()
+    assert torch.equal(out, want) and torch.equal(lse, lse0) and torch.equal(call.weigh(lse0), w0)
+
+
 def test_infinities_and_nan_in_what_is_not_seen():
     """NaN in the query of one token stays there, and the largest centres in positions
     that are not seen (scores of infinity) change nothing."""
