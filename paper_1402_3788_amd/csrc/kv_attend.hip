@@ -379,7 +379,7 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
         if (tid == 0) first[a.seqs] = tiles;
         __syncthreads();
     }
-    const int used = splits_used(tiles, splits, W);
+    const int used = splits_used(tiles, splits, FEW ? kFewShare : W);
     const auto unit_of = [&](int u) {
         if constexpr (FEW) return u < kUnits ? units[u] : a.units.unit[u];
         else return KvUnit{};
@@ -1211,6 +1211,10 @@ KvFewPlan plan_kv_few(const KvCache &c, const KvNew &n)
     p.in_lanes = n.seqs <= kWave && units <= kWave;
     const int64_t span = ((int64_t)n.table_pages << c.page_log2) / kKvTile + 1;
     p.splits = splits_of(c, 1, units * span);
+    if (p.splits > 1) {
+        const int64_t most = kCUs / c.heads, tiles = units * span;
+        p.splits = (int)(most < 1 ? 1 : most * kFewShare < tiles ? most : (tiles + kFewShare - 1) / kFewShare);
+    }
     const size_t wgs = (size_t)c.heads * p.splits;
     p.total = 0;
     for (size_t x : {sizeof(int32_t), sizeof(int32_t) * (p.units + 1), sizeof(KvUnit) * p.units,
