@@ -262,7 +262,7 @@ __device__ inline int wave_scan(int x)
 // each of which sees positions of its own. A decode step of 32 sequences of 512 to 4096, 4 heads
 // to each of 8 key heads of 128, with distance slopes: 25 us and 4 us for the joining launch; the
 // first tile begins 4 to 6 us after the launch does, when the units are known and the centres
-// are in LDS, and of short contexts the joining of what waves hold takes 1 us to a unit.
+// are in LDS.
 template <int D, int SUB, bool FP16, bool WIDE, typename A>
 __global__ __launch_bounds__((Form<D, SUB>::kThreads)) void
 kv_attend_kernel(KvCache c, A a, int splits, int qblocks)

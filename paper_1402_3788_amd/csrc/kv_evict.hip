@@ -17,8 +17,11 @@ namespace lloyd {
 
 namespace {
 
-constexpr int kPick = 512;           // threads that pick
-constexpr int kPickWaves = kPick / kWave;
+// Threads that pick, of a row's positions up to kLong and beyond (as many as the table has room
+// for). In us, with 512 and 1024, and the move after it: 72 and 79 (64 sequences of 8192, 8
+// heads), 22 and 20 (4 of 8192), 36 and 30 (4 of 16000), 80 and 71 (32 of 16000), 174 and 76 (one
+// of 65536), 271 and 152 (4 of 100000).
+constexpr int kUsual = 512, kMost = 1024, kLong = 8192;
 constexpr int kMove = 256;           // threads that move
 // Positions between a tile's first and last that LDS holds. Half of 8192 kept, a tile of 256
 // places spans some 512: with 512 half of the tiles were picked from memory, and the values
@@ -38,22 +41,24 @@ __device__ inline int length_of(const KvCache &c, const KvEvict &e, int b)
     return min(max(e.lengths[b], 0), e.table_pages << c.page_log2);
 }
 
-// How many of a row's weights a thread holds; longer rows are read again in each pass.
-constexpr int kHeld = 32;
+// How many of a row's weights a thread holds at most; longer rows are read again in each pass.
+// (26 of 64 go to memory, and 65536 positions take 76 us; read again, 100.)
+constexpr int kHeld = 64;
+static_assert(kLong <= 16 * kUsual, "all are held");
 
 struct PickLds {
     int counts[2048];
-    int wave_sum[kPickWaves], wave_eq[kPickWaves];
+    int wave_sum[16], wave_eq[16];
     int found[2];
 };
 
 // The positions [from, to) of a row, wave after wave and in each 64 at a time: f(i, the
 // order of its weight), of 64 whole ones that may go beyond `to`, where that is 0.
-template <int HELD, typename G, typename F>
+template <int T, int HELD, typename G, typename F>
 __device__ inline void each_of(int from, int to, const uint32_t (&held)[HELD ? HELD : 1], const G &order_at, const F &f)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int each = ((to - from + kPick - 1) / kPick) * kWave, w0 = from + wave * each;
+    const int each = ((to - from + T - 1) / T) * kWave, w0 = from + wave * each;
     if constexpr (HELD) {
 #pragma unroll
         for (int r = 0; r < HELD; ++r) {
@@ -68,13 +73,14 @@ __device__ inline void each_of(int from, int to, const uint32_t (&held)[HELD ? H
 }
 
 // Writes the `left` (at least 1) positions of [from, to) with the largest weights, in order.
-template <int HELD, typename G>
+template <int T, int HELD, typename G>
 __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *out, const G &order_at)
 {
+    constexpr int B = 2048 / T;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t held[HELD ? HELD : 1];
     if constexpr (HELD) {
-        const int each = ((to - from + kPick - 1) / kPick) * kWave, i0 = from + wave * each + lane;
+        const int each = ((to - from + T - 1) / T) * kWave, i0 = from + wave * each + lane;
 #pragma unroll
         for (int r = 0; r < HELD; ++r)
             held[r] = r * kWave < each && i0 + r * kWave < to ? order_at(i0 + r * kWave) : 0u;
@@ -86,9 +92,10 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
         // lanes seldom count the same value
         const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
         const uint32_t bins = digit == 2 ? 1023u : 2047u;
-        reinterpret_cast<int4 *>(lds.counts)[tid] = make_int4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < B; ++k) lds.counts[B * tid + k] = 0;
         __syncthreads();
-        each_of<HELD>(from, to, held, order_at, [&](int, uint32_t u) {
+        each_of<T, HELD>(from, to, held, order_at, [&](int, uint32_t u) {
             // many weights may be alike: what the first lane counts is counted at once for all
             const bool counts = (u & mask) == last;
             const uint64_t some = __ballot(counts);
@@ -100,9 +107,10 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
             if (counts && bin != of) atomicAdd(&lds.counts[bin], 1);
         });
         __syncthreads();
-        // thread t has bins 4 t to 4 t + 3; how many lie above those
-        const int4 n4 = reinterpret_cast<const int4 *>(lds.counts)[tid];
-        const int n[4] = {n4.x, n4.y, n4.z, n4.w}, own = n4.x + n4.y + n4.z + n4.w;
+        // thread t has bins B t to B t + B - 1; how many lie above those
+        int n[B], own = 0;
+#pragma unroll
+        for (int k = 0; k < B; ++k) own += n[k] = lds.counts[B * tid + k];
         int above = own;
 #pragma unroll
         for (int k = 1; k < kWave; k *= 2) {
@@ -113,12 +121,12 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
         __syncthreads();
         above -= own;
 #pragma unroll
-        for (int k = 1; k < kPickWaves; ++k) above += k > wave ? lds.wave_sum[k] : 0;
+        for (int k = 1; k < T / kWave; ++k) above += k > wave ? lds.wave_sum[k] : 0;
         if (above < left && above + own >= left) {
 #pragma unroll
-            for (int k = 3; k >= 0; --k) {
+            for (int k = B - 1; k >= 0; --k) {
                 if (above < left && above + n[k] >= left) {
-                    lds.found[0] = 4 * tid + k;
+                    lds.found[0] = B * tid + k;
                     lds.found[1] = left - above;
                 }
                 above += n[k];
@@ -131,7 +139,7 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
     }
     // All above `last`, and the first `left` of those alike.
     int gt = 0, eq = 0;
-    each_of<HELD>(from, to, held, order_at, [&](int, uint32_t u) {
+    each_of<T, HELD>(from, to, held, order_at, [&](int, uint32_t u) {
         gt += __popcll(__ballot(u > last));
         eq += __popcll(__ballot(u == last));
     });
@@ -142,13 +150,13 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
     __syncthreads();
     int alike = 0, at = 0;
 #pragma unroll
-    for (int k = 0; k < kPickWaves - 1; ++k) {
+    for (int k = 0; k < T / kWave - 1; ++k) {
         at += k < wave ? lds.wave_sum[k] : 0;
         alike += k < wave ? lds.wave_eq[k] : 0;
     }
     at += min(alike, left);
     const uint64_t below = (1ull << lane) - 1;
-    each_of<HELD>(from, to, held, order_at, [&](int i, uint32_t u) {
+    each_of<T, HELD>(from, to, held, order_at, [&](int i, uint32_t u) {
         const uint64_t same = __ballot(u == last);
         const bool take = u > last || (u == last && alike + __popcll(same & below) < left);
         const uint64_t taken = __ballot(take);
@@ -158,7 +166,8 @@ __device__ inline void pick(PickLds &lds, int from, int to, int left, int32_t *o
     });
 }
 
-__global__ __launch_bounds__(kPick) void kv_pick_kernel(KvCache c, KvEvict e)
+template <int T>
+__global__ __launch_bounds__(T) void kv_pick_kernel(KvCache c, KvEvict e)
 {
     __shared__ PickLds lds;
     const int tid = threadIdx.x;
@@ -166,23 +175,25 @@ __global__ __launch_bounds__(kPick) void kv_pick_kernel(KvCache c, KvEvict e)
     const int n = length_of(c, e, b);
     int32_t *const kept = e.kept + ((int64_t)b * c.heads + h) * e.keep;
     if (n <= e.keep) {
-        for (int j = tid; j < e.keep; j += kPick) kept[j] = j < n ? j : -1;
+        for (int j = tid; j < e.keep; j += T) kept[j] = j < n ? j : -1;
         return;
     }
     const float *const w = e.weights + b * e.weights_seq + h * e.weights_head;
     const auto order_at = [&](int i) { return i < e.positions ? order_of(w[i]) : order_of(0.f); };
     const int from = e.first, to = n - e.recent, left = e.keep - e.first - e.recent;
-    for (int j = tid; j < e.first; j += kPick) kept[j] = j;
-    for (int j = tid; j < e.recent; j += kPick) kept[e.keep - e.recent + j] = to + j;
+    for (int j = tid; j < e.first; j += T) kept[j] = j;
+    for (int j = tid; j < e.recent; j += T) kept[e.keep - e.recent + j] = to + j;
     if (left == 0) return;
-    if (to - from <= kHeld / 8 * kPick)
-        pick<kHeld / 8>(lds, from, to, left, kept + e.first, order_at);
-    else if (to - from <= kHeld / 2 * kPick)
-        pick<kHeld / 2>(lds, from, to, left, kept + e.first, order_at);
-    else if (to - from <= kHeld * kPick)
-        pick<kHeld>(lds, from, to, left, kept + e.first, order_at);
-    else
-        pick<0>(lds, from, to, left, kept + e.first, order_at);
+    if (to - from <= 4 * T)
+        pick<T, 4>(lds, from, to, left, kept + e.first, order_at);
+    else if (T == kUsual || to - from <= 16 * T)
+        pick<T, 16>(lds, from, to, left, kept + e.first, order_at);
+    else if constexpr (T == kMost) {
+        if (to - from <= kHeld * T)
+            pick<T, kHeld>(lds, from, to, left, kept + e.first, order_at);
+        else
+            pick<T, 0>(lds, from, to, left, kept + e.first, order_at);
+    }
 }
 
 // What a workgroup moves: weights, keys' codes or values' codes of a head of a sequence; out
@@ -455,7 +466,11 @@ void move(const KvCache &c, const KvEvict &e, hipStream_t s)
 
 hipError_t launch_kv_evict(const KvCache &c, const KvEvict &e, hipStream_t s)
 {
-    hipLaunchKernelGGL(kv_pick_kernel, dim3((unsigned)(c.heads * e.seqs)), dim3(kPick), 0, s, c, e);
+    const dim3 rows((unsigned)(c.heads * e.seqs));
+    if ((int64_t)e.table_pages << c.page_log2 > kLong)
+        hipLaunchKernelGGL(kv_pick_kernel<kMost>, rows, dim3(kMost), 0, s, c, e);
+    else
+        hipLaunchKernelGGL(kv_pick_kernel<kUsual>, rows, dim3(kUsual), 0, s, c, e);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess) return rc;
     switch (c.dim / c.sub) {

@@ -539,6 +539,12 @@ def run_evict(lengths, keep, recent, first, positions, in_place, dim, sub, page,
 
 
 @pytest.mark.parametrize("in_place", [False, True])
+def test_evict_from_long_rows(in_place):
+    """Rows beyond what a workgroup holds, beside short ones."""
+    run_evict([70000, 9000, 100, 4097], 5000, 100, 4, None, in_place, 64, 8, 1024, heads=2)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
 def test_evict_unusual_weights(in_place):
     run_evict([500, 300], 250, 20, 3, None, in_place, 64, 4, 16, kind="odd")
     run_evict([500, 300], 450, 0, 0, None, in_place, 64, 4, 16, kind="odd")
