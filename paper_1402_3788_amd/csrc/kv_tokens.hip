@@ -739,15 +739,19 @@ __global__ __launch_bounds__(1024) void kv_units_kernel(KvCache c, KvNew a, KvUn
     }
 }
 
-// Units of few rows (kv_attend.hip) read the cache once for every 16 rows, units of 256 take
+// Units of few rows (kv_attend.hip) read the cache once for every 16 rows; units of 256 take
 // longer to begin and cost the same however few of their rows there are. bf16, 8 heads of 128,
 // in us, units of few and of 256: 64 rows of each sequence 23 and 47 (8 of 2000 positions),
 // 32 and 71 (one of 30000), 54 and 62 (64 of 500), 93 and 131 (256 of 300); 128 rows 42 and 48,
-// 49 and 75, 144 and 164 (16 of 8000), but where few positions are cut to many units 54 and 37
-// (32 of 500, 288 units), 88 and 69 (64 of 500, 576 units); 256 rows 60 and 55, 74 and 73.
-constexpr int kFewRows = 64;         // of a sequence on average, up to which units are of few,
-constexpr int kFewMore = 128;        // and where that makes no more than
-constexpr int kFewUnits = 256;       // of them
+// 49 and 75, 144 and 164 (16 of 8000), but of many units 52 and 38 (32 of 500, 288 units), 88 and
+// 69 (64 of 500, 576 units). More rows, by the tiles of units of few to a workgroup: with 22 of
+// them 21 and 33 (128 tokens of 4 heads behind 500), 67: 38 and 48 (a prompt of 500), 134: 34
+// and 57 (64 tokens behind 8000), 146: 45 and 48 (256 behind 2000), 259: 67 and 58 (a prompt of
+// 1000), 280: 62 and 57 (8 of 64 behind 2000), 335: 57 and 42 (8 prompts to 1000, 12 heads of 64).
+constexpr int kFewRows = 64;         // of a sequence on average, up to which units are of few;
+constexpr int kFewUnits = 256;       // where that makes no more than those,
+constexpr int kFewMore = 128;        // up to these, or
+constexpr int kFewTiles = 192;       // where a workgroup has no more than these
 
 KvTokensPlan plan_of(const KvCache &c, const KvNew &a, char *ws)
 {
@@ -787,8 +791,10 @@ hipError_t launch_kv_units(const KvCache &c, const KvNew &n, const KvUnits &to, 
 static bool few(const KvCache &c, const KvNew &a, const KvFewPlan &p)
 {
     const int64_t rows = a.tokens * a.group, seqs = a.seqs;
+    const int64_t span = ((int64_t)a.table_pages << c.page_log2) / kKvTile + 1;
+    const int64_t workgroups = c.heads < kCUs ? kCUs / c.heads : 1;
     return (rows <= kFewRows * seqs && p.units <= kKvMaxFew) ||
-           (rows <= kFewMore * seqs && p.units <= kFewUnits);
+           (p.units <= kFewUnits && (rows <= kFewMore * seqs || p.units * span <= kFewTiles * workgroups));
 }
 
 size_t kv_attend_tokens_bytes(const KvCache &c, const KvNew &a)

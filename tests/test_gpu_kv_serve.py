@@ -237,6 +237,62 @@ def test_every_form(dim, sub, dtype):
         assert ((call.weigh(lse).double() - w).abs() <= d).all()
 
 
+# More rows than units of few are taken for.
+MANY = [
+    ([(400, 390), (330, 330), (0, 0), (70, 5), (3, 9)], dict(group=8, heads=1)),
+    ([(1100, 1100)], dict(group=4, heads=2, page=64)),
+    ([(290, 33)] + [(120 - b, 120 - b) for b in range(0, 110, 3)], dict(group=4, heads=3, page=8)),
+    ([(500, 40), (77, 35)], dict(group=128, heads=1, page=1024)),
+    ([(700, 300), (33, 0), (50, 60), (650, 300)], dict(group=8, heads=2, K=31)),
+]
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_many_rows(case, mode):
+    sizes, kw = MANY[case]
+    dim, sub, dtype = [(64, 2, BF), (128, 4, FP), (96, 8, FP), (128, 8, BF), (96, 4, BF)][case]
+    call = Call(sizes, dim=dim, sub=sub, dtype=dtype, seed=200 + case, **kw)
+    set_mode(call, mode)
+    out, lse = check_attention(call)
+    again = call.attend()
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("sub", [2, 4, 8])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_every_form_of_many_rows(dim, sub, dtype):
+    for page in (16, 32):
+        call = Call([(520, 510), (90, 90)], heads=1, group=8, dim=dim, sub=sub, dtype=dtype, seed=dim + sub,
+                    page=page)
+        set_mode(call, "slopes")
+        check_attention(call)
+
+
+def test_long_context_of_many_rows():
+    """Cut by many workgroups; captured, and replayed with other lengths and bounds."""
+    call = Call([(3000, 600), (6000, 500)], heads=2, group=4, dim=64, page=64, seed=240)
+    out, lse = check_attention(call)
+    n = km.kmeans_kv_attend_tokens_workspace_bytes(call.cache, call.q.shape[0], 2, 8, call.table.shape[1])
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    o, l = torch.zeros_like(out), torch.zeros_like(lse)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call.attend(out=o, lse=l, ws=ws)
+    for _ in range(3):
+        ws.fill_(255)
+        o.fill_(1.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, out) and torch.equal(l, lse)
+    call.lengths[0] = 700
+    call.bounds[1] = 650
+    ws.fill_(255)
+    g.replay()
+    check_attention(call, (o, l))
+
+
 # Rows and positions that are shared out in other ways: to units of few and of many rows, to
 # waves alone and to all of a workgroup.
 SHARES = [
