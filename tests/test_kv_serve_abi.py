@@ -108,6 +108,27 @@ def test_new_tokens(kw, code):
         assert lib.kmeans_kv_attend_tokens_workspace_bytes(d, tokens(**kw)) == 0
 
 
+def test_the_limit_of_tokens_times_positions():
+    """(seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27"""
+    size = lib.kmeans_kv_attend_tokens_workspace_bytes
+    d = ctypes.byref(desc(page=32, pages=1 << 20))
+    for seqs, new, pages in ((4096, 1, 32766), (1024, 1, (1 << 17) - 2), (1, (128 << 13) - 128, 16382)):
+        t = dict(seqs=seqs, tokens=new, q_heads=4, table_pages=pages, table_stride=pages)
+        assert size(d, tokens(**{**t, "table_pages": pages - 1})) > 0
+        assert size(d, tokens(**t)) == 0
+        assert attend(d, **t) == weigh(d, **t) == UNSUPPORTED
+
+
+def test_workspaces():
+    """Every number of rows has one, whichever units it is cut to."""
+    size = lib.kmeans_kv_attend_tokens_workspace_bytes
+    d = ctypes.byref(desc(page=32, pages=1 << 20))
+    for seqs in (1, 3, 64, 65, 300, 4096):
+        for new in (1, 2, 7, 31, 33, 64, 65, 128, 129, 1000, 5000):
+            for pages in (1, 20, 1000):
+                assert size(d, tokens(seqs=seqs, tokens=new, table_pages=pages, table_stride=pages)) > 0
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(out=None), INVALID), (dict(out=ODD), INVALID), (dict(oa=7), INVALID), (dict(ob=-8), INVALID),
     (dict(ws=None), WORKSPACE), (dict(ws=ODD), WORKSPACE), (dict(nbytes=0), WORKSPACE),
