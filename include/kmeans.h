@@ -498,8 +498,9 @@ typedef struct kmeans_kv_evict {
  * position kept[b][h][j] (int32 [seqs][heads][keep], contiguous; -1 past the last).
  * lengths_out[b] = min(lengths[b], keep). weights_out ([seqs][heads][positions], strides of
  * its own) gets the kept positions' weights, in order, and zeros after them. lengths_out may
- * be lengths, weights_out may be weights with the same strides. A sequence of up to `keep`
- * positions keeps them all (with `to`, its codes are copied). Heads keep different
+ * be lengths, weights_out may be weights with the same strides, with and without `to`; no
+ * two of its rows overlap, and else the outputs overlap nothing that is read. A sequence of
+ * up to `keep` positions keeps them all (with `to`, its codes are copied). Heads keep different
  * positions, so that a place stands for no one position of the sequence any more: slopes,
  * windows and starts of later calls count places.
  * Sequences share no page that is written to; pages of `to` are no pages of table, and have

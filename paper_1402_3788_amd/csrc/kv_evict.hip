@@ -198,7 +198,8 @@ __global__ __launch_bounds__(T) void kv_pick_kernel(KvCache c, KvEvict e)
 
 // What a workgroup moves: weights, keys' codes or values' codes of a head of a sequence; out
 // of place one tile of places, in place all tiles one after the other (of a share of the
-// sub-vectors, for values). Each thread asks for all that it moves of a tile before it
+// sub-vectors, for values). Weights may be moved in place while codes go to other pages,
+// and the other way about. Each thread asks for all that it moves of a tile before it
 // waits: the way from a kept position over the table to the codes is three trips to
 // memory, and bytes under way are what the card's rate takes.
 struct MoveGrid {
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(kMove) void kv_move_kernel(KvCache c, KvEvict e, Mo
 #pragma unroll
             for (int k = 0; k < kHold; ++k)
                 if (j0 + k * kMove >= m || i[k] >= e.positions) x[k] = 0.f;
-            if (IN_PLACE) __syncthreads();
+            if (e.weights_in_place) __syncthreads();
 #pragma unroll
             for (int k = 0; k < kHold; ++k)
                 if (j0 + k * kMove < e.positions) out[j0 + k * kMove] = x[k];
@@ -450,7 +451,8 @@ void move(const KvCache &c, const KvEvict &e, hipStream_t s)
             n = (n + tile - 1) / tile;
             return (int)(n > room ? room : n < 1 ? 1 : n);
         };
-        grid = MoveGrid{tiles(e.positions, kFloats), tiles(most, kKeys<S>), tiles(most, kValues)};
+        grid = MoveGrid{e.weights_in_place ? 1 : tiles(e.positions, kFloats), tiles(most, kKeys<S>),
+                        tiles(most, kValues)};
         // of values, no more than are at work at once
         const int64_t values = kResident * kCUs / rows;
         if (grid.values > values) grid.values = (int)(values < 1 ? 1 : values);

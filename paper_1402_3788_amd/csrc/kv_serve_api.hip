@@ -204,6 +204,7 @@ int kmeans_kv_evict(const kmeans_kv_t *kv, const kmeans_kv_evict_t *e, int32_t *
     x.recent = e->recent;
     x.first = e->first;
     x.in_place = e->to == nullptr;
+    x.weights_in_place = weights_out == e->weights;
     x.to = e->to ? e->to : e->table;
     x.to_stride = e->to ? e->to_stride : e->table_stride;
     x.to_pages = (int)(e->to ? e->to_pages : e->table_pages);

@@ -67,7 +67,8 @@ struct KvEvict {
     const int32_t *to;               // the table itself: in place
     int64_t to_stride;
     int to_pages;
-    bool in_place;
+    bool in_place;                   // codes
+    bool weights_in_place;           // whether codes are or not
     int32_t *kept, *lengths_out;
     float *weights_out;
     int64_t out_seq, out_head;
