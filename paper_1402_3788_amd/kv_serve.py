@@ -117,7 +117,7 @@ def kmeans_kv_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.T
     amplitude    factor of the turned features
 
     Returns the turned tensors (q, k). `out` may supply them, among them q and k
-    themselves."""
+    themselves, or others of the same memory with the same strides."""
     flags = (_INTERLEAVED if interleaved else 0) | (_INVERSE if inverse else 0)
     if _kv._fast is not None and out is None:
         index = _current_device()
@@ -156,8 +156,10 @@ def kmeans_kv_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.T
             to, oa, ob = o.data_ptr(), a, b
         else:
             o, to, oa, ob = _target(like, o, shape, what)
-        if o.data_ptr() == at:
-            a, b = oa, ob = _strides(o)[:2]
+        if at and o.data_ptr() == at:       # in place, whichever tensor says so
+            a, b, oa, ob = *_strides(rows)[:2], *_strides(o)[:2]
+            if (a, b) != (oa, ob):
+                raise ValueError(f"out for {what} begins where {what} does, with other strides")
         args += [at, a, b, shape[1], to, oa, ob]
         got.append(o)
     if 2 * frequencies.shape[0] > like.dim:

@@ -1,5 +1,7 @@
 """Calls of serving from the key-value cache that its documentation allows, or refuses,
 with tensors that share memory or carry gradients."""
+import math
+
 import pytest
 import torch
 
@@ -9,6 +11,54 @@ from paper_1402_3788_amd.kv import _call
 from paper_1402_3788_amd.kv_serve import _Evict
 
 pytestmark = pytest.mark.gpu
+
+
+def rotate_inputs(tokens=3, heads=4, half=16, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    room = torch.randn(heads, tokens, 64, generator=g).to(BF).to(DEV)
+    positions = torch.arange(5, 5 + tokens, device=DEV)
+    return room, positions, torch.rand(half, dtype=torch.float64, generator=g).to(DEV)
+
+
+@pytest.mark.parametrize("which", ["q", "k"])
+@pytest.mark.parametrize("fast", [True, False])
+def test_rotate_to_another_view_of_the_same_memory(which, fast, monkeypatch):
+    """An output that begins where its input does has the input's strides, or the call is
+    refused and nothing written."""
+    if not fast:
+        monkeypatch.setattr(km.kv, "_fast", None)
+    room, positions, f = rotate_inputs()
+    was = room.clone()
+    x = room.transpose(0, 1)                             # [tokens, heads, dim]
+    other = torch.randn(3, 4, 64).to(BF).to(DEV)
+    view = room.view(3, 4, 64)
+    args, out = ((x, other), (view, None)) if which == "q" else ((other, x), (None, view))
+    with pytest.raises((ValueError, km.KmeansError)):
+        km.kmeans_kv_rotate(*args, positions, f, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(room, was)
+    # another tensor of the same layout is in place
+    want = km.kmeans_kv_rotate(x, None, positions, f)[0]
+    again = room.as_strided((3, 4, 64), x.stride())
+    args, out = ((x, other), (again, None)) if which == "q" else ((other, x), (None, again))
+    got = km.kmeans_kv_rotate(*args, positions, f, out=out)[0 if which == "q" else 1]
+    assert got is again and torch.equal(x, want)
+
+
+@pytest.mark.parametrize("shape,strides", [
+    ((1, 4, 64), (4096, 64, 1)), ((1, 4, 64), (3, 64, 1)), ((3, 1, 64), (64, 1000, 1)),
+    ((3, 1, 64), (64, 5, 1)),
+])
+def test_rotate_in_place_whatever_the_stride_of_a_single_row(shape, strides):
+    room, positions, f = rotate_inputs(tokens=3, heads=4)
+    x = room.flatten()[:math.prod(shape)].view(shape)
+    again = room.as_strided(shape, strides)
+    want = km.kmeans_kv_rotate(x, None, positions[:shape[0]], f)[0]
+    was = room.clone()
+    for q, out in ((x, again), (again, x), (again, again)):
+        room.copy_(was)
+        got = km.kmeans_kv_rotate(q, None, positions[:shape[0]], f, out=(out, None))[0]
+        assert got is out and torch.equal(x, want)
 
 
 @pytest.mark.parametrize("positions", [700, 2000, 2100, 9000, 70000])
