@@ -202,7 +202,7 @@ PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor *positions = ints(a[4], q, at::kLong, q.size(0));
     const at::Tensor *frequencies = plain(a[5], q, at::kDouble, 1);
     if (!positions || !frequencies || !frequencies->is_contiguous() || 2 * frequencies->size(0) > q.size(2) ||
-        q.size(2) > INT32_MAX || frequencies->is_conj())
+        q.size(2) > INT32_MAX || frequencies->is_conj() || needs_gradient(*frequencies))
         Py_RETURN_NONE;
     if (k && (k->size(0) != q.size(0) || k->size(2) != q.size(2))) Py_RETURN_NONE;
     for (const at::Tensor *t : {&q, k})

@@ -110,7 +110,8 @@ def kmeans_kv_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.T
                  their heads (k may be None); dim a multiple of 8 up to 512
     positions    int64 [tokens]
     frequencies  float64 [pairs], radians to a position; 2 * pairs <= dim features
-                 of every head are turned, the others copied
+                 of every head are turned, the others copied; constants, as
+                 everywhere here: those that need a gradient are refused
     interleaved  pairs are features (2i, 2i + 1), else (i, i + pairs)
     inverse      by the negative angle: what takes gradients of the outputs to
                  those of q and k
@@ -133,6 +134,7 @@ def kmeans_kv_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.T
     if not (isinstance(frequencies, torch.Tensor) and frequencies.dtype is torch.float64
             and frequencies.dim() == 1 and frequencies.get_device() == like.index):
         raise ValueError("frequencies must be a float64 [pairs] tensor on q's GPU")
+    _no_gradient(frequencies, "frequencies")
     tokens = q.shape[0]
     positions = _ints(like, positions, torch.int64, tokens, "positions")
     frequencies = frequencies.contiguous()

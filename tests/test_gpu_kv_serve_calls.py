@@ -4,6 +4,7 @@ import math
 
 import pytest
 import torch
+import torch.autograd.forward_ad as fwd
 
 import paper_1402_3788_amd as km
 from kv_serve_reference import BF, DEV, evicted, make_cache
@@ -59,6 +60,29 @@ def test_rotate_in_place_whatever_the_stride_of_a_single_row(shape, strides):
         room.copy_(was)
         got = km.kmeans_kv_rotate(q, None, positions[:shape[0]], f, out=(out, None))[0]
         assert got is out and torch.equal(x, want)
+
+
+@pytest.mark.parametrize("fast", [True, False])
+def test_rotate_by_frequencies_that_need_a_gradient(fast, monkeypatch):
+    """Learned frequencies would lose their gradient without a word."""
+    if not fast:
+        monkeypatch.setattr(km.kv, "_fast", None)
+    room, positions, f = rotate_inputs()
+    x = room.transpose(0, 1)
+    want = km.kmeans_kv_rotate(x, None, positions, f)[0]
+    leaf = f.clone().requires_grad_()
+    for t in (leaf, leaf * 1):
+        with pytest.raises(ValueError, match="gradient"):
+            km.kmeans_kv_rotate(x, None, positions, t)
+        with pytest.raises(ValueError, match="gradient"):
+            km.kmeans_kv_rotate(x, None, positions, t, out=(torch.empty_like(want), None))
+        with torch.no_grad():
+            assert torch.equal(km.kmeans_kv_rotate(x, None, positions, t)[0], want)
+        assert torch.equal(km.kmeans_kv_rotate(x, None, positions, t.detach())[0], want)
+    with fwd.dual_level():
+        with pytest.raises(ValueError, match="gradient"):
+            km.kmeans_kv_rotate(x, None, positions, fwd.make_dual(f, f))
+        assert torch.equal(km.kmeans_kv_rotate(x, None, positions, f)[0], want)
 
 
 @pytest.mark.parametrize("positions", [700, 2000, 2100, 9000, 70000])
