@@ -420,7 +420,7 @@ typedef struct kmeans_kv_tokens {
     const int32_t *lengths;      /* [seqs], DEVICE: cached positions, new ones included */
     const int32_t *starts;       /* [tokens], DEVICE, or NULL                           */
     const int32_t *prefixes;     /* [seqs], DEVICE, or NULL                             */
-    const float *slopes;         /* [q_heads], DEVICE, or NULL; finite                  */
+    const float *slopes;         /* [q_heads], DEVICE, or NULL; up to 2.35e38           */
     int64_t tokens;              /* rows of q                                           */
     int32_t seqs;                /* 0 to 4096; seqs * heads < 2^18                      */
     int32_t q_heads;             /* a multiple of the cache's heads, up to 128 to each  */
@@ -446,8 +446,8 @@ size_t kmeans_kv_attend_tokens_workspace_bytes(const kmeans_kv_t *kv, const kmea
  * and no two of their elements lie in one place.
  * tokens * q_heads < 2^30, table_pages * page <= 2^30, as many of both together that
  * (seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27,
- * |scale| <= 2.35e38, cap finite, 0 or so large that scale / cap is finite
- * (KMEANS_EINVAL otherwise). Scores, their maximum
+ * |scale| <= 2.35e38, cap 0 or up to 1.17e38 with a scale / cap that is 0 or a normal
+ * fp32 number (KMEANS_EINVAL otherwise). Scores, their maximum
  * and sum and the output are held in fp32; a weight enters the product with the values as
  * one or two 16-bit numbers, off by at most half a step of the cache's type. The same
  * inputs give the same bits; the order of a sequence's sums may depend on what else the

@@ -3,6 +3,7 @@
 #include "kv_check.h"
 #include "kv_tokens.h"
 
+#include <float.h>
 #include <math.h>
 
 using namespace lloyd;
@@ -34,9 +35,10 @@ int check_new(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t)
         (t->seqs + t->tokens * (t->q_heads / kv->heads) / kKvRows) *
                 (t->table_pages * kv->page / kKvTile + 2) >= (int64_t)1 << 27)
         return KMEANS_EUNSUPPORTED;
-    if (!isfinite(t->scale * kLog2e) || !(t->cap >= 0.f) || !isfinite(t->cap * kLog2e))
+    if (!isfinite(t->scale * kLog2e) || !(t->cap >= 0.f) || !isfinite(2.f * (t->cap * kLog2e)))
         return KMEANS_EINVAL;
-    if (t->cap > 0.f && !isfinite(t->scale / t->cap)) return KMEANS_EINVAL;
+    const float x = t->cap > 0.f ? t->scale / t->cap : 0.f;
+    if (!isfinite(x) || (t->scale != 0.f && t->cap > 0.f && fabsf(x) < FLT_MIN)) return KMEANS_EINVAL;
     return KMEANS_OK;
 }
 

@@ -234,7 +234,8 @@ def kmeans_kv_attend_tokens(cache: KVCodes, q: torch.Tensor, bounds: torch.Tenso
     table     int32 [seqs, pages of a sequence]: page numbers
     lengths   int32 [seqs]: cached positions, the new tokens' included
     scale     of the scores, 1 / sqrt(dim) if None
-    cap       scores become cap * tanh(score / cap), 0: they do not
+    cap       scores become cap * tanh(score / cap), 0: they do not; scale / cap is
+              0 or a normal fp32 number, as most caps up to 1e36 make it
     slopes    float32 [q_heads]: a score loses slope * distance in positions
     window    a token sees its own position and the window - 1 before it, 0: all
     prefixes  int32 [seqs]: first positions that every token of a sequence sees

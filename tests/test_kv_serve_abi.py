@@ -108,6 +108,19 @@ def test_new_tokens(kw, code):
         assert lib.kmeans_kv_attend_tokens_workspace_bytes(d, tokens(**kw)) == 0
 
 
+@pytest.mark.parametrize("scale,cap,code", [
+    (2.0, 1.17e38, OK), (2.0, 1.19e38, INVALID), (2.0, 2.3e38, INVALID),
+    (0.1, 8e36, OK), (0.1, 9e36, INVALID), (-1e-3, 1e37, INVALID), (0.0, 1e38, OK),
+])
+def test_the_limits_of_caps(scale, cap, code):
+    """Twice the cap to base 2, which far scores are worked out with, is a finite fp32 number,
+    and scale / cap has all bits of one."""
+    d = ctypes.byref(desc())
+    kw = dict(scale=scale, cap=cap, tokens=0)
+    assert attend(d, **kw) == weigh(d, **kw, add=1) == code
+    assert (lib.kmeans_kv_attend_tokens_workspace_bytes(d, tokens(**kw)) > 0) == (code == OK)
+
+
 def test_the_limit_of_tokens_times_positions():
     """(seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27"""
     size = lib.kmeans_kv_attend_tokens_workspace_bytes
