@@ -430,7 +430,7 @@ typedef struct kmeans_kv_tokens {
 } kmeans_kv_tokens_t;
 
 /* Bytes of device workspace that kmeans_kv_attend_tokens needs; 0 for arguments it
- * refuses. Pure host computation; no pointer is looked at but whether starts is NULL. */
+ * refuses. Pure host computation; no pointer is looked at. */
 size_t kmeans_kv_attend_tokens_workspace_bytes(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t);
 
 /*
@@ -447,11 +447,12 @@ size_t kmeans_kv_attend_tokens_workspace_bytes(const kmeans_kv_t *kv, const kmea
  * tokens * q_heads < 2^30, table_pages * page <= 2^30, as many of both together that
  * (seqs + tokens * q_heads / heads / 256) * (table_pages * page / 32 + 2) < 2^27,
  * |scale| <= 2.35e38, cap 0 or up to 1.17e38 with a scale / cap that is 0 or a normal
- * fp32 number (KMEANS_EINVAL otherwise). Scores, their maximum
- * and sum and the output are held in fp32; a weight enters the product with the values as
- * one or two 16-bit numbers, off by at most half a step of the cache's type. The same
- * inputs give the same bits; the order of a sequence's sums may depend on what else the
- * call has. Asynchronous on `stream`.
+ * fp32 number (KMEANS_EINVAL otherwise). Scores, their maximum and sum and the output
+ * are held in fp32. A weight enters the product with the values as two 16-bit numbers, as
+ * of kmeans_kv_attend, where new tokens * q_heads / heads are few (64 to a sequence as a
+ * rule), and as one, off by at most half a step of the cache's type, where they are many.
+ * The same inputs give the same bits; that choice, and the order of a sequence's sums, may
+ * depend on what else the call has. Asynchronous on `stream`.
  */
 int kmeans_kv_attend_tokens(const kmeans_kv_t *kv, const kmeans_kv_tokens_t *t, const void *q,
                             int64_t q_token, int64_t q_head, void *out, int64_t out_token,

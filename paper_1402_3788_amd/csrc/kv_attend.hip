@@ -259,7 +259,9 @@ __device__ inline int wave_scan(int x)
 //
 // A is KvAttend, or KvFew for few new tokens of every sequence: then what is said of a
 // sequence here holds for a unit, up to 8 or 16 (WIDE) query heads of its new tokens,
-// each of which sees positions of its own. A decode step of 32 sequences of 512 to 4096, 4 heads
+// each of which sees positions of its own; a row that a unit does not have sees none, so
+// that units which are not full (4 query heads of a single token in 8 columns) mask every
+// tile, and the scores of one twice. A decode step of 32 sequences of 512 to 4096, 4 heads
 // to each of 8 key heads of 128, with distance slopes: 25 us and 4 us for the joining launch; the
 // first tile begins 4 to 6 us after the launch does, when the units are known and the centres
 // are in LDS.
@@ -675,7 +677,8 @@ kv_attend_kernel(KvCache c, A a, int splits, int qblocks)
     if (a0 < a1) {
         const uint32_t k_base = F::kValues + g * (F::SL * 512 * SUB);
         // One tile of 32 positions from `pos` on. What the span leaves out of it
-        // is masked in branches of its own, which most tiles skip.
+        // is masked in branches of its own, which most tiles skip (of single tokens'
+        // attention and of full units).
         const auto step = [&](int t, int pos) {
             const Span &sp = cur.sp;
             bool partial = pos < sp.start || pos + 32 > sp.len;

@@ -6,10 +6,11 @@
 // by 0.03), their cosines and sines go to LDS once for all heads, and each thread turns
 // runs of 8 features, 16 bytes, of one head after the other. Pairs side by side lie in a
 // run. Pairs half of the turned part apart lie in two runs that one thread has where that
-// half is whole runs; otherwise the partners come over LDS. 8192 tokens of 32 query and 8
-// key heads of 128 features, bf16: 27 us, 6.2 TB/s of reads and writes, side by side or
-// half of it apart; 36 us with 46 features turned over LDS, where one pair at a time to a
-// thread, with its loads and stores of 2 bytes, took 111.
+// half is whole runs; otherwise the partners come over LDS. 8192 tokens of 72 heads of
+// 128 features, bf16: 58 us, 5.2 TB/s of reads and writes, a copy's rate. 40 heads, whose 168 MB
+// the last-level cache holds from one pass to the next: 27 us, 6.2 TB/s, side by side or half
+// of it apart; 36 us with 46 features turned over LDS, where one pair at a time to a thread,
+// with its loads and stores of 2 bytes, took 111.
 #include "kv_device.h"
 #include "kv_tokens.h"
 

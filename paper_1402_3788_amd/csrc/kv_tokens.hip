@@ -19,11 +19,13 @@
 // that way is joined by a second launch. A launch before says where units begin.
 //
 // Products bound long prompts, and beside them the exponentials: 4096 tokens of 64 heads on
-// 16384 positions, 8 key heads of 128, bf16: 1.84 ms, 1040 TFLOP/s, the vector ALU at work for
-// 46 % of the time, the matrix cores for 46 %, LDS for 44 %, at a clock that falls to 2.1 GHz. A
-// cap and slopes add 14 operations to a score, and the vector ALU bounds it (83 % of the time):
-// 256 tokens on 65536 positions 0.82 ms, 670 TFLOP/s. Short prompts are three launches: 8 of 101 to 1000
-// tokens, 12 heads of 64, documents of 150, 5 us for the units, 24 for this, 9 for the joins.
+// 16384 positions, 8 key heads of 128, bf16: 1.84 to 1.93 ms, 1000 to 1050 TFLOP/s, the vector ALU
+// at work for 46 % of the time, the matrix cores for 46 %, LDS for 44 %, at a clock that falls to
+// 2.1 GHz. A cap and slopes add 14 operations to a score, and the vector ALU bounds it (83 % of the
+// time): 256 tokens on 65536 positions 0.82 to 0.87 ms, 640 to 670 TFLOP/s. Short prompts are three
+// launches: 8 of 101 to 1000 tokens, 12 heads of 64, documents of 150, 5 us for the units, 25 for
+// this, 9 for the joins. Every wave works on all tiles of its unit, also where none of its rows
+// sees a position of one, and masks them where it has fewer than 32 rows.
 #include "kv_few.h"
 
 #include <type_traits>

@@ -138,7 +138,8 @@ __device__ inline KvSeen kv_seen(const KvNew &a, const KvSeq &s, int i)
 // cap * tanh(scale * z / cap) to base 2, of a lane's N products z. With x = scale * z / cap,
 // up to 5/8 tanh x = x + x^3 P(x^2), P of degree 4 fitted to it there (off by 2^-27 of it);
 // beyond 1 - 2 / (1 + e^2x), which for small x would be off by 2^-23 of 1, 4e-6 of a score for
-// a cap of 50. Most scores are far below their cap: a wave whose scores all are saves the
+// a cap of 50. The two ranges and their forms are Moshier's (Methods and Programs for
+// Mathematical Functions, 1989), the coefficients a fit of this file's own. Most scores are far below their cap: a wave whose scores all are saves the
 // exponentials.
 template <int N, typename V>
 __device__ inline void kv_cap(V &z, const KvNew &a)

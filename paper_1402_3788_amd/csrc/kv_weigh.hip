@@ -9,11 +9,13 @@
 // and one writer.
 //
 // The keys' codes are the bytes that must come from memory. For a single new token it is their
-// way that takes the time, and what a launch takes before its first tile (the centres to LDS,
-// some 9 us): 32 sequences of 512 to 4096, 4 heads to each of 8 key heads of 128, bf16, 19.7 us.
+// way that takes the time, and what a launch takes before its first tile (some 9 us: the
+// centres to LDS, behind them the first page numbers, codes and rows, one after the other): 32
+// sequences of 512 to 4096, 4 heads to each of 8 key heads of 128, bf16, 19.7 us.
 // For many the vector ALU does, with 19 operations to a score under a cap, 9 without, and the
 // way that tiles fall to waves (some 3 to one): the last 33 to 64 tokens of 4 prompts of 5000
-// to 8000, 8 heads to a key head, capped, 82 us, 0.25 PFLOP/s of products.
+// to 8000, 8 heads to a key head, capped, 82 to 85 us, 0.25 PFLOP/s of products. Tiles before
+// what a window shows are left out; those that starts hide are worked on and weigh nothing.
 #include "kv_tokens_device.h"
 
 #include <type_traits>
@@ -464,10 +466,11 @@ hipError_t launch(const KvCache &c, const KvNew &a, const KvWeigh &w, hipStream_
     };
     // A tile to a wave, or, of few positions and many rows, to all waves of a workgroup, its
     // rows shared: what takes less work, were all sequences as long as the table's rows. In us,
-    // alone and shared, 8 heads of 128, bf16, measured with the queries not yet over LDS: 52 and
-    // 69 (4 sequences of 5000, 33 tokens of 8 heads), 121 and 151 (of 8000, 64 tokens), 35 and 29
-    // (of 1000, 128 tokens of 4), 63 and 31 (one of 2000, 256 tokens); of one head of 300
-    // positions, 1000 tokens of 8, 384 and 61.
+    // alone and shared, 8 heads of 128, bf16: 47 and 71 (4 sequences of 5000, 33 tokens of 8
+    // heads), 92 and 121 (of 8000, 64 tokens), 20 and 32 (of 2000, 33 tokens), 27 and 24 (of 1000,
+    // 128 tokens of 4), 48 and 25 (one of 2000, 256 tokens), 18 and 11 (64 tokens); of one head of
+    // 300 positions, 1000 tokens of 8, 313 and 46. Where the rule gives both about the same: 38 and
+    // 36 (8 of 2000, 64 tokens of 4: alone), 25 and 26 (4 heads, 3 of 3000, 100 tokens of 4: shared).
     const int64_t alone = splits_of(over(tiles, kWaves)), together = splits_of(tiles);
     const int64_t blocks = over(over(a.tokens * a.group, a.seqs), 32);
     const bool team = over(tiles, together) * (1 + 2 * over(blocks, kWaves)) < over(tiles, alone * kWaves) * (1 + 2 * blocks);
